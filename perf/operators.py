@@ -451,6 +451,15 @@ def _regroups(c):
     return c["bits"] != 16 and c["axis"] == PER_CHANNEL and c["unit"] % c["group"] != 0
 
 
+def _whole_groups(idx, c):
+    """Which of the survivors' groups were one group before, and the groups' first tokens, [heads, groups]"""
+    kept, g = idx.shape[1], c["group"]
+    start = torch.arange(0, kept, g, device=DEV)
+    end = (start + g).clamp(max=kept)
+    first, last = idx[:, start], idx[:, end - 1]
+    return (first % g == 0) & (last - first == end - start - 1) & (end - start == (c["tokens"] - first).clamp(max=g)), first
+
+
 def _evict_plain(s):
     c = s["case"]
     heads = _heads(c)
@@ -464,6 +473,11 @@ def _evict_plain(s):
         x = _read(_key_codes(s["k_codes"], c["bits"])[:, :c["tokens"]], s["k_scale"], s["k_zero"], c, True, torch.float64)
         x = _rows_at(x.float().clamp(-65504, 65504).half(), idx)      # (one rounding to 32 bits, one to 16)
         kc, out["k_scale"], out["k_zero"] = _per_channel(x, c)
+        # a group whose tokens were one group before stays as it was
+        whole, first = _whole_groups(idx, c)
+        kc = torch.where(whole.repeat_interleave(c["group"], 1)[:, :idx.shape[1]].unsqueeze(-1), _rows_at(_key_codes(s["k_codes"], c["bits"]), idx), kc)
+        for k in ("k_scale", "k_zero"):
+            out[k] = torch.where(whole.unsqueeze(-1), _rows_at(s[k], first // c["group"]), out[k])
     else:
         kc = _rows_at(_key_codes(s["k_codes"], c["bits"]), idx)
         if c["bits"] != 16 and c["axis"] == PER_CHANNEL:
@@ -586,8 +600,11 @@ def exact(case, seed):
         if _regroups(c):
             x = _exact_head(s, h)[0][at].float().clamp(-65504, 65504).half().double()
             parts = x.split(c["group"])
-            kz.append(torch.stack([p.amin(0) for p in parts]))
-            ks.append(torch.stack([(p.amax(0) - p.amin(0)) / (2 ** c["bits"] - 1) for p in parts]))
+            sets, g = [idx[j:j + c["group"]] for j in range(0, kept, c["group"])], c["group"]
+            old = [p[0] // g if list(p) == list(range(p[0] // g * g, min(n, p[0] // g * g + g))) else None for p in sets]
+            kz.append(torch.stack([p.amin(0) if o is None else s["k_zero"][h][o].double() for p, o in zip(parts, old)]))
+            ks.append(torch.stack([(p.amax(0) - p.amin(0)) / (2 ** c["bits"] - 1) if o is None else s["k_scale"][h][o].double()
+                                   for p, o in zip(parts, old)]))
     res["weights"] = torch.stack(weights).view(c["batch"], c["hkv"], -1)
     if c["bits"] != 16:
         res.update(k_scale=torch.stack(ks), k_zero=torch.stack(kz), v_scale=torch.stack(vs), v_zero=torch.stack(vz))
