@@ -305,6 +305,7 @@ def _handle(s):
     s["kvqp"], s["cfg"], s["cache"] = kvqp, cfg, cache
     if c["do"] == "tree":
         s["workspace"] = kvqp.alloc_tree_workspace(cfg, c["rows"])
+        s["trees"] = s["mask"] if c["trees"] == "own" else s["mask"][0]
     elif c["do"] == "evict":
         kept = _kept(c)
         rows, groups = _up(kept, 32), _up(kept, c["group"]) // c["group"]
@@ -495,7 +496,7 @@ def run(s):
     if own:
         kvqp = s["kvqp"]
         if c["do"] == "tree":
-            out = kvqp.tree_attn(s["cfg"], s["q"], s["k_new"], s["v_new"], s["mask"], s["cache"], lse=s["lse"], workspace=s["workspace"])
+            out = kvqp.tree_attn(s["cfg"], s["q"], s["k_new"], s["v_new"], s["trees"], s["cache"], lse=s["lse"], workspace=s["workspace"])
             return out, s["lse"]
         if c["do"] == "weights":
             return kvqp.accumulate_weights(s["cfg"], s["q"], s["lse"], s["cache"], s["weights"], decay=c["decay"])
