@@ -414,6 +414,109 @@ int kvqp_append_tail(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_tokens, v
 int kvqp_append_tail_ragged(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_tokens,
                             const int32_t *head_count, void *hip_stream);
 
+/*
+ * ---- Several query rows per call, and eviction (decode time) ----
+ *
+ * A program that decodes speculatively verifies N drafted tokens in one step; one that keeps a
+ * cache within its budget while it decodes evicts the tokens that received least attention (H2O,
+ * one of the pruning methods that Table 1 pairs with quantization, goes by accumulated attention).
+ * The three calls below are used together: kvqp_tree_attn gives the drafted tokens' outputs and
+ * the logarithm of each row's softmax sum; the caller appends the accepted tokens' K / V rows to
+ * the tail; kvqp_accumulate_weights adds up, for the accepted rows, the attention that every
+ * cached token received; kvqp_append_tail moves the oldest tail rows into the packed part; and
+ * kvqp_evict takes the cache back to its budget.
+ *
+ * Common to the three: cfg fields used are batch, heads, head_dim, bits, group_size, key_axis and
+ * sm_scale.  Caches with outlier filtering are not taken (UNSUPPORTED).  Head-level counts
+ * (cache->head_n_kept) are read on the device, where a count above n_kept is cut to n_kept.
+ * q, k_new, v_new, out and the cache's codes, per-channel scales and zeros and tails have to be aligned to
+ * 16 bytes, everything else to its own size and the scales and zeros that belong to tokens to 4 (INVALID_ARG).
+ */
+
+/* The most query rows per query head of kvqp_tree_attn and kvqp_accumulate_weights. */
+#define KVQP_MOST_ROWS 256
+
+/* Workspace bytes of kvqp_tree_attn for n_rows drafted tokens and a cache of any token count
+ * (0: none is needed, and NULL is taken).  Host only. */
+int kvqp_tree_workspace_bytes(const kvqp_cfg *cfg, int32_t n_rows, size_t *bytes);
+
+/*
+ * Attention of n_rows drafted tokens (1 .. KVQP_MOST_ROWS; a tree, a chain, or the one token of an ordinary
+ * step) over the compressed cache (Eq. (3) as in kvqp_decode_attn): row i attends over the packed
+ * tokens, the tail_len tail rows, and those drafted tokens whose bit is set in its mask.
+ *   q      half [batch, Hq, n_rows, D]
+ *   k_new, v_new  half [batch, Hkv, n_rows, D]  the drafted tokens' own rows; they are not
+ *          part of the cache, and the cache is not changed
+ *   mask   uint32 [n_rows, M] or, with mask_per_batch != 0, [batch, n_rows, M], M = ceil(n_rows / 32):
+ *          bit j % 32 of word j / 32 of row i says whether token i attends token j (itself
+ *          included).  Bits of tokens past n_rows are ignored.  NULL: a chain, row i attends 0 .. i.
+ *   out    half [batch, Hq, n_rows, D]   binary32 accumulation, rounded once at the end
+ *   lse    float [batch, Hq, n_rows] or NULL: natural logarithm of the sum of exp(logit)
+ *          over everything the row attends
+ * A row that attends nothing (an empty cache and an empty mask) gets zeros and -inf.  What a row
+ * does not attend does not reach it, whatever it holds, infinities and NaN included.
+ * n_kept and tail_len may be 0.  Reproducible bit for bit.
+ * Numerical range: the product of a query element, scaled so that its row's largest is 64 .. 128,
+ * and its channel's key scale must stay below 65504 (a scale of 511), and with per-token keys a
+ * code times its scale; weights are exact to 2^-22, values are rounded to binary16 once.
+ * Workspace: kvqp_tree_workspace_bytes, 16-byte aligned, no preparation; calls that share one must not
+ * overlap in time.
+ */
+int kvqp_tree_attn(const kvqp_cfg *cfg, const void *q, const void *k_new, const void *v_new, const uint32_t *mask,
+                   int32_t mask_per_batch, int32_t n_rows, const kvqp_cache *cache, void *out, float *lse, void *workspace,
+                   size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Adds the attention weight that every cached token receives from n_rows query rows (1 .. KVQP_MOST_ROWS) to running
+ * sums:  weights[t] = decay * weights[t] + sum over the query heads of t's KV head and the rows
+ * that see t of exp(logit - lse).  The rows are those of the last n_rows tail rows, in order: row i sees
+ * all packed tokens and the first tail_len - n_rows + 1 + i tail rows (none where that is negative),
+ * as in a plain decode step (n_rows = 1) or for an accepted branch whose rows have joined the tail.
+ *   q        half [batch, Hq, n_rows, D]
+ *   lse      float [batch, Hq, n_rows], as kvqp_tree_attn gives it; a row whose lse is -inf adds nothing
+ *   weights  float [batch, Hkv, w_cap], w_cap >= n_kept + tail_len: entry t < count of a head is
+ *            its packed token t, entry count + j its tail row j (count: n_kept, or the head's own).  So
+ *            a token keeps its entry when kvqp_append_tail moves it.  Entries past the tail are left
+ *            alone; one that a new tail row will take has to be 0.
+ *   decay    finite, >= 0: 1 adds up, less lets old weights fade, 0 stores this call's weights without reading the old
+ * Sums are binary32, in one order: reproducible bit for bit.  Needs no workspace.
+ * Numerical range as for kvqp_tree_attn.
+ */
+int kvqp_accumulate_weights(const kvqp_cfg *cfg, const void *q, const float *lse, int32_t n_rows, const kvqp_cache *cache,
+                            float *weights, int32_t w_cap, float decay, void *hip_stream);
+
+/* Workspace bytes of kvqp_evict for a cache of at most n_kept packed tokens per head.  Host only. */
+int kvqp_evict_workspace_bytes(const kvqp_cfg *cfg, int32_t n_kept, size_t *bytes);
+
+/*
+ * Eviction: the packed tokens of src with the highest weights move to dst, in their order; the tail
+ * moves as it is.  src is not changed.
+ *   weights  float [batch, Hkv, w_cap], laid out as for kvqp_accumulate_weights
+ *   n_keep   >= 1: packed tokens that a head may keep; a head with no more than that keeps all
+ *   unit     1, 32, 64 or 128 (<= n_keep): tokens t with the same t / unit stay or leave together,
+ *            by the sum of their weights (formed in binary64 and rounded to binary32).  An incomplete last unit always
+ *            stays (its tokens are the newest), and as many whole units as then fit: a head of c > n_keep tokens
+ *            keeps (c % unit) + unit * floor((n_keep - c % unit) / unit) of them.
+ *            Equal scores: the lower position stays.  A weight that is NaN counts as the lowest.
+ *   dst      a cache of its own, of the same cfg: buffers apart from src's, laid out (n_cap) for as many
+ *            tokens as stay, or 0 for exactly those; tail_cap >= src->tail_len.  n_kept and tail_len are set.
+ *            With head-level counts in src, dst->head_n_kept receives the heads' new counts, and n_kept, the
+ *            bound, becomes min(n_keep, src->n_kept); without them it has to be NULL.
+ *   weights_out  float [batch, Hkv, w_cap_out] or NULL: the weights of what stays, in dst's places, and
+ *            zeros behind the tail; w_cap_out >= dst's n_kept + tail_len; apart from weights
+ *   idx_out  int32 [batch, Hkv, dst's n_kept] or NULL: the survivors' positions in src, ascending; with head-level
+ *            counts the rest of a head's row is unspecified
+ * Codes, scales and zeros move unchanged, with one exception: per-channel keys (below 16 bits)
+ * with a unit that is no multiple of group_size.  There new key groups form, G consecutive survivors each, and are quantized again as
+ * the cache's quantizer states, from half(fma(code, scale, zero)) -- binary32, one rounding each, cut to +-65504 --
+ * unless the group's tokens were one whole group before: that one moves unchanged.
+ * Workspace: kvqp_evict_workspace_bytes, 16-byte aligned, no preparation; calls that share one must not
+ * overlap in time.
+ */
+int kvqp_evict(const kvqp_cfg *cfg, const kvqp_cache *src, const float *weights, int32_t w_cap, int32_t n_keep, int32_t unit,
+               kvqp_cache *dst, float *weights_out, int32_t w_cap_out, int32_t *idx_out, void *workspace, size_t workspace_bytes,
+               void *hip_stream);
+
 /* Static string for a return code. */
 const char *kvqp_strerror(int code);
 

@@ -126,6 +126,21 @@ hipError_t launch_quant_pack(const kvqp_cfg& cfg, const void* k, const void* v, 
                              int n_kept, const int32_t* head_n, const kvqp_cache& cache, hipStream_t stream);
 hipError_t launch_decode(const kvqp_cfg& cfg, const void* q, const kvqp_cache& cache, void* out,
                          void* ws, const DecodePlan& plan, hipStream_t stream);
+// Several query rows per KV head over the cache (kvqp_tree_attn, kvqp_accumulate_weights).
+struct TreePlan {
+    int row_tiles, row_blocks;     // rows of a workgroup in tiles of 16, and how many such blocks a KV head's rows make
+    int n_splits, most_splits;     // token-axis splits of this call, and of any with the same rows
+    size_t ws_bytes, ws_bound;     // workspace of this call, and of any
+};
+TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len);
+hipError_t launch_tree(const kvqp_cfg& cfg, const void* q, const void* k_new, const void* v_new, const uint32_t* mask, bool mask_per_batch,
+                       int n_rows, const kvqp_cache& cache, void* out, float* lse, void* ws, const TreePlan& plan, hipStream_t stream);
+hipError_t launch_weights(const kvqp_cfg& cfg, const void* q, const float* lse, int n_rows, const kvqp_cache& cache, float* weights, int w_cap,
+                          float decay, hipStream_t stream);
+int evict_kept(int n, int n_keep, int unit);     // tokens that stay of a head's n
+// Eviction (kvqp_evict): idx (workspace) [heads, bound] receives the survivors, list the same where it is given.
+hipError_t launch_evict(const kvqp_cfg& cfg, const kvqp_cache& src, const float* weights, int w_cap, int n_keep, int unit, int bound,
+                        const kvqp_cache& dst, float* weights_out, int w_cap_out, int32_t* list, int32_t* idx, hipStream_t stream);
 // n host integers into a device array, enqueued on the stream; src_host is read before the call returns.
 constexpr int kCountsPerLaunch = 768;   // (kernel arguments: 3 KB per launch)
 hipError_t upload_counts(int32_t* dst, const int32_t* src_host, int n, hipStream_t stream, int add = 0);   // dst[i] = src_host[i] + add (src_host == NULL: zeros)

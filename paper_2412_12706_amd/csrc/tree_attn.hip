@@ -1,0 +1,985 @@
+// Attention of several query rows over the packed cache: the drafted tokens of a speculative step
+// (kvqp_tree_attn), and the attention weight that every cached token receives from such rows
+// (kvqp_accumulate_weights, which is what an eviction goes by).
+//
+// Per KV head there are R = Gq * N query rows (N tokens, Gq query heads).  With l[r, t] =
+// sm_scale q[r] . K[t] over all tokens that row r sees,
+//   lse[r] = log sum_t exp(l[r, t])      out[r] = sum_t exp(l[r, t] - lse[r]) V[t]
+//   weight[t] = sum_r exp(l[r, t] - lse[r])
+// K and V are code * scale + zero of the packed part, and plain rows of the tail and of the drafted
+// tokens.  The cache is read once per 64 rows; a row costs 512 multiply-adds per token, so up to
+// some 64 rows the call is bound by memory at 4 bits, beyond that by instruction issue.
+//
+// Layout on gfx950.  A wave takes blocks of 32 tokens, for all rows of its workgroup (16, 32 or 64).
+// Both products run transposed, S^T[token, row] = K Q^T and O^T[channel, row] = V^T P^T, with
+// v_mfma_f32_16x16x32_f16: lane (n = lane % 16, kb = lane / 16) then holds, of row n, the logits of
+// tokens 16 H + 4 kb + i, and these are exactly the tokens whose value codes the cache's
+// tile-transposed layout gives the same lane as the other operand.  Probabilities stay in the lane
+// that computed them, a row's reference, sum and output are that lane's (times four), and nothing
+// crosses lanes inside the loop except the rare change of a reference.
+//
+// Exactness.  Logits are exact to about 2^-22 although the operands are binary16:
+//   keys per channel: the codes times q * s split into binary16 hi + lo parts (v_pk_mul, and v_pk_fma for
+//     what the product lost); q . z of the block's group comes from four more instructions.  (Codes are
+//     whole numbers: as subnormals code * 2^-24, which cost one AND, the matrix unit lines products up by their nominal exponents
+//     and loses what lies below, 2e-5 of a weight);
+//   keys per token: code * s split the same way times q, and z (its rows are constant over a group of
+//     channels) times the sums of q over 32 channels, again hi + lo.
+// Query rows are scaled by a power of two to a largest element of 64 .. 128, so that the lo parts do
+// not run into binary16's subnormals; products above 65504 would overflow (a scale of 512 and more).
+// Weights enter the second product as hi + lo too; values as one binary16 number, code * s + z
+// rounded once, which is the accuracy of the value itself at 16 bits.
+#include <algorithm>
+
+#include "kvqp_internal.h"
+
+namespace kvqp {
+namespace {
+
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef float f4v __attribute__((ext_vector_type(4)));
+
+union Frag {  // one MFMA 16x16x32 f16 input operand of a lane: 8 halves
+    h8v v;
+    uint32_t u[4];
+    h2v h[4];
+    uint4 q;
+};
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNegBig = -1.0e30f;     // reference of a row that has seen nothing
+// A row's reference moves when a logit (log2) passes it by kSlack, and then to kBoost below that logit: weights stay
+// under 2^kSlack, and those of 2^-22 of the largest keep all bits of their hi + lo parts.
+constexpr float kSlack = 12.0f, kBoost = 8.0f;
+
+__device__ __forceinline__ h2v as_h2(uint32_t u) { union { uint32_t u; h2v h; } c; c.u = u; return c.h; }
+__device__ __forceinline__ uint32_t as_u32(h2v h) { union { uint32_t u; h2v h; } c; c.h = h; return c.u; }
+__device__ __forceinline__ float half_to_float(uint16_t u) { return __half2float(__ushort_as_half(u)); }
+__device__ __forceinline__ h2v splat(float x) { return h2v{(_Float16)x, (_Float16)x}; }
+// two binary32 values cut (toward zero) to binary16, (lo, hi) half-words
+__device__ __forceinline__ uint32_t pack_rtz(float lo, float hi) {
+    typedef __fp16 fp16x2 __attribute__((ext_vector_type(2)));
+    union { fp16x2 h; uint32_t u; } c; c.h = __builtin_amdgcn_cvt_pkrtz(lo, hi); return c.u;
+}
+// Data that passes between lanes of one wave through its own LDS: the hardware keeps a wave's LDS accesses in order, this keeps
+// the compiler from moving accesses of different types across each other.
+__device__ __forceinline__ void lds_order() { asm volatile("" ::: "memory"); }
+__device__ __forceinline__ f4v mfma(const Frag& a, const Frag& b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
+
+// sum / max over the four lanes that share lane % 16
+__device__ __forceinline__ float rows4_max(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float rows4_add(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kQuadXor1 = 0xB1, kQuadXor2 = 0x4E, kRowHalfMirror = 0x141, kRowMirror = 0x140;
+// sum / max over the 16 lanes of a row of lanes, in every lane
+__device__ __forceinline__ float row16_add(float v) {
+    v += dpp<kQuadXor1>(v); v += dpp<kQuadXor2>(v); v += dpp<kRowHalfMirror>(v); v += dpp<kRowMirror>(v);
+    return v;
+}
+__device__ __forceinline__ float row16_max(float v) {
+    v = fmaxf(v, dpp<kQuadXor1>(v)); v = fmaxf(v, dpp<kQuadXor2>(v)); v = fmaxf(v, dpp<kRowHalfMirror>(v)); v = fmaxf(v, dpp<kRowMirror>(v));
+    return v;
+}
+
+// ---- codes ----
+// A pair of fields as whole numbers in binary16: with the exponent of 1024 put over a field that begins at bit SH of its
+// half-word (and ends below bit 10) it reads 1024 + 2^SH code.
+template <int SH> __device__ __forceinline__ h2v whole(uint32_t masked) {
+    const h2v x = as_h2(masked | 0x64006400u);
+    if constexpr (SH == 0) return x - splat(1024.0f);
+    else return __builtin_elementwise_fma(x, splat(1.0f / (1 << SH)), splat(-1024.0f / (1 << SH)));
+}
+// Eight consecutive channels of a key row (step s of a lane's 32 channels): c[r] is the pair 8 s + 2 r, + 1.  Fields keep their
+// places where they end below bit 10.
+template <int BITS>
+__device__ __forceinline__ void key_whole(const uint32_t (&w)[BITS], int s, h2v (&c)[4]) {
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[r] = whole<0>((w[2 * s + (r >> 1)] >> (8 * (r & 1))) & 0x00FF00FFu);
+    } else if constexpr (BITS == 4) {
+        const uint32_t a = w[s], b = a >> 8;
+        c[0] = whole<0>(a & 0x000F000Fu); c[1] = whole<4>(a & 0x00F000F0u);
+        c[2] = whole<0>(b & 0x000F000Fu); c[3] = whole<4>(b & 0x00F000F0u);
+    } else if constexpr (BITS == 2) {
+        const uint32_t a = w[s >> 1] >> (8 * (s & 1));
+        c[0] = whole<0>(a & 0x00030003u); c[1] = whole<2>(a & 0x000C000Cu);
+        c[2] = whole<4>(a & 0x00300030u); c[3] = whole<6>(a & 0x00C000C0u);
+    }
+}
+// Value codes of a 32-token block, channel tile `tile`: pair i holds tokens 4 kb + i and 16 + 4 kb + i of channel 16 tile + n.
+template <int BITS> struct VGeom {
+    static constexpr int kWpt = v_words_per_tile(BITS);
+    static constexpr int kWords = 8 * kWpt;            // a lane's words of a superblock
+};
+template <int BITS>
+__device__ __forceinline__ void value_whole(const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v (&c)[4]) {
+    if constexpr (BITS == 8) {
+        const uint32_t a = w[2 * tile], b = w[2 * tile + 1];
+        c[0] = whole<0>(a & 0x00FF00FFu); c[1] = whole<0>((a >> 8) & 0x00FF00FFu);
+        c[2] = whole<0>(b & 0x00FF00FFu); c[3] = whole<0>((b >> 8) & 0x00FF00FFu);
+    } else if constexpr (BITS == 4) {
+        const uint32_t a = w[tile], b = a >> 8;
+        c[0] = whole<0>(a & 0x000F000Fu); c[1] = whole<4>(a & 0x00F000F0u);
+        c[2] = whole<0>(b & 0x000F000Fu); c[3] = whole<4>(b & 0x00F000F0u);
+    } else if constexpr (BITS == 2) {
+        const uint32_t a = w[tile] >> (8 * odd);
+        c[0] = whole<0>(a & 0x00030003u); c[1] = whole<2>(a & 0x000C000Cu);
+        c[2] = whole<4>(a & 0x00300030u); c[3] = whole<6>(a & 0x00C000C0u);
+    }
+}
+
+}  // namespace
+
+struct TreeArgs {
+    const uint16_t* q;        // [B*Hkv, R, D]
+    const uint32_t* k_codes;
+    const uint32_t* v_codes;
+    const uint16_t* k_scale;
+    const uint16_t* k_zero;
+    const uint16_t* v_scale;
+    const uint16_t* v_zero;
+    const uint16_t* tail_k;
+    const uint16_t* tail_v;
+    const uint16_t* k_new;    // [B*Hkv, N, D]
+    const uint16_t* v_new;
+    const uint32_t* mask;     // [B or 1, N, mask_words], or NULL: row i sees new tokens 0 .. i
+    float* part;              // [groups][8 RT][64] float4 of outputs, then [groups][16 RT] (reference, sum)
+    uint16_t* out;            // [B*Hkv, R, D]
+    float* lse;               // [B*Hkv, R] (read by the weights kernel), or NULL
+    float* weights;           // [B*Hkv, w_cap]
+    const int32_t* head_n_kept;
+    size_t mask_stride;       // words from one batch item's mask to the next
+    long long w_cap;
+    int n_kept, n_cap, tail_len, tail_cap;
+    int heads, n_kv_heads;
+    int rows, n_new;          // R, N
+    int row_blocks, n_splits;
+    int group;                // G
+    float sm_scale, decay;
+};
+
+namespace {
+
+// Tokens of one head, cut to the launch's bound so that no value found in memory leads a load past the buffers.
+__device__ __forceinline__ int head_tokens(const TreeArgs& a, int bh) {
+    if (!a.head_n_kept) return a.n_kept;
+    const int n = a.head_n_kept[bh];
+    return n < 0 ? 0 : (n > a.n_kept ? a.n_kept : n);
+}
+
+// ---- query rows in LDS ----
+// Row tile rt, step s: lane (n, kb) finds channels 32 kb + 8 s .. + 7 of row 16 rt + n at [(4 rt + s) * 64 + lane].
+template <int RT> struct QueryTiles {
+    uint4 frag[RT * 4 * 64];
+    uint32_t sums[RT * 64];       // per (row, kb): the sum of the row's 32 channels as binary16 hi, lo
+    float factor[RT * 16];        // 2^-k of a row that was scaled by 2^k
+};
+// Rows row0 .. of one head, by all threads of the workgroup; rows past the last are zeros.
+template <int RT, int THREADS>
+__device__ __forceinline__ void stage_queries(const TreeArgs& a, int bh, int row0, QueryTiles<RT>& sq) {
+    const int seg = threadIdx.x & 15;
+    for (int r = threadIdx.x >> 4; r < RT * 16; r += THREADS / 16) {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (row0 + r < a.rows) w = *reinterpret_cast<const uint4*>(a.q + ((size_t)bh * a.rows + row0 + r) * kHeadDim + 8 * seg);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        float x[8], top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] = half_to_float((uint16_t)(u[j] & 0xffffu)); x[2 * j + 1] = half_to_float((uint16_t)(u[j] >> 16));
+            top = fmaxf(top, fmaxf(fabsf(x[2 * j]), fabsf(x[2 * j + 1])));
+        }
+        top = row16_max(top);
+        // (a power of two, so nothing is rounded that matters: the largest element becomes 64 .. 128)
+        const int k = top > 0.0f ? 133 - (int)((__float_as_uint(top) >> 23) & 0xffu) : 0;
+        const float up = ldexpf(1.0f, k);
+        Frag f;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] *= up; x[2 * j + 1] *= up;
+            f.h[j] = h2v{(_Float16)x[2 * j], (_Float16)x[2 * j + 1]};
+            sum += (float)f.h[j][0] + (float)f.h[j][1];
+        }
+        sum += dpp<kQuadXor1>(sum); sum += dpp<kQuadXor2>(sum);
+        const int rt = r >> 4, n = r & 15, kb = seg >> 2;
+        sq.frag[(4 * rt + (seg & 3)) * 64 + kb * 16 + n] = f.q;
+        if ((seg & 3) == 0) {
+            const _Float16 hi = (_Float16)sum, lo = (_Float16)(sum - (float)hi);
+            sq.sums[rt * 64 + kb * 16 + n] = as_u32(h2v{hi, lo});
+        }
+        if (seg == 0) sq.factor[r] = ldexpf(1.0f, -k);
+    }
+}
+
+// ---- keys of a block: what a wave holds of 32 tokens, two tiles of 16 ----
+// One wave's private LDS: the block's scale rows, one request per row and wave, read back where they are needed.
+struct __align__(16) ScaleStrip {
+    uint32_t k_scale[64], k_zero[64];        // per channel: one group's row
+    uint32_t v_scale[64], v_zero[64];        // [group of channels][kb][i][H]
+};
+
+template <int BITS, int AXIS> struct KeyWords {
+    uint32_t w[2][BITS];
+    uint32_t scale[2], zero[2];      // keys per channel: a dword of the group's row; per token: the lane's own group of its two tokens
+};
+template <int BITS, int AXIS>
+__device__ __forceinline__ void load_keys(const TreeArgs& a, int bh, int blk, int lane, KeyWords<BITS, AXIS>& k) {
+    const int n = lane & 15, kb = lane >> 4;
+    const size_t tok = (size_t)bh * a.n_cap + 32 * blk + n;
+#pragma unroll
+    for (int H = 0; H < 2; ++H) {
+        const uint32_t* p = a.k_codes + (tok + 16 * H) * (kHeadDim * BITS / 32) + kb * BITS;
+        if constexpr (BITS == 2) {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            k.w[H][0] = u.x; k.w[H][1] = u.y;
+        } else {
+#pragma unroll
+            for (int j = 0; j < BITS / 4; ++j) {
+                const uint4 u = *reinterpret_cast<const uint4*>(p + 4 * j);
+                k.w[H][4 * j] = u.x; k.w[H][4 * j + 1] = u.y; k.w[H][4 * j + 2] = u.z; k.w[H][4 * j + 3] = u.w;
+            }
+        }
+    }
+    if constexpr (BITS != 16) {
+        if constexpr (AXIS == KVQP_KEY_PER_CHANNEL) {
+            const size_t groups = (size_t)(a.n_cap + a.group - 1) / a.group;
+            const size_t row = ((size_t)bh * groups + (32 * blk) / a.group) * (kHeadDim / 2) + lane;
+            k.scale[0] = reinterpret_cast<const uint32_t*>(a.k_scale)[row];
+            k.zero[0] = reinterpret_cast<const uint32_t*>(a.k_zero)[row];
+        } else {
+            const int cg = kHeadDim / a.group;
+#pragma unroll
+            for (int H = 0; H < 2; ++H) {
+                const size_t at = (tok + 16 * H) * cg + kb * 32 / a.group;
+                k.scale[H] = a.k_scale[at];
+                k.zero[H] = a.k_zero[at];
+            }
+        }
+    }
+}
+
+// Operands of a block's key product, the same for every row tile.
+template <int BITS, int AXIS> struct KeyOperand {
+    static constexpr bool kChannel = BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL;
+    static constexpr bool kToken = BITS != 16 && AXIS == KVQP_KEY_PER_TOKEN;
+    Frag a[2][4];                     // codes, code * s hi parts, or the keys themselves
+    Frag b[kToken ? 2 : 1][kToken ? 4 : 1];   // code * s lo parts
+    Frag s[kChannel ? 4 : 1], z[kChannel ? 4 : 1];   // the group's scales and zeros of the lane's channels
+    uint32_t zt[2];                   // the tokens' zeros, twice
+};
+template <int BITS, int AXIS>
+__device__ __forceinline__ void key_operand(const KeyWords<BITS, AXIS>& k, ScaleStrip& strip, int lane, KeyOperand<BITS, AXIS>& o) {
+    using O = KeyOperand<BITS, AXIS>;
+    if constexpr (O::kChannel) {
+        lds_order();
+        strip.k_scale[lane] = k.scale[0];
+        strip.k_zero[lane] = k.zero[0];
+        lds_order();
+        const int kb = lane >> 4;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            o.s[s].q = *reinterpret_cast<const uint4*>(&strip.k_scale[16 * kb + 4 * s]);
+            o.z[s].q = *reinterpret_cast<const uint4*>(&strip.k_zero[16 * kb + 4 * s]);
+        }
+    }
+#pragma unroll
+    for (int H = 0; H < 2; ++H) {
+        if constexpr (O::kToken) {
+            const h2v sc = as_h2(k.scale[H] * 0x10001u);
+            o.zt[H] = k.zero[H] * 0x10001u;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                h2v c[4];
+                key_whole<BITS>(k.w[H], s, c);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    o.a[H][s].h[r] = c[r] * sc;
+                    o.b[H][s].h[r] = __builtin_elementwise_fma(c[r], sc, -o.a[H][s].h[r]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if constexpr (BITS == 16) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o.a[H][s].u[r] = k.w[H][4 * s + r];
+                } else {
+                    h2v c[4];
+                    key_whole<BITS>(k.w[H], s, c);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o.a[H][s].h[r] = c[r];
+                }
+            }
+        }
+    }
+}
+// Logits of one row tile: x = (acc + base) * the row's factor.
+template <int BITS, int AXIS, int RT>
+__device__ __forceinline__ void key_product(const KeyOperand<BITS, AXIS>& o, const QueryTiles<RT>& sq, int rt, int lane, f4v (&acc)[2], float& base) {
+    using O = KeyOperand<BITS, AXIS>;
+    acc[0] = acc[1] = f4v{0.f, 0.f, 0.f, 0.f};
+    f4v az = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        Frag q;
+        q.q = sq.frag[(4 * rt + s) * 64 + lane];
+        if constexpr (O::kChannel) {
+            Frag hi, lo;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                hi.h[r] = q.h[r] * o.s[s].h[r];
+                lo.h[r] = __builtin_elementwise_fma(q.h[r], o.s[s].h[r], -hi.h[r]);
+            }
+            az = mfma(o.z[s], q, az);
+            acc[0] = mfma(o.a[0][s], hi, acc[0]); acc[1] = mfma(o.a[1][s], hi, acc[1]);
+            acc[0] = mfma(o.a[0][s], lo, acc[0]); acc[1] = mfma(o.a[1][s], lo, acc[1]);
+        } else {
+            acc[0] = mfma(o.a[0][s], q, acc[0]); acc[1] = mfma(o.a[1][s], q, acc[1]);
+            if constexpr (O::kToken) { acc[0] = mfma(o.b[0][s], q, acc[0]); acc[1] = mfma(o.b[1][s], q, acc[1]); }
+        }
+    }
+    if constexpr (O::kToken) {
+        Frag qs, z;
+        qs.u[0] = sq.sums[rt * 64 + lane]; qs.u[1] = qs.u[2] = qs.u[3] = 0u;
+        z.u[1] = z.u[2] = z.u[3] = 0u;
+#pragma unroll
+        for (int H = 0; H < 2; ++H) { z.u[0] = o.zt[H]; acc[H] = mfma(z, qs, acc[H]); }
+    }
+    base = O::kChannel ? az[0] : 0.0f;
+}
+// ---- state of a wave's rows ----
+template <int RT> struct RowState {
+    f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n
+    float ref[RT], sum[RT];
+};
+template <int RT>
+__device__ __forceinline__ void clear(RowState<RT>& st) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        st.ref[rt] = kNegBig; st.sum[rt] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) st.o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
+    }
+}
+// Moves references where x (logits of a block in log2, -inf where unseen) has passed them, turns x into weights, adds them up.
+template <int RT>
+__device__ __forceinline__ void softmax_step(RowState<RT>& st, float (&x)[RT][8]) {
+    bool past = false;
+    float top[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        top[rt] = fmaxf(fmaxf(fmaxf(x[rt][0], x[rt][1]), fmaxf(x[rt][2], x[rt][3])), fmaxf(fmaxf(x[rt][4], x[rt][5]), fmaxf(x[rt][6], x[rt][7])));
+        past |= top[rt] > st.ref[rt] + kSlack;
+    }
+    if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float t = rows4_max(top[rt]);          // (all four lanes of a row decide alike)
+            const float ref = t > st.ref[rt] + kSlack ? t - kBoost : st.ref[rt];
+            const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref);
+            st.ref[rt] = ref;
+            st.sum[rt] *= f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) st.o[rt][c] *= f;
+        }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[rt][j] = __builtin_amdgcn_exp2f(x[rt][j] - st.ref[rt]);
+            st.sum[rt] += x[rt][j];
+        }
+}
+// Weights as operands: pair i holds tokens 4 kb + i and 16 + 4 kb + i; hi + lo parts, cut toward zero.
+struct WeightOperand { Frag hi, lo; };
+__device__ __forceinline__ void weight_operand(const float (&p)[8], WeightOperand& o) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        o.hi.u[i] = pack_rtz(p[i], p[4 + i]);
+        o.lo.u[i] = pack_rtz(p[i] - (float)o.hi.h[i][0], p[4 + i] - (float)o.hi.h[i][1]);
+    }
+}
+template <int RT>
+__device__ __forceinline__ void value_product(RowState<RT>& st, const Frag& v, int tile, const WeightOperand (&p)[RT]) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        st.o[rt][tile] = mfma(v, p[rt].hi, st.o[rt][tile]);
+        st.o[rt][tile] = mfma(v, p[rt].lo, st.o[rt][tile]);
+    }
+}
+
+// ---- values of a packed block ----
+template <int BITS> struct ValueWords {
+    uint32_t w[VGeom<BITS>::kWords];
+    uint32_t scale, zero;
+};
+template <int BITS>
+__device__ __forceinline__ void load_values(const TreeArgs& a, int bh, int blk, int lane, ValueWords<BITS>& v) {
+    constexpr int SB = v_superblock(BITS), SBW = v_superblock_words(BITS);
+    const size_t per_head = (size_t)((a.n_cap + SB - 1) / SB) * SBW;
+    const uint32_t* p = a.v_codes + (size_t)bh * per_head + (size_t)(32 * blk / SB) * SBW + 4 * lane;
+#pragma unroll
+    for (int j = 0; j < VGeom<BITS>::kWords / 4; ++j) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p + 256 * j);
+        v.w[4 * j] = u.x; v.w[4 * j + 1] = u.y; v.w[4 * j + 2] = u.z; v.w[4 * j + 3] = u.w;
+    }
+    if constexpr (BITS != 16) {
+        // 32 tokens' scales are 32 D / G numbers in a row; lanes past the last repeat it
+        const int cg = kHeadDim / a.group;
+        const size_t at = ((size_t)bh * a.n_cap + 32 * blk) * cg / 2 + min(lane, 16 * cg - 1);
+        v.scale = reinterpret_cast<const uint32_t*>(a.v_scale)[at];
+        v.zero = reinterpret_cast<const uint32_t*>(a.v_zero)[at];
+    }
+}
+// Scales and zeros to the strip, in the order in which the lanes of a token's block want them.
+template <int BITS>
+__device__ __forceinline__ void strip_values(const TreeArgs& a, const ValueWords<BITS>& v, ScaleStrip& strip, int lane) {
+    const int cg = kHeadDim / a.group;
+    uint16_t* s = reinterpret_cast<uint16_t*>(strip.v_scale);
+    uint16_t* z = reinterpret_cast<uint16_t*>(strip.v_zero);
+    lds_order();
+    if (lane < 16 * cg) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int t = (2 * lane + e) / cg, g = (2 * lane + e) % cg;
+            const int at = g * 32 + (t & 15) * 2 + (t >> 4);
+            s[at] = (uint16_t)(v.scale >> (16 * e));
+            z[at] = (uint16_t)(v.zero >> (16 * e));
+        }
+    }
+    lds_order();
+}
+
+// ---- plain rows (tail, drafted tokens) ----
+constexpr int kPlainStride = kHeadDim + 8;      // halves between two rows of a value tile in LDS
+struct __align__(16) PlainTile { uint16_t v[32 * kPlainStride]; };
+
+// A workgroup's LDS: while blocks are worked on, then while the waves' states are joined.
+union WaveScratch { ScaleStrip strip; PlainTile tile; };
+template <int RT> struct MergeSlot { f4v o[RT][8][64]; float2 m[RT][64]; };      // outputs; reference and sum
+template <int RT> union __align__(16) TreeShared {
+    struct { QueryTiles<RT> sq; WaveScratch wave[kWaves]; } run;
+    MergeSlot<RT> merge[kWaves / 2];
+};
+
+template <int BITS, int AXIS, int RT>
+__global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const TreeArgs a) {
+    __shared__ TreeShared<RT> sh;
+    QueryTiles<RT>& sq = sh.run.sq;
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, kb = lane >> 4;
+    // Workgroups go to the eight dies in turn: the row blocks of one stretch of a cache get numbers eight apart, so that
+    // they run on one die at about the same time and share what its L2 holds.
+    const int pair = blockIdx.x / (8 * a.row_blocks) * 8 + blockIdx.x % 8, rb = blockIdx.x / 8 % a.row_blocks;
+    if (pair >= a.heads * a.n_splits) return;
+    const int bh = pair / a.n_splits, split = pair % a.n_splits;
+    const int row0 = rb * RT * 16;
+    stage_queries<RT, kThreads>(a, bh, row0, sq);
+
+    const int n_tok = head_tokens(a, bh);
+    const int packed = (n_tok + 31) / 32, tail = (a.tail_len + 31) / 32, fresh = (a.n_new + 31) / 32;
+    const int units = packed + tail + fresh;
+    const int u0 = (int)((long long)units * split / a.n_splits), u1 = (int)((long long)units * (split + 1) / a.n_splits);
+    ScaleStrip& strip = sh.run.wave[wave].strip;
+
+    RowState<RT> st;
+    clear(st);
+    __syncthreads();
+    const float c_q = a.sm_scale * kLog2e;
+    float factor[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) factor[rt] = sq.factor[16 * rt + n] * c_q;
+
+    // ---- packed blocks ----
+    {
+        const int end = min(u1, packed);
+        int blk = u0 + wave;
+        if (blk < end) {
+            KeyWords<BITS, AXIS> kw;
+            ValueWords<BITS> vw;
+            load_keys<BITS, AXIS>(a, bh, blk, lane, kw);
+            load_values<BITS>(a, bh, blk, lane, vw);
+#pragma unroll 1
+            for (; blk < end; blk += kWaves) {
+                const int next = min(blk + kWaves, end - 1);
+                float x[RT][8];
+                {
+                    KeyOperand<BITS, AXIS> ko;
+                    key_operand<BITS, AXIS>(kw, strip, lane, ko);
+                    load_keys<BITS, AXIS>(a, bh, next, lane, kw);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        f4v acc[2];
+                        float base;
+                        key_product<BITS, AXIS, RT>(ko, sq, rt, lane, acc, base);
+                        base *= factor[rt];
+#pragma unroll
+                        for (int H = 0; H < 2; ++H)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[rt][4 * H + i] = __builtin_fmaf(acc[H][i], factor[rt], base);
+                    }
+                }
+                if (32 * blk + 32 > n_tok) {     // (uniform) the head's last block: tokens past its count are unseen
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (32 * blk + 16 * (j >> 2) + 4 * kb + (j & 3) >= n_tok) x[rt][j] = -INFINITY;
+                }
+                softmax_step<RT>(st, x);
+                WeightOperand p[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], p[rt]);
+                if constexpr (BITS != 16) strip_values<BITS>(a, vw, strip, lane);
+#pragma unroll
+                for (int tile = 0; tile < 8; ++tile) {
+                    Frag v;
+                    if constexpr (BITS == 16) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v.u[i] = vw.w[4 * tile + i];
+                    } else {
+                        h2v c[4];
+                        value_whole<BITS>(vw.w, tile, blk & 1, c);
+                        Frag s, z;
+                        const int g = tile * 16 / a.group;
+                        s.q = *reinterpret_cast<const uint4*>(&strip.v_scale[16 * g + 4 * kb]);
+                        z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * g + 4 * kb]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v.h[i] = __builtin_elementwise_fma(c[i], s.h[i], z.h[i]);
+                    }
+                    value_product<RT>(st, v, tile, p);
+                }
+                load_values<BITS>(a, bh, next, lane, vw);
+            }
+        }
+    }
+
+    // ---- tail rows and drafted tokens ----
+    {
+        PlainTile& tile_v = sh.run.wave[wave].tile;
+        const int first = max(u0, packed);
+#pragma unroll 1
+        for (int u = first + wave; u < u1; u += kWaves) {
+            const bool drafted = u >= packed + tail;
+            const int t0 = 32 * (drafted ? u - packed - tail : u - packed), len = drafted ? a.n_new : a.tail_len;
+            const size_t row = drafted ? (size_t)bh * a.n_new : (size_t)bh * a.tail_cap;
+            const uint16_t* kp = (drafted ? a.k_new : a.tail_k) + row * kHeadDim;
+            const uint16_t* vp = (drafted ? a.v_new : a.tail_v) + row * kHeadDim;
+            KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
+#pragma unroll
+            for (int H = 0; H < 2; ++H) {
+                const uint16_t* p = kp + (size_t)min(t0 + 16 * H + n, len - 1) * kHeadDim + 32 * kb;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
+                    kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
+                }
+            }
+            lds_order();
+            bool odd_value = false;       // a value that is not finite
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int t = 4 * j + kb;
+                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                if (t0 + t < len) w = *reinterpret_cast<const uint4*>(vp + (size_t)(t0 + t) * kHeadDim + 8 * n);
+                const uint32_t u4[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd_value |= (u4[e] & 0x7C00u) == 0x7C00u || (u4[e] & 0x7C000000u) == 0x7C000000u;
+                *reinterpret_cast<uint4*>(&tile_v.v[t * kPlainStride + 8 * n]) = w;
+            }
+            lds_order();
+            float x[RT][8];
+            {
+                KeyOperand<16, KVQP_KEY_PER_CHANNEL> ko;
+                key_operand<16, KVQP_KEY_PER_CHANNEL>(kw, strip, lane, ko);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    f4v acc[2];
+                    float base;
+                    key_product<16, KVQP_KEY_PER_CHANNEL, RT>(ko, sq, rt, lane, acc, base);
+                    // which of the block's 32 tokens the row sees
+                    uint32_t seen = t0 + 32 <= len ? 0xFFFFFFFFu : (1u << (len - t0)) - 1u;
+                    if (drafted) {
+                        const int r = row0 + 16 * rt + n;
+                        const int i = r < a.rows ? r % a.n_new : 0;
+                        if (a.mask) seen &= a.mask[(size_t)(bh / a.n_kv_heads) * a.mask_stride + (size_t)i * ((a.n_new + 31) / 32) + t0 / 32];
+                        else seen &= i >= t0 + 31 ? 0xFFFFFFFFu : i < t0 ? 0u : (2u << (i - t0)) - 1u;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float l = acc[j >> 2][j & 3] * factor[rt];
+                        x[rt][j] = (seen >> (16 * (j >> 2) + 4 * kb + (j & 3))) & 1u ? l : -INFINITY;
+                    }
+                }
+            }
+            softmax_step<RT>(st, x);
+            if (drafted && __builtin_amdgcn_ballot_w64(odd_value) != 0ull) {
+                // Values that are not finite reach only the rows that see them: a weight of 0 would make them NaN in the matrix product.
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll 1
+                        for (int b = 0; b < 4; ++b) {
+                            const float p = __shfl(x[rt][j], 16 * b + n);
+                            const uint16_t* v = &tile_v.v[(16 * (j >> 2) + 4 * b + (j & 3)) * kPlainStride + 4 * kb];
+#pragma unroll
+                            for (int t = 0; t < 8; ++t)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    st.o[rt][t][i] = p != 0.0f ? __builtin_fmaf(p, half_to_float(v[16 * t + i]), st.o[rt][t][i]) : st.o[rt][t][i];
+                        }
+            } else {
+                WeightOperand p[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], p[rt]);
+#pragma unroll
+                for (int tile = 0; tile < 8; ++tile) {
+                    Frag v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t lo = tile_v.v[(4 * kb + i) * kPlainStride + 16 * tile + n], hi = tile_v.v[(16 + 4 * kb + i) * kPlainStride + 16 * tile + n];
+                        v.u[i] = lo | (hi << 16);
+                    }
+                    value_product<RT>(st, v, tile, p);
+                }
+            }
+        }
+    }
+
+    // ---- the waves' states become one ----
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) st.sum[rt] = rows4_add(st.sum[rt]);
+#pragma unroll 1
+    for (int half = kWaves / 2; half >= 1; half >>= 1) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) sh.merge[wave - half].o[rt][t][lane] = st.o[rt][t];
+                sh.merge[wave - half].m[rt][lane] = make_float2(st.ref[rt], st.sum[rt]);
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float2 other = sh.merge[wave].m[rt][lane];
+                const float ref = fmaxf(st.ref[rt], other.x);
+                const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref), g = __builtin_amdgcn_exp2f(other.x - ref);
+                st.ref[rt] = ref;
+                st.sum[rt] = st.sum[rt] * f + other.y * g;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) st.o[rt][t] = st.o[rt][t] * f + sh.merge[wave].o[rt][t][lane] * g;
+            }
+        }
+    }
+    if (wave != 0) return;
+    if (a.n_splits > 1) {
+        const size_t group = (size_t)(bh * a.row_blocks + rb) * a.n_splits + split;
+        f4v* po = reinterpret_cast<f4v*>(a.part) + group * (RT * 8 * 64);
+        float2* ps = reinterpret_cast<float2*>(a.part + (size_t)a.heads * a.row_blocks * a.n_splits * (RT * 16 * kHeadDim)) + group * (RT * 16);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t) po[(rt * 8 + t) * 64 + lane] = st.o[rt][t];
+            if (kb == 0) ps[rt * 16 + n] = make_float2(st.ref[rt], st.sum[rt]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = row0 + 16 * rt + n;
+        if (r < a.rows) {
+            const float inv = st.sum[rt] > 0.0f ? 1.0f / st.sum[rt] : st.sum[rt];      // (a row that sees nothing: zeros)
+            uint16_t* o = a.out + ((size_t)bh * a.rows + r) * kHeadDim + 4 * kb;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                Frag h;
+                h.h[0] = h2v{(_Float16)(st.o[rt][t][0] * inv), (_Float16)(st.o[rt][t][1] * inv)};
+                h.h[1] = h2v{(_Float16)(st.o[rt][t][2] * inv), (_Float16)(st.o[rt][t][3] * inv)};
+                *reinterpret_cast<uint2*>(o + 16 * t) = make_uint2(h.u[0], h.u[1]);
+            }
+            if (a.lse && kb == 0) a.lse[(size_t)bh * a.rows + r] = st.sum[rt] == 0.0f ? -INFINITY : (st.ref[rt] + __builtin_amdgcn_logf(st.sum[rt])) * kLn2;
+        }
+    }
+}
+
+// Joins the splits of a row block: a thread has four channels of one row.
+template <int RT>
+__global__ __launch_bounds__(256) void tree_merge(const TreeArgs a) {
+    const int item = blockIdx.x * 256 + threadIdx.x;              // [bh, rb][rt][tile][lane]
+    const int lane = item & 63, tile = (item >> 6) & 7, rt = (item >> 9) % RT;
+    const int rest = (item >> 9) / RT;
+    if (rest >= a.heads * a.row_blocks) return;
+    const int bh = rest / a.row_blocks, rb = rest % a.row_blocks;
+    const int n = lane & 15, kb = lane >> 4;
+    const int r = rb * RT * 16 + rt * 16 + n;
+    if (r >= a.rows) return;
+    const f4v* po = reinterpret_cast<const f4v*>(a.part) + (size_t)rest * a.n_splits * (RT * 8 * 64) + (rt * 8 + tile) * 64 + lane;
+    const float2* ps = reinterpret_cast<const float2*>(a.part + (size_t)a.heads * a.row_blocks * a.n_splits * (RT * 16 * kHeadDim)) +
+                       (size_t)rest * a.n_splits * (RT * 16) + rt * 16 + n;
+    float ref = kNegBig, sum = 0.f;
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < a.n_splits; s0 += 8) {
+        f4v v[8];
+        float2 m[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int s = min(s0 + u, a.n_splits - 1);
+            v[u] = po[(size_t)s * (RT * 8 * 64)];
+            m[u] = ps[(size_t)s * (RT * 16)];
+        }
+        float top = ref;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) top = fmaxf(top, m[u].x);
+        const float f = __builtin_amdgcn_exp2f(ref - top);
+        o *= f; sum *= f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float g = s0 + u < a.n_splits ? __builtin_amdgcn_exp2f(m[u].x - top) : 0.f;
+            o += v[u] * g;
+            sum = __builtin_fmaf(m[u].y, g, sum);
+        }
+        ref = top;
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : sum;
+    Frag h;
+    h.h[0] = h2v{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv)};
+    h.h[1] = h2v{(_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * tile + 4 * kb) = make_uint2(h.u[0], h.u[1]);
+    if (a.lse && tile == 0 && kb == 0) a.lse[(size_t)bh * a.rows + r] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// ---- weights that tokens receive ----
+// A wave has one block of 32 tokens for good and goes over all rows, 64 of them in LDS at a time; the sum of a token's
+// column is that wave's alone, so it is added to the running one without atomics, in one fixed order.
+constexpr int kWeightRT = 4, kWeightWaves = 4, kWeightThreads = 64 * kWeightWaves;
+
+template <int BITS, int AXIS>
+__device__ __forceinline__ void weigh(const KeyOperand<BITS, AXIS>& ko, const TreeArgs& a, int bh, QueryTiles<kWeightRT>& sq,
+                                      float (&s_lse)[kWeightRT * 16], bool live, int tail0, float (&cs)[8]) {
+    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
+#pragma unroll 1
+    for (int row0 = 0; row0 < a.rows; row0 += kWeightRT * 16) {
+        if (row0) __syncthreads();
+        stage_queries<kWeightRT, kWeightThreads>(a, bh, row0, sq);
+        if (threadIdx.x < kWeightRT * 16) {
+            const int r = row0 + threadIdx.x;
+            const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;
+            s_lse[threadIdx.x] = l == -INFINITY ? INFINITY : l;        // (a row that sees nothing gives nothing)
+        }
+        __syncthreads();
+        if (!live) continue;
+        const int tiles = min(kWeightRT, (a.rows - row0 + 15) / 16);
+#pragma unroll 1
+        for (int rt = 0; rt < tiles; ++rt) {
+            f4v acc[2];
+            float base;
+            key_product<BITS, AXIS, kWeightRT>(ko, sq, rt, lane, acc, base);
+            // (in natural units up to the exponential: sm_scale and the rows' powers of two are exact)
+            const float f = sq.factor[16 * rt + n] * a.sm_scale;
+            base = __builtin_fmaf(base, f, -s_lse[16 * rt + n]);
+            const int i = (row0 + 16 * rt + n) % a.n_new;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j >> 2][j & 3], f, base) * kLog2e);
+                // (tail0 < 0: packed tokens, which every row sees)
+                if (tail0 >= 0 && tail0 + 16 * (j >> 2) + 4 * kb + (j & 3) > a.tail_len - a.n_new + i) p = 0.0f;
+                cs[j] += p;
+            }
+        }
+    }
+}
+
+template <int BITS, int AXIS>
+__global__ __launch_bounds__(kWeightThreads) void add_weights(const TreeArgs a) {
+    __shared__ QueryTiles<kWeightRT> sq;
+    __shared__ ScaleStrip s_strip[kWeightWaves];
+    __shared__ float s_lse[kWeightRT * 16];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, kb = lane >> 4;
+    const int bh = blockIdx.y;
+    const int n_tok = head_tokens(a, bh);
+    const int packed = (n_tok + 31) / 32, units = packed + (a.tail_len + 31) / 32;
+    // (workgroups of a shorter head beyond its blocks leave at once)
+    if ((int)blockIdx.x * kWeightWaves >= units) return;
+    const int u = blockIdx.x * kWeightWaves + wave;
+    const bool live = u < units, is_tail = u >= packed;
+    const int t0 = 32 * (is_tail ? u - packed : u), len = is_tail ? a.tail_len : n_tok;
+    float cs[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cs[j] = 0.0f;
+    // (a workgroup may have both kinds of blocks: each goes through the rows by itself, and the other's waves only help to stage them)
+    const int u_first = blockIdx.x * kWeightWaves, u_last = min(u_first + kWeightWaves, units) - 1;
+    if (u_first < packed) {
+        KeyOperand<BITS, AXIS> ko;
+        KeyWords<BITS, AXIS> kw;
+        load_keys<BITS, AXIS>(a, bh, min(u, packed - 1), lane, kw);
+        key_operand<BITS, AXIS>(kw, s_strip[wave], lane, ko);
+        weigh<BITS, AXIS>(ko, a, bh, sq, s_lse, live && !is_tail, -1, cs);
+    }
+    if (u_last >= packed) {
+        if (u_first < packed) __syncthreads();
+        KeyOperand<16, KVQP_KEY_PER_CHANNEL> ko;
+        KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
+        const int tt = is_tail && live ? t0 : 0;
+#pragma unroll
+        for (int H = 0; H < 2; ++H) {
+            const uint16_t* p = a.tail_k + ((size_t)bh * a.tail_cap + min(tt + 16 * H + n, a.tail_len - 1)) * kHeadDim + 32 * kb;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
+                kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
+            }
+        }
+        key_operand<16, KVQP_KEY_PER_CHANNEL>(kw, s_strip[wave], lane, ko);
+        weigh<16, KVQP_KEY_PER_CHANNEL>(ko, a, bh, sq, s_lse, live && is_tail, t0, cs);
+    }
+    if (!live) return;
+    // lane i of a row of 16 lanes stores token 4 kb + i of both tiles
+#pragma unroll
+    for (int H = 0; H < 2; ++H) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = row16_add(cs[4 * H + i]);
+        const float mine = n == 0 ? v[0] : n == 1 ? v[1] : n == 2 ? v[2] : v[3];
+        const int t = t0 + 16 * H + 4 * kb + n;
+        if (n < 4 && t < len) {
+            float* w = a.weights + (size_t)bh * a.w_cap + (is_tail ? n_tok : 0) + t;
+            *w = a.decay != 0.0f ? __builtin_fmaf(a.decay, *w, mine) : mine;
+        }
+    }
+}
+
+template <int BITS, int AXIS, int RT>
+hipError_t run_tree(const TreeArgs& a, hipStream_t stream) {
+    const int pairs = (a.heads * a.n_splits + 7) / 8 * 8;
+    tree_attn<BITS, AXIS, RT><<<dim3(pairs * a.row_blocks), dim3(kThreads), 0, stream>>>(a);
+    if (a.n_splits > 1) tree_merge<RT><<<dim3((a.heads * a.row_blocks * RT * 512 + 255) / 256), dim3(256), 0, stream>>>(a);
+    return hipGetLastError();
+}
+template <int BITS, int AXIS>
+hipError_t run_tree_rt(const TreeArgs& a, int rt, hipStream_t stream) {
+    if (rt == 1) return run_tree<BITS, AXIS, 1>(a, stream);
+    if (rt == 2) return run_tree<BITS, AXIS, 2>(a, stream);
+    return run_tree<BITS, AXIS, 4>(a, stream);
+}
+template <int BITS, int AXIS>
+hipError_t run_weights(const TreeArgs& a, hipStream_t stream) {
+    const int units = (a.n_kept + 31) / 32 + (a.tail_len + 31) / 32;
+    add_weights<BITS, AXIS><<<dim3((units + kWeightWaves - 1) / kWeightWaves, a.heads), dim3(kWeightThreads), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// (one object per bit width, side by side)
+template <int BITS> hipError_t tree_bits(const TreeArgs& a, int rt, int axis, hipStream_t stream);
+template <int BITS> hipError_t weights_bits(const TreeArgs& a, int axis, hipStream_t stream);
+#ifdef KVQP_TREE_BITS
+template <> hipError_t tree_bits<KVQP_TREE_BITS>(const TreeArgs& a, int rt, int axis, hipStream_t stream) {
+    if constexpr (KVQP_TREE_BITS != 16) {
+        if (axis == KVQP_KEY_PER_TOKEN) return run_tree_rt<KVQP_TREE_BITS, KVQP_KEY_PER_TOKEN>(a, rt, stream);
+    }
+    return run_tree_rt<KVQP_TREE_BITS, KVQP_KEY_PER_CHANNEL>(a, rt, stream);
+}
+template <> hipError_t weights_bits<KVQP_TREE_BITS>(const TreeArgs& a, int axis, hipStream_t stream) {
+    if constexpr (KVQP_TREE_BITS != 16) {
+        if (axis == KVQP_KEY_PER_TOKEN) return run_weights<KVQP_TREE_BITS, KVQP_KEY_PER_TOKEN>(a, stream);
+    }
+    return run_weights<KVQP_TREE_BITS, KVQP_KEY_PER_CHANNEL>(a, stream);
+}
+#else
+template <> hipError_t tree_bits<2>(const TreeArgs&, int, int, hipStream_t);
+template <> hipError_t tree_bits<4>(const TreeArgs&, int, int, hipStream_t);
+template <> hipError_t tree_bits<8>(const TreeArgs&, int, int, hipStream_t);
+template <> hipError_t tree_bits<16>(const TreeArgs&, int, int, hipStream_t);
+template <> hipError_t weights_bits<2>(const TreeArgs&, int, hipStream_t);
+template <> hipError_t weights_bits<4>(const TreeArgs&, int, hipStream_t);
+template <> hipError_t weights_bits<8>(const TreeArgs&, int, hipStream_t);
+template <> hipError_t weights_bits<16>(const TreeArgs&, int, hipStream_t);
+
+TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len) {
+    TreePlan p;
+    const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_rows;
+    p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.row_blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
+    // one workgroup of eight waves per CU, two where the rows' registers leave room for them
+    const long long base = (long long)cfg.batch * cfg.n_kv_heads * p.row_blocks;
+    const long long want = (p.row_tiles == 1 ? 512 : 256) / base;
+    p.most_splits = (int)std::max(1LL, std::min(want, 64LL));
+    const int units = (n_kept + 31) / 32 + (tail_len + 31) / 32 + (n_rows + 31) / 32;
+    p.n_splits = std::max(1, std::min(p.most_splits, (units + kWaves - 1) / kWaves));
+    const size_t one = (size_t)base * (16 * p.row_tiles) * (kHeadDim + 2) * sizeof(float);
+    p.ws_bytes = p.n_splits > 1 ? one * p.n_splits : 0;
+    p.ws_bound = p.most_splits > 1 ? one * p.most_splits : 0;
+    return p;
+}
+
+static TreeArgs common_args(const kvqp_cfg& cfg, const kvqp_cache& c, int n_rows) {
+    TreeArgs a = {};
+    a.k_codes = (const uint32_t*)c.k_codes; a.v_codes = (const uint32_t*)c.v_codes;
+    a.k_scale = (const uint16_t*)c.k_scale; a.k_zero = (const uint16_t*)c.k_zero;
+    a.v_scale = (const uint16_t*)c.v_scale; a.v_zero = (const uint16_t*)c.v_zero;
+    a.tail_k = (const uint16_t*)c.tail_k; a.tail_v = (const uint16_t*)c.tail_v;
+    a.head_n_kept = c.head_n_kept;
+    a.n_kept = c.n_kept; a.n_cap = layout_tokens(c, c.n_kept); a.tail_len = c.tail_len; a.tail_cap = c.tail_cap;
+    a.heads = cfg.batch * cfg.n_kv_heads; a.n_kv_heads = cfg.n_kv_heads;
+    a.n_new = n_rows; a.rows = cfg.n_q_heads / cfg.n_kv_heads * n_rows;
+    a.group = cfg.bits == 16 ? kHeadDim : cfg.group_size;
+    a.sm_scale = cfg.sm_scale;
+    a.row_blocks = a.n_splits = 1;
+    return a;
+}
+
+hipError_t launch_tree(const kvqp_cfg& cfg, const void* q, const void* k_new, const void* v_new, const uint32_t* mask, bool mask_per_batch,
+                       int n_rows, const kvqp_cache& cache, void* out, float* lse, void* ws, const TreePlan& plan, hipStream_t stream) {
+    TreeArgs a = common_args(cfg, cache, n_rows);
+    a.q = (const uint16_t*)q; a.k_new = (const uint16_t*)k_new; a.v_new = (const uint16_t*)v_new;
+    a.mask = mask; a.mask_stride = mask_per_batch ? (size_t)n_rows * ((n_rows + 31) / 32) : 0;
+    a.out = (uint16_t*)out; a.lse = lse; a.part = (float*)ws;
+    a.row_blocks = plan.row_blocks; a.n_splits = plan.n_splits;
+    switch (cfg.bits) {
+        case 2: return tree_bits<2>(a, plan.row_tiles, cfg.key_axis, stream);
+        case 4: return tree_bits<4>(a, plan.row_tiles, cfg.key_axis, stream);
+        case 8: return tree_bits<8>(a, plan.row_tiles, cfg.key_axis, stream);
+        default: return tree_bits<16>(a, plan.row_tiles, cfg.key_axis, stream);
+    }
+}
+
+hipError_t launch_weights(const kvqp_cfg& cfg, const void* q, const float* lse, int n_rows, const kvqp_cache& cache, float* weights, int w_cap,
+                          float decay, hipStream_t stream) {
+    TreeArgs a = common_args(cfg, cache, n_rows);
+    a.q = (const uint16_t*)q; a.lse = const_cast<float*>(lse); a.weights = weights; a.w_cap = w_cap; a.decay = decay;
+    switch (cfg.bits) {
+        case 2: return weights_bits<2>(a, cfg.key_axis, stream);
+        case 4: return weights_bits<4>(a, cfg.key_axis, stream);
+        case 8: return weights_bits<8>(a, cfg.key_axis, stream);
+        default: return weights_bits<16>(a, cfg.key_axis, stream);
+    }
+}
+#endif
+
+}  // namespace kvqp

@@ -19,7 +19,10 @@ KEY_PER_CHANNEL = 0
 KEY_PER_TOKEN = 1
 CACHE_AUTO, CACHE_STREAM, CACHE_KEEP = 0, 1, 2     # kvqp_cfg.decode_cache_hint
 EXPORTS = ["kvqp_cache_sizes", "kvqp_cache_sizes_cap", "kvqp_outlier_sizes", "kvqp_workspace_bytes", "kvqp_compress",
-           "kvqp_compress_ragged", "kvqp_quantize_selected", "kvqp_quantize_selected_ragged", "kvqp_append_tail", "kvqp_append_tail_ragged", "kvqp_decode_attn", "kvqp_decode_attn_static", "kvqp_decode_workspace_init", "kvqp_strerror", "kvqp_version"]
+           "kvqp_compress_ragged", "kvqp_quantize_selected", "kvqp_quantize_selected_ragged", "kvqp_append_tail", "kvqp_append_tail_ragged", "kvqp_decode_attn", "kvqp_decode_attn_static", "kvqp_decode_workspace_init",
+           "kvqp_tree_workspace_bytes", "kvqp_tree_attn", "kvqp_accumulate_weights", "kvqp_evict_workspace_bytes", "kvqp_evict",
+           "kvqp_strerror", "kvqp_version"]
+MOST_ROWS = 256     # KVQP_MOST_ROWS
 
 
 class KvqpError(RuntimeError):
@@ -53,6 +56,7 @@ assert _struct.calcsize("12i2f2i") == C.sizeof(CfgStruct) and _struct.calcsize("
 _lib = None
 # Entry points once more, for this module's own calls: a cfg (and a cache that is only read) goes in as its bytes, a pointer as a number.
 _fn = {}
+_fn_rows = {}       # ... those of several query rows, and eviction
 
 
 def lib():
@@ -83,6 +87,13 @@ def lib():
                                        C.c_void_p, C.c_size_t, C.c_void_p]
         L.kvqp_decode_attn_static.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.POINTER(CacheStruct), C.c_void_p, C.c_void_p]
         L.kvqp_decode_workspace_init.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.kvqp_tree_workspace_bytes.argtypes = L.kvqp_evict_workspace_bytes.argtypes = [C.POINTER(CfgStruct), C.c_int32, C.POINTER(C.c_size_t)]
+        L.kvqp_tree_attn.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                     C.POINTER(CacheStruct), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.kvqp_accumulate_weights.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(CacheStruct),
+                                              C.c_void_p, C.c_int32, C.c_float, C.c_void_p]
+        L.kvqp_evict.argtypes = [C.POINTER(CfgStruct), C.POINTER(CacheStruct), C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                                 C.POINTER(CacheStruct), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         cfg, ptr, size, i32 = C.c_char_p, C.c_void_p, C.c_size_t, C.c_int32
         for name, args in {"kvqp_compress": (cfg, ptr, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr),
                            "kvqp_append_tail": (cfg, ptr, i32, ptr),
@@ -91,6 +102,12 @@ def lib():
             entry = L[name]
             entry.argtypes = args       # (before another thread, which may have loaded the library already, can find it)
             _fn[name] = entry
+        for name, args in {"kvqp_tree_attn": (cfg, ptr, ptr, ptr, ptr, i32, i32, C.c_char_p, ptr, ptr, ptr, size, ptr),
+                           "kvqp_accumulate_weights": (cfg, ptr, ptr, i32, C.c_char_p, ptr, i32, C.c_float, ptr),
+                           "kvqp_evict": (cfg, C.c_char_p, ptr, i32, i32, i32, ptr, ptr, i32, ptr, ptr, size, ptr)}.items():
+            entry = L[name]
+            entry.argtypes = args
+            _fn_rows[name] = entry
         _lib = L
     return _lib
 
@@ -372,3 +389,147 @@ def decode_attn_static(cfg: Cfg, q, cache: Cache, out, stream=None):
     if rc:
         raise KvqpError(rc, "kvqp_decode_attn_static")
     return out
+
+
+# ---- several query rows per call, and eviction ----
+
+def _want(what, t, dtype, shape):
+    """A tensor argument as the library takes it: its type and shape, contiguous, on the GPU."""
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on the GPU is needed, not {t.dtype} {tuple(t.shape)}"
+                         f"{'' if t.is_contiguous() else ', strided'} on {t.device}")
+    return t
+
+
+def _call(name, anchor, others, stream, temporary, args):
+    """Calls an entry point on the device of `anchor`, with that device current; a buffer that this call made itself stays
+    the stream's until the work is done."""
+    import torch
+    for t in others:
+        if t is not None and t.device != anchor.device:
+            raise ValueError(f"{name}: tensors on {anchor.device} and {t.device}")
+    if _lib is None:
+        lib()
+    if anchor.device.index != torch.cuda.current_device():
+        with torch.cuda.device(anchor.device):
+            rc = _fn_rows[name](*args, _stream_handle(stream))
+    else:
+        rc = _fn_rows[name](*args, _stream_handle(stream))
+    if rc:
+        raise KvqpError(rc, name)
+    if temporary is not None and stream is not None:
+        temporary.record_stream(stream)
+
+
+def _sized(entry, cfg: Cfg, n: int) -> int:
+    out = C.c_size_t()
+    rc = getattr(lib(), entry)(C.byref(cfg.struct()), n, C.byref(out))
+    if rc:
+        raise KvqpError(rc, entry)
+    return out.value
+
+
+def tree_workspace_bytes(cfg: Cfg, n_rows: int) -> int:
+    return _sized("kvqp_tree_workspace_bytes", cfg, n_rows)
+
+
+def alloc_tree_workspace(cfg: Cfg, n_rows: int, device="cuda"):
+    """A workspace for tree_attn calls of n_rows rows on caches of any token count."""
+    return alloc_workspace(tree_workspace_bytes(cfg, n_rows), device)
+
+
+def evict_workspace_bytes(cfg: Cfg, n_kept: int) -> int:
+    return _sized("kvqp_evict_workspace_bytes", cfg, n_kept)
+
+
+def alloc_evict_workspace(cfg: Cfg, cache: Cache, device="cuda"):
+    """A workspace for evictions from caches of at most this one's count of packed tokens."""
+    return alloc_workspace(evict_workspace_bytes(cfg, cache.n_kept), device)
+
+
+def tree_mask(parents, device="cuda"):
+    """The mask of a drafted tree: parents[i] is the number of the drafted token that token i follows, or -1 where it follows the
+    sequence itself; a sequence of such sequences makes one mask per batch item.  Every token sees itself and its ancestors.
+    int32 [n, ceil(n / 32)] or [batch, n, ceil(n / 32)]."""
+    import torch
+    several = len(parents) > 0 and hasattr(parents[0], "__len__")
+    out = []
+    for tree in (parents if several else [parents]):
+        seen = []
+        for i, p in enumerate(tree):
+            p = int(p)
+            if not -1 <= p < i:
+                raise ValueError(f"token {i} cannot follow token {p}: a parent comes before its children")
+            seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+        words = (len(seen) + 31) // 32
+        out.append([[_signed32(s >> 32 * w & 0xFFFFFFFF) for w in range(words)] for s in seen])
+    return torch.tensor(out if several else out[0], dtype=torch.int32).to(device)
+
+
+def _signed32(u: int) -> int:
+    return u - (1 << 32) if u >> 31 else u
+
+
+def tree_attn(cfg: Cfg, q, k_new, v_new, mask, cache: Cache, out=None, lse=None, workspace=None, stream=None):
+    """kvqp_tree_attn: q [B,Hq,N,D], k_new / v_new [B,Hkv,N,D] half -> out [B,Hq,N,D] half; mask int32 [N,ceil(N/32)] or
+    [B,N,ceil(N/32)] (tree_mask makes one), or None for a chain; lse float32 [B,Hq,N] or None."""
+    import torch
+    n = int(q.shape[2]) if q.dim() == 4 else 0
+    b, words = cfg.batch, (n + 31) // 32
+    _want("q", q, torch.float16, (b, cfg.n_q_heads, n, cfg.head_dim))
+    _want("k_new", k_new, torch.float16, (b, cfg.n_kv_heads, n, cfg.head_dim))
+    _want("v_new", v_new, torch.float16, (b, cfg.n_kv_heads, n, cfg.head_dim))
+    if mask is not None:
+        _want("mask", mask, torch.int32, (b, n, words) if mask.dim() == 3 else (n, words))
+    if lse is not None:
+        _want("lse", lse, torch.float32, (b, cfg.n_q_heads, n))
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _want("out", out, torch.float16, tuple(q.shape))
+    made = None
+    if workspace is None:
+        workspace = made = alloc_tree_workspace(cfg, n, q.device)
+    _call("kvqp_tree_attn", q, (k_new, v_new, mask, cache.buffers["k_codes"], out, lse, workspace), stream, made,
+          (cfg._bytes(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _addr(mask), int(mask is not None and mask.dim() == 3), n,
+           cache._bytes(), out.data_ptr(), _addr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size()))
+    return out
+
+
+def accumulate_weights(cfg: Cfg, q, lse, cache: Cache, weights, decay: float = 1.0, stream=None):
+    """kvqp_accumulate_weights: q [B,Hq,N,D] half and lse [B,Hq,N] float32 of the last N tail rows' queries; weights float32
+    [B,Hkv,w_cap] is updated in place and returned."""
+    import torch
+    n = int(q.shape[2]) if q.dim() == 4 else 0
+    _want("q", q, torch.float16, (cfg.batch, cfg.n_q_heads, n, cfg.head_dim))
+    _want("lse", lse, torch.float32, (cfg.batch, cfg.n_q_heads, n))
+    _want("weights", weights, torch.float32, (cfg.batch, cfg.n_kv_heads, int(weights.shape[-1])))
+    _call("kvqp_accumulate_weights", q, (lse, weights, cache.buffers["k_codes"]), stream, None,
+          (cfg._bytes(), q.data_ptr(), lse.data_ptr(), n, cache._bytes(), weights.data_ptr(), int(weights.shape[-1]), decay))
+    return weights
+
+
+def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=None, unit: int = 1, idx_out=None, workspace=None,
+          stream=None):
+    """kvqp_evict: the n_keep packed tokens per head with the highest weights (float32 [B,Hkv,w_cap]) go to dst, a cache with
+    buffers of its own, with the tail; weights_out float32 [B,Hkv,w_cap_out], idx_out int32 [B,Hkv,kept] or None.  Returns dst."""
+    import torch
+    _want("weights", weights, torch.float32, (cfg.batch, cfg.n_kv_heads, int(weights.shape[-1])))
+    if weights_out is not None:
+        _want("weights_out", weights_out, torch.float32, (cfg.batch, cfg.n_kv_heads, int(weights_out.shape[-1])))
+    if idx_out is not None:
+        short = cache.n_kept % unit if unit > 1 else 0
+        kept = min(n_keep, cache.n_kept)
+        if cache.head_n_kept is None and n_keep < cache.n_kept and unit > 0:
+            kept = short + (n_keep - short) // unit * unit
+        _want("idx_out", idx_out, torch.int32, (cfg.batch, cfg.n_kv_heads, kept))
+    made = None
+    if workspace is None:
+        workspace = made = alloc_evict_workspace(cfg, cache, weights.device)
+    cs = dst.struct()
+    _call("kvqp_evict", weights, (cache.buffers["k_codes"], dst.buffers["k_codes"], weights_out, idx_out, workspace), stream, made,
+          (cfg._bytes(), cache._bytes(), weights.data_ptr(), int(weights.shape[-1]), n_keep, unit, C.byref(cs), _addr(weights_out),
+           0 if weights_out is None else int(weights_out.shape[-1]), _addr(idx_out), workspace.data_ptr(),
+           workspace.numel() * workspace.element_size()))
+    dst.n_kept, dst.tail_len = cs.n_kept, cs.tail_len
+    return dst
