@@ -129,6 +129,7 @@ hipError_t launch_decode(const kvqp_cfg& cfg, const void* q, const kvqp_cache& c
 // Several query rows per KV head over the cache (kvqp_tree_attn, kvqp_accumulate_weights).
 struct TreePlan {
     int row_tiles, row_blocks;     // rows of a workgroup in tiles of 16, and how many such blocks a KV head's rows make
+    int n_waves;                   // waves of a workgroup
     int n_splits, most_splits;     // token-axis splits of this call, and of any with the same rows
     size_t ws_bytes, ws_bound;     // workspace of this call, and of any
 };

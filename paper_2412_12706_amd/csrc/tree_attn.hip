@@ -47,8 +47,9 @@ union Frag {  // one MFMA 16x16x32 f16 input operand of a lane: 8 halves
     uint4 q;
 };
 
-constexpr int kWaves = 8;
-constexpr int kThreads = 64 * kWaves;
+// The most waves of a workgroup, by its rows in tiles of 16: 16, 12 or 8, as many as the registers of a CU leave room for
+// (124, 168 and 256 per lane).  A launch may use fewer.
+constexpr int most_waves(int rt) { return rt == 1 ? 16 : rt == 2 ? 12 : 8; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegBig = -1.0e30f;     // reference of a row that has seen nothing
@@ -98,29 +99,43 @@ __device__ __forceinline__ float row16_max(float v) {
 }
 
 // ---- codes ----
-// A pair of fields as whole numbers in binary16: with the exponent of 1024 put over a field that begins at bit SH of its
-// half-word (and ends below bit 10) it reads 1024 + 2^SH code.
-template <int SH> __device__ __forceinline__ h2v whole(uint32_t masked) {
-    const h2v x = as_h2(masked | 0x64006400u);
-    if constexpr (SH == 0) return x - splat(1024.0f);
-    else return __builtin_elementwise_fma(x, splat(1.0f / (1 << SH)), splat(-1024.0f / (1 << SH)));
-}
-// Eight consecutive channels of a key row (step s of a lane's 32 channels): c[r] is the pair 8 s + 2 r, + 1.  Fields keep their
-// places where they end below bit 10.
-template <int BITS>
-__device__ __forceinline__ void key_whole(const uint32_t (&w)[BITS], int s, h2v (&c)[4]) {
-    if constexpr (BITS == 8) {
+// Pairs of fields as whole numbers in binary16.  With the exponent of 1024 put over a field that begins at bit SH of its half-word (and
+// ends below bit 10) it reads 1024 + 2^SH code; fields keep their places where they can.  The masks come from vector registers:
+// v_and_or_b32 takes one constant, and masking and setting the exponent are one instruction then.
+template <int BITS> struct Fields {
+    uint32_t mask[BITS == 2 ? 4 : BITS == 4 ? 2 : 1];
+    __device__ __forceinline__ Fields() {
+        if constexpr (BITS == 8) mask[0] = 0x00FF00FFu;
+        else if constexpr (BITS == 4) { mask[0] = 0x000F000Fu; mask[1] = 0x00F000F0u; }
+        else if constexpr (BITS == 2) { mask[0] = 0x00030003u; mask[1] = 0x000C000Cu; mask[2] = 0x00300030u; mask[3] = 0x00C000C0u; }
+        if constexpr (BITS != 16)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) c[r] = whole<0>((w[2 * s + (r >> 1)] >> (8 * (r & 1))) & 0x00FF00FFu);
-    } else if constexpr (BITS == 4) {
-        const uint32_t a = w[s], b = a >> 8;
-        c[0] = whole<0>(a & 0x000F000Fu); c[1] = whole<4>(a & 0x00F000F0u);
-        c[2] = whole<0>(b & 0x000F000Fu); c[3] = whole<4>(b & 0x00F000F0u);
-    } else if constexpr (BITS == 2) {
-        const uint32_t a = w[s >> 1] >> (8 * (s & 1));
-        c[0] = whole<0>(a & 0x00030003u); c[1] = whole<2>(a & 0x000C000Cu);
-        c[2] = whole<4>(a & 0x00300030u); c[3] = whole<6>(a & 0x00C000C0u);
+            for (uint32_t& m : mask) asm("" : "+v"(m));
     }
+    template <int SH> __device__ __forceinline__ static h2v whole(uint32_t w, uint32_t m) {
+        const h2v x = as_h2((w & m) | 0x64006400u);
+        if constexpr (SH == 0) return x - splat(1024.0f);
+        else return __builtin_elementwise_fma(x, splat(1.0f / (1 << SH)), splat(-1024.0f / (1 << SH)));
+    }
+    // eight codes of one (4 bits, 2 bits: half of one) or two words
+    __device__ __forceinline__ void eight(uint32_t a, uint32_t b, h2v* c) const {
+        if constexpr (BITS == 8) {
+            c[0] = whole<0>(a, mask[0]); c[1] = whole<0>(a >> 8, mask[0]);
+            c[2] = whole<0>(b, mask[0]); c[3] = whole<0>(b >> 8, mask[0]);
+        } else if constexpr (BITS == 4) {
+            c[0] = whole<0>(a, mask[0]); c[1] = whole<4>(a, mask[1]);
+            c[2] = whole<0>(a >> 8, mask[0]); c[3] = whole<4>(a >> 8, mask[1]);
+        } else if constexpr (BITS == 2) {
+            c[0] = whole<0>(a, mask[0]); c[1] = whole<2>(a, mask[1]); c[2] = whole<4>(a, mask[2]); c[3] = whole<6>(a, mask[3]);
+        }
+    }
+};
+// Eight consecutive channels of a key row (step s of a lane's 32 channels): c[r] is the pair 8 s + 2 r, + 1.
+template <int BITS>
+__device__ __forceinline__ void key_whole(const Fields<BITS>& f, const uint32_t (&w)[BITS], int s, h2v* c) {
+    if constexpr (BITS == 8) f.eight(w[2 * s], w[2 * s + 1], c);
+    else if constexpr (BITS == 4) f.eight(w[s], 0u, c);
+    else if constexpr (BITS == 2) f.eight((s & 1) ? w[s >> 1] >> 8 : w[s >> 1], 0u, c);
 }
 // Value codes of a 32-token block, channel tile `tile`: pair i holds tokens 4 kb + i and 16 + 4 kb + i of channel 16 tile + n.
 template <int BITS> struct VGeom {
@@ -128,20 +143,10 @@ template <int BITS> struct VGeom {
     static constexpr int kWords = 8 * kWpt;            // a lane's words of a superblock
 };
 template <int BITS>
-__device__ __forceinline__ void value_whole(const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v (&c)[4]) {
-    if constexpr (BITS == 8) {
-        const uint32_t a = w[2 * tile], b = w[2 * tile + 1];
-        c[0] = whole<0>(a & 0x00FF00FFu); c[1] = whole<0>((a >> 8) & 0x00FF00FFu);
-        c[2] = whole<0>(b & 0x00FF00FFu); c[3] = whole<0>((b >> 8) & 0x00FF00FFu);
-    } else if constexpr (BITS == 4) {
-        const uint32_t a = w[tile], b = a >> 8;
-        c[0] = whole<0>(a & 0x000F000Fu); c[1] = whole<4>(a & 0x00F000F0u);
-        c[2] = whole<0>(b & 0x000F000Fu); c[3] = whole<4>(b & 0x00F000F0u);
-    } else if constexpr (BITS == 2) {
-        const uint32_t a = w[tile] >> (8 * odd);
-        c[0] = whole<0>(a & 0x00030003u); c[1] = whole<2>(a & 0x000C000Cu);
-        c[2] = whole<4>(a & 0x00300030u); c[3] = whole<6>(a & 0x00C000C0u);
-    }
+__device__ __forceinline__ void value_whole(const Fields<BITS>& f, const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v* c) {
+    if constexpr (BITS == 8) f.eight(w[2 * tile], w[2 * tile + 1], c);
+    else if constexpr (BITS == 4) f.eight(w[tile], 0u, c);
+    else if constexpr (BITS == 2) f.eight(w[tile] >> (8 * odd), 0u, c);
 }
 
 }  // namespace
@@ -169,8 +174,8 @@ struct TreeArgs {
     int n_kept, n_cap, tail_len, tail_cap;
     int heads, n_kv_heads;
     int rows, n_new;          // R, N
-    int row_blocks, n_splits;
-    int group;                // G
+    int row_blocks, n_splits, n_waves;
+    int group_log2;           // G = 32, 64 or 128
     float sm_scale, decay;
 };
 
@@ -190,11 +195,11 @@ template <int RT> struct QueryTiles {
     uint32_t sums[RT * 64];       // per (row, kb): the sum of the row's 32 channels as binary16 hi, lo
     float factor[RT * 16];        // 2^-k of a row that was scaled by 2^k
 };
-// Rows row0 .. of one head, by all threads of the workgroup; rows past the last are zeros.
-template <int RT, int THREADS>
-__device__ __forceinline__ void stage_queries(const TreeArgs& a, int bh, int row0, QueryTiles<RT>& sq) {
+// Rows row0 .. row0 + n_rows - 1 of one head, by all threads of the workgroup; rows past the head's last are zeros.
+template <int RT>
+__device__ __forceinline__ void stage_queries(const TreeArgs& a, int bh, int row0, int n_rows, int threads, QueryTiles<RT>& sq) {
     const int seg = threadIdx.x & 15;
-    for (int r = threadIdx.x >> 4; r < RT * 16; r += THREADS / 16) {
+    for (int r = threadIdx.x >> 4; r < n_rows; r += threads >> 4) {
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
         if (row0 + r < a.rows) w = *reinterpret_cast<const uint4*>(a.q + ((size_t)bh * a.rows + row0 + r) * kHeadDim + 8 * seg);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -258,15 +263,14 @@ __device__ __forceinline__ void load_keys(const TreeArgs& a, int bh, int blk, in
     }
     if constexpr (BITS != 16) {
         if constexpr (AXIS == KVQP_KEY_PER_CHANNEL) {
-            const size_t groups = (size_t)(a.n_cap + a.group - 1) / a.group;
-            const size_t row = ((size_t)bh * groups + (32 * blk) / a.group) * (kHeadDim / 2) + lane;
+            const size_t groups = (size_t)((a.n_cap + (1 << a.group_log2) - 1) >> a.group_log2);
+            const size_t row = ((size_t)bh * groups + (size_t)((32 * blk) >> a.group_log2)) * (kHeadDim / 2) + lane;
             k.scale[0] = reinterpret_cast<const uint32_t*>(a.k_scale)[row];
             k.zero[0] = reinterpret_cast<const uint32_t*>(a.k_zero)[row];
         } else {
-            const int cg = kHeadDim / a.group;
 #pragma unroll
             for (int H = 0; H < 2; ++H) {
-                const size_t at = (tok + 16 * H) * cg + kb * 32 / a.group;
+                const size_t at = ((tok + 16 * H) << (7 - a.group_log2)) + (size_t)((32 * kb) >> a.group_log2);
                 k.scale[H] = a.k_scale[at];
                 k.zero[H] = a.k_zero[at];
             }
@@ -274,95 +278,109 @@ __device__ __forceinline__ void load_keys(const TreeArgs& a, int bh, int blk, in
     }
 }
 
-// Operands of a block's key product, the same for every row tile.
-template <int BITS, int AXIS> struct KeyOperand {
-    static constexpr bool kChannel = BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL;
-    static constexpr bool kToken = BITS != 16 && AXIS == KVQP_KEY_PER_TOKEN;
-    Frag a[2][4];                     // codes, code * s hi parts, or the keys themselves
-    Frag b[kToken ? 2 : 1][kToken ? 4 : 1];   // code * s lo parts
-    Frag s[kChannel ? 4 : 1], z[kChannel ? 4 : 1];   // the group's scales and zeros of the lane's channels
-    uint32_t zt[2];                   // the tokens' zeros, twice
-};
+// Logits of a block for RT row tiles, before the rows' factors: acc[rt][H][i] is token 16 H + 4 kb + i of row 16 rt + n.  The four
+// steps of eight channels run outermost, so that only one step's operands are held beside the sums.
+template <int BITS, int AXIS, int RT>
+__device__ __forceinline__ void key_product(const Fields<BITS>& fields, const KeyWords<BITS, AXIS>& k, const uint4* frag, const uint32_t* sums, ScaleStrip& strip, int lane, f4v (&acc)[RT][2]) {
+    constexpr bool kChannel = BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL, kToken = BITS != 16 && AXIS == KVQP_KEY_PER_TOKEN;
+    const int kb = lane >> 4;
+    auto query = [&](int rt, int s) {
+        Frag q;
+        q.q = frag[(4 * rt + s) * 64 + lane];
+        return q;
+    };
+    if constexpr (kChannel) {
+        // q . z first, the same for all tokens of the group: both tiles' sums begin with it
+        f4v az[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) az[rt] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            Frag z;
+            z.q = *reinterpret_cast<const uint4*>(&strip.k_zero[16 * kb + 4 * s]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) az[rt] = mfma(z, query(rt, s), az[rt]);
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = az[rt];
+    } else {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        Frag a[2];
+        if constexpr (BITS == 16) {
+#pragma unroll
+            for (int H = 0; H < 2; ++H)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) a[H].u[r] = k.w[H][4 * s + r];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const Frag q = query(rt, s);
+                acc[rt][0] = mfma(a[0], q, acc[rt][0]); acc[rt][1] = mfma(a[1], q, acc[rt][1]);
+            }
+        } else if constexpr (kChannel) {
+            Frag sc;
+            sc.q = *reinterpret_cast<const uint4*>(&strip.k_scale[16 * kb + 4 * s]);
+#pragma unroll
+            for (int H = 0; H < 2; ++H) key_whole<BITS>(fields, k.w[H], s, a[H].h);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const Frag q = query(rt, s);
+                Frag hi, lo;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    hi.h[r] = q.h[r] * sc.h[r];
+                    lo.h[r] = __builtin_elementwise_fma(q.h[r], sc.h[r], -hi.h[r]);
+                }
+                acc[rt][0] = mfma(a[0], hi, acc[rt][0]); acc[rt][1] = mfma(a[1], hi, acc[rt][1]);
+                acc[rt][0] = mfma(a[0], lo, acc[rt][0]); acc[rt][1] = mfma(a[1], lo, acc[rt][1]);
+            }
+        } else if constexpr (kToken) {
+            Frag b[2];
+#pragma unroll
+            for (int H = 0; H < 2; ++H) {
+                const h2v sc = as_h2(k.scale[H] * 0x10001u);
+                h2v c[4];
+                key_whole<BITS>(fields, k.w[H], s, c);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    a[H].h[r] = c[r] * sc;
+                    b[H].h[r] = __builtin_elementwise_fma(c[r], sc, -a[H].h[r]);
+                }
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const Frag q = query(rt, s);
+                acc[rt][0] = mfma(a[0], q, acc[rt][0]); acc[rt][1] = mfma(a[1], q, acc[rt][1]);
+                acc[rt][0] = mfma(b[0], q, acc[rt][0]); acc[rt][1] = mfma(b[1], q, acc[rt][1]);
+            }
+        }
+    }
+    if constexpr (kToken) {
+        Frag z[2];
+#pragma unroll
+        for (int H = 0; H < 2; ++H) { z[H].u[0] = k.zero[H] * 0x10001u; z[H].u[1] = z[H].u[2] = z[H].u[3] = 0u; }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            Frag qs;
+            qs.u[0] = sums[rt * 64 + lane]; qs.u[1] = qs.u[2] = qs.u[3] = 0u;
+            acc[rt][0] = mfma(z[0], qs, acc[rt][0]); acc[rt][1] = mfma(z[1], qs, acc[rt][1]);
+        }
+    }
+}
+// Keys per channel: the group's scales and zeros to the strip, whence every lane reads its 32 channels.
 template <int BITS, int AXIS>
-__device__ __forceinline__ void key_operand(const KeyWords<BITS, AXIS>& k, ScaleStrip& strip, int lane, KeyOperand<BITS, AXIS>& o) {
-    using O = KeyOperand<BITS, AXIS>;
-    if constexpr (O::kChannel) {
+__device__ __forceinline__ void strip_keys(const KeyWords<BITS, AXIS>& k, ScaleStrip& strip, int lane) {
+    if constexpr (BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL) {
         lds_order();
         strip.k_scale[lane] = k.scale[0];
         strip.k_zero[lane] = k.zero[0];
         lds_order();
-        const int kb = lane >> 4;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            o.s[s].q = *reinterpret_cast<const uint4*>(&strip.k_scale[16 * kb + 4 * s]);
-            o.z[s].q = *reinterpret_cast<const uint4*>(&strip.k_zero[16 * kb + 4 * s]);
-        }
-    }
-#pragma unroll
-    for (int H = 0; H < 2; ++H) {
-        if constexpr (O::kToken) {
-            const h2v sc = as_h2(k.scale[H] * 0x10001u);
-            o.zt[H] = k.zero[H] * 0x10001u;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                h2v c[4];
-                key_whole<BITS>(k.w[H], s, c);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    o.a[H][s].h[r] = c[r] * sc;
-                    o.b[H][s].h[r] = __builtin_elementwise_fma(c[r], sc, -o.a[H][s].h[r]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if constexpr (BITS == 16) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o.a[H][s].u[r] = k.w[H][4 * s + r];
-                } else {
-                    h2v c[4];
-                    key_whole<BITS>(k.w[H], s, c);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o.a[H][s].h[r] = c[r];
-                }
-            }
-        }
     }
 }
-// Logits of one row tile: x = (acc + base) * the row's factor.
-template <int BITS, int AXIS, int RT>
-__device__ __forceinline__ void key_product(const KeyOperand<BITS, AXIS>& o, const QueryTiles<RT>& sq, int rt, int lane, f4v (&acc)[2], float& base) {
-    using O = KeyOperand<BITS, AXIS>;
-    acc[0] = acc[1] = f4v{0.f, 0.f, 0.f, 0.f};
-    f4v az = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        Frag q;
-        q.q = sq.frag[(4 * rt + s) * 64 + lane];
-        if constexpr (O::kChannel) {
-            Frag hi, lo;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                hi.h[r] = q.h[r] * o.s[s].h[r];
-                lo.h[r] = __builtin_elementwise_fma(q.h[r], o.s[s].h[r], -hi.h[r]);
-            }
-            az = mfma(o.z[s], q, az);
-            acc[0] = mfma(o.a[0][s], hi, acc[0]); acc[1] = mfma(o.a[1][s], hi, acc[1]);
-            acc[0] = mfma(o.a[0][s], lo, acc[0]); acc[1] = mfma(o.a[1][s], lo, acc[1]);
-        } else {
-            acc[0] = mfma(o.a[0][s], q, acc[0]); acc[1] = mfma(o.a[1][s], q, acc[1]);
-            if constexpr (O::kToken) { acc[0] = mfma(o.b[0][s], q, acc[0]); acc[1] = mfma(o.b[1][s], q, acc[1]); }
-        }
-    }
-    if constexpr (O::kToken) {
-        Frag qs, z;
-        qs.u[0] = sq.sums[rt * 64 + lane]; qs.u[1] = qs.u[2] = qs.u[3] = 0u;
-        z.u[1] = z.u[2] = z.u[3] = 0u;
-#pragma unroll
-        for (int H = 0; H < 2; ++H) { z.u[0] = o.zt[H]; acc[H] = mfma(z, qs, acc[H]); }
-    }
-    base = O::kChannel ? az[0] : 0.0f;
-}
+
 // ---- state of a wave's rows ----
 template <int RT> struct RowState {
     f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n
@@ -377,14 +395,17 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
         for (int t = 0; t < 8; ++t) st.o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
     }
 }
-// Moves references where x (logits of a block in log2, -inf where unseen) has passed them, turns x into weights, adds them up.
+// Moves references where logits have passed them, turns acc (a block's logits before the rows' factors, -inf where unseen) into weights x
+// and adds them up.
 template <int RT>
-__device__ __forceinline__ void softmax_step(RowState<RT>& st, float (&x)[RT][8]) {
+__device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[RT][2], const float (&factor)[RT], float (&x)[RT][8]) {
     bool past = false;
     float top[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        top[rt] = fmaxf(fmaxf(fmaxf(x[rt][0], x[rt][1]), fmaxf(x[rt][2], x[rt][3])), fmaxf(fmaxf(x[rt][4], x[rt][5]), fmaxf(x[rt][6], x[rt][7])));
+        const float m0 = fmaxf(fmaxf(acc[rt][0][0], acc[rt][0][1]), fmaxf(acc[rt][0][2], acc[rt][0][3]));
+        const float m1 = fmaxf(fmaxf(acc[rt][1][0], acc[rt][1][1]), fmaxf(acc[rt][1][2], acc[rt][1][3]));
+        top[rt] = fmaxf(m0, m1) * factor[rt];
         past |= top[rt] > st.ref[rt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
@@ -403,26 +424,26 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, float (&x)[RT][8]
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x[rt][j] = __builtin_amdgcn_exp2f(x[rt][j] - st.ref[rt]);
+            x[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], -st.ref[rt]));
             st.sum[rt] += x[rt][j];
         }
 }
 // Weights as operands: pair i holds tokens 4 kb + i and 16 + 4 kb + i; hi + lo parts, cut toward zero.
 struct WeightOperand { Frag hi, lo; };
-__device__ __forceinline__ void weight_operand(const float (&p)[8], WeightOperand& o) {
+// (minus is -1 that the compiler does not know: the widening and the exact subtraction are one v_fma_mix_f32)
+__device__ __forceinline__ void weight_operand(const float (&p)[8], float minus, WeightOperand& o) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         o.hi.u[i] = pack_rtz(p[i], p[4 + i]);
-        o.lo.u[i] = pack_rtz(p[i] - (float)o.hi.h[i][0], p[4 + i] - (float)o.hi.h[i][1]);
+        o.lo.u[i] = pack_rtz(__builtin_fmaf((float)o.hi.h[i][0], minus, p[i]), __builtin_fmaf((float)o.hi.h[i][1], minus, p[4 + i]));
     }
 }
 template <int RT>
 __device__ __forceinline__ void value_product(RowState<RT>& st, const Frag& v, int tile, const WeightOperand (&p)[RT]) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        st.o[rt][tile] = mfma(v, p[rt].hi, st.o[rt][tile]);
-        st.o[rt][tile] = mfma(v, p[rt].lo, st.o[rt][tile]);
-    }
+    for (int rt = 0; rt < RT; ++rt) st.o[rt][tile] = mfma(v, p[rt].hi, st.o[rt][tile]);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) st.o[rt][tile] = mfma(v, p[rt].lo, st.o[rt][tile]);
 }
 
 // ---- values of a packed block ----
@@ -442,8 +463,7 @@ __device__ __forceinline__ void load_values(const TreeArgs& a, int bh, int blk, 
     }
     if constexpr (BITS != 16) {
         // 32 tokens' scales are 32 D / G numbers in a row; lanes past the last repeat it
-        const int cg = kHeadDim / a.group;
-        const size_t at = ((size_t)bh * a.n_cap + 32 * blk) * cg / 2 + min(lane, 16 * cg - 1);
+        const size_t at = ((((size_t)bh * a.n_cap + 32 * blk) << (7 - a.group_log2)) >> 1) + min(lane, (16 << (7 - a.group_log2)) - 1);
         v.scale = reinterpret_cast<const uint32_t*>(a.v_scale)[at];
         v.zero = reinterpret_cast<const uint32_t*>(a.v_zero)[at];
     }
@@ -451,14 +471,14 @@ __device__ __forceinline__ void load_values(const TreeArgs& a, int bh, int blk, 
 // Scales and zeros to the strip, in the order in which the lanes of a token's block want them.
 template <int BITS>
 __device__ __forceinline__ void strip_values(const TreeArgs& a, const ValueWords<BITS>& v, ScaleStrip& strip, int lane) {
-    const int cg = kHeadDim / a.group;
+    const int cg_log2 = 7 - a.group_log2;
     uint16_t* s = reinterpret_cast<uint16_t*>(strip.v_scale);
     uint16_t* z = reinterpret_cast<uint16_t*>(strip.v_zero);
     lds_order();
-    if (lane < 16 * cg) {
+    if (lane < 16 << cg_log2) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int t = (2 * lane + e) / cg, g = (2 * lane + e) % cg;
+            const int t = (2 * lane + e) >> cg_log2, g = (2 * lane + e) & ((1 << cg_log2) - 1);
             const int at = g * 32 + (t & 15) * 2 + (t >> 4);
             s[at] = (uint16_t)(v.scale >> (16 * e));
             z[at] = (uint16_t)(v.zero >> (16 * e));
@@ -475,34 +495,37 @@ struct __align__(16) PlainTile { uint16_t v[32 * kPlainStride]; };
 union WaveScratch { ScaleStrip strip; PlainTile tile; };
 template <int RT> struct MergeSlot { f4v o[RT][8][64]; float2 m[RT][64]; };      // outputs; reference and sum
 template <int RT> union __align__(16) TreeShared {
-    struct { QueryTiles<RT> sq; WaveScratch wave[kWaves]; } run;
-    MergeSlot<RT> merge[kWaves / 2];
+    struct { QueryTiles<RT> sq; WaveScratch wave[most_waves(RT)]; } run;
+    MergeSlot<RT> merge[most_waves(RT) / 2];
 };
 
 template <int BITS, int AXIS, int RT>
-__global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const TreeArgs a) {
+__global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_attn(const TreeArgs a) {
     __shared__ TreeShared<RT> sh;
     QueryTiles<RT>& sq = sh.run.sq;
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 15, kb = lane >> 4;
+    const int n = lane & 15, kb = lane >> 4, waves = blockDim.x >> 6;
     // Workgroups go to the eight dies in turn: the row blocks of one stretch of a cache get numbers eight apart, so that
     // they run on one die at about the same time and share what its L2 holds.
     const int pair = blockIdx.x / (8 * a.row_blocks) * 8 + blockIdx.x % 8, rb = blockIdx.x / 8 % a.row_blocks;
     if (pair >= a.heads * a.n_splits) return;
     const int bh = pair / a.n_splits, split = pair % a.n_splits;
     const int row0 = rb * RT * 16;
-    stage_queries<RT, kThreads>(a, bh, row0, sq);
+    stage_queries<RT>(a, bh, row0, RT * 16, 64 * waves, sq);
 
     const int n_tok = head_tokens(a, bh);
     const int packed = (n_tok + 31) / 32, tail = (a.tail_len + 31) / 32, fresh = (a.n_new + 31) / 32;
     const int units = packed + tail + fresh;
-    const int u0 = (int)((long long)units * split / a.n_splits), u1 = (int)((long long)units * (split + 1) / a.n_splits);
+    const int share = (int)((unsigned)units / (unsigned)a.n_splits), rest = units - share * a.n_splits;
+    const int u0 = share * split + min(split, rest), u1 = u0 + share + (split < rest ? 1 : 0);
     ScaleStrip& strip = sh.run.wave[wave].strip;
 
     RowState<RT> st;
     clear(st);
+    float minus = -1.0f;
+    asm("" : "+s"(minus));
     __syncthreads();
     const float c_q = a.sm_scale * kLog2e;
     float factor[RT];
@@ -511,6 +534,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
 
     // ---- packed blocks ----
     {
+        const Fields<BITS> fields;
         const int end = min(u1, packed);
         int blk = u0 + wave;
         if (blk < end) {
@@ -519,37 +543,26 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
             load_keys<BITS, AXIS>(a, bh, blk, lane, kw);
             load_values<BITS>(a, bh, blk, lane, vw);
 #pragma unroll 1
-            for (; blk < end; blk += kWaves) {
-                const int next = min(blk + kWaves, end - 1);
-                float x[RT][8];
-                {
-                    KeyOperand<BITS, AXIS> ko;
-                    key_operand<BITS, AXIS>(kw, strip, lane, ko);
-                    load_keys<BITS, AXIS>(a, bh, next, lane, kw);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        f4v acc[2];
-                        float base;
-                        key_product<BITS, AXIS, RT>(ko, sq, rt, lane, acc, base);
-                        base *= factor[rt];
-#pragma unroll
-                        for (int H = 0; H < 2; ++H)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) x[rt][4 * H + i] = __builtin_fmaf(acc[H][i], factor[rt], base);
-                    }
-                }
+            for (; blk < end; blk += waves) {
+                const int next = min(blk + waves, end - 1);
+                f4v acc[RT][2];
+                strip_keys<BITS, AXIS>(kw, strip, lane);
+                key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
+                load_keys<BITS, AXIS>(a, bh, next, lane, kw);
                 if (32 * blk + 32 > n_tok) {     // (uniform) the head's last block: tokens past its count are unseen
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
-                            if (32 * blk + 16 * (j >> 2) + 4 * kb + (j & 3) >= n_tok) x[rt][j] = -INFINITY;
+                            if (32 * blk + 16 * (j >> 2) + 4 * kb + (j & 3) >= n_tok) acc[rt][j >> 2][j & 3] = -INFINITY;
                 }
-                softmax_step<RT>(st, x);
+                float x[RT][8];
+                softmax_step<RT>(st, acc, factor, x);
                 WeightOperand p[RT];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], p[rt]);
+                for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
                 if constexpr (BITS != 16) strip_values<BITS>(a, vw, strip, lane);
+                Frag s, z;
 #pragma unroll
                 for (int tile = 0; tile < 8; ++tile) {
                     Frag v;
@@ -558,11 +571,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
                         for (int i = 0; i < 4; ++i) v.u[i] = vw.w[4 * tile + i];
                     } else {
                         h2v c[4];
-                        value_whole<BITS>(vw.w, tile, blk & 1, c);
-                        Frag s, z;
-                        const int g = tile * 16 / a.group;
-                        s.q = *reinterpret_cast<const uint4*>(&strip.v_scale[16 * g + 4 * kb]);
-                        z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * g + 4 * kb]);
+                        value_whole<BITS>(fields, vw.w, tile, blk & 1, c);
+                        if ((tile & 1) == 0) {       // (a group has at least two tiles)
+                            const int g = (16 * tile) >> a.group_log2;
+                            s.q = *reinterpret_cast<const uint4*>(&strip.v_scale[16 * g + 4 * kb]);
+                            z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * g + 4 * kb]);
+                        }
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v.h[i] = __builtin_elementwise_fma(c[i], s.h[i], z.h[i]);
                     }
@@ -578,22 +592,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
         PlainTile& tile_v = sh.run.wave[wave].tile;
         const int first = max(u0, packed);
 #pragma unroll 1
-        for (int u = first + wave; u < u1; u += kWaves) {
+        for (int u = first + wave; u < u1; u += waves) {
             const bool drafted = u >= packed + tail;
             const int t0 = 32 * (drafted ? u - packed - tail : u - packed), len = drafted ? a.n_new : a.tail_len;
             const size_t row = drafted ? (size_t)bh * a.n_new : (size_t)bh * a.tail_cap;
             const uint16_t* kp = (drafted ? a.k_new : a.tail_k) + row * kHeadDim;
             const uint16_t* vp = (drafted ? a.v_new : a.tail_v) + row * kHeadDim;
-            KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
-#pragma unroll
-            for (int H = 0; H < 2; ++H) {
-                const uint16_t* p = kp + (size_t)min(t0 + 16 * H + n, len - 1) * kHeadDim + 32 * kb;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
-                    kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
-                }
-            }
             lds_order();
             bool odd_value = false;       // a value that is not finite
 #pragma unroll
@@ -607,15 +611,21 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
                 *reinterpret_cast<uint4*>(&tile_v.v[t * kPlainStride + 8 * n]) = w;
             }
             lds_order();
-            float x[RT][8];
+            KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
+#pragma unroll
+            for (int H = 0; H < 2; ++H) {
+                const uint16_t* p = kp + (size_t)min(t0 + 16 * H + n, len - 1) * kHeadDim + 32 * kb;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
+                    kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
+                }
+            }
+            f4v acc[RT][2];
             {
-                KeyOperand<16, KVQP_KEY_PER_CHANNEL> ko;
-                key_operand<16, KVQP_KEY_PER_CHANNEL>(kw, strip, lane, ko);
+                key_product<16, KVQP_KEY_PER_CHANNEL, RT>(Fields<16>(), kw, sq.frag, sq.sums, strip, lane, acc);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    f4v acc[2];
-                    float base;
-                    key_product<16, KVQP_KEY_PER_CHANNEL, RT>(ko, sq, rt, lane, acc, base);
                     // which of the block's 32 tokens the row sees
                     uint32_t seen = t0 + 32 <= len ? 0xFFFFFFFFu : (1u << (len - t0)) - 1u;
                     if (drafted) {
@@ -625,43 +635,58 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
                         else seen &= i >= t0 + 31 ? 0xFFFFFFFFu : i < t0 ? 0u : (2u << (i - t0)) - 1u;
                     }
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float l = acc[j >> 2][j & 3] * factor[rt];
-                        x[rt][j] = (seen >> (16 * (j >> 2) + 4 * kb + (j & 3))) & 1u ? l : -INFINITY;
-                    }
+                    for (int j = 0; j < 8; ++j)
+                        if (!((seen >> (16 * (j >> 2) + 4 * kb + (j & 3))) & 1u)) acc[rt][j >> 2][j & 3] = -INFINITY;
                 }
             }
-            softmax_step<RT>(st, x);
+            float x[RT][8];
+            softmax_step<RT>(st, acc, factor, x);
+            WeightOperand p[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
             if (drafted && __builtin_amdgcn_ballot_w64(odd_value) != 0ull) {
-                // Values that are not finite reach only the rows that see them: a weight of 0 would make them NaN in the matrix product.
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
+                // Values that are not finite reach only the rows that see them (a weight of 0 would make them NaN in the matrix product):
+                // they are added here, one token at a time, and taken out of the tile.
 #pragma unroll 1
-                        for (int b = 0; b < 4; ++b) {
-                            const float p = __shfl(x[rt][j], 16 * b + n);
-                            const uint16_t* v = &tile_v.v[(16 * (j >> 2) + 4 * b + (j & 3)) * kPlainStride + 4 * kb];
+                for (int t = 0; t < 32; ++t) {
+                    const int j = 4 * (t >> 4) + (t & 3);
+                    float w[RT];
 #pragma unroll
-                            for (int t = 0; t < 8; ++t)
+                    for (int rt = 0; rt < RT; ++rt) {
+                        float mine = x[rt][0];
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    st.o[rt][t][i] = p != 0.0f ? __builtin_fmaf(p, half_to_float(v[16 * t + i]), st.o[rt][t][i]) : st.o[rt][t][i];
-                        }
-            } else {
-                WeightOperand p[RT];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], p[rt]);
-#pragma unroll
-                for (int tile = 0; tile < 8; ++tile) {
-                    Frag v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t lo = tile_v.v[(4 * kb + i) * kPlainStride + 16 * tile + n], hi = tile_v.v[(16 + 4 * kb + i) * kPlainStride + 16 * tile + n];
-                        v.u[i] = lo | (hi << 16);
+                        for (int e = 1; e < 8; ++e) mine = j == e ? x[rt][e] : mine;
+                        w[rt] = __shfl(mine, 16 * ((t >> 2) & 3) + n);
                     }
-                    value_product<RT>(st, v, tile, p);
+                    const uint16_t* row = &tile_v.v[t * kPlainStride + 4 * kb];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t u = row[16 * c + i];
+                            const float v = (u & 0x7C00u) == 0x7C00u ? half_to_float((uint16_t)u) : 0.0f;
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) st.o[rt][c][i] += w[rt] != 0.0f ? w[rt] * v : 0.0f;
+                        }
                 }
+                lds_order();
+#pragma unroll 1
+                for (int t = 0; t < 32; ++t) {
+                    uint32_t* two = reinterpret_cast<uint32_t*>(&tile_v.v[t * kPlainStride + 2 * lane]);
+                    const uint32_t u = *two;
+                    *two = ((u & 0x7C00u) == 0x7C00u ? 0u : u & 0xFFFFu) | ((u & 0x7C000000u) == 0x7C000000u ? 0u : u & 0xFFFF0000u);
+                }
+                lds_order();
+            }
+#pragma unroll
+            for (int tile = 0; tile < 8; ++tile) {
+                Frag v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t lo = tile_v.v[(4 * kb + i) * kPlainStride + 16 * tile + n], hi = tile_v.v[(16 + 4 * kb + i) * kPlainStride + 16 * tile + n];
+                    v.u[i] = lo | (hi << 16);
+                }
+                value_product<RT>(st, v, tile, p);
             }
         }
     }
@@ -670,9 +695,10 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) st.sum[rt] = rows4_add(st.sum[rt]);
 #pragma unroll 1
-    for (int half = kWaves / 2; half >= 1; half >>= 1) {
+    for (int left = waves; left > 1;) {
+        const int half = (left + 1) / 2;
         __syncthreads();
-        if (wave >= half && wave < 2 * half) {
+        if (wave >= half && wave < left) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
@@ -681,7 +707,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
             }
         }
         __syncthreads();
-        if (wave < half) {
+        if (wave < left - half) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const float2 other = sh.merge[wave].m[rt][lane];
@@ -693,6 +719,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 4 : 2) void tree_attn(const Tre
                 for (int t = 0; t < 8; ++t) st.o[rt][t] = st.o[rt][t] * f + sh.merge[wave].o[rt][t][lane] * g;
             }
         }
+        left = half;
     }
     if (wave != 0) return;
     if (a.n_splits > 1) {
@@ -777,13 +804,15 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeArgs a) {
 constexpr int kWeightRT = 4, kWeightWaves = 4, kWeightThreads = 64 * kWeightWaves;
 
 template <int BITS, int AXIS>
-__device__ __forceinline__ void weigh(const KeyOperand<BITS, AXIS>& ko, const TreeArgs& a, int bh, QueryTiles<kWeightRT>& sq,
+__device__ __forceinline__ void weigh(const KeyWords<BITS, AXIS>& kw, const TreeArgs& a, int bh, QueryTiles<kWeightRT>& sq, ScaleStrip& strip,
                                       float (&s_lse)[kWeightRT * 16], bool live, int tail0, float (&cs)[8]) {
     const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
+    const Fields<BITS> fields;
 #pragma unroll 1
     for (int row0 = 0; row0 < a.rows; row0 += kWeightRT * 16) {
         if (row0) __syncthreads();
-        stage_queries<kWeightRT, kWeightThreads>(a, bh, row0, sq);
+        const int tiles = min(kWeightRT, (a.rows - row0 + 15) / 16);
+        stage_queries<kWeightRT>(a, bh, row0, 16 * tiles, kWeightThreads, sq);
         if (threadIdx.x < kWeightRT * 16) {
             const int r = row0 + threadIdx.x;
             const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;
@@ -791,19 +820,17 @@ __device__ __forceinline__ void weigh(const KeyOperand<BITS, AXIS>& ko, const Tr
         }
         __syncthreads();
         if (!live) continue;
-        const int tiles = min(kWeightRT, (a.rows - row0 + 15) / 16);
 #pragma unroll 1
         for (int rt = 0; rt < tiles; ++rt) {
-            f4v acc[2];
-            float base;
-            key_product<BITS, AXIS, kWeightRT>(ko, sq, rt, lane, acc, base);
+            f4v acc[1][2];
+            key_product<BITS, AXIS, 1>(fields, kw, sq.frag + rt * 256, sq.sums + rt * 64, strip, lane, acc);
             // (in natural units up to the exponential: sm_scale and the rows' powers of two are exact)
             const float f = sq.factor[16 * rt + n] * a.sm_scale;
-            base = __builtin_fmaf(base, f, -s_lse[16 * rt + n]);
+            const float base = -s_lse[16 * rt + n];
             const int i = (row0 + 16 * rt + n) % a.n_new;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j >> 2][j & 3], f, base) * kLog2e);
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[0][j >> 2][j & 3], f, base) * kLog2e);
                 // (tail0 < 0: packed tokens, which every row sees)
                 if (tail0 >= 0 && tail0 + 16 * (j >> 2) + 4 * kb + (j & 3) > a.tail_len - a.n_new + i) p = 0.0f;
                 cs[j] += p;
@@ -834,15 +861,13 @@ __global__ __launch_bounds__(kWeightThreads) void add_weights(const TreeArgs a) 
     // (a workgroup may have both kinds of blocks: each goes through the rows by itself, and the other's waves only help to stage them)
     const int u_first = blockIdx.x * kWeightWaves, u_last = min(u_first + kWeightWaves, units) - 1;
     if (u_first < packed) {
-        KeyOperand<BITS, AXIS> ko;
         KeyWords<BITS, AXIS> kw;
         load_keys<BITS, AXIS>(a, bh, min(u, packed - 1), lane, kw);
-        key_operand<BITS, AXIS>(kw, s_strip[wave], lane, ko);
-        weigh<BITS, AXIS>(ko, a, bh, sq, s_lse, live && !is_tail, -1, cs);
+        strip_keys<BITS, AXIS>(kw, s_strip[wave], lane);
+        weigh<BITS, AXIS>(kw, a, bh, sq, s_strip[wave], s_lse, live && !is_tail, -1, cs);
     }
     if (u_last >= packed) {
         if (u_first < packed) __syncthreads();
-        KeyOperand<16, KVQP_KEY_PER_CHANNEL> ko;
         KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
         const int tt = is_tail && live ? t0 : 0;
 #pragma unroll
@@ -854,8 +879,7 @@ __global__ __launch_bounds__(kWeightThreads) void add_weights(const TreeArgs a) 
                 kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
             }
         }
-        key_operand<16, KVQP_KEY_PER_CHANNEL>(kw, s_strip[wave], lane, ko);
-        weigh<16, KVQP_KEY_PER_CHANNEL>(ko, a, bh, sq, s_lse, live && is_tail, t0, cs);
+        weigh<16, KVQP_KEY_PER_CHANNEL>(kw, a, bh, sq, s_strip[wave], s_lse, live && is_tail, t0, cs);
     }
     if (!live) return;
     // lane i of a row of 16 lanes stores token 4 kb + i of both tiles
@@ -876,7 +900,7 @@ __global__ __launch_bounds__(kWeightThreads) void add_weights(const TreeArgs a) 
 template <int BITS, int AXIS, int RT>
 hipError_t run_tree(const TreeArgs& a, hipStream_t stream) {
     const int pairs = (a.heads * a.n_splits + 7) / 8 * 8;
-    tree_attn<BITS, AXIS, RT><<<dim3(pairs * a.row_blocks), dim3(kThreads), 0, stream>>>(a);
+    tree_attn<BITS, AXIS, RT><<<dim3(pairs * a.row_blocks), dim3(64 * a.n_waves), 0, stream>>>(a);
     if (a.n_splits > 1) tree_merge<RT><<<dim3((a.heads * a.row_blocks * RT * 512 + 255) / 256), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -926,12 +950,11 @@ TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len) {
     const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_rows;
     p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     p.row_blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
-    // one workgroup of eight waves per CU, two where the rows' registers leave room for them
     const long long base = (long long)cfg.batch * cfg.n_kv_heads * p.row_blocks;
-    const long long want = (p.row_tiles == 1 ? 512 : 256) / base;
-    p.most_splits = (int)std::max(1LL, std::min(want, 64LL));
+    p.n_waves = most_waves(p.row_tiles);
+    p.most_splits = (int)std::max(1LL, std::min(256 / base, 64LL));
     const int units = (n_kept + 31) / 32 + (tail_len + 31) / 32 + (n_rows + 31) / 32;
-    p.n_splits = std::max(1, std::min(p.most_splits, (units + kWaves - 1) / kWaves));
+    p.n_splits = std::max(1, std::min(p.most_splits, (units + p.n_waves - 1) / p.n_waves));
     const size_t one = (size_t)base * (16 * p.row_tiles) * (kHeadDim + 2) * sizeof(float);
     p.ws_bytes = p.n_splits > 1 ? one * p.n_splits : 0;
     p.ws_bound = p.most_splits > 1 ? one * p.most_splits : 0;
@@ -948,7 +971,7 @@ static TreeArgs common_args(const kvqp_cfg& cfg, const kvqp_cache& c, int n_rows
     a.n_kept = c.n_kept; a.n_cap = layout_tokens(c, c.n_kept); a.tail_len = c.tail_len; a.tail_cap = c.tail_cap;
     a.heads = cfg.batch * cfg.n_kv_heads; a.n_kv_heads = cfg.n_kv_heads;
     a.n_new = n_rows; a.rows = cfg.n_q_heads / cfg.n_kv_heads * n_rows;
-    a.group = cfg.bits == 16 ? kHeadDim : cfg.group_size;
+    a.group_log2 = cfg.bits == 16 || cfg.group_size == 128 ? 7 : cfg.group_size == 64 ? 6 : 5;
     a.sm_scale = cfg.sm_scale;
     a.row_blocks = a.n_splits = 1;
     return a;
@@ -960,7 +983,7 @@ hipError_t launch_tree(const kvqp_cfg& cfg, const void* q, const void* k_new, co
     a.q = (const uint16_t*)q; a.k_new = (const uint16_t*)k_new; a.v_new = (const uint16_t*)v_new;
     a.mask = mask; a.mask_stride = mask_per_batch ? (size_t)n_rows * ((n_rows + 31) / 32) : 0;
     a.out = (uint16_t*)out; a.lse = lse; a.part = (float*)ws;
-    a.row_blocks = plan.row_blocks; a.n_splits = plan.n_splits;
+    a.row_blocks = plan.row_blocks; a.n_splits = plan.n_splits; a.n_waves = plan.n_waves;
     switch (cfg.bits) {
         case 2: return tree_bits<2>(a, plan.row_tiles, cfg.key_axis, stream);
         case 4: return tree_bits<4>(a, plan.row_tiles, cfg.key_axis, stream);
