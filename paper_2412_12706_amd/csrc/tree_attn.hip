@@ -84,6 +84,8 @@ __device__ __forceinline__ float rows4_add(float v) {
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// (one instruction, without the two that quiet NaNs first)
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
@@ -243,40 +245,72 @@ template <int BITS, int AXIS> struct KeyWords {
     uint32_t w[2][BITS];
     uint32_t scale[2], zero[2];      // keys per channel: a dword of the group's row; per token: the lane's own group of its two tokens
 };
+// Where a head's packed arrays begin.  A block's address is the same for the whole wave (scalar registers); a lane adds 32 bits that never change.
+struct HeadBase { const char *k, *v, *ks, *kz, *vs, *vz; };
+__device__ __forceinline__ size_t uniform(size_t x) {
+    return (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) | (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32;
+}
 template <int BITS, int AXIS>
-__device__ __forceinline__ void load_keys(const TreeArgs& a, int bh, int blk, int lane, KeyWords<BITS, AXIS>& k) {
+__device__ __forceinline__ HeadBase head_base(const TreeArgs& a, int bh) {
+    constexpr int SB = v_superblock(BITS), SBW = v_superblock_words(BITS);
+    HeadBase h;
+    h.k = reinterpret_cast<const char*>(a.k_codes) + uniform((size_t)bh * a.n_cap * (kHeadDim * BITS / 8));
+    h.v = reinterpret_cast<const char*>(a.v_codes) + uniform((size_t)bh * (size_t)((a.n_cap + SB - 1) / SB) * (SBW * 4));
+    const size_t per_token = uniform((size_t)bh * a.n_cap << (8 - a.group_log2));      // bytes: D / G numbers a token
+    const size_t per_group = uniform((size_t)bh * (size_t)((a.n_cap + (1 << a.group_log2) - 1) >> a.group_log2) * (kHeadDim * 2));
+    const size_t key = AXIS == KVQP_KEY_PER_CHANNEL ? per_group : per_token;
+    h.ks = reinterpret_cast<const char*>(a.k_scale) + key;
+    h.kz = reinterpret_cast<const char*>(a.k_zero) + key;
+    h.vs = reinterpret_cast<const char*>(a.v_scale) + per_token;
+    h.vz = reinterpret_cast<const char*>(a.v_zero) + per_token;
+    return h;
+}
+template <typename T> __device__ __forceinline__ T load_at(const char* uniform, uint32_t lane_bytes) { return *reinterpret_cast<const T*>(uniform + lane_bytes); }
+// (unseen, or the compiler adds it to the head's address before the loop, 64 bits per lane and array, and a block's to that)
+__device__ __forceinline__ uint32_t unseen(uint32_t lane_bytes) { asm volatile("" : "+v"(lane_bytes)); return lane_bytes; }
+
+template <int BITS, int AXIS>
+__device__ __forceinline__ void load_keys(const HeadBase& h, int group_log2, int blk, int lane, KeyWords<BITS, AXIS>& k) {
     const int n = lane & 15, kb = lane >> 4;
-    const size_t tok = (size_t)bh * a.n_cap + 32 * blk + n;
+    const char* p = h.k + (size_t)blk * (32 * kHeadDim * BITS / 8);
+    const uint32_t off = unseen((uint32_t)(n * (kHeadDim * BITS / 8) + kb * (4 * BITS)));
 #pragma unroll
     for (int H = 0; H < 2; ++H) {
-        const uint32_t* p = a.k_codes + (tok + 16 * H) * (kHeadDim * BITS / 32) + kb * BITS;
+        const char* pH = p + H * (16 * kHeadDim * BITS / 8);
         if constexpr (BITS == 2) {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            const uint2 u = load_at<uint2>(pH, off);
             k.w[H][0] = u.x; k.w[H][1] = u.y;
         } else {
 #pragma unroll
             for (int j = 0; j < BITS / 4; ++j) {
-                const uint4 u = *reinterpret_cast<const uint4*>(p + 4 * j);
+                const uint4 u = load_at<uint4>(pH + 16 * j, off);
                 k.w[H][4 * j] = u.x; k.w[H][4 * j + 1] = u.y; k.w[H][4 * j + 2] = u.z; k.w[H][4 * j + 3] = u.w;
             }
         }
     }
     if constexpr (BITS != 16) {
         if constexpr (AXIS == KVQP_KEY_PER_CHANNEL) {
-            const size_t groups = (size_t)((a.n_cap + (1 << a.group_log2) - 1) >> a.group_log2);
-            const size_t row = ((size_t)bh * groups + (size_t)((32 * blk) >> a.group_log2)) * (kHeadDim / 2) + lane;
-            k.scale[0] = reinterpret_cast<const uint32_t*>(a.k_scale)[row];
-            k.zero[0] = reinterpret_cast<const uint32_t*>(a.k_zero)[row];
+            const size_t row = (size_t)((32 * blk) >> group_log2) * (kHeadDim * 2);
+            const uint32_t at = unseen(4u * lane);
+            k.scale[0] = load_at<uint32_t>(h.ks + row, at);
+            k.zero[0] = load_at<uint32_t>(h.kz + row, at);
         } else {
+            const size_t row = (size_t)blk << (13 - group_log2);         // 32 tokens of 256 / G bytes
+            const uint32_t at = unseen((uint32_t)((n << (7 - group_log2)) + ((32 * kb) >> group_log2)) * 2u);
 #pragma unroll
             for (int H = 0; H < 2; ++H) {
-                const size_t at = ((tok + 16 * H) << (7 - a.group_log2)) + (size_t)((32 * kb) >> a.group_log2);
-                k.scale[H] = a.k_scale[at];
-                k.zero[H] = a.k_zero[at];
+                const size_t half = (size_t)H << (12 - group_log2);
+                k.scale[H] = load_at<uint16_t>(h.ks + row + half, at);
+                k.zero[H] = load_at<uint16_t>(h.kz + row + half, at);
             }
         }
     }
 }
+
+// With two or four row tiles the compiler forms operands far ahead and spills them; nothing moves across the end of a step then.  (A spilled
+// register's reload waits for every load in flight: 32 layers of 8192 tokens, 64 rows: 306 -> 165 us.  Spreading vector instructions evenly
+// between the matrix instructions, by hand or by s_setprio, changed nothing.)
+template <int RT> __device__ __forceinline__ void end_step() { if constexpr (RT >= 2) __builtin_amdgcn_sched_barrier(0); }
 
 // Logits of a block for RT row tiles, before the rows' factors: acc[rt][H][i] is token 16 H + 4 kb + i of row 16 rt + n.  The four
 // steps of eight channels run outermost, so that only one step's operands are held beside the sums.
@@ -309,6 +343,7 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const Ke
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
+        end_step<RT>();
         Frag a[2];
         if constexpr (BITS == 16) {
 #pragma unroll
@@ -403,9 +438,8 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
     float top[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const float m0 = fmaxf(fmaxf(acc[rt][0][0], acc[rt][0][1]), fmaxf(acc[rt][0][2], acc[rt][0][3]));
-        const float m1 = fmaxf(fmaxf(acc[rt][1][0], acc[rt][1][1]), fmaxf(acc[rt][1][2], acc[rt][1][3]));
-        top[rt] = fmaxf(m0, m1) * factor[rt];
+        const f4v &p = acc[rt][0], &q = acc[rt][1];
+        top[rt] = max3(max3(max3(p[0], p[1], p[2]), p[3], q[0]), max3(q[1], q[2], q[3]), q[3]) * factor[rt];
         past |= top[rt] > st.ref[rt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
@@ -452,20 +486,21 @@ template <int BITS> struct ValueWords {
     uint32_t scale, zero;
 };
 template <int BITS>
-__device__ __forceinline__ void load_values(const TreeArgs& a, int bh, int blk, int lane, ValueWords<BITS>& v) {
+__device__ __forceinline__ void load_values(const HeadBase& h, int group_log2, int blk, int lane, ValueWords<BITS>& v) {
     constexpr int SB = v_superblock(BITS), SBW = v_superblock_words(BITS);
-    const size_t per_head = (size_t)((a.n_cap + SB - 1) / SB) * SBW;
-    const uint32_t* p = a.v_codes + (size_t)bh * per_head + (size_t)(32 * blk / SB) * SBW + 4 * lane;
+    const char* p = h.v + (size_t)(32 * blk / SB) * (SBW * 4);
+    const uint32_t at_lane = unseen(16u * lane);
 #pragma unroll
     for (int j = 0; j < VGeom<BITS>::kWords / 4; ++j) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p + 256 * j);
+        const uint4 u = load_at<uint4>(p + 1024 * j, at_lane);
         v.w[4 * j] = u.x; v.w[4 * j + 1] = u.y; v.w[4 * j + 2] = u.z; v.w[4 * j + 3] = u.w;
     }
     if constexpr (BITS != 16) {
         // 32 tokens' scales are 32 D / G numbers in a row; lanes past the last repeat it
-        const size_t at = ((((size_t)bh * a.n_cap + 32 * blk) << (7 - a.group_log2)) >> 1) + min(lane, (16 << (7 - a.group_log2)) - 1);
-        v.scale = reinterpret_cast<const uint32_t*>(a.v_scale)[at];
-        v.zero = reinterpret_cast<const uint32_t*>(a.v_zero)[at];
+        const size_t row = (size_t)blk << (13 - group_log2);
+        const uint32_t at = unseen(4u * min(lane, (16 << (7 - group_log2)) - 1));
+        v.scale = load_at<uint32_t>(h.vs + row, at);
+        v.zero = load_at<uint32_t>(h.vz + row, at);
     }
 }
 // Scales and zeros to the strip, in the order in which the lanes of a token's block want them.
@@ -509,16 +544,16 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     const int n = lane & 15, kb = lane >> 4, waves = blockDim.x >> 6;
     // Workgroups go to the eight dies in turn: the row blocks of one stretch of a cache get numbers eight apart, so that
     // they run on one die at about the same time and share what its L2 holds.
-    const int pair = blockIdx.x / (8 * a.row_blocks) * 8 + blockIdx.x % 8, rb = blockIdx.x / 8 % a.row_blocks;
+    const int pair = __builtin_amdgcn_readfirstlane(blockIdx.x / (8 * a.row_blocks) * 8 + blockIdx.x % 8), rb = __builtin_amdgcn_readfirstlane(blockIdx.x / 8 % a.row_blocks);
     if (pair >= a.heads * a.n_splits) return;
-    const int bh = pair / a.n_splits, split = pair % a.n_splits;
+    const int bh = __builtin_amdgcn_readfirstlane(pair / a.n_splits), split = pair - bh * a.n_splits;
     const int row0 = rb * RT * 16;
     stage_queries<RT>(a, bh, row0, RT * 16, 64 * waves, sq);
 
-    const int n_tok = head_tokens(a, bh);
+    const int n_tok = __builtin_amdgcn_readfirstlane(head_tokens(a, bh));
     const int packed = (n_tok + 31) / 32, tail = (a.tail_len + 31) / 32, fresh = (a.n_new + 31) / 32;
     const int units = packed + tail + fresh;
-    const int share = (int)((unsigned)units / (unsigned)a.n_splits), rest = units - share * a.n_splits;
+    const int share = __builtin_amdgcn_readfirstlane((int)((unsigned)units / (unsigned)a.n_splits)), rest = units - share * a.n_splits;
     const int u0 = share * split + min(split, rest), u1 = u0 + share + (split < rest ? 1 : 0);
     ScaleStrip& strip = sh.run.wave[wave].strip;
 
@@ -535,20 +570,21 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     // ---- packed blocks ----
     {
         const Fields<BITS> fields;
+        const HeadBase base = head_base<BITS, AXIS>(a, bh);
         const int end = min(u1, packed);
         int blk = u0 + wave;
         if (blk < end) {
             KeyWords<BITS, AXIS> kw;
             ValueWords<BITS> vw;
-            load_keys<BITS, AXIS>(a, bh, blk, lane, kw);
-            load_values<BITS>(a, bh, blk, lane, vw);
+            load_keys<BITS, AXIS>(base, a.group_log2, blk, lane, kw);
+            load_values<BITS>(base, a.group_log2, blk, lane, vw);
 #pragma unroll 1
             for (; blk < end; blk += waves) {
                 const int next = min(blk + waves, end - 1);
                 f4v acc[RT][2];
                 strip_keys<BITS, AXIS>(kw, strip, lane);
                 key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
-                load_keys<BITS, AXIS>(a, bh, next, lane, kw);
+                load_keys<BITS, AXIS>(base, a.group_log2, next, lane, kw);
                 if (32 * blk + 32 > n_tok) {     // (uniform) the head's last block: tokens past its count are unseen
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
@@ -581,8 +617,9 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                         for (int i = 0; i < 4; ++i) v.h[i] = __builtin_elementwise_fma(c[i], s.h[i], z.h[i]);
                     }
                     value_product<RT>(st, v, tile, p);
+                    if (tile & 1) end_step<RT>();
                 }
-                load_values<BITS>(a, bh, next, lane, vw);
+                load_values<BITS>(base, a.group_log2, next, lane, vw);
             }
         }
     }
@@ -862,7 +899,7 @@ __global__ __launch_bounds__(kWeightThreads) void add_weights(const TreeArgs a) 
     const int u_first = blockIdx.x * kWeightWaves, u_last = min(u_first + kWeightWaves, units) - 1;
     if (u_first < packed) {
         KeyWords<BITS, AXIS> kw;
-        load_keys<BITS, AXIS>(a, bh, min(u, packed - 1), lane, kw);
+        load_keys<BITS, AXIS>(head_base<BITS, AXIS>(a, bh), a.group_log2, min(u, packed - 1), lane, kw);
         strip_keys<BITS, AXIS>(kw, s_strip[wave], lane);
         weigh<BITS, AXIS>(kw, a, bh, sq, s_strip[wave], s_lse, live && !is_tail, -1, cs);
     }
