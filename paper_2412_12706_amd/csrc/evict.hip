@@ -17,7 +17,7 @@
 namespace kvqp {
 namespace {
 
-constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kBins = 2048;
+constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256;
 
 struct EvictArgs {
@@ -29,7 +29,7 @@ struct EvictArgs {
     long long w_cap, w_cap_out;
     int n_kept, src_cap, dst_cap;
     int n_keep, unit, bound;
-    int group, token_blocks;
+    int group_log2, token_blocks;
 };
 
 __device__ __forceinline__ int source_tokens(const EvictArgs& a, int bh) {
@@ -53,19 +53,41 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);
     return x != x ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
+// (a unit's weights are requested 32 at a time)
 __device__ __forceinline__ uint32_t unit_key(const float* w, int u, int unit) {
     if (unit == 1) return order_key(w[u]);
     double sum = 0.0;
-    for (int t = 0; t < unit; ++t) sum += (double)w[u * unit + t];
+#pragma unroll 1
+    for (int b = 0; b < unit; b += 32) {
+        float x[32];
+#pragma unroll
+        for (int t = 0; t < 32; ++t) x[t] = w[u * unit + b + t];
+#pragma unroll
+        for (int t = 0; t < 32; ++t) sum += (double)x[t];
+    }
     return order_key((float)sum);
 }
 
-__global__ __launch_bounds__(kPickThreads) void pick_heaviest(const EvictArgs a) {
-    __shared__ uint32_t s_hist[kBins];
-    __shared__ uint32_t s_wave[kPickWaves], s_wave2[kPickWaves];
-    __shared__ uint32_t s_found[2];
+// Sum of the first `wave` of at most 16 numbers in LDS.
+__device__ __forceinline__ uint32_t waves_before(const uint32_t* s, int wave, int lane) {
+    uint32_t v = (lane & 15) < wave ? s[lane & 15] : 0u;
+    v += __builtin_amdgcn_update_dpp(0u, v, 0xB1 /* quad_perm [1,0,3,2] */, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x4E /* quad_perm [2,3,0,1] */, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x141 /* row_half_mirror */, 0xF, 0xF, true);
+    return v + __builtin_amdgcn_update_dpp(0u, v, 0x140 /* row_mirror */, 0xF, 0xF, true);
+}
+
+// One head per workgroup.  Every wave has a stretch of consecutive units, 64 at a time; The keys of up to
+// KEYS such steps stay in LDS (KEYS == 0: any number, read again in every pass).
+template <int KEYS, int THREADS>
+__global__ __launch_bounds__(THREADS) void pick_heaviest(const EvictArgs a) {
+    constexpr int WAVES = THREADS / 64, PER = kBins / THREADS;
+    __shared__ uint32_t s_hist[2][kBins];
+    __shared__ uint32_t s_key[KEYS > 0 ? KEYS * THREADS : 1];
+    __shared__ uint32_t s_wave[3][WAVES];
+    __shared__ uint32_t s_found[3];
     const int bh = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = source_tokens(a, bh);
     const Cut cut = cut_of(n, a.n_keep, a.unit);
     const float* w = a.weights + (size_t)bh * a.w_cap;
@@ -77,204 +99,138 @@ __global__ __launch_bounds__(kPickThreads) void pick_heaviest(const EvictArgs a)
         if (list) list[at] = token;
     };
     if (cut.keep_units == cut.units) {       // nothing leaves
-        for (int t = tid; t < n; t += kPickThreads) put(t, t);
+        for (int t = tid; t < n; t += THREADS) put(t, t);
         return;
     }
-    for (int t = tid; t < cut.short_unit; t += kPickThreads) put(cut.keep_units * a.unit + t, cut.units * a.unit + t);
+    for (int t = tid; t < cut.short_unit; t += THREADS) put(cut.keep_units * a.unit + t, cut.units * a.unit + t);
     if (cut.keep_units == 0) return;
 
-    // The key of the last unit that stays, and how many of those with that very key do.
+    const int steps = (cut.units + THREADS - 1) / THREADS, u0 = wave * steps * 64;
+    uint32_t* own = s_key + wave * KEYS * 64 + lane;         // the lane's keys, 64 words apart
+    if constexpr (KEYS > 0) {
+        if (a.unit == 1) {       // (requested eight at a time: a branch per step would wait for each)
+#pragma unroll 1
+            for (int j0 = 0; j0 < steps; j0 += 8) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = w[min(u0 + 64 * (j0 + j) + lane, cut.units - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j0 + j < KEYS) own[64 * (j0 + j)] = order_key(x[j]);
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < steps; ++j) own[64 * j] = u0 + 64 * j + lane < cut.units ? unit_key(w, u0 + 64 * j + lane, a.unit) : 0u;
+        }
+    }
+    // body(unit, its key, whether there is such a unit) for the wave's units, in order.  (Rolled up: every launch fetches its code anew, and
+    // keys in registers, with the loops unrolled, took 20 us instead of 15 for 16 heads of 12003.)
+    auto each = [&](auto body) {
+#pragma unroll 2
+        for (int j = 0; j < steps; ++j) {
+            const int u = u0 + 64 * j + lane;
+            body(u, KEYS > 0 ? own[64 * j] : u < cut.units ? unit_key(w, u, a.unit) : 0u, u < cut.units);
+        }
+    };
+
+    // The leading bits of the last unit's key that stays, and how many of the units with those very bits do.  Mostly two passes tell them
+    // apart: as soon as all units of a bin stay, the rest of their keys does not matter.
     uint32_t prefix = 0u, mask = 0u, want = (uint32_t)cut.keep_units;
+#pragma unroll
+    for (int b = 0; b < PER; ++b) s_hist[0][tid + b * THREADS] = s_hist[1][tid + b * THREADS] = 0u;
+    __syncthreads();
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int b = tid; b < kBins; b += kPickThreads) s_hist[b] = 0u;
+        uint32_t* hist = s_hist[pass & 1];
+        each([&](int, uint32_t k, bool valid) {
+            if (valid && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1u);
+        });
         __syncthreads();
-        for (int u = tid; u < cut.units; u += kPickThreads) {
-            const uint32_t k = unit_key(w, u, a.unit);
-            if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & ((1u << bits) - 1u)], 1u);
+        // bins from the highest down: thread t has PER of them
+        uint32_t c[PER], all = 0u;
+#pragma unroll
+        for (int b = 0; b < PER; ++b) {
+            c[b] = hist[kBins - 1 - PER * tid - b];
+            hist[kBins - 1 - PER * tid - b] = 0u;           // (for the pass after the next)
+            all += c[b];
         }
-        __syncthreads();
-        // bins from the highest down: thread t has bins kBins - 1 - 2 t and the one below
-        const int hi = kBins - 1 - 2 * tid;
-        const uint32_t c0 = s_hist[hi], c1 = s_hist[hi - 1];
-        uint32_t before = c0 + c1;
+        uint32_t before = all;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = __shfl_up(before, d);
             if (lane >= d) before += o;
         }
-        if (lane == 63) s_wave[wave] = before;
+        if (lane == 63) s_wave[0][wave] = before;
         __syncthreads();
-        before -= c0 + c1;
-        for (int v = 0; v < wave; ++v) before += s_wave[v];
-        if (before < want && want <= before + c0) { s_found[0] = (uint32_t)hi; s_found[1] = want - before; }
-        else if (before + c0 < want && want <= before + c0 + c1) { s_found[0] = (uint32_t)hi - 1u; s_found[1] = want - before - c0; }
+        before += waves_before(s_wave[0], wave, lane) - all;
+#pragma unroll
+        for (int b = 0; b < PER; ++b) {
+            if (before < want && want <= before + c[b]) {
+                s_found[0] = (uint32_t)(kBins - 1 - PER * tid - b); s_found[1] = want - before; s_found[2] = c[b];
+            }
+            before += c[b];
+        }
         __syncthreads();
         prefix |= s_found[0] << shift;
         mask |= ((1u << bits) - 1u) << shift;
         want = s_found[1];
+        if (want == s_found[2]) break;        // (uniform)
     }
 
-    // Every wave has a stretch of its own: how many stay in the stretches before it, then its own in order.
-    const int seg = ((cut.units + kPickWaves - 1) / kPickWaves + 63) / 64 * 64;
-    const int u0 = wave * seg, u1 = min(u0 + seg, cut.units);
+    // How many stay in the stretches before this wave's, then its own in order.
     uint32_t above = 0u, equal = 0u;
-    for (int u = u0; u < u1; u += 64) {
-        const uint32_t k = u + lane < u1 ? unit_key(w, u + lane, a.unit) : 0u;
-        above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(u + lane < u1 && k > prefix));
-        equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(u + lane < u1 && k == prefix));
-    }
-    if (lane == 0) { s_wave[wave] = above; s_wave2[wave] = equal; }
+    each([&](int, uint32_t k, bool valid) {
+        above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(valid && (k & mask) > prefix));
+        equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(valid && (k & mask) == prefix));
+    });
+    if (lane == 0) { s_wave[1][wave] = above; s_wave[2][wave] = equal; }
     __syncthreads();
-    above = equal = 0u;
-    for (int v = 0; v < wave; ++v) { above += s_wave[v]; equal += s_wave2[v]; }
+    above = waves_before(s_wave[1], wave, lane);
+    equal = waves_before(s_wave[2], wave, lane);
     const unsigned long long below = (1ull << lane) - 1ull;
-    for (int u = u0; u < u1; u += 64) {
-        const uint32_t k = u + lane < u1 ? unit_key(w, u + lane, a.unit) : 0u;
-        const unsigned long long ba = __builtin_amdgcn_ballot_w64(u + lane < u1 && k > prefix);
-        const unsigned long long be = __builtin_amdgcn_ballot_w64(u + lane < u1 && k == prefix);
+    each([&](int u, uint32_t k, bool valid) {
+        k &= mask;
+        const unsigned long long ba = __builtin_amdgcn_ballot_w64(valid && k > prefix), be = __builtin_amdgcn_ballot_w64(valid && k == prefix);
         const uint32_t e = equal + (uint32_t)__builtin_popcountll(be & below);
         const uint32_t at = above + (uint32_t)__builtin_popcountll(ba & below) + min(e, want);
-        const bool stays = u + lane < u1 && (k > prefix || (k == prefix && e < want));
-        if (stays)
-            for (int t = 0; t < a.unit; ++t) put((int)at * a.unit + t, (u + lane) * a.unit + t);
+        if (valid && (k > prefix || (k == prefix && e < want)))
+            for (int t = 0; t < a.unit; ++t) put((int)at * a.unit + t, u * a.unit + t);
         above += (uint32_t)__builtin_popcountll(ba);
         equal += (uint32_t)__builtin_popcountll(be);
-    }
+    });
 }
 
 __device__ __forceinline__ float half_to_float(uint32_t u) { return __half2float(__ushort_as_half((unsigned short)u)); }
 
-// One field of a value word: where token t keeps channel 16 tile + n (layout statement in kvqp.h).
-template <int BITS> struct ValuePlace {
-    static constexpr int kWpt = v_words_per_tile(BITS), kFields = 16 / BITS, kSb = v_superblock(BITS);
-    uint32_t word;      // of the head, for tile 0 and n = 0
-    int wl, shift;
-    __device__ __forceinline__ explicit ValuePlace(int t) {
-        const int low = t % kSb, blk = low / 32, H = low / 16 % 2, kb = low / 4 % 4, i = low % 4;
-        const int run = 4 * blk + i;
-        wl = run / kFields;
-        shift = 16 * H + BITS * (run % kFields);
-        word = (uint32_t)(t / kSb) * v_superblock_words(BITS) + kb * 64;
-    }
-    __device__ __forceinline__ uint32_t at(int tile, int n) const {
-        const int y = tile * kWpt + wl;
-        return word + (uint32_t)((y / 4) * 256 + n * 4 + y % 4);
-    }
-};
-
-// Quantizes keys of new groups (keys per channel): the WG's TB survivors, whole groups of them.
-template <int BITS, int TB>
-__device__ __forceinline__ void regroup_keys(const EvictArgs& a, int bh, int n_src, int t0, int ntok, const int (&s_idx)[TB], float (&s_min)[4][2][kHeadDim], float (&s_max)[4][2][kHeadDim]) {
-    constexpr int R = TB / 16;
-    const int c8 = threadIdx.x & 15, r = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-    const int rows_per_group = a.group / 16, n_groups = (ntok + a.group - 1) / a.group;      // 2, 4 or 8 of a thread's rows
-    const uint32_t* kc = (const uint32_t*)a.src.k_codes + (size_t)bh * a.src_cap * (kHeadDim * BITS / 32);
-    const size_t src_groups = (size_t)(a.src_cap + a.group - 1) / a.group;
-    const uint16_t* ks = (const uint16_t*)a.src.k_scale + (size_t)bh * src_groups * kHeadDim;
-    const uint16_t* kz = (const uint16_t*)a.src.k_zero + (size_t)bh * src_groups * kHeadDim;
-    _Float16 x[R][8];
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        const int t = s_idx[min(r + 16 * j, ntok - 1)];
-        uint32_t w[2];
-        if constexpr (BITS == 8) { const uint2 u = *reinterpret_cast<const uint2*>(kc + (size_t)t * 32 + 2 * c8); w[0] = u.x; w[1] = u.y; }
-        else if constexpr (BITS == 4) w[0] = w[1] = kc[(size_t)t * 16 + c8];
-        else w[0] = w[1] = kc[(size_t)t * 8 + c8 / 2] >> (8 * (c8 & 1));
-        const size_t row = (size_t)(t / a.group) * kHeadDim + 8 * c8;
-        const uint4 s4 = *reinterpret_cast<const uint4*>(ks + row), z4 = *reinterpret_cast<const uint4*>(kz + row);
-        const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int shift = BITS == 8 ? 8 * ((e % 4) / 2) + 16 * (e % 2) : BITS * (e / 2) + 16 * (e % 2);
-            const float code = (float)((w[BITS == 8 ? e / 4 : 0] >> shift) & ((1u << BITS) - 1u));
-            const uint32_t sh = (s[e / 2] >> (16 * (e % 2))) & 0xffffu, zh = (z[e / 2] >> (16 * (e % 2))) & 0xffffu;
-            // (a group that reaches the largest binary16 number may read back above it: its scale was rounded up)
-            x[j][e] = (_Float16)fminf(fmaxf(__builtin_fmaf(code, half_to_float(sh), half_to_float(zh)), -65504.0f), 65504.0f);
-        }
-    }
-    // minima and maxima of the groups' channels: a thread's rows, the wave's four row lanes, the four waves
-    for (int g = 0; g < n_groups; ++g) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float lo = 65504.0f, hi = -65504.0f;
-#pragma unroll
-            for (int j = 0; j < R; ++j)        // (rows past the count repeat the last token, which is of the last group)
-                if (j / rows_per_group == g || (r + 16 * j >= ntok && g == n_groups - 1)) { lo = fminf(lo, (float)x[j][e]); hi = fmaxf(hi, (float)x[j][e]); }
-            lo = fminf(lo, __shfl_xor(lo, 16)); hi = fmaxf(hi, __shfl_xor(hi, 16));
-            lo = fminf(lo, __shfl_xor(lo, 32)); hi = fmaxf(hi, __shfl_xor(hi, 32));
-            if ((threadIdx.x & 48) == 0) { s_min[wave][g][8 * c8 + e] = lo; s_max[wave][g][8 * c8 + e] = hi; }
-        }
-    }
-    __syncthreads();
-    uint32_t* out = (uint32_t*)a.dst.k_codes + ((size_t)bh * a.dst_cap + t0) * (kHeadDim * BITS / 32);
-    const size_t dst_groups = (size_t)(a.dst_cap + a.group - 1) / a.group;
-    const size_t row0 = ((size_t)bh * dst_groups + t0 / a.group) * kHeadDim + 8 * c8;
-    for (int g = 0; g < n_groups; ++g) {
-        // (uniform) one group as it was: it begins where one began, has no gap, and is as long as that one
-        const int members = min(a.group, ntok - g * a.group), first = s_idx[g * a.group], last = s_idx[g * a.group + members - 1];
-        const bool same = first % a.group == 0 && last - first == members - 1 && members == min(a.group, n_src - first);
-        float zf[8], inv[8];
-        uint32_t sw[4] = {0u, 0u, 0u, 0u}, zw[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = 8 * c8 + e;
-            const float lo = fminf(fminf(s_min[0][g][d], s_min[1][g][d]), fminf(s_min[2][g][d], s_min[3][g][d]));
-            const float hi = fmaxf(fmaxf(s_max[0][g][d], s_max[1][g][d]), fmaxf(s_max[2][g][d], s_max[3][g][d]));
-            const __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), (float)((1 << BITS) - 1)));
-            const float sf = __half2float(sh);
-            zf[e] = lo;
-            inv[e] = sf == 0.0f ? 0.0f : __fdiv_rn(1.0f, sf);
-            sw[e / 2] |= (uint32_t)__half_as_ushort(sh) << (16 * (e % 2));
-            zw[e / 2] |= (uint32_t)__half_as_ushort(__float2half_rn(lo)) << (16 * (e % 2));
-        }
-        if (same) {
-            const size_t row = (size_t)(first / a.group) * kHeadDim + 8 * c8;
-            const uint4 s4 = *reinterpret_cast<const uint4*>(ks + row), z4 = *reinterpret_cast<const uint4*>(kz + row);
-            sw[0] = s4.x; sw[1] = s4.y; sw[2] = s4.z; sw[3] = s4.w;
-            zw[0] = z4.x; zw[1] = z4.y; zw[2] = z4.z; zw[3] = z4.w;
-        }
-        if (r == 0) {
-            *reinterpret_cast<uint4*>((uint16_t*)a.dst.k_scale + row0 + (size_t)g * kHeadDim) = make_uint4(sw[0], sw[1], sw[2], sw[3]);
-            *reinterpret_cast<uint4*>((uint16_t*)a.dst.k_zero + row0 + (size_t)g * kHeadDim) = make_uint4(zw[0], zw[1], zw[2], zw[3]);
-        }
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int t = r + 16 * j;
-            // (a group of 32 or more takes all of a thread's rows j .. at once: no lane of a row of lanes is left out)
-            if (j / rows_per_group != g || t >= rows32(ntok)) continue;
-            uint32_t w[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float c = rintf(__fmul_rn(__fsub_rn((float)x[j][e], zf[e]), inv[e]));
-                const uint32_t code = (uint32_t)fminf(fmaxf(c, 0.0f), (float)((1 << BITS) - 1));
-                const int shift = BITS == 8 ? 8 * ((e % 4) / 2) + 16 * (e % 2) : BITS * (e / 2) + 16 * (e % 2);
-                w[BITS == 8 ? e / 4 : 0] |= code << shift;
-            }
-            if (same && t < ntok) {
-                const size_t row = (size_t)s_idx[t];
-                if constexpr (BITS == 8) { const uint2 u = *reinterpret_cast<const uint2*>(kc + row * 32 + 2 * c8); w[0] = u.x; w[1] = u.y; }
-                else if constexpr (BITS == 4) w[0] = kc[row * 16 + c8];
-                else w[0] = (kc[row * 8 + c8 / 2] >> (8 * (c8 & 1))) & 0x00FF00FFu;
-            }
-            if (t >= ntok) w[0] = w[1] = 0u;
-            if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out + (size_t)t * 32 + 2 * c8) = make_uint2(w[0], w[1]);
-            else if constexpr (BITS == 4) out[(size_t)t * 16 + c8] = w[0];
-            else {
-                // the word spans this lane's channels and its neighbour's
-                uint32_t whole = w[0] << (8 * (c8 & 1));
-                whole |= __shfl_xor(whole, 1);
-                if (!(c8 & 1)) out[(size_t)t * 8 + c8 / 2] = whole;
-            }
-        }
-    }
+// Where a token keeps its values (layout statement in kvqp.h): channel 16 tile + n is in word `word` + place(tile, n) of the head, BITS bits from bit `shift`.
+struct ValuePlace { uint32_t word, shift; };
+template <int BITS> __device__ __forceinline__ ValuePlace value_place(int t) {
+    constexpr int kFields = 16 / BITS, kSb = v_superblock(BITS);
+    const int low = t % kSb, run = 4 * (low / 32) + low % 4;
+    return {(uint32_t)(t / kSb) * v_superblock_words(BITS) + (uint32_t)(low / 4 % 4 * 64 + run / kFields),
+            (uint32_t)(16 * (low / 16 % 2) + BITS * (run % kFields))};
 }
+
+__device__ __forceinline__ uint32_t xor_rows(uint32_t v, bool far) {     // the lane 16 (far: 32) further
+    const auto r = far ? __builtin_amdgcn_permlane32_swap(v, v, false, false) : __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return (threadIdx.x & (far ? 32 : 16)) ? r[0] : r[1];
+}
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ h2v as_h2(uint32_t u) { union { uint32_t u; h2v h; } c; c.u = u; return c.h; }
+__device__ __forceinline__ uint32_t as_u32(h2v h) { union { uint32_t u; h2v h; } c; c.h = h; return c.u; }
+
+// One key group's parameters, by channel.
+struct GroupParams { float zero, inv; };
 
 template <int BITS, int TB, bool REGROUP>
 __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, int key_axis) {
+    constexpr bool QUANT = BITS != 16;
+    constexpr int GROUPS = REGROUP ? TB / 32 < 4 ? TB / 32 : 4 : 1;
     __shared__ int s_idx[TB];
-    __shared__ float s_min[REGROUP ? 4 : 1][2][REGROUP ? kHeadDim : 1], s_max[REGROUP ? 4 : 1][2][REGROUP ? kHeadDim : 1];
+    __shared__ ValuePlace s_place[TB];
+    __shared__ uint32_t s_min[REGROUP ? 4 * GROUPS * 64 : 1], s_max[REGROUP ? 4 * GROUPS * 64 : 1];    // [wave][group][channel pair]
+    __shared__ GroupParams s_par[REGROUP ? GROUPS * kHeadDim : 1];
     const int bh = blockIdx.y, tid = threadIdx.x;
     const int n_src = source_tokens(a, bh);
     const int kept = cut_of(n_src, a.n_keep, a.unit).kept;
@@ -295,82 +251,219 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
     const int t0 = blockIdx.x * TB;
     if (t0 >= kept) return;
     const int ntok = min(TB, kept - t0), rows = rows32(ntok);
-    for (int t = tid; t < TB; t += kMoveThreads) s_idx[t] = a.idx[(size_t)bh * a.bound + t0 + min(t, ntok - 1)];
+    if (tid < TB) {
+        const int t = a.idx[(size_t)bh * a.bound + t0 + min(tid, ntok - 1)];
+        s_idx[tid] = t;
+        s_place[tid] = value_place<BITS>(t);
+    }
     __syncthreads();
-    if (a.weights_out)
-        for (int t = tid; t < ntok; t += kMoveThreads) a.weights_out[(size_t)bh * a.w_cap_out + t0 + t] = a.weights[(size_t)bh * a.w_cap + s_idx[t]];
 
-    // value codes, a word at a time: all its fields' source words are requested before they are put together
-    {
-        using P = ValuePlace<BITS>;
-        constexpr int SBW = v_superblock_words(BITS), E = 32 / BITS;
-        const size_t src_sb = (size_t)(a.src_cap + P::kSb - 1) / P::kSb, dst_sb = (size_t)(a.dst_cap + P::kSb - 1) / P::kSb;
-        const uint32_t* vs = (const uint32_t*)a.src.v_codes + (size_t)bh * src_sb * SBW;
-        uint32_t* vd = (uint32_t*)a.dst.v_codes + ((size_t)bh * dst_sb + t0 / P::kSb) * SBW;
-        const int words = (ntok + P::kSb - 1) / P::kSb * SBW;
-        for (int i = tid; i < words; i += kMoveThreads) {
-            const int sb = i / SBW, in = i % SBW;
-            const int y = in / 256 * 4 + in % 4, n = in / 4 % 16, kb = in / 64 % 4;
-            const int tile = y / P::kWpt, wl = y % P::kWpt;
-            uint32_t got[E];
-            int shift[E];
+    // Everything is requested before anything is stored: one trip to memory for a workgroup, not one per kind of data
+    // (32 heads of 8192 tokens to 6144, 4 bits: 211 us with a trip for each, 113 this way).
+    float weight = 0.0f;
+    if (a.weights_out && tid < ntok) weight = a.weights[(size_t)bh * a.w_cap + s_idx[tid]];
+    // scales and zeros that belong to tokens: 4, 2 or 1 numbers a token and array; a thread has one token of one or two of four arrays
+    constexpr int META = QUANT ? (4 * TB) / kMoveThreads : 0;
+    const int cg_log2 = 7 - a.group_log2;
+    uint2 meta[META > 0 ? META : 1];
+    const uint16_t* const meta_src[4] = {(const uint16_t*)a.src.v_scale, (const uint16_t*)a.src.v_zero, (const uint16_t*)a.src.k_scale, (const uint16_t*)a.src.k_zero};
+    uint16_t* const meta_dst[4] = {(uint16_t*)a.dst.v_scale, (uint16_t*)a.dst.v_zero, (uint16_t*)a.dst.k_scale, (uint16_t*)a.dst.k_zero};
+    const int arrays = key_axis == KVQP_KEY_PER_TOKEN ? 4 : 2;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int H = e / P::kFields, run = wl * P::kFields + e % P::kFields;
-                const int t = sb * P::kSb + 32 * (run / 4) + 16 * H + 4 * kb + run % 4;
-                const P p(s_idx[min(t, ntok - 1)]);
-                got[e] = vs[p.at(tile, n)];
-                shift[e] = p.shift;
-            }
-            uint32_t w = 0u;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int H = e / P::kFields, run = wl * P::kFields + e % P::kFields;
-                const int t = sb * P::kSb + 32 * (run / 4) + 16 * H + 4 * kb + run % 4;
-                const uint32_t field = (got[e] >> shift[e]) & (uint32_t)((1ull << BITS) - 1ull);
-                w |= t < ntok ? field << (16 * H + BITS * (e % P::kFields)) : 0u;
-            }
-            vd[i] = w;
+    for (int m = 0; m < META; ++m) {
+        const int item = m * kMoveThreads + tid, which = item / TB, t = item % TB;
+        meta[m] = make_uint2(0u, 0u);
+        if (which < arrays && t < ntok) {
+            const uint16_t* p = (which == 0 ? meta_src[0] : which == 1 ? meta_src[1] : which == 2 ? meta_src[2] : meta_src[3]) +
+                                (((size_t)bh * a.src_cap + s_idx[t]) << cg_log2);
+            if (cg_log2 == 2) meta[m] = *reinterpret_cast<const uint2*>(p);
+            else if (cg_log2 == 1) meta[m].x = *reinterpret_cast<const uint32_t*>(p);
+            else meta[m].x = *p;
         }
     }
-    if constexpr (BITS != 16) {
-        // scales and zeros that belong to tokens: 4, 2 or 1 numbers each
-        const int cg = kHeadDim / a.group;
-        auto copy = [&](const void* from, void* to) {
-            const uint16_t* f = (const uint16_t*)from + (size_t)bh * a.src_cap * cg;
-            uint16_t* o = (uint16_t*)to + ((size_t)bh * a.dst_cap + t0) * cg;
-            for (int i = tid; i < rows * cg; i += kMoveThreads) {
-                const int t = i / cg;
-                o[i] = t < ntok ? f[(size_t)s_idx[t] * cg + i % cg] : (uint16_t)0;
-            }
-        };
-        copy(a.src.v_scale, a.dst.v_scale);
-        copy(a.src.v_zero, a.dst.v_zero);
-        if (key_axis == KVQP_KEY_PER_TOKEN) {
-            copy(a.src.k_scale, a.dst.k_scale);
-            copy(a.src.k_zero, a.dst.k_zero);
-        } else if constexpr (!REGROUP) {
-            // whole groups: their rows of scales and zeros
-            const size_t sg = (size_t)(a.src_cap + a.group - 1) / a.group, dg = (size_t)(a.dst_cap + a.group - 1) / a.group;
-            for (int i = tid; i < (ntok + a.group - 1) / a.group * (kHeadDim / 2); i += kMoveThreads) {
-                const int g = i / (kHeadDim / 2), d = i % (kHeadDim / 2);
-                if ((t0 + g * a.group) % a.group) continue;      // (a group that began in an earlier workgroup's tokens)
-                const size_t from = ((size_t)bh * sg + s_idx[g * a.group] / a.group) * (kHeadDim / 2) + d;
-                const size_t to = ((size_t)bh * dg + t0 / a.group + g) * (kHeadDim / 2) + d;
-                ((uint32_t*)a.dst.k_scale)[to] = ((const uint32_t*)a.src.k_scale)[from];
-                ((uint32_t*)a.dst.k_zero)[to] = ((const uint32_t*)a.src.k_zero)[from];
-            }
-        }
-    }
-    if constexpr (REGROUP) {
-        regroup_keys<BITS, TB>(a, bh, n_src, t0, ntok, s_idx, s_min, s_max);
-    } else {
-        // key code rows: BITS pieces of 16 bytes
+    // key code rows: BITS pieces of 16 bytes
+    constexpr int PIECES = REGROUP ? 0 : TB * BITS / kMoveThreads;
+    uint4 piece[PIECES > 0 ? PIECES : 1];
+    if constexpr (!REGROUP) {
         const uint4* f = (const uint4*)a.src.k_codes + (size_t)bh * a.src_cap * BITS;
+#pragma unroll
+        for (int i = 0; i < (PIECES > 0 ? PIECES : 1); ++i) {
+            const int item = i * kMoveThreads + tid, t = item / BITS;
+            piece[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (t < ntok) piece[i] = f[(size_t)s_idx[t] * BITS + item % BITS];
+        }
+    }
+    // value codes: a thread makes WORDS words of E fields each
+    constexpr int SB = v_superblock(BITS), SBW = v_superblock_words(BITS), WPT = v_words_per_tile(BITS), E = 32 / BITS, HALF = E / 2;
+    constexpr int WORDS = TB / SB * SBW / kMoveThreads;
+    const uint32_t* vs = (const uint32_t*)a.src.v_codes + (size_t)bh * (size_t)((a.src_cap + SB - 1) / SB) * SBW;
+    uint32_t* vd = (uint32_t*)a.dst.v_codes + ((size_t)bh * (size_t)((a.dst_cap + SB - 1) / SB) + t0 / SB) * SBW;
+    uint32_t got[WORDS][E];
+    auto token_of = [&](int w, int e) {       // which of the workgroup's tokens field e of the thread's word w holds
+        const int i = w * kMoveThreads + tid, y = i % SBW / 256 * 4 + i % 4, kb = i / 64 % 4, run = y % WPT * HALF + e % HALF;
+        return i / SBW * SB + 32 * (run / 4) + 16 * (e / HALF) + 4 * kb + run % 4;
+    };
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        const int i = w * kMoveThreads + tid, y = i % SBW / 256 * 4 + i % 4;
+        const uint32_t place = (uint32_t)(y / WPT * WPT / 4 * 256 + i / 4 % 16 * 4 + y / WPT * WPT % 4);
+#pragma unroll
+        for (int e = 0; e < E; ++e) got[w][e] = vs[s_place[token_of(w, e)].word + place];
+    }
+
+    if (a.weights_out && tid < ntok) a.weights_out[(size_t)bh * a.w_cap_out + t0 + tid] = weight;
+#pragma unroll
+    for (int m = 0; m < META; ++m) {
+        const int item = m * kMoveThreads + tid, which = item / TB, t = item % TB;
+        if (which < arrays && t < rows) {
+            uint16_t* p = (which == 0 ? meta_dst[0] : which == 1 ? meta_dst[1] : which == 2 ? meta_dst[2] : meta_dst[3]) +
+                          (((size_t)bh * a.dst_cap + t0 + t) << cg_log2);
+            if (cg_log2 == 2) *reinterpret_cast<uint2*>(p) = meta[m];
+            else if (cg_log2 == 1) *reinterpret_cast<uint32_t*>(p) = meta[m].x;
+            else *p = (uint16_t)meta[m].x;
+        }
+    }
+    if constexpr (!REGROUP) {
         uint4* o = (uint4*)a.dst.k_codes + ((size_t)bh * a.dst_cap + t0) * BITS;
-        for (int i = tid; i < rows * BITS; i += kMoveThreads) {
-            const int t = i / BITS;
-            o[i] = t < ntok ? f[(size_t)s_idx[t] * BITS + i % BITS] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int i = 0; i < (PIECES > 0 ? PIECES : 1); ++i) {
+            const int item = i * kMoveThreads + tid;
+            if (item / BITS < rows) o[item] = piece[i];
+        }
+    }
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        uint32_t word = 0u;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int t = token_of(w, e);
+            const uint32_t field = BITS == 16 ? (got[w][e] >> s_place[t].shift) & 0xFFFFu : __builtin_amdgcn_ubfe(got[w][e], s_place[t].shift, BITS);
+            word |= (t < ntok ? field : 0u) << (16 * (e / HALF) + BITS * (e % HALF));
+        }
+        const int i = w * kMoveThreads + tid;
+        if (i / SBW * SB < ntok) vd[i] = word;
+    }
+
+    if constexpr (QUANT) {
+        if (key_axis == KVQP_KEY_PER_CHANNEL) {
+            // keys per channel: the groups' rows of scales and zeros, and (REGROUP) the codes of groups that are formed anew
+            const int group = 1 << a.group_log2;
+            const size_t sg = (size_t)((a.src_cap + group - 1) >> a.group_log2), dg = (size_t)((a.dst_cap + group - 1) >> a.group_log2);
+            const int groups = (ntok + group - 1) >> a.group_log2;
+            if constexpr (!REGROUP) {
+                for (int i = tid; i < groups * (kHeadDim / 2); i += kMoveThreads) {
+                    const int g = i / (kHeadDim / 2), d = i % (kHeadDim / 2);
+                    if (t0 & (group - 1)) continue;      // (a group that began in an earlier workgroup's tokens)
+                    const size_t from = ((size_t)bh * sg + (s_idx[g << a.group_log2] >> a.group_log2)) * (kHeadDim / 2) + d;
+                    const size_t to = ((size_t)bh * dg + (t0 >> a.group_log2) + g) * (kHeadDim / 2) + d;
+                    ((uint32_t*)a.dst.k_scale)[to] = ((const uint32_t*)a.src.k_scale)[from];
+                    ((uint32_t*)a.dst.k_zero)[to] = ((const uint32_t*)a.src.k_zero)[from];
+                }
+            } else {
+                constexpr int R = TB / 16;          // a thread's rows: r, r + 16, ..., channels 8 c8 .. 8 c8 + 7
+                const int c8 = tid & 15, r = tid >> 4, wave = tid >> 6;
+                const int rpg_log2 = a.group_log2 - 4;         // 2, 4 or 8 of a thread's rows make a group
+                const uint32_t* kc = (const uint32_t*)a.src.k_codes + (size_t)bh * a.src_cap * (4 * BITS);
+                const uint16_t* ks = (const uint16_t*)a.src.k_scale + (size_t)bh * sg * kHeadDim + 8 * c8;
+                const uint16_t* kz = (const uint16_t*)a.src.k_zero + (size_t)bh * sg * kHeadDim + 8 * c8;
+                uint32_t code[R][BITS == 8 ? 2 : 1];
+                h2v x[R][4];
+                uint4 s4[R], z4[R];
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    const int t = s_idx[min(r + 16 * j, ntok - 1)];
+                    if constexpr (BITS == 8) { const uint2 u = *reinterpret_cast<const uint2*>(kc + (size_t)t * 32 + 2 * c8); code[j][0] = u.x; code[j][1] = u.y; }
+                    else if constexpr (BITS == 4) code[j][0] = kc[(size_t)t * 16 + c8];
+                    else code[j][0] = kc[(size_t)t * 8 + c8 / 2] >> (8 * (c8 & 1));
+                    s4[j] = *reinterpret_cast<const uint4*>(ks + (size_t)(t >> a.group_log2) * kHeadDim);
+                    z4[j] = *reinterpret_cast<const uint4*>(kz + (size_t)(t >> a.group_log2) * kHeadDim);
+                }
+                // bit of element e's field in its word
+                auto bit_of = [](int e) { return BITS == 8 ? 8 * (e % 4 / 2) + 16 * (e % 2) : BITS * (e / 2) + 16 * (e % 2); };
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    const uint32_t s[4] = {s4[j].x, s4[j].y, s4[j].z, s4[j].w}, z[4] = {z4[j].x, z4[j].y, z4[j].z, z4[j].w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float c = (float)__builtin_amdgcn_ubfe(code[j][BITS == 8 ? e / 4 : 0], bit_of(e), BITS);
+                        const float v = __builtin_fmaf(c, half_to_float((s[e / 2] >> (16 * (e % 2))) & 0xffffu), half_to_float((z[e / 2] >> (16 * (e % 2))) & 0xffffu));
+                        // (a group that reaches the largest binary16 number may read back above it: its scale was rounded up)
+                        x[j][e / 2][e % 2] = (_Float16)fminf(fmaxf(v, -65504.0f), 65504.0f);
+                    }
+                }
+                // minima and maxima of the groups' channels: a thread's rows, the wave's four row lanes, the four waves.  Rows past
+                // the count repeat the last token, which is of the last group.
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    if (g >= groups) break;       // (uniform)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        h2v lo = {(_Float16)65504.0f, (_Float16)65504.0f}, hi = -lo;
+#pragma unroll
+                        for (int j = 0; j < R; ++j)
+                            if (min(j >> rpg_log2, groups - 1) == g) { lo = __builtin_elementwise_min(lo, x[j][q]); hi = __builtin_elementwise_max(hi, x[j][q]); }
+                        lo = __builtin_elementwise_min(lo, as_h2(xor_rows(as_u32(lo), false))); hi = __builtin_elementwise_max(hi, as_h2(xor_rows(as_u32(hi), false)));
+                        lo = __builtin_elementwise_min(lo, as_h2(xor_rows(as_u32(lo), true))); hi = __builtin_elementwise_max(hi, as_h2(xor_rows(as_u32(hi), true)));
+                        if ((tid & 48) == 0) { s_min[(wave * GROUPS + g) * 64 + 4 * c8 + q] = as_u32(lo); s_max[(wave * GROUPS + g) * 64 + 4 * c8 + q] = as_u32(hi); }
+                    }
+                }
+                __syncthreads();
+                // A group whose tokens were one group before: it begins where one began, has no gap, and is as long as that one.
+                auto same_group = [&](int g, int& first) {
+                    const int members = min(group, ntok - (g << a.group_log2));
+                    first = s_idx[g << a.group_log2];
+                    return (first & (group - 1)) == 0 && s_idx[(g << a.group_log2) + members - 1] - first == members - 1 && members == min(group, n_src - first);
+                };
+                for (int i = tid; i < groups * kHeadDim; i += kMoveThreads) {
+                    const int g = i / kHeadDim, d = i % kHeadDim;
+                    float lo = 65504.0f, hi = -65504.0f;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        lo = fminf(lo, (float)as_h2(s_min[(v * GROUPS + g) * 64 + d / 2])[d % 2]);
+                        hi = fmaxf(hi, (float)as_h2(s_max[(v * GROUPS + g) * 64 + d / 2])[d % 2]);
+                    }
+                    const __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), (float)((1 << BITS) - 1)));
+                    const float sf = __half2float(sh);
+                    s_par[i] = {lo, sf == 0.0f ? 0.0f : __fdiv_rn(1.0f, sf)};
+                    int first;
+                    const bool same = same_group(g, first);
+                    const size_t from = ((size_t)bh * sg + (first >> a.group_log2)) * kHeadDim + d, to = ((size_t)bh * dg + (t0 >> a.group_log2) + g) * kHeadDim + d;
+                    ((uint16_t*)a.dst.k_scale)[to] = same ? ((const uint16_t*)a.src.k_scale)[from] : __half_as_ushort(sh);
+                    ((uint16_t*)a.dst.k_zero)[to] = same ? ((const uint16_t*)a.src.k_zero)[from] : __half_as_ushort(__float2half_rn(lo));
+                }
+                __syncthreads();
+                uint32_t* out = (uint32_t*)a.dst.k_codes + ((size_t)bh * a.dst_cap + t0) * (4 * BITS);
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    if (g >= groups) break;
+                    GroupParams par[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) par[e] = s_par[g * kHeadDim + 8 * c8 + e];
+                    int first;
+                    const bool same = same_group(g, first);
+#pragma unroll
+                    for (int j = 0; j < R; ++j) {
+                        const int t = r + 16 * j;
+                        if ((j >> rpg_log2) != g || t >= rows) continue;      // (the same for the 16 lanes of a row)
+                        uint32_t w[2] = {0u, 0u};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float c = rintf(__fmul_rn(__fsub_rn((float)x[j][e / 2][e % 2], par[e].zero), par[e].inv));
+                            w[BITS == 8 ? e / 4 : 0] |= (uint32_t)fminf(fmaxf(c, 0.0f), (float)((1 << BITS) - 1)) << bit_of(e);
+                        }
+                        if (same) { w[0] = BITS == 2 ? code[j][0] & 0x00FF00FFu : code[j][0]; if constexpr (BITS == 8) w[1] = code[j][1]; }
+                        if (t >= ntok) w[0] = w[1] = 0u;
+                        if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out + (size_t)t * 32 + 2 * c8) = make_uint2(w[0], w[1]);
+                        else if constexpr (BITS == 4) out[(size_t)t * 16 + c8] = w[0];
+                        else {
+                            // the word spans this lane's channels and its neighbour's
+                            uint32_t both = w[0] << (8 * (c8 & 1));
+                            both |= __builtin_amdgcn_update_dpp(0u, both, 0xB1 /* quad_perm [1,0,3,2] */, 0xF, 0xF, true);
+                            if (!(c8 & 1)) out[(size_t)t * 8 + c8 / 2] = both;
+                        }
+                    }
+                }
+            }
         }
     }
 }
@@ -378,7 +471,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
 template <int BITS>
 hipError_t move_bits(const EvictArgs& a0, int heads, int key_axis, bool regroup, hipStream_t stream) {
     EvictArgs a = a0;
-    const int tb = regroup && a.group == 128 ? 128 : 64;
+    const int tb = regroup && a.group_log2 == 7 ? 128 : 64;
     a.token_blocks = (a.bound + tb - 1) / tb;
     const dim3 grid(a.token_blocks + 1, heads), block(kMoveThreads);
     if constexpr (BITS != 16) {
@@ -401,9 +494,13 @@ hipError_t launch_evict(const kvqp_cfg& cfg, const kvqp_cache& src, const float*
     a.w_cap = w_cap; a.w_cap_out = w_cap_out;
     a.n_kept = src.n_kept; a.src_cap = layout_tokens(src, src.n_kept); a.dst_cap = layout_tokens(dst, bound);
     a.n_keep = n_keep; a.unit = unit; a.bound = bound;
-    a.group = cfg.bits == 16 ? kHeadDim : cfg.group_size;
+    a.group_log2 = cfg.bits == 16 || cfg.group_size == 128 ? 7 : cfg.group_size == 64 ? 6 : 5;
     const int heads = cfg.batch * cfg.n_kv_heads;
-    pick_heaviest<<<dim3(heads), dim3(kPickThreads), 0, stream>>>(a);
+    const int units = src.n_kept / unit;
+    if (units <= 1024) pick_heaviest<4, 256><<<dim3(heads), dim3(256), 0, stream>>>(a);
+    else if (units <= 8192) pick_heaviest<8, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
+    else if (units <= 32768) pick_heaviest<32, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
+    else pick_heaviest<0, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
     const hipError_t rc = hipGetLastError();
     if (rc != hipSuccess) return rc;
     const bool regroup = cfg.bits != 16 && cfg.key_axis == KVQP_KEY_PER_CHANNEL && unit % cfg.group_size != 0;

@@ -177,6 +177,7 @@ struct TreeArgs {
     int heads, n_kv_heads;
     int rows, n_new;          // R, N
     int row_blocks, n_splits, n_waves;
+    int units_per_wg;         // weights: blocks of 32 tokens of a workgroup
     int group_log2;           // G = 32, 64 or 128
     float sm_scale, decay;
 };
@@ -836,100 +837,107 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeArgs a) {
 }
 
 // ---- weights that tokens receive ----
-// A wave has one block of 32 tokens for good and goes over all rows, 64 of them in LDS at a time; the sum of a token's
+// A wave has its blocks of 32 tokens for good and goes over all rows, up to 64 of them in LDS at a time; the sum of a token's
 // column is that wave's alone, so it is added to the running one without atomics, in one fixed order.
-constexpr int kWeightRT = 4, kWeightWaves = 4, kWeightThreads = 64 * kWeightWaves;
+constexpr int kWeightWaves = 8, kWeightThreads = 64 * kWeightWaves;
 
-template <int BITS, int AXIS>
-__device__ __forceinline__ void weigh(const KeyWords<BITS, AXIS>& kw, const TreeArgs& a, int bh, QueryTiles<kWeightRT>& sq, ScaleStrip& strip,
-                                      float (&s_lse)[kWeightRT * 16], bool live, int tail0, float (&cs)[8]) {
-    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
-    const Fields<BITS> fields;
-#pragma unroll 1
-    for (int row0 = 0; row0 < a.rows; row0 += kWeightRT * 16) {
-        if (row0) __syncthreads();
-        const int tiles = min(kWeightRT, (a.rows - row0 + 15) / 16);
-        stage_queries<kWeightRT>(a, bh, row0, 16 * tiles, kWeightThreads, sq);
-        if (threadIdx.x < kWeightRT * 16) {
-            const int r = row0 + threadIdx.x;
-            const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;
-            s_lse[threadIdx.x] = l == -INFINITY ? INFINITY : l;        // (a row that sees nothing gives nothing)
-        }
-        __syncthreads();
-        if (!live) continue;
-#pragma unroll 1
-        for (int rt = 0; rt < tiles; ++rt) {
-            f4v acc[1][2];
-            key_product<BITS, AXIS, 1>(fields, kw, sq.frag + rt * 256, sq.sums + rt * 64, strip, lane, acc);
-            // (in natural units up to the exponential: sm_scale and the rows' powers of two are exact)
-            const float f = sq.factor[16 * rt + n] * a.sm_scale;
-            const float base = -s_lse[16 * rt + n];
-            const int i = (row0 + 16 * rt + n) % a.n_new;
+// Sums of eight values over the 16 lanes of a row of lanes; lane n gets that of value n % 8.  (Two values become one at every exchange:
+// 22 instructions where a sum for each takes 32 and a choice.)
+__device__ __forceinline__ float column_sums(const float (&v)[8], int n) {
+    float a[4], b[2];
+    auto join = [](bool odd, float x, float y, auto other) { const float keep = odd ? y : x, give = odd ? x : y; return keep + other(give); };
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[0][j >> 2][j & 3], f, base) * kLog2e);
-                // (tail0 < 0: packed tokens, which every row sees)
-                if (tail0 >= 0 && tail0 + 16 * (j >> 2) + 4 * kb + (j & 3) > a.tail_len - a.n_new + i) p = 0.0f;
-                cs[j] += p;
-            }
-        }
-    }
+    for (int j = 0; j < 4; ++j) a[j] = join(n & 1, v[2 * j], v[2 * j + 1], [](float x) { return dpp<kQuadXor1>(x); });
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b[j] = join(n & 2, a[2 * j], a[2 * j + 1], [](float x) { return dpp<kQuadXor2>(x); });
+    const float c = join(n & 4, b[0], b[1], [](float x) { return dpp<kRowHalfMirror>(dpp<0x1B /* quad_perm [3,2,1,0] */>(x)); });      // (lane ^ 4)
+    return c + dpp<0x128 /* row_ror:8 */>(c);
 }
 
-template <int BITS, int AXIS>
-__global__ __launch_bounds__(kWeightThreads) void add_weights(const TreeArgs a) {
-    __shared__ QueryTiles<kWeightRT> sq;
+template <int BITS, int AXIS, int RT>
+__global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs a) {
+    __shared__ QueryTiles<RT> sq;
     __shared__ ScaleStrip s_strip[kWeightWaves];
-    __shared__ float s_lse[kWeightRT * 16];
+    __shared__ float s_lse[RT * 16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, kb = lane >> 4;
     const int bh = blockIdx.y;
-    const int n_tok = head_tokens(a, bh);
+    const int n_tok = __builtin_amdgcn_readfirstlane(head_tokens(a, bh));
     const int packed = (n_tok + 31) / 32, units = packed + (a.tail_len + 31) / 32;
-    // (workgroups of a shorter head beyond its blocks leave at once)
-    if ((int)blockIdx.x * kWeightWaves >= units) return;
-    const int u = blockIdx.x * kWeightWaves + wave;
-    const bool live = u < units, is_tail = u >= packed;
-    const int t0 = 32 * (is_tail ? u - packed : u), len = is_tail ? a.tail_len : n_tok;
-    float cs[8];
+    const int u0 = blockIdx.x * a.units_per_wg, u1 = min(u0 + a.units_per_wg, units);
+    if (u0 >= units) return;              // (a workgroup of a shorter head, beyond its blocks)
+    float* weights = a.weights + (size_t)bh * a.w_cap;
+    ScaleStrip& strip = s_strip[wave];
+
+#pragma unroll 1
+    for (int row0 = 0; row0 < a.rows; row0 += RT * 16) {
+        if (row0) __syncthreads();
+        stage_queries<RT>(a, bh, row0, RT * 16, kWeightThreads, sq);
+        if (threadIdx.x < RT * 16) {
+            const int r = row0 + threadIdx.x;
+            const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;
+            s_lse[threadIdx.x] = l == -INFINITY ? -INFINITY : -l;        // (a row that sees nothing gives nothing)
+        }
+        __syncthreads();
+        const float decay = row0 ? 1.0f : a.decay;
+        // (in natural units up to the exponential: sm_scale and the rows' powers of two are exact)
+        float factor[RT], minus_lse[RT];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) cs[j] = 0.0f;
-    // (a workgroup may have both kinds of blocks: each goes through the rows by itself, and the other's waves only help to stage them)
-    const int u_first = blockIdx.x * kWeightWaves, u_last = min(u_first + kWeightWaves, units) - 1;
-    if (u_first < packed) {
-        KeyWords<BITS, AXIS> kw;
-        load_keys<BITS, AXIS>(head_base<BITS, AXIS>(a, bh), a.group_log2, min(u, packed - 1), lane, kw);
-        strip_keys<BITS, AXIS>(kw, s_strip[wave], lane);
-        weigh<BITS, AXIS>(kw, a, bh, sq, s_strip[wave], s_lse, live && !is_tail, -1, cs);
-    }
-    if (u_last >= packed) {
-        if (u_first < packed) __syncthreads();
-        KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
-        const int tt = is_tail && live ? t0 : 0;
+        for (int rt = 0; rt < RT; ++rt) { factor[rt] = sq.factor[16 * rt + n] * a.sm_scale; minus_lse[rt] = s_lse[16 * rt + n]; }
+        auto weight = [&](float logit, int rt) { return __builtin_amdgcn_exp2f(__builtin_fmaf(logit, factor[rt], minus_lse[rt]) * kLog2e); };
+        // lane n < 8 of a row of lanes stores token 16 (n / 4) + 4 kb + n % 4
+        auto store = [&](const float (&cs)[8], float* w, int t0, int len) {
+            const float mine = column_sums(cs, n);
+            const int t = t0 + 16 * (n >> 2) + 4 * kb + (n & 3);
+            if (n < 8 && t < len) w[t] = decay != 0.0f ? __builtin_fmaf(decay, w[t], mine) : mine;
+        };
+        const int end = min(u1, packed);
+        int blk = u0 + wave;
+        if (blk < end) {
+            const Fields<BITS> fields;
+            const HeadBase base = head_base<BITS, AXIS>(a, bh);
+            KeyWords<BITS, AXIS> kw;
+            load_keys<BITS, AXIS>(base, a.group_log2, blk, lane, kw);
+#pragma unroll 1
+            for (; blk < end; blk += kWeightWaves) {
+                f4v acc[RT][2];
+                strip_keys<BITS, AXIS>(kw, strip, lane);
+                key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
+                load_keys<BITS, AXIS>(base, a.group_log2, min(blk + kWeightWaves, end - 1), lane, kw);
+                float cs[8];
 #pragma unroll
-        for (int H = 0; H < 2; ++H) {
-            const uint16_t* p = a.tail_k + ((size_t)bh * a.tail_cap + min(tt + 16 * H + n, a.tail_len - 1)) * kHeadDim + 32 * kb;
+                for (int j = 0; j < 8; ++j) {
+                    cs[j] = weight(acc[0][j >> 2][j & 3], 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
-                kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
+                    for (int rt = 1; rt < RT; ++rt) cs[j] += weight(acc[rt][j >> 2][j & 3], rt);
+                }
+                store(cs, weights, 32 * blk, n_tok);
             }
         }
-        weigh<16, KVQP_KEY_PER_CHANNEL>(kw, a, bh, sq, s_strip[wave], s_lse, live && is_tail, t0, cs);
-    }
-    if (!live) return;
-    // lane i of a row of 16 lanes stores token 4 kb + i of both tiles
+#pragma unroll 1
+        for (int u = max(u0, packed) + wave; u < u1; u += kWeightWaves) {
+            const int t0 = 32 * (u - packed);
+            KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
 #pragma unroll
-    for (int H = 0; H < 2; ++H) {
-        float v[4];
+            for (int H = 0; H < 2; ++H) {
+                const uint16_t* p = a.tail_k + ((size_t)bh * a.tail_cap + min(t0 + 16 * H + n, a.tail_len - 1)) * kHeadDim + 32 * kb;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = row16_add(cs[4 * H + i]);
-        const float mine = n == 0 ? v[0] : n == 1 ? v[1] : n == 2 ? v[2] : v[3];
-        const int t = t0 + 16 * H + 4 * kb + n;
-        if (n < 4 && t < len) {
-            float* w = a.weights + (size_t)bh * a.w_cap + (is_tail ? n_tok : 0) + t;
-            *w = a.decay != 0.0f ? __builtin_fmaf(a.decay, *w, mine) : mine;
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
+                    kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
+                }
+            }
+            f4v acc[RT][2];
+            key_product<16, KVQP_KEY_PER_CHANNEL, RT>(Fields<16>(), kw, sq.frag, sq.sums, strip, lane, acc);
+            float cs[8] = {};
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int last = a.tail_len - a.n_new + (row0 + 16 * rt + n) % a.n_new - t0 - 4 * kb;      // the last row of the tail that the query row sees
+#pragma unroll
+                for (int j = 0; j < 8; ++j) cs[j] += 16 * (j >> 2) + (j & 3) <= last ? weight(acc[rt][j >> 2][j & 3], rt) : 0.0f;
+            }
+            store(cs, weights + n_tok, t0, a.tail_len);
         }
     }
 }
@@ -948,9 +956,15 @@ hipError_t run_tree_rt(const TreeArgs& a, int rt, hipStream_t stream) {
     return run_tree<BITS, AXIS, 4>(a, stream);
 }
 template <int BITS, int AXIS>
-hipError_t run_weights(const TreeArgs& a, hipStream_t stream) {
-    const int units = (a.n_kept + 31) / 32 + (a.tail_len + 31) / 32;
-    add_weights<BITS, AXIS><<<dim3((units + kWeightWaves - 1) / kWeightWaves, a.heads), dim3(kWeightThreads), 0, stream>>>(a);
+hipError_t run_weights(const TreeArgs& a0, hipStream_t stream) {
+    TreeArgs a = a0;
+    // Two workgroups per CU are there at a time: as many blocks to each as make that one round, and at least one per wave.
+    const int units = (a.n_kept + 31) / 32 + (a.tail_len + 31) / 32, per_head = std::max(1, 512 / a.heads);
+    a.units_per_wg = ((units + per_head - 1) / per_head + kWeightWaves - 1) / kWeightWaves * kWeightWaves;
+    const dim3 grid((units + a.units_per_wg - 1) / a.units_per_wg, a.heads), block(kWeightThreads);
+    if (a.rows <= 16) add_weights<BITS, AXIS, 1><<<grid, block, 0, stream>>>(a);
+    else if (a.rows <= 32) add_weights<BITS, AXIS, 2><<<grid, block, 0, stream>>>(a);
+    else add_weights<BITS, AXIS, 4><<<grid, block, 0, stream>>>(a);
     return hipGetLastError();
 }
 
