@@ -427,7 +427,7 @@ int kvqp_append_tail_ragged(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_to
  * kvqp_evict takes the cache back to its budget.
  *
  * Common to the three: cfg fields used are batch, heads, head_dim, bits, group_size, key_axis and
- * sm_scale.  Caches with outlier filtering are not taken (UNSUPPORTED).  Head-level counts
+ * sm_scale, and decode_cache_hint, where AUTO here means STREAM for calls on more than 96 MB of codes and KEEP for others.  Caches with outlier filtering are not taken (UNSUPPORTED).  Head-level counts
  * (cache->head_n_kept) are read on the device, where a count above n_kept is cut to n_kept.
  * q, k_new, v_new, out and the cache's codes, per-channel scales and zeros and tails have to be aligned to
  * 16 bytes, everything else to its own size and the scales and zeros that belong to tokens to 4 (INVALID_ARG).
