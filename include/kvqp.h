@@ -441,6 +441,13 @@ int kvqp_append_tail_ragged(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_to
 int kvqp_tree_workspace_bytes(const kvqp_cfg *cfg, int32_t n_rows, size_t *bytes);
 
 /*
+ * Prepares a workspace of kvqp_tree_attn, once after its allocation: zeroes the 4 KB of arrival counters at its head with a small kernel
+ * enqueued on the stream.  Every launch that completes leaves them zero; after one that did not, the workspace is prepared again.
+ * Errors: WORKSPACE when it is NULL or smaller than the counters, INVALID_ARG when it is not aligned to 16 bytes.
+ */
+int kvqp_tree_workspace_init(void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Attention of n_rows drafted tokens (1 .. KVQP_MOST_ROWS; a tree, a chain, or the one token of an ordinary
  * step) over the compressed cache (Eq. (3) as in kvqp_decode_attn): row i attends over the packed
  * tokens, the tail_len tail rows, and those drafted tokens whose bit is set in its mask.
@@ -459,8 +466,9 @@ int kvqp_tree_workspace_bytes(const kvqp_cfg *cfg, int32_t n_rows, size_t *bytes
  * Numerical range: the product of a query element, scaled so that its row's largest is 64 .. 128,
  * and its channel's key scale must stay below 65504 (a scale of 511), and with per-token keys a
  * code times its scale; weights are exact to 2^-22, values are rounded to binary16 once.
- * Workspace: kvqp_tree_workspace_bytes, 16-byte aligned, no preparation; calls that share one must not
- * overlap in time.
+ * Workspace: kvqp_tree_workspace_bytes, 16-byte aligned, prepared once with kvqp_tree_workspace_init.  One may
+ * serve calls of any configurations for which it is large enough; calls that share one must not overlap in time
+ * (calls issued on one stream never do), calls with different ones are independent.
  */
 int kvqp_tree_attn(const kvqp_cfg *cfg, const void *q, const void *k_new, const void *v_new, const uint32_t *mask,
                    int32_t mask_per_batch, int32_t n_rows, const kvqp_cache *cache, void *out, float *lse, void *workspace,

@@ -126,7 +126,6 @@ __global__ __launch_bounds__(THREADS) void pick_heaviest(const EvictArgs a) {
     // body(unit, its key, whether there is such a unit) for the wave's units, in order.  (Rolled up: every launch fetches its code anew, and
     // keys in registers, with the loops unrolled, took 20 us instead of 15 for 16 heads of 12003.)
     auto each = [&](auto body) {
-#pragma unroll 2
         for (int j = 0; j < steps; ++j) {
             const int u = u0 + 64 * j + lane;
             body(u, KEYS > 0 ? own[64 * j] : u < cut.units ? unit_key(w, u, a.unit) : 0u, u < cut.units);

@@ -133,9 +133,12 @@ struct TreePlan {
     int n_splits, most_splits;     // token-axis splits of this call, and of any with the same rows
     size_t ws_bytes, ws_bound;     // workspace of this call, and of any
 };
+// Arrival counters at the head of a workspace, one per head and block of rows: launches with splits have at most 256 of these.
+constexpr size_t kTreeCounterBytes = 4096;
 TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len);
 hipError_t launch_tree(const kvqp_cfg& cfg, const void* q, const void* k_new, const void* v_new, const uint32_t* mask, bool mask_per_batch,
                        int n_rows, const kvqp_cache& cache, void* out, float* lse, void* ws, const TreePlan& plan, hipStream_t stream);
+hipError_t launch_tree_init(void* ws, hipStream_t stream);      // zeroes the counters
 hipError_t launch_weights(const kvqp_cfg& cfg, const void* q, const float* lse, int n_rows, const kvqp_cache& cache, float* weights, int w_cap,
                           float decay, hipStream_t stream);
 int evict_kept(int n, int n_keep, int unit);     // tokens that stay of a head's n

@@ -40,6 +40,12 @@ int kvqp_tree_workspace_bytes(const kvqp_cfg* cfg, int32_t n_rows, size_t* bytes
     return KVQP_OK;
 }
 
+int kvqp_tree_workspace_init(void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!workspace || workspace_bytes < kTreeCounterBytes) return KVQP_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return KVQP_ERR_INVALID_ARG;
+    return launch_tree_init(workspace, (hipStream_t)hip_stream) == hipSuccess ? KVQP_OK : KVQP_ERR_HIP;
+}
+
 int kvqp_tree_attn(const kvqp_cfg* cfg, const void* q, const void* k_new, const void* v_new, const uint32_t* mask, int32_t mask_per_batch,
                    int32_t n_rows, const kvqp_cache* cache, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
     const int rc = check_read_cache(cfg, cache);

@@ -48,8 +48,8 @@ union Frag {  // one MFMA 16x16x32 f16 input operand of a lane: 8 halves
 };
 
 // The most waves of a workgroup, by its rows in tiles of 16: 16, 12 or 8, as many as the registers of a CU leave room for
-// (124, 168 and 256 per lane).  A launch may use fewer.
-constexpr int most_waves(int rt) { return rt == 1 ? 16 : rt == 2 ? 12 : 8; }
+// (128, 168 and 256 per lane; codes of 16 bits want 168 for one tile, too).  A launch may use fewer.
+constexpr int most_waves(int bits, int rt) { return rt == 1 ? (bits == 16 ? 12 : 16) : rt == 2 ? 12 : 8; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegBig = -1.0e30f;     // reference of a row that has seen nothing
@@ -166,7 +166,8 @@ struct TreeArgs {
     const uint16_t* k_new;    // [B*Hkv, N, D]
     const uint16_t* v_new;
     const uint32_t* mask;     // [B or 1, N, mask_words], or NULL: row i sees new tokens 0 .. i
-    float* part;              // [groups][8 RT][64] float4 of outputs, then [groups][16 RT] (reference, sum)
+    unsigned int* arrivals;   // [heads * row_blocks] at the head of the workspace, zero between launches
+    float* part;              // per (head, row block): [splits][8 RT][64] float4 of outputs, then [splits][16 RT] (reference, sum)
     uint16_t* out;            // [B*Hkv, R, D]
     float* lse;               // [B*Hkv, R] (read by the weights kernel), or NULL
     float* weights;           // [B*Hkv, w_cap]
@@ -199,14 +200,29 @@ template <int RT> struct QueryTiles {
     uint32_t sums[RT * 64];       // per (row, kb): the sum of the row's 32 channels as binary16 hi, lo
     float factor[RT * 16];        // 2^-k of a row that was scaled by 2^k
 };
-// Rows row0 .. row0 + n_rows - 1 of one head, by all threads of the workgroup; rows past the head's last are zeros.
+// A thread's share of the rows row0 .. row0 + 16 RT - 1 of one head, eight channels each (zeros past the head's last row): requested first ...
+template <int RT> struct QueryPieces { uint4 w[RT]; };        // (at least 256 threads)
 template <int RT>
-__device__ __forceinline__ void stage_queries(const TreeArgs& a, int bh, int row0, int n_rows, int threads, QueryTiles<RT>& sq) {
-    const int seg = threadIdx.x & 15;
-    for (int r = threadIdx.x >> 4; r < n_rows; r += threads >> 4) {
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
-        if (row0 + r < a.rows) w = *reinterpret_cast<const uint4*>(a.q + ((size_t)bh * a.rows + row0 + r) * kHeadDim + 8 * seg);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ QueryPieces<RT> request_queries(const TreeArgs& a, int bh, int row0) {
+    QueryPieces<RT> p;
+    const int per = blockDim.x >> 4;
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+        const int r = (threadIdx.x >> 4) + j * per;
+        p.w[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < 16 * RT && row0 + r < a.rows) p.w[j] = *reinterpret_cast<const uint4*>(a.q + ((size_t)bh * a.rows + row0 + r) * kHeadDim + 8 * (threadIdx.x & 15));
+    }
+    return p;
+}
+// ... and, behind whatever else the caller has requested meanwhile, put into LDS.
+template <int RT>
+__device__ __forceinline__ void stage_queries(const QueryPieces<RT>& p, QueryTiles<RT>& sq) {
+    const int seg = threadIdx.x & 15, per = blockDim.x >> 4;
+#pragma unroll
+    for (int j0 = 0; j0 < RT; ++j0) {
+        const int r = (threadIdx.x >> 4) + j0 * per;
+        if (r >= 16 * RT) break;
+        const uint32_t u[4] = {p.w[j0].x, p.w[j0].y, p.w[j0].z, p.w[j0].w};
         float x[8], top = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -216,7 +232,7 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, int bh, int row
         top = row16_max(top);
         // (a power of two, so nothing is rounded that matters: the largest element becomes 64 .. 128)
         const int k = top > 0.0f ? 133 - (int)((__float_as_uint(top) >> 23) & 0xffu) : 0;
-        const float up = ldexpf(1.0f, k);
+        const float up = __uint_as_float((uint32_t)(127 + k) << 23);
         Frag f;
         float sum = 0.0f;
 #pragma unroll
@@ -232,7 +248,7 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, int bh, int row
             const _Float16 hi = (_Float16)sum, lo = (_Float16)(sum - (float)hi);
             sq.sums[rt * 64 + kb * 16 + n] = as_u32(h2v{hi, lo});
         }
-        if (seg == 0) sq.factor[r] = ldexpf(1.0f, -k);
+        if (seg == 0) sq.factor[r] = __uint_as_float((uint32_t)(127 - k) << 23);
     }
 }
 
@@ -539,17 +555,59 @@ __device__ __forceinline__ void strip_values(const TreeArgs& a, const ValueWords
 constexpr int kPlainStride = kHeadDim + 8;      // halves between two rows of a value tile in LDS
 struct __align__(16) PlainTile { uint16_t v[32 * kPlainStride]; };
 
-// A workgroup's LDS: while blocks are worked on, then while the waves' states are joined.
+// A workgroup's LDS: while blocks are worked on, and while the waves' states become one (outputs of JOIN row tiles at a time).
 union WaveScratch { ScaleStrip strip; PlainTile tile; };
-template <int RT> struct MergeSlot { f4v o[RT][8][64]; float2 m[RT][64]; };      // outputs; reference and sum
-template <int RT> union __align__(16) TreeShared {
-    struct { QueryTiles<RT> sq; WaveScratch wave[most_waves(RT)]; } run;
-    MergeSlot<RT> merge[most_waves(RT) / 2];
+constexpr int kMostSplits = 64;
+constexpr int join_tiles(int rt) { return rt == 4 ? 2 : 1; }
+template <int BITS, int RT> union __align__(16) TreeShared {
+    struct { QueryTiles<RT> sq; WaveScratch wave[most_waves(BITS, RT)]; } run;
+    struct { f4v o[most_waves(BITS, RT)][join_tiles(RT) * 8][64]; float ref[most_waves(BITS, RT)][16 * RT], sum[most_waves(BITS, RT)][16 * RT]; } join;
+    struct { float weight[kMostSplits][16 * RT], sum[kMostSplits][16 * RT], inverse[16 * RT]; } last;       // of a row block's splits
 };
+// One row block's partial results in the workspace, written and read with accesses at device scope (sc1): workgroups of one row block
+// run on different dies, whose L2 caches do not see each other within a launch.
+constexpr int kDeviceScope = 16;      // sc1 in a buffer access' cache policy
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+template <int I> struct IntC { static constexpr int value = I; };
+struct Partials {
+    __amdgpu_buffer_rsrc_t at;
+    int states, rt;                   // where references and sums begin
+    __device__ __forceinline__ Partials(const TreeArgs& a, int group, int rt_) : states(a.n_splits * rt_ * 8192), rt(rt_) {
+        const int bytes = states + a.n_splits * rt_ * 128;
+        at = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(a.part) + (size_t)group * bytes, 0, bytes, 0x00020000);
+    }
+    __device__ __forceinline__ void put_output(int split, int item, f4v o) const {
+        u4v v = {__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3])};
+        __builtin_amdgcn_raw_buffer_store_b128(v, at, (split * rt * 512 + item) * 16, 0, kDeviceScope);
+    }
+    __device__ __forceinline__ void put_state(int split, int row, float ref, float sum) const {
+        u2v v = {__float_as_uint(ref), __float_as_uint(sum)};
+        __builtin_amdgcn_raw_buffer_store_b64(v, at, states + (split * rt * 16 + row) * 8, 0, kDeviceScope);
+    }
+    __device__ __forceinline__ f4v output(int split, int item) const {
+        const u4v v = __builtin_amdgcn_raw_buffer_load_b128(at, (split * rt * 512 + item) * 16, 0, kDeviceScope);
+        return f4v{__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])};
+    }
+    __device__ __forceinline__ float2 state(int split, int row) const {
+        const u2v v = __builtin_amdgcn_raw_buffer_load_b64(at, states + (split * rt * 16 + row) * 8, 0, kDeviceScope);
+        return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1]));
+    }
+};
+__device__ __forceinline__ uint2 halves_of(const f4v& o, float by) {
+    Frag h;
+    h.h[0] = h2v{(_Float16)(o[0] * by), (_Float16)(o[1] * by)};
+    h.h[1] = h2v{(_Float16)(o[2] * by), (_Float16)(o[3] * by)};
+    return make_uint2(h.u[0], h.u[1]);
+}
+// (a row that sees nothing: zeros, and minus infinity)
+__device__ __forceinline__ float inverse_sum(float sum) { return sum > 0.0f ? 1.0f / sum : sum; }
+__device__ __forceinline__ float log_sum(float ref, float sum) { return sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2; }
 
 template <int BITS, int AXIS, int RT, bool ONCE>
-__global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_attn(const TreeArgs a) {
-    __shared__ TreeShared<RT> sh;
+__global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4) void tree_attn(const TreeArgs a) {
+    __shared__ TreeShared<BITS, RT> sh;
+    __shared__ int s_last;
     QueryTiles<RT>& sq = sh.run.sq;
 
     const int lane = threadIdx.x & 63;
@@ -561,13 +619,24 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     if (pair >= a.heads * a.n_splits) return;
     const int bh = __builtin_amdgcn_readfirstlane(pair / a.n_splits), split = pair - bh * a.n_splits;
     const int row0 = rb * RT * 16;
-    stage_queries<RT>(a, bh, row0, RT * 16, 64 * waves, sq);
+    // (loads return in order: the queries first, then the wave's first block, which is on its way while they are put into LDS)
+    const QueryPieces<RT> pieces = request_queries<RT>(a, bh, row0);
 
     const int n_tok = __builtin_amdgcn_readfirstlane(head_tokens(a, bh));
     const int packed = (n_tok + 31) / 32, tail = (a.tail_len + 31) / 32, fresh = (a.n_new + 31) / 32;
     const int units = packed + tail + fresh;
     const int share = __builtin_amdgcn_readfirstlane((int)((unsigned)units / (unsigned)a.n_splits)), rest = units - share * a.n_splits;
     const int u0 = share * split + min(split, rest), u1 = u0 + share + (split < rest ? 1 : 0);
+    const int end = min(u1, packed);
+    int blk = u0 + wave;
+    const HeadBase base = head_base<BITS, AXIS>(a, bh);
+    KeyWords<BITS, AXIS> kw;
+    ValueWords<BITS> vw;
+    if (blk < end) {
+        load_keys<BITS, AXIS, ONCE>(base, a.group_log2, blk, lane, kw);
+        load_values<BITS, ONCE>(base, a.group_log2, blk, lane, vw);
+    }
+    stage_queries<RT>(pieces, sq);
     ScaleStrip& strip = sh.run.wave[wave].strip;
 
     RowState<RT> st;
@@ -583,14 +652,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     // ---- packed blocks ----
     {
         const Fields<BITS> fields;
-        const HeadBase base = head_base<BITS, AXIS>(a, bh);
-        const int end = min(u1, packed);
-        int blk = u0 + wave;
         if (blk < end) {
-            KeyWords<BITS, AXIS> kw;
-            ValueWords<BITS> vw;
-            load_keys<BITS, AXIS, ONCE>(base, a.group_log2, blk, lane, kw);
-            load_values<BITS, ONCE>(base, a.group_log2, blk, lane, vw);
 #pragma unroll 1
             for (; blk < end; blk += waves) {
                 const int next = min(blk + waves, end - 1);
@@ -648,32 +710,35 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
             const size_t row = drafted ? (size_t)bh * a.n_new : (size_t)bh * a.tail_cap;
             const uint16_t* kp = (drafted ? a.k_new : a.tail_k) + row * kHeadDim;
             const uint16_t* vp = (drafted ? a.v_new : a.tail_v) + row * kHeadDim;
-            lds_order();
-            bool odd_value = false;       // a value that is not finite
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int t = 4 * j + kb;
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (t0 + t < len) w = *reinterpret_cast<const uint4*>(vp + (size_t)(t0 + t) * kHeadDim + 8 * n);
-                const uint32_t u4[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) odd_value |= (u4[e] & 0x7C00u) == 0x7C00u || (u4[e] & 0x7C000000u) == 0x7C000000u;
-                *reinterpret_cast<uint4*>(&tile_v.v[t * kPlainStride + 8 * n]) = w;
-            }
-            lds_order();
-            KeyWords<16, KVQP_KEY_PER_CHANNEL> kw;
+            KeyWords<16, KVQP_KEY_PER_CHANNEL> pk;
 #pragma unroll
             for (int H = 0; H < 2; ++H) {
                 const uint16_t* p = kp + (size_t)min(t0 + 16 * H + n, len - 1) * kHeadDim + 32 * kb;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint4 w = *reinterpret_cast<const uint4*>(p + 8 * j);
-                    kw.w[H][4 * j] = w.x; kw.w[H][4 * j + 1] = w.y; kw.w[H][4 * j + 2] = w.z; kw.w[H][4 * j + 3] = w.w;
+                    pk.w[H][4 * j] = w.x; pk.w[H][4 * j + 1] = w.y; pk.w[H][4 * j + 2] = w.z; pk.w[H][4 * j + 3] = w.w;
                 }
             }
+            uint4 rows[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                rows[j] = make_uint4(0u, 0u, 0u, 0u);
+                if (t0 + 4 * j + kb < len) rows[j] = *reinterpret_cast<const uint4*>(vp + (size_t)(t0 + 4 * j + kb) * kHeadDim + 8 * n);
+            }
+            lds_order();
+            bool odd_value = false;       // a value that is not finite
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t u4[4] = {rows[j].x, rows[j].y, rows[j].z, rows[j].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd_value |= (u4[e] & 0x7C00u) == 0x7C00u || (u4[e] & 0x7C000000u) == 0x7C000000u;
+                *reinterpret_cast<uint4*>(&tile_v.v[(4 * j + kb) * kPlainStride + 8 * n]) = rows[j];
+            }
+            lds_order();
             f4v acc[RT][2];
             {
-                key_product<16, KVQP_KEY_PER_CHANNEL, RT>(Fields<16>(), kw, sq.frag, sq.sums, strip, lane, acc);
+                key_product<16, KVQP_KEY_PER_CHANNEL, RT>(Fields<16>(), pk, sq.frag, sq.sums, strip, lane, acc);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     // which of the block's 32 tokens the row sees
@@ -742,110 +807,189 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     }
 
     // ---- the waves' states become one ----
+    // Every wave brings its outputs to the rows' highest reference; then the threads share the sums over the waves among them, JOIN row
+    // tiles at a time.  (Pairs of waves, halving their number, took 3.9 us for twelve waves of 32 rows, this 3.)
+    constexpr int JOIN = join_tiles(RT);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) st.sum[rt] = rows4_add(st.sum[rt]);
-#pragma unroll 1
-    for (int left = waves; left > 1;) {
-        const int half = (left + 1) / 2;
-        __syncthreads();
-        if (wave >= half && wave < left) {
+    __syncthreads();
+    if (kb == 0)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-                for (int t = 0; t < 8; ++t) sh.merge[wave - half].o[rt][t][lane] = st.o[rt][t];
-                sh.merge[wave - half].m[rt][lane] = make_float2(st.ref[rt], st.sum[rt]);
-            }
-        }
-        __syncthreads();
-        if (wave < left - half) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float2 other = sh.merge[wave].m[rt][lane];
-                const float ref = fmaxf(st.ref[rt], other.x);
-                const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref), g = __builtin_amdgcn_exp2f(other.x - ref);
-                st.ref[rt] = ref;
-                st.sum[rt] = st.sum[rt] * f + other.y * g;
-#pragma unroll
-                for (int t = 0; t < 8; ++t) st.o[rt][t] = st.o[rt][t] * f + sh.merge[wave].o[rt][t][lane] * g;
-            }
-        }
-        left = half;
-    }
-    if (wave != 0) return;
-    if (a.n_splits > 1) {
-        const size_t group = (size_t)(bh * a.row_blocks + rb) * a.n_splits + split;
-        f4v* po = reinterpret_cast<f4v*>(a.part) + group * (RT * 8 * 64);
-        float2* ps = reinterpret_cast<float2*>(a.part + (size_t)a.heads * a.row_blocks * a.n_splits * (RT * 16 * kHeadDim)) + group * (RT * 16);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-            for (int t = 0; t < 8; ++t) po[(rt * 8 + t) * 64 + lane] = st.o[rt][t];
-            if (kb == 0) ps[rt * 16 + n] = make_float2(st.ref[rt], st.sum[rt]);
-        }
-        return;
-    }
+        for (int rt = 0; rt < RT; ++rt) { sh.join.ref[wave][16 * rt + n] = st.ref[rt]; sh.join.sum[wave][16 * rt + n] = st.sum[rt]; }
+    __syncthreads();
+    float ref[RT], sum[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int r = row0 + 16 * rt + n;
-        if (r < a.rows) {
-            const float inv = st.sum[rt] > 0.0f ? 1.0f / st.sum[rt] : st.sum[rt];      // (a row that sees nothing: zeros)
-            uint16_t* o = a.out + ((size_t)bh * a.rows + r) * kHeadDim + 4 * kb;
+        // (all of them requested at once; a wave that is not there repeats the first, at weight 0)
+        float r[most_waves(BITS, RT)], s[most_waves(BITS, RT)];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                Frag h;
-                h.h[0] = h2v{(_Float16)(st.o[rt][t][0] * inv), (_Float16)(st.o[rt][t][1] * inv)};
-                h.h[1] = h2v{(_Float16)(st.o[rt][t][2] * inv), (_Float16)(st.o[rt][t][3] * inv)};
-                *reinterpret_cast<uint2*>(o + 16 * t) = make_uint2(h.u[0], h.u[1]);
+        for (int w = 0; w < most_waves(BITS, RT); ++w) { r[w] = sh.join.ref[w < waves ? w : 0][16 * rt + n]; s[w] = sh.join.sum[w < waves ? w : 0][16 * rt + n]; }
+        ref[rt] = r[0];
+#pragma unroll
+        for (int w = 1; w < most_waves(BITS, RT); ++w) ref[rt] = fmaxf(ref[rt], r[w]);
+        sum[rt] = 0.f;
+#pragma unroll
+        for (int w = 0; w < most_waves(BITS, RT); ++w) sum[rt] = __builtin_fmaf(w < waves ? s[w] : 0.f, __builtin_amdgcn_exp2f(r[w] - ref[rt]), sum[rt]);
+        const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref[rt]);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) st.o[rt][t] *= f;
+    }
+    const Partials parts(a, bh * a.row_blocks + rb, RT);
+    if (wave == 0 && kb == 0) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int r = row0 + 16 * rt + n;
+            if (a.n_splits > 1) parts.put_state(split, 16 * rt + n, ref[rt], sum[rt]);
+            else if (a.lse && r < a.rows) a.lse[(size_t)bh * a.rows + r] = log_sum(ref[rt], sum[rt]);
+        }
+    }
+#pragma unroll
+    for (int j0 = 0; j0 < RT; j0 += JOIN) {
+        if (j0) __syncthreads();
+#pragma unroll
+        for (int rt = 0; rt < JOIN; ++rt)
+#pragma unroll
+            for (int t = 0; t < 8; ++t) sh.join.o[wave][8 * rt + t][lane] = st.o[j0 + rt][t];
+        __syncthreads();
+        for (int slot = wave; slot < 8 * JOIN; slot += waves) {
+            f4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int w = 0; w < waves; w += 4) {          // (workgroups have whole fours of waves)
+                f4v four[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) four[u] = sh.join.o[w + u][slot][lane];
+                o += (four[0] + four[1]) + (four[2] + four[3]);
             }
-            if (a.lse && kb == 0) a.lse[(size_t)bh * a.rows + r] = st.sum[rt] == 0.0f ? -INFINITY : (st.ref[rt] + __builtin_amdgcn_logf(st.sum[rt])) * kLn2;
+            const int t = slot & 7;
+            if (a.n_splits > 1) {
+                parts.put_output(split, (j0 * 8 + slot) * 64 + lane, o);
+            } else {
+                float total = sum[j0];
+#pragma unroll
+                for (int rt = 1; rt < JOIN; ++rt) total = (slot >> 3) == rt ? sum[j0 + rt] : total;
+                const int r = row0 + 16 * (j0 + (slot >> 3)) + n;
+                if (r < a.rows) *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * t + 4 * kb) = halves_of(o, inverse_sum(total));
+            }
         }
     }
-}
+    if (a.n_splits == 1) return;
 
-// Joins the splits of a row block: a thread has four channels of one row.
-template <int RT>
-__global__ __launch_bounds__(256) void tree_merge(const TreeArgs a) {
-    const int item = blockIdx.x * 256 + threadIdx.x;              // [bh, rb][rt][tile][lane]
-    const int lane = item & 63, tile = (item >> 6) & 7, rt = (item >> 9) % RT;
-    const int rest = (item >> 9) / RT;
-    if (rest >= a.heads * a.row_blocks) return;
-    const int bh = rest / a.row_blocks, rb = rest % a.row_blocks;
-    const int n = lane & 15, kb = lane >> 4;
-    const int r = rb * RT * 16 + rt * 16 + n;
-    if (r >= a.rows) return;
-    const f4v* po = reinterpret_cast<const f4v*>(a.part) + (size_t)rest * a.n_splits * (RT * 8 * 64) + (rt * 8 + tile) * 64 + lane;
-    const float2* ps = reinterpret_cast<const float2*>(a.part + (size_t)a.heads * a.row_blocks * a.n_splits * (RT * 16 * kHeadDim)) +
-                       (size_t)rest * a.n_splits * (RT * 16) + rt * 16 + n;
-    float ref = kNegBig, sum = 0.f;
-    f4v o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < a.n_splits; s0 += 8) {
-        f4v v[8];
-        float2 m[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int s = min(s0 + u, a.n_splits - 1);
-            v[u] = po[(size_t)s * (RT * 8 * 64)];
-            m[u] = ps[(size_t)s * (RT * 16)];
-        }
-        float top = ref;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) top = fmaxf(top, m[u].x);
-        const float f = __builtin_amdgcn_exp2f(ref - top);
-        o *= f; sum *= f;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float g = s0 + u < a.n_splits ? __builtin_amdgcn_exp2f(m[u].x - top) : 0.f;
-            o += v[u] * g;
-            sum = __builtin_fmaf(m[u].y, g, sum);
-        }
-        ref = top;
+    // ---- the last workgroup of a row block to arrive joins its splits ----
+    // The partials were stored past this die's L2, and the wait returns when the stores have been acknowledged from there; so whoever sees the
+    // counter sees them, with loads that do not look into its own L2.
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned int* count = &a.arrivals[bh * a.row_blocks + rb];
+        const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = before == (unsigned)(a.n_splits - 1);
+        if (s_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : sum;
-    Frag h;
-    h.h[0] = h2v{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv)};
-    h.h[1] = h2v{(_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
-    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * tile + 4 * kb) = make_uint2(h.u[0], h.u[1]);
-    if (a.lse && tile == 0 && kb == 0) a.lse[(size_t)bh * a.rows + r] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+    __syncthreads();
+    if (!s_last) return;
+    if constexpr (RT <= 2) {
+        // A thread has its item's splits to itself, states and outputs together, four or eight at a time: what is requested
+        // beyond the last split costs time too (sixteen at a time: 16.6 us where three splits take 14.4).
+        auto join = [&](auto batch) {
+            constexpr int BATCH = decltype(batch)::value;
+#pragma unroll 1
+            for (int item = threadIdx.x; item < RT * 512; item += blockDim.x) {
+                const int row = 16 * (item >> 9) + n, r = row0 + row;         // (64 items of one wave: one tile of one row tile)
+                float top = kNegBig, total = 0.f;
+                f4v o = {0.f, 0.f, 0.f, 0.f};
+                for (int s0 = 0; s0 < a.n_splits; s0 += BATCH) {
+                    f4v v[BATCH];
+                    float2 m[BATCH];
+#pragma unroll
+                    for (int u = 0; u < BATCH; ++u) {
+                        const int s = min(s0 + u, a.n_splits - 1);
+                        v[u] = parts.output(s, item);
+                        m[u] = parts.state(s, row);
+                    }
+                    float higher = top;
+#pragma unroll
+                    for (int u = 0; u < BATCH; ++u) higher = fmaxf(higher, m[u].x);
+                    const float f = __builtin_amdgcn_exp2f(top - higher);
+                    o *= f; total *= f;
+#pragma unroll
+                    for (int u = 0; u < BATCH; ++u) {
+                        const float g = s0 + u < a.n_splits ? __builtin_amdgcn_exp2f(m[u].x - higher) : 0.f;
+                        o += v[u] * g;
+                        total = __builtin_fmaf(m[u].y, g, total);
+                    }
+                    top = higher;
+                }
+                if (r < a.rows) {
+                    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * ((item >> 6) & 7) + 4 * kb) = halves_of(o, inverse_sum(total));
+                    if (a.lse && (item & 0x1C0) == 0 && kb == 0) a.lse[(size_t)bh * a.rows + r] = log_sum(top, total);
+                }
+            }
+        };
+        if (a.n_splits <= 4) join(IntC<4>{});
+        else join(IntC<8>{});
+    } else {
+        // (two items a thread and eight splits of each in flight; the first of them while 16 RT threads turn the splits' states into weights)
+        constexpr int ITEMS = 2;
+        const int stride = blockDim.x;
+#pragma unroll 1
+        for (int item0 = 0; item0 < RT * 512; item0 += ITEMS * stride) {
+            f4v o[ITEMS];
+#pragma unroll
+            for (int e = 0; e < ITEMS; ++e) o[e] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int s0 = 0; s0 < a.n_splits; s0 += 8) {
+                f4v v[ITEMS][8];
+#pragma unroll
+                for (int e = 0; e < ITEMS; ++e)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) v[e][u] = parts.output(min(s0 + u, a.n_splits - 1), min(item0 + e * stride + (int)threadIdx.x, RT * 512 - 1));
+                if (item0 == 0 && s0 == 0) {
+                    if ((int)threadIdx.x < 16 * RT) {
+                        float top = kNegBig, total = 0.f;
+                        for (int s1 = 0; s1 < a.n_splits; s1 += 16) {
+                            float2 m[16];
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) m[u] = parts.state(min(s1 + u, a.n_splits - 1), threadIdx.x);
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) {
+                                top = fmaxf(top, m[u].x);
+                                sh.last.weight[s1 + u][threadIdx.x] = m[u].x;
+                                sh.last.sum[s1 + u][threadIdx.x] = m[u].y;
+                            }
+                        }
+                        for (int s1 = 0; s1 < a.n_splits; s1 += 16) {
+                            float g[16], l[16];
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) { g[u] = sh.last.weight[s1 + u][threadIdx.x]; l[u] = sh.last.sum[s1 + u][threadIdx.x]; }
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) {
+                                g[u] = s1 + u < a.n_splits ? __builtin_amdgcn_exp2f(g[u] - top) : 0.f;
+                                total = __builtin_fmaf(s1 + u < a.n_splits ? l[u] : 0.f, g[u], total);
+                                sh.last.weight[s1 + u][threadIdx.x] = g[u];
+                            }
+                        }
+                        sh.last.inverse[threadIdx.x] = inverse_sum(total);
+                        const int r = row0 + threadIdx.x;
+                        if (a.lse && r < a.rows) a.lse[(size_t)bh * a.rows + r] = log_sum(top, total);
+                    }
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int e = 0; e < ITEMS; ++e) {
+                    const int row = 16 * (min(item0 + e * stride + (int)threadIdx.x, RT * 512 - 1) >> 9) + n;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) o[e] += v[e][u] * sh.last.weight[s0 + u][row];      // (0 past the last split)
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < ITEMS; ++e) {
+                const int item = item0 + e * stride + threadIdx.x, row = 16 * (item >> 9) + n, r = row0 + row;       // (64 items of a wave: one tile of a row tile)
+                if (item < RT * 512 && r < a.rows)
+                    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * ((item >> 6) & 7) + 4 * kb) = halves_of(o[e], sh.last.inverse[row]);
+            }
+        }
+    }
 }
 
 // ---- weights that tokens receive ----
@@ -885,7 +1029,7 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
 #pragma unroll 1
     for (int row0 = 0; row0 < a.rows; row0 += RT * 16) {
         if (row0) __syncthreads();
-        stage_queries<RT>(a, bh, row0, RT * 16, kWeightThreads, sq);
+        stage_queries<RT>(request_queries<RT>(a, bh, row0), sq);
         if (threadIdx.x < RT * 16) {
             const int r = row0 + threadIdx.x;
             const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;
@@ -961,7 +1105,6 @@ hipError_t run_tree(const TreeArgs& a, hipStream_t stream) {
     constexpr bool kOnce = RT <= 2 || BITS == 16;
     if (kOnce && a.once) tree_attn<BITS, AXIS, RT, kOnce><<<grid, block, 0, stream>>>(a);
     else tree_attn<BITS, AXIS, RT, false><<<grid, block, 0, stream>>>(a);
-    if (a.n_splits > 1) tree_merge<RT><<<dim3((a.heads * a.row_blocks * RT * 512 + 255) / 256), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
 template <int BITS, int AXIS>
@@ -1018,13 +1161,13 @@ TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len) {
     p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     p.row_blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
     const long long base = (long long)cfg.batch * cfg.n_kv_heads * p.row_blocks;
-    p.n_waves = most_waves(p.row_tiles);
-    p.most_splits = (int)std::max(1LL, std::min(256 / base, 64LL));
+    p.n_waves = most_waves(cfg.bits, p.row_tiles);
+    p.most_splits = (int)std::max(1LL, std::min(256 / base, (long long)kMostSplits));
     const int units = (n_kept + 31) / 32 + (tail_len + 31) / 32 + (n_rows + 31) / 32;
     p.n_splits = std::max(1, std::min(p.most_splits, (units + p.n_waves - 1) / p.n_waves));
     const size_t one = (size_t)base * (16 * p.row_tiles) * (kHeadDim + 2) * sizeof(float);
-    p.ws_bytes = p.n_splits > 1 ? one * p.n_splits : 0;
-    p.ws_bound = p.most_splits > 1 ? one * p.most_splits : 0;
+    p.ws_bytes = p.n_splits > 1 ? kTreeCounterBytes + one * p.n_splits : 0;
+    p.ws_bound = p.most_splits > 1 ? kTreeCounterBytes + one * p.most_splits : 0;
     return p;
 }
 
@@ -1057,7 +1200,7 @@ hipError_t launch_tree(const kvqp_cfg& cfg, const void* q, const void* k_new, co
     a.q = (const uint16_t*)q; a.k_new = (const uint16_t*)k_new; a.v_new = (const uint16_t*)v_new;
     a.mask = mask; a.mask_stride = mask_per_batch ? (size_t)n_rows * ((n_rows + 31) / 32) : 0;
     a.once = rows_once(cfg, cache, 2);
-    a.out = (uint16_t*)out; a.lse = lse; a.part = (float*)ws;
+    a.out = (uint16_t*)out; a.lse = lse; a.arrivals = (unsigned int*)ws; a.part = (float*)((char*)ws + kTreeCounterBytes);
     a.row_blocks = plan.row_blocks; a.n_splits = plan.n_splits; a.n_waves = plan.n_waves;
     switch (cfg.bits) {
         case 2: return tree_bits<2>(a, plan.row_tiles, cfg.key_axis, stream);
@@ -1065,6 +1208,14 @@ hipError_t launch_tree(const kvqp_cfg& cfg, const void* q, const void* k_new, co
         case 8: return tree_bits<8>(a, plan.row_tiles, cfg.key_axis, stream);
         default: return tree_bits<16>(a, plan.row_tiles, cfg.key_axis, stream);
     }
+}
+
+__global__ __launch_bounds__(256) void clear_counters(uint32_t* at) {
+    for (int i = threadIdx.x; i < (int)(kTreeCounterBytes / 4); i += 256) at[i] = 0u;
+}
+hipError_t launch_tree_init(void* ws, hipStream_t stream) {
+    clear_counters<<<dim3(1), dim3(256), 0, stream>>>((uint32_t*)ws);
+    return hipGetLastError();
 }
 
 hipError_t launch_weights(const kvqp_cfg& cfg, const void* q, const float* lse, int n_rows, const kvqp_cache& cache, float* weights, int w_cap,

@@ -20,7 +20,7 @@ KEY_PER_TOKEN = 1
 CACHE_AUTO, CACHE_STREAM, CACHE_KEEP = 0, 1, 2     # kvqp_cfg.decode_cache_hint
 EXPORTS = ["kvqp_cache_sizes", "kvqp_cache_sizes_cap", "kvqp_outlier_sizes", "kvqp_workspace_bytes", "kvqp_compress",
            "kvqp_compress_ragged", "kvqp_quantize_selected", "kvqp_quantize_selected_ragged", "kvqp_append_tail", "kvqp_append_tail_ragged", "kvqp_decode_attn", "kvqp_decode_attn_static", "kvqp_decode_workspace_init",
-           "kvqp_tree_workspace_bytes", "kvqp_tree_attn", "kvqp_accumulate_weights", "kvqp_evict_workspace_bytes", "kvqp_evict",
+           "kvqp_tree_workspace_bytes", "kvqp_tree_workspace_init", "kvqp_tree_attn", "kvqp_accumulate_weights", "kvqp_evict_workspace_bytes", "kvqp_evict",
            "kvqp_strerror", "kvqp_version"]
 MOST_ROWS = 256     # KVQP_MOST_ROWS
 
@@ -88,6 +88,7 @@ def lib():
         L.kvqp_decode_attn_static.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.POINTER(CacheStruct), C.c_void_p, C.c_void_p]
         L.kvqp_decode_workspace_init.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.c_size_t, C.c_void_p]
         L.kvqp_tree_workspace_bytes.argtypes = L.kvqp_evict_workspace_bytes.argtypes = [C.POINTER(CfgStruct), C.c_int32, C.POINTER(C.c_size_t)]
+        L.kvqp_tree_workspace_init.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p]
         L.kvqp_tree_attn.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                      C.POINTER(CacheStruct), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.kvqp_accumulate_weights.argtypes = [C.POINTER(CfgStruct), C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(CacheStruct),
@@ -393,25 +394,26 @@ def decode_attn_static(cfg: Cfg, q, cache: Cache, out, stream=None):
 
 # ---- several query rows per call, and eviction ----
 
-def _want(what, t, dtype, shape):
-    """A tensor argument as the library takes it: its type and shape, contiguous, on the GPU."""
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on the GPU is needed, not {t.dtype} {tuple(t.shape)}"
+def _want(what, t, dtype, shape, device):
+    """A tensor argument as the library takes it: its type and shape, contiguous, on the GPU of the others (its number)."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device or device < 0:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {device} is needed, not {t.dtype} {tuple(t.shape)}"
                          f"{'' if t.is_contiguous() else ', strided'} on {t.device}")
-    return t
 
 
-def _call(name, anchor, others, stream, temporary, args):
-    """Calls an entry point on the device of `anchor`, with that device current; a buffer that this call made itself stays
-    the stream's until the work is done."""
+def _same_device(name, device, *tensors):
+    for t in tensors:
+        if t.numel() and t.get_device() != device:
+            raise ValueError(f"{name}: a buffer on {t.device} and tensors on GPU {device}")
+
+
+def _call(name, device, stream, temporary, args):
+    """Calls an entry point with that GPU as the current one; a buffer that the call made itself stays the stream's until the work is done."""
     import torch
-    for t in others:
-        if t is not None and t.device != anchor.device:
-            raise ValueError(f"{name}: tensors on {anchor.device} and {t.device}")
     if _lib is None:
         lib()
-    if anchor.device.index != torch.cuda.current_device():
-        with torch.cuda.device(anchor.device):
+    if torch.cuda.current_device() != device:
+        with torch.cuda.device(device):
             rc = _fn_rows[name](*args, _stream_handle(stream))
     else:
         rc = _fn_rows[name](*args, _stream_handle(stream))
@@ -433,9 +435,21 @@ def tree_workspace_bytes(cfg: Cfg, n_rows: int) -> int:
     return _sized("kvqp_tree_workspace_bytes", cfg, n_rows)
 
 
-def alloc_tree_workspace(cfg: Cfg, n_rows: int, device="cuda"):
-    """A workspace for tree_attn calls of n_rows rows on caches of any token count."""
-    return alloc_workspace(tree_workspace_bytes(cfg, n_rows), device)
+def tree_workspace_init(workspace, stream=None):
+    """kvqp_tree_workspace_init: zero the arrival counters at the head of a workspace of tree_attn."""
+    import torch
+    with torch.cuda.device(workspace.device):
+        rc = lib().kvqp_tree_workspace_init(_ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if rc:
+        raise KvqpError(rc, "kvqp_tree_workspace_init")
+    return workspace
+
+
+def alloc_tree_workspace(cfg: Cfg, n_rows: int, device="cuda", stream=None):
+    """A workspace for tree_attn calls of n_rows rows on caches of any token count, prepared for its first use."""
+    nbytes = tree_workspace_bytes(cfg, n_rows)
+    workspace = alloc_workspace(nbytes, device)
+    return tree_workspace_init(workspace, stream) if nbytes else workspace
 
 
 def evict_workspace_bytes(cfg: Cfg, n_kept: int) -> int:
@@ -474,25 +488,30 @@ def tree_attn(cfg: Cfg, q, k_new, v_new, mask, cache: Cache, out=None, lse=None,
     """kvqp_tree_attn: q [B,Hq,N,D], k_new / v_new [B,Hkv,N,D] half -> out [B,Hq,N,D] half; mask int32 [N,ceil(N/32)] or
     [B,N,ceil(N/32)] (tree_mask makes one), or None for a chain; lse float32 [B,Hq,N] or None."""
     import torch
-    n = int(q.shape[2]) if q.dim() == 4 else 0
-    b, words = cfg.batch, (n + 31) // 32
-    _want("q", q, torch.float16, (b, cfg.n_q_heads, n, cfg.head_dim))
-    _want("k_new", k_new, torch.float16, (b, cfg.n_kv_heads, n, cfg.head_dim))
-    _want("v_new", v_new, torch.float16, (b, cfg.n_kv_heads, n, cfg.head_dim))
+    b, half, device = cfg.batch, torch.float16, q.get_device()
+    n = q.shape[2] if q.dim() == 4 else 0
+    _want("q", q, half, (b, cfg.n_q_heads, n, cfg.head_dim), device)
+    kv = (b, cfg.n_kv_heads, n, cfg.head_dim)
+    _want("k_new", k_new, half, kv, device)
+    _want("v_new", v_new, half, kv, device)
+    per_batch = 0
     if mask is not None:
-        _want("mask", mask, torch.int32, (b, n, words) if mask.dim() == 3 else (n, words))
+        per_batch = int(mask.dim() == 3)
+        words = (n + 31) // 32
+        _want("mask", mask, torch.int32, (b, n, words) if per_batch else (n, words), device)
     if lse is not None:
-        _want("lse", lse, torch.float32, (b, cfg.n_q_heads, n))
+        _want("lse", lse, torch.float32, (b, cfg.n_q_heads, n), device)
     if out is None:
         out = torch.empty_like(q)
     else:
-        _want("out", out, torch.float16, tuple(q.shape))
+        _want("out", out, half, q.shape, device)
     made = None
     if workspace is None:
-        workspace = made = alloc_tree_workspace(cfg, n, q.device)
-    _call("kvqp_tree_attn", q, (k_new, v_new, mask, cache.buffers["k_codes"], out, lse, workspace), stream, made,
-          (cfg._bytes(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _addr(mask), int(mask is not None and mask.dim() == 3), n,
-           cache._bytes(), out.data_ptr(), _addr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size()))
+        workspace = made = alloc_tree_workspace(cfg, n, q.device, stream)
+    _same_device("tree_attn", device, workspace, cache.buffers["k_codes"])
+    _call("kvqp_tree_attn", device, stream, made,
+          (cfg._bytes(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _addr(mask), per_batch, n, cache._bytes(), out.data_ptr(), _addr(lse),
+           workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     return out
 
 
@@ -500,12 +519,14 @@ def accumulate_weights(cfg: Cfg, q, lse, cache: Cache, weights, decay: float = 1
     """kvqp_accumulate_weights: q [B,Hq,N,D] half and lse [B,Hq,N] float32 of the last N tail rows' queries; weights float32
     [B,Hkv,w_cap] is updated in place and returned."""
     import torch
-    n = int(q.shape[2]) if q.dim() == 4 else 0
-    _want("q", q, torch.float16, (cfg.batch, cfg.n_q_heads, n, cfg.head_dim))
-    _want("lse", lse, torch.float32, (cfg.batch, cfg.n_q_heads, n))
-    _want("weights", weights, torch.float32, (cfg.batch, cfg.n_kv_heads, int(weights.shape[-1])))
-    _call("kvqp_accumulate_weights", q, (lse, weights, cache.buffers["k_codes"]), stream, None,
-          (cfg._bytes(), q.data_ptr(), lse.data_ptr(), n, cache._bytes(), weights.data_ptr(), int(weights.shape[-1]), decay))
+    b, device = cfg.batch, q.get_device()
+    n, cap = (q.shape[2] if q.dim() == 4 else 0), weights.shape[-1]
+    _want("q", q, torch.float16, (b, cfg.n_q_heads, n, cfg.head_dim), device)
+    _want("lse", lse, torch.float32, (b, cfg.n_q_heads, n), device)
+    _want("weights", weights, torch.float32, (b, cfg.n_kv_heads, cap), device)
+    _same_device("accumulate_weights", device, cache.buffers["k_codes"])
+    _call("kvqp_accumulate_weights", device, stream, None,
+          (cfg._bytes(), q.data_ptr(), lse.data_ptr(), n, cache._bytes(), weights.data_ptr(), cap, decay))
     return weights
 
 
@@ -514,22 +535,24 @@ def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=
     """kvqp_evict: the n_keep packed tokens per head with the highest weights (float32 [B,Hkv,w_cap]) go to dst, a cache with
     buffers of its own, with the tail; weights_out float32 [B,Hkv,w_cap_out], idx_out int32 [B,Hkv,kept] or None.  Returns dst."""
     import torch
-    _want("weights", weights, torch.float32, (cfg.batch, cfg.n_kv_heads, int(weights.shape[-1])))
+    heads, device, cap, cap_out = (cfg.batch, cfg.n_kv_heads), weights.get_device(), weights.shape[-1], 0
+    _want("weights", weights, torch.float32, (*heads, cap), device)
     if weights_out is not None:
-        _want("weights_out", weights_out, torch.float32, (cfg.batch, cfg.n_kv_heads, int(weights_out.shape[-1])))
+        cap_out = weights_out.shape[-1]
+        _want("weights_out", weights_out, torch.float32, (*heads, cap_out), device)
     if idx_out is not None:
-        short = cache.n_kept % unit if unit > 1 else 0
         kept = min(n_keep, cache.n_kept)
-        if cache.head_n_kept is None and n_keep < cache.n_kept and unit > 0:
+        if cache.head_n_kept is None and n_keep < cache.n_kept and unit > 1:
+            short = cache.n_kept % unit
             kept = short + (n_keep - short) // unit * unit
-        _want("idx_out", idx_out, torch.int32, (cfg.batch, cfg.n_kv_heads, kept))
+        _want("idx_out", idx_out, torch.int32, (*heads, kept), device)
     made = None
     if workspace is None:
         workspace = made = alloc_evict_workspace(cfg, cache, weights.device)
+    _same_device("evict", device, workspace, cache.buffers["k_codes"], dst.buffers["k_codes"])
     cs = dst.struct()
-    _call("kvqp_evict", weights, (cache.buffers["k_codes"], dst.buffers["k_codes"], weights_out, idx_out, workspace), stream, made,
-          (cfg._bytes(), cache._bytes(), weights.data_ptr(), int(weights.shape[-1]), n_keep, unit, C.byref(cs), _addr(weights_out),
-           0 if weights_out is None else int(weights_out.shape[-1]), _addr(idx_out), workspace.data_ptr(),
-           workspace.numel() * workspace.element_size()))
+    _call("kvqp_evict", device, stream, made,
+          (cfg._bytes(), cache._bytes(), weights.data_ptr(), cap, n_keep, unit, C.byref(cs), _addr(weights_out), cap_out, _addr(idx_out),
+           workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     dst.n_kept, dst.tail_len = cs.n_kept, cs.tail_len
     return dst

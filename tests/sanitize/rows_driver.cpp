@@ -18,6 +18,7 @@ TreePlan plan_tree(const kvqp_cfg&, int n_rows, int n_kept, int tail_len) {
 }
 hipError_t launch_tree(const kvqp_cfg&, const void*, const void*, const void*, const uint32_t*, bool, int, const kvqp_cache&, void*, float*, void*,
                        const TreePlan&, hipStream_t) { ++g_launches; return hipSuccess; }
+hipError_t launch_tree_init(void*, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_weights(const kvqp_cfg&, const void*, const float*, int, const kvqp_cache&, float*, int, float, hipStream_t) { ++g_launches; return hipSuccess; }
 int evict_kept(int n, int n_keep, int unit) { return n <= n_keep ? n : n % unit + (n_keep - n % unit) / unit * unit; }
 hipError_t launch_evict(const kvqp_cfg&, const kvqp_cache&, const float*, int, int, int, int, const kvqp_cache&, float*, int, int32_t*, int32_t*, hipStream_t) {

@@ -140,6 +140,7 @@ def test_long_caches_are_cut_into_splits(orc, bits, G, axis):
         q, kn, vn = draft(rng, 1, 1, Gq, N)
         ws = kvqp.alloc_tree_workspace(cfg, N)
         ws.fill_(0xFF)
+        kvqp.tree_workspace_init(ws)
         check(cfg, cache, keys, values, q, kn, vn, np.tril(np.ones((1, N, N), bool)), None, workspace=ws)
 
 

@@ -53,7 +53,7 @@ def evict(c=None, src=None, dst=None, w=FAR, w_cap=1000, keep=128, unit=1, w_out
 @pytest.mark.parametrize("code,kw", [
     (INVALID, dict(n=0)), (UNSUPPORTED, dict(n=257)), (INVALID, dict(q=None)), (INVALID, dict(kn=None)), (INVALID, dict(vn=None)), (INVALID, dict(out=None)),
     (INVALID, dict(q=FAR + 8)), (INVALID, dict(kn=FAR + 2)), (INVALID, dict(vn=FAR + 4)), (INVALID, dict(out=FAR + 8)), (INVALID, dict(mask=FAR + 2)),
-    (INVALID, dict(lse=FAR + 1)), (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws_bytes=64)), (INVALID, dict(ws=FAR + 8)),
+    (INVALID, dict(lse=FAR + 1)), (WORKSPACE, dict(ws=None, cache=struct(n_kept=65536))), (WORKSPACE, dict(ws_bytes=4096, cache=struct(n_kept=65536))), (INVALID, dict(ws=FAR + 8)),
     (INVALID, dict(c=cfg(sm_scale=0.0))), (INVALID, dict(c=cfg(bits=3))), (UNSUPPORTED, dict(c=cfg(head_dim=64))), (UNSUPPORTED, dict(c=cfg(n_q_heads=6))),
     (UNSUPPORTED, dict(c=cfg(outlier_threshold=6.0))), (INVALID, dict(cache=struct(n_kept=-1))), (INVALID, dict(cache=struct(tail_len=33))),
     (INVALID, dict(cache=struct(k_codes=0))), (INVALID, dict(cache=struct(v_zero=0))), (INVALID, dict(cache=struct(tail_v=0))),
@@ -113,9 +113,12 @@ def test_workspace_sizes(kw):
         tiles = 1 if rows <= 16 else 2 if rows <= 32 else 4
         blocks = -(-rows // (16 * tiles))
         base = c.batch * c.n_kv_heads * blocks
-        splits = max(1, min(64, (512 if tiles == 1 else 256) // base))
-        assert have >= (base * splits * 16 * tiles * 130 * 4 if splits > 1 else 0)
+        splits = max(1, min(64, 256 // base))
+        assert have >= (4096 + base * splits * 16 * tiles * 130 * 4 if splits > 1 else 0)
     assert kvqp.evict_workspace_bytes(c, 1000) >= c.batch * c.n_kv_heads * 4000
+    assert kvqp.lib().kvqp_tree_workspace_init(None, 4096, None) == WORKSPACE
+    assert kvqp.lib().kvqp_tree_workspace_init(FAR, 4095, None) == WORKSPACE
+    assert kvqp.lib().kvqp_tree_workspace_init(FAR + 8, 4096, None) == INVALID
     for bad in (0, -1, 257):
         with pytest.raises(kvqp.KvqpError):
             kvqp.tree_workspace_bytes(c, bad)
