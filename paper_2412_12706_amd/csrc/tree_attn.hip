@@ -30,6 +30,7 @@
 // Weights enter the second product as hi + lo too; values as one binary16 number, code * s + z
 // rounded once, which is the accuracy of the value itself at 16 bits.
 #include <algorithm>
+#include <initializer_list>
 
 #include "kvqp_internal.h"
 
@@ -1161,10 +1162,14 @@ TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len) {
     p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     p.row_blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
     const long long base = (long long)cfg.batch * cfg.n_kv_heads * p.row_blocks;
-    p.n_waves = most_waves(cfg.bits, p.row_tiles);
-    p.most_splits = (int)std::max(1LL, std::min(256 / base, (long long)kMostSplits));
     const int units = (n_kept + 31) / 32 + (tail_len + 31) / 32 + (n_rows + 31) / 32;
-    p.n_splits = std::max(1, std::min(p.most_splits, (units + p.n_waves - 1) / p.n_waves));
+    // By 105 shapes of 1 to 48 sequences, 32 to 16384 tokens and 4 to 80 rows, each with 4 to 16 waves and 1 to 32 splits: eight waves
+    // are within 3 % of the best nearly everywhere (four where there are no more blocks, twelve 3 to 8 % faster where every CU has a long
+    // head to itself); a split pays from 20 blocks of 32 tokens on (34 blocks, 16 rows: 9.7 us in four, 11.0 in one), with a block for every wave, on
+    // every CU, but sixteen splits are enough until each has 32 blocks (joining them takes longer than what the others save).
+    p.most_splits = (int)std::max(1LL, std::min(256 / base, (long long)kMostSplits));
+    p.n_splits = units <= 20 ? 1 : std::max(1, std::min({p.most_splits, (units + 4) / 8, std::max(16, units / 32)}));
+    p.n_waves = units <= 4 ? 4 : std::min(base >= 128 && p.n_splits == 1 ? 12 : 8, most_waves(cfg.bits, p.row_tiles));
     const size_t one = (size_t)base * (16 * p.row_tiles) * (kHeadDim + 2) * sizeof(float);
     p.ws_bytes = p.n_splits > 1 ? kTreeCounterBytes + one * p.n_splits : 0;
     p.ws_bound = p.most_splits > 1 ? kTreeCounterBytes + one * p.most_splits : 0;
