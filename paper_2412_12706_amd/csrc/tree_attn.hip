@@ -20,7 +20,7 @@
 //
 // Exactness.  Logits are exact to about 2^-22 although the operands are binary16:
 //   keys per channel: the codes times q * s split into binary16 hi + lo parts (v_pk_mul, and v_pk_fma for
-//     what the product lost); q . z of the block's group comes from four more instructions.  (Codes are
+//     what the product lost); q . z comes from a product of sixteen groups' zeros at a time.  (Codes are
 //     whole numbers: as subnormals code * 2^-24, which cost one AND, the matrix unit lines products up by their nominal exponents
 //     and loses what lies below, 2e-5 of a weight);
 //   keys per token: code * s split the same way times q, and z (its rows are constant over a group of
@@ -256,13 +256,13 @@ __device__ __forceinline__ void stage_queries(const QueryPieces<RT>& p, QueryTil
 // ---- keys of a block: what a wave holds of 32 tokens, two tiles of 16 ----
 // One wave's private LDS: the block's scale rows, one request per row and wave, read back where they are needed.
 struct __align__(16) ScaleStrip {
-    uint32_t k_scale[64], k_zero[64];        // per channel: one group's row
+    uint32_t k_scale[64];                    // per channel: one group's row
     uint32_t v_scale[64], v_zero[64];        // [group of channels][kb][i][H]
 };
 
 template <int BITS, int AXIS> struct KeyWords {
     uint32_t w[2][BITS];
-    uint32_t scale[2], zero[2];      // keys per channel: a dword of the group's row; per token: the lane's own group of its two tokens
+    uint32_t scale[2], zero[2];      // keys per channel: a dword of the group's scales; per token: the lane's own group of its two tokens
 };
 // Where a head's packed arrays begin.  A block's address is the same for the whole wave (scalar registers); a lane adds 32 bits that never change.
 struct HeadBase { const char *k, *v, *ks, *kz, *vs, *vz; };
@@ -323,7 +323,6 @@ __device__ __forceinline__ void load_keys(const HeadBase& h, int group_log2, int
             const size_t row = (size_t)((32 * blk) >> group_log2) * (kHeadDim * 2);
             const uint32_t at = unseen(4u * lane);
             k.scale[0] = load_at<uint32_t>(h.ks + row, at);
-            k.zero[0] = load_at<uint32_t>(h.kz + row, at);
         } else {
             const size_t row = (size_t)blk << (13 - group_log2);         // 32 tokens of 256 / G bytes
             const uint32_t at = unseen((uint32_t)((n << (7 - group_log2)) + ((32 * kb) >> group_log2)) * 2u);
@@ -342,7 +341,34 @@ __device__ __forceinline__ void load_keys(const HeadBase& h, int group_log2, int
 // between the matrix instructions, by hand or by s_setprio, changed nothing.)
 template <int RT> __device__ __forceinline__ void end_step() { if constexpr (RT >= 2) __builtin_amdgcn_sched_barrier(0); }
 
-// Logits of a block for RT row tiles, before the rows' factors: acc[rt][H][i] is token 16 H + 4 kb + i of row 16 rt + n.  The four
+// Keys per channel: q . z of the key groups of the wave's next sixteen blocks (blk, blk + step, ... , none beyond last), by one product of sixteen
+// rows of zeros instead of one row sixteen times: bias[j][row] for the j-th of them.  (A product per block: 4 of 36 matrix instructions a row tile;
+// 32 layers of 8192 tokens, 32 rows: 100.6 us with them, 97.5 without.)
+constexpr int kBiasBlocks = 16;
+template <int RT>
+__device__ __forceinline__ void refresh_bias(const HeadBase& h, int group_log2, int blk, int step, int last, int lane, const uint4* frag, float* bias) {
+    const int n = lane & 15, kb = lane >> 4;
+    const char* row = h.kz + (size_t)((32 * min(blk + n * step, last)) >> group_log2) * (kHeadDim * 2) + 64 * kb;
+    Frag z[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) z[s].q = *reinterpret_cast<const uint4*>(row + 16 * s);
+    lds_order();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        f4v az = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            Frag q;
+            q.q = frag[(4 * rt + s) * 64 + lane];
+            az = mfma(z[s], q, az);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bias[(4 * kb + i) * (16 * RT) + 16 * rt + n] = az[i];
+    }
+    lds_order();
+}
+
+// Logits of a block for RT row tiles, before the rows' factors (and, keys per channel, without q . z): acc[rt][H][i] is token 16 H + 4 kb + i of row 16 rt + n.  The four
 // steps of eight channels run outermost, so that only one step's operands are held beside the sums.
 template <int BITS, int AXIS, int RT>
 __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const KeyWords<BITS, AXIS>& k, const uint4* frag, const uint32_t* sums, ScaleStrip& strip, int lane, f4v (&acc)[RT][2]) {
@@ -353,24 +379,8 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const Ke
         q.q = frag[(4 * rt + s) * 64 + lane];
         return q;
     };
-    if constexpr (kChannel) {
-        // q . z first, the same for all tokens of the group: both tiles' sums begin with it
-        f4v az[RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) az[rt] = f4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            Frag z;
-            z.q = *reinterpret_cast<const uint4*>(&strip.k_zero[16 * kb + 4 * s]);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) az[rt] = mfma(z, query(rt, s), az[rt]);
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = az[rt];
-    } else {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
         end_step<RT>();
@@ -441,7 +451,6 @@ __device__ __forceinline__ void strip_keys(const KeyWords<BITS, AXIS>& k, ScaleS
     if constexpr (BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL) {
         lds_order();
         strip.k_scale[lane] = k.scale[0];
-        strip.k_zero[lane] = k.zero[0];
         lds_order();
     }
 }
@@ -460,16 +469,17 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
         for (int t = 0; t < 8; ++t) st.o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
     }
 }
-// Moves references where logits have passed them, turns acc (a block's logits before the rows' factors, -inf where unseen) into weights x
+// Moves references where logits have passed them, turns acc + bias (a block's logits before the rows' factors, -inf where unseen) into weights x
 // and adds them up.
 template <int RT>
-__device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[RT][2], const float (&factor)[RT], float (&x)[RT][8]) {
+__device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[RT][2], const float (&factor)[RT], const float (&bias)[RT], float (&x)[RT][8]) {
     bool past = false;
     float top[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const f4v &p = acc[rt][0], &q = acc[rt][1];
-        top[rt] = max3(max3(max3(p[0], p[1], p[2]), p[3], q[0]), max3(q[1], q[2], q[3]), q[3]) * factor[rt];
+        top[rt] = max3(max3(max3(p[0], p[1], p[2]), p[3], q[0]), max3(q[1], q[2], q[3]), q[3]) + bias[rt];
+        top[rt] *= factor[rt];
         past |= top[rt] > st.ref[rt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
@@ -485,12 +495,14 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
         }
     }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < RT; ++rt) {
+        const float add = __builtin_fmaf(bias[rt], factor[rt], -st.ref[rt]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], -st.ref[rt]));
+            x[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], add));
             st.sum[rt] += x[rt][j];
         }
+    }
 }
 // Weights as operands: pair i holds tokens 4 kb + i and 16 + 4 kb + i; hi + lo parts, cut toward zero.
 struct WeightOperand { Frag hi, lo; };
@@ -557,11 +569,11 @@ constexpr int kPlainStride = kHeadDim + 8;      // halves between two rows of a 
 struct __align__(16) PlainTile { uint16_t v[32 * kPlainStride]; };
 
 // A workgroup's LDS: while blocks are worked on, and while the waves' states become one (outputs of JOIN row tiles at a time).
-union WaveScratch { ScaleStrip strip; PlainTile tile; };
+template <int RT> union WaveScratch { struct { ScaleStrip strip; float bias[kBiasBlocks * 16 * RT]; } packed; PlainTile tile; };
 constexpr int kMostSplits = 64;
 constexpr int join_tiles(int rt) { return rt == 4 ? 2 : 1; }
 template <int BITS, int RT> union __align__(16) TreeShared {
-    struct { QueryTiles<RT> sq; WaveScratch wave[most_waves(BITS, RT)]; } run;
+    struct { QueryTiles<RT> sq; WaveScratch<RT> wave[most_waves(BITS, RT)]; } run;
     struct { f4v o[most_waves(BITS, RT)][join_tiles(RT) * 8][64]; float ref[most_waves(BITS, RT)][16 * RT], sum[most_waves(BITS, RT)][16 * RT]; } join;
     struct { float weight[kMostSplits][16 * RT], sum[kMostSplits][16 * RT], inverse[16 * RT]; } last;       // of a row block's splits
 };
@@ -638,7 +650,8 @@ __global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4
         load_values<BITS, ONCE>(base, a.group_log2, blk, lane, vw);
     }
     stage_queries<RT>(pieces, sq);
-    ScaleStrip& strip = sh.run.wave[wave].strip;
+    ScaleStrip& strip = sh.run.wave[wave].packed.strip;
+    float* biases = sh.run.wave[wave].packed.bias;
 
     RowState<RT> st;
     clear(st);
@@ -653,11 +666,19 @@ __global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4
     // ---- packed blocks ----
     {
         const Fields<BITS> fields;
+        int turn = 0;
         if (blk < end) {
 #pragma unroll 1
             for (; blk < end; blk += waves) {
                 const int next = min(blk + waves, end - 1);
                 f4v acc[RT][2];
+                float bias[RT] = {};
+                if constexpr (BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL) {
+                    if (turn == 0) refresh_bias<RT>(base, a.group_log2, blk, waves, end - 1, lane, sq.frag, biases);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) bias[rt] = biases[turn * (16 * RT) + 16 * rt + n];
+                    turn = (turn + 1) % kBiasBlocks;
+                }
                 strip_keys<BITS, AXIS>(kw, strip, lane);
                 key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
                 load_keys<BITS, AXIS, ONCE>(base, a.group_log2, next, lane, kw);
@@ -669,7 +690,7 @@ __global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4
                             if (32 * blk + 16 * (j >> 2) + 4 * kb + (j & 3) >= n_tok) acc[rt][j >> 2][j & 3] = -INFINITY;
                 }
                 float x[RT][8];
-                softmax_step<RT>(st, acc, factor, x);
+                softmax_step<RT>(st, acc, factor, bias, x);
                 WeightOperand p[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
@@ -756,7 +777,8 @@ __global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4
                 }
             }
             float x[RT][8];
-            softmax_step<RT>(st, acc, factor, x);
+            const float none[RT] = {};
+            softmax_step<RT>(st, acc, factor, none, x);
             WeightOperand p[RT];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
@@ -1016,6 +1038,8 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
     __shared__ QueryTiles<RT> sq;
     __shared__ ScaleStrip s_strip[kWeightWaves];
     __shared__ float s_lse[RT * 16];
+    constexpr bool kBias = BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL;
+    __shared__ float s_bias[kBias ? kWeightWaves * kBiasBlocks * 16 * RT : 1];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, kb = lane >> 4;
@@ -1042,7 +1066,7 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
         float factor[RT], minus_lse[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) { factor[rt] = sq.factor[16 * rt + n] * a.sm_scale; minus_lse[rt] = s_lse[16 * rt + n]; }
-        auto weight = [&](float logit, int rt) { return __builtin_amdgcn_exp2f(__builtin_fmaf(logit, factor[rt], minus_lse[rt]) * kLog2e); };
+        auto weight = [&](float logit, int rt, float add) { return __builtin_amdgcn_exp2f(__builtin_fmaf(logit, factor[rt], add) * kLog2e); };
         // lane n < 8 of a row of lanes stores token 16 (n / 4) + 4 kb + n % 4
         auto store = [&](const float (&cs)[8], float* w, int t0, int len) {
             const float mine = column_sums(cs, n);
@@ -1056,18 +1080,29 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
             const HeadBase base = head_base<BITS, AXIS>(a, bh);
             KeyWords<BITS, AXIS> kw;
             load_keys<BITS, AXIS, ONCE>(base, a.group_log2, blk, lane, kw);
+            float* biases = s_bias + (kBias ? wave * kBiasBlocks * 16 * RT : 0);
+            int turn = 0;
 #pragma unroll 1
             for (; blk < end; blk += kWeightWaves) {
                 f4v acc[RT][2];
+                float add[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) add[rt] = minus_lse[rt];
+                if constexpr (kBias) {
+                    if (turn == 0) refresh_bias<RT>(base, a.group_log2, blk, kWeightWaves, end - 1, lane, sq.frag, biases);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) add[rt] = __builtin_fmaf(biases[turn * (16 * RT) + 16 * rt + n], factor[rt], minus_lse[rt]);
+                    turn = (turn + 1) % kBiasBlocks;
+                }
                 strip_keys<BITS, AXIS>(kw, strip, lane);
                 key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
                 load_keys<BITS, AXIS, ONCE>(base, a.group_log2, min(blk + kWeightWaves, end - 1), lane, kw);
                 float cs[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    cs[j] = weight(acc[0][j >> 2][j & 3], 0);
+                    cs[j] = weight(acc[0][j >> 2][j & 3], 0, add[0]);
 #pragma unroll
-                    for (int rt = 1; rt < RT; ++rt) cs[j] += weight(acc[rt][j >> 2][j & 3], rt);
+                    for (int rt = 1; rt < RT; ++rt) cs[j] += weight(acc[rt][j >> 2][j & 3], rt, add[rt]);
                 }
                 store(cs, weights, 32 * blk, n_tok);
             }
@@ -1092,7 +1127,7 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
             for (int rt = 0; rt < RT; ++rt) {
                 const int last = a.tail_len - a.n_new + (row0 + 16 * rt + n) % a.n_new - t0 - 4 * kb;      // the last row of the tail that the query row sees
 #pragma unroll
-                for (int j = 0; j < 8; ++j) cs[j] += 16 * (j >> 2) + (j & 3) <= last ? weight(acc[rt][j >> 2][j & 3], rt) : 0.0f;
+                for (int j = 0; j < 8; ++j) cs[j] += 16 * (j >> 2) + (j & 3) <= last ? weight(acc[rt][j >> 2][j & 3], rt, minus_lse[rt]) : 0.0f;
             }
             store(cs, weights + n_tok, t0, a.tail_len);
         }
