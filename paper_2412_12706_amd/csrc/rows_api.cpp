@@ -17,8 +17,8 @@ static bool cache_aligned(const kvqp_cfg* c, const kvqp_cache* cache) {
            aligned(cache->v_scale, 4) && aligned(cache->v_zero, 4) && aligned(cache->tail_k, 16) && aligned(cache->tail_v, 16) &&
            aligned(cache->head_n_kept, 4);
 }
-// (token numbers, and the blocks of them, are 32 bits in the kernels)
-constexpr int kMostTokens = 1 << 28;
+// (token numbers, and the words of a head's value codes, at most 64 a token, are 32 bits in the kernels)
+constexpr int kMostTokens = 1 << 26;
 // Checks of a cache that several query rows or an eviction read.
 static int check_read_cache(const kvqp_cfg* cfg, const kvqp_cache* cache) {
     int rc = check_common(cfg);

@@ -661,7 +661,7 @@ __global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4
     const float c_q = a.sm_scale * kLog2e;
     float factor[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) factor[rt] = sq.factor[16 * rt + n] * c_q;
+    for (int rt = 0; rt < RT; ++rt) factor[rt] = fmaxf(sq.factor[16 * rt + n] * c_q, 1.2e-38f);      // (above 0, for the -inf of unseen tokens)
 
     // ---- packed blocks ----
     {
@@ -1046,15 +1046,24 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
     const int bh = blockIdx.y;
     const int n_tok = __builtin_amdgcn_readfirstlane(head_tokens(a, bh));
     const int packed = (n_tok + 31) / 32, units = packed + (a.tail_len + 31) / 32;
-    const int u0 = blockIdx.x * a.units_per_wg, u1 = min(u0 + a.units_per_wg, units);
-    if (u0 >= units) return;              // (a workgroup of a shorter head, beyond its blocks)
+    // (A head with a count of its own is divided among all the workgroups that the longest one has: 32 rows
+    // over heads of 4,000 to 32,000 tokens took 28.2 us so, 31.3 where each took the longest head's share.)
+    const int per_wg = a.head_n_kept ? (int)((unsigned)(units + gridDim.x - 1) / gridDim.x) : a.units_per_wg;
+    const int u0 = blockIdx.x * per_wg, u1 = min(u0 + per_wg, units);
+    if (u0 >= units) return;
     float* weights = a.weights + (size_t)bh * a.w_cap;
     ScaleStrip& strip = s_strip[wave];
 
 #pragma unroll 1
     for (int row0 = 0; row0 < a.rows; row0 += RT * 16) {
         if (row0) __syncthreads();
-        stage_queries<RT>(request_queries<RT>(a, bh, row0), sq);
+        QueryPieces<RT> pieces = request_queries<RT>(a, bh, row0);
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {        // (a row that sees nothing may hold anything)
+            const int r = row0 + (threadIdx.x >> 4) + j * (kWeightThreads >> 4);
+            if (r < a.rows && a.lse[(size_t)bh * a.rows + r] == -INFINITY) pieces.w[j] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        stage_queries<RT>(pieces, sq);
         if (threadIdx.x < RT * 16) {
             const int r = row0 + threadIdx.x;
             const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;

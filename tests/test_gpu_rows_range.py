@@ -1,0 +1,161 @@
+"""Several query rows and eviction over the range of calls: the hints about caching, launches that many heads and long heads lead
+to, one workspace for unlike calls, rows that hold anything."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2412_12706_amd import kvqp
+from tests.gpu_util import dev
+from tests.rows_util import D, attention, half, logit_error, make, out_error
+from tests.test_gpu_evict import check as check_evict
+from tests.test_gpu_evict import target
+from tests.test_gpu_tree import check as check_tree
+from tests.test_gpu_tree import draft
+from tests.test_gpu_weights import run as check_weights
+
+pytestmark = pytest.mark.gpu
+
+
+def chain(N):
+    return np.tril(np.ones((1, N, N), bool))
+
+
+def many(cfg, cache, heads):
+    """The one head of a cache, for so many batch items."""
+    c = kvqp.Cfg(**{**cfg.__dict__, "batch": heads})
+    return c, kvqp.Cache({k: t.repeat(heads) for k, t in cache.buffers.items()}, cache.n_kept, cache.tail_len, cache.tail_cap, cache.n_cap)
+
+
+@pytest.mark.parametrize("bits,axis", [(2, 0), (4, 0), (8, 0), (16, 0), (2, 1), (4, 1), (8, 1)])
+def test_hints_change_no_bit(orc, bits, axis):
+    """What the calls compute does not depend on which caches their loads go through."""
+    rng = np.random.default_rng(31)
+    cfg, cache, keys, values = make(orc, rng, 1, 2, 4, 1500, 20, bits, 32, axis)
+    for N in (3, 7, 16):           # one, two and four tiles of rows
+        q, kn, vn = draft(rng, 1, 2, 4, N)
+        got = []
+        for hint in (kvqp.CACHE_AUTO, kvqp.CACHE_STREAM, kvqp.CACHE_KEEP):
+            c = kvqp.Cfg(**{**cfg.__dict__, "decode_cache_hint": hint})
+            out, lse = check_tree(c, cache, keys, values, q, kn, vn, chain(N), None)
+            got.append((out, lse, check_weights(c, cache, keys, [1500, 1500], 20, q, 0.5)))
+        for other in got[1:]:
+            assert all(np.array_equal(a, b) for a, b in zip(got[0], other))
+
+
+@pytest.mark.parametrize("bits,axis", [(4, 0), (2, 0), (8, 1), (16, 0)])
+def test_one_workspace_for_unlike_calls(orc, bits, axis):
+    """Calls of other row counts, token counts and heads, in turn, with the workspace that the largest of them asks for."""
+    rng = np.random.default_rng(32)
+    made = [make(orc, rng, *shape, bits, 32, axis) + (shape[2], N) for shape, N in
+            [((1, 1, 4, 3000, 40), 9), ((1, 2, 8, 900, 3), 20), ((3, 2, 1, 700, 0), 1), ((1, 1, 8, 40, 0), 33)]]
+    size = max(kvqp.tree_workspace_bytes(m[0], m[5]) for m in made)
+    ws = kvqp.tree_workspace_init(kvqp.alloc_workspace(size))
+    for order in ((0, 1, 2, 3), (1, 0, 3, 0, 2, 1)):
+        for i in order:
+            cfg, cache, keys, values, Gq, N = made[i]
+            q, kn, vn = draft(rng, cfg.batch, cfg.n_kv_heads, Gq, N)
+            check_tree(cfg, cache, keys, values, q, kn, vn, chain(N), None, workspace=ws)
+    assert not ws[:4096].any()          # every launch leaves the counters as it found them
+
+
+@pytest.mark.parametrize("bits,axis", [(4, 0), (2, 0), (8, 0), (16, 0), (4, 1), (2, 1)])
+@pytest.mark.parametrize("Gq,N", [(1, 4), (8, 4), (8, 11)])
+def test_every_head_of_many_long_ones(orc, bits, axis, Gq, N):
+    """A workgroup to a whole head, more than sixteen blocks to a wave: the result is the same for each of many equal heads, and the formula's."""
+    rng = np.random.default_rng(33)
+    heads = 160 if N < 11 else 90
+    cfg, one, keys, values = make(orc, rng, 1, 1, Gq, 7003, 33, bits, 64, axis)
+    c, cache = many(cfg, one, heads)
+    q, kn, vn = draft(rng, 1, 1, Gq, N)
+    lse = torch.empty((heads, Gq, N), device="cuda")
+    out = kvqp.tree_attn(c, *(dev(np.repeat(x, heads, 0)) for x in (q, kn, vn)), None, cache, lse=lse)
+    assert torch.equal(out, out[:1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))
+    k64, v64 = (np.concatenate([a[0], b[0, 0].astype(np.float64)]) for a, b in ((keys, kn), (values, vn)))
+    seen = np.concatenate([np.ones((N, 7003 + 33), bool), chain(N)[0]], 1)
+    for a in range(Gq):
+        rows = q[0, a].astype(np.float64)
+        ref, ref_lse, spread = attention(rows, k64, v64, seen)
+        delta = logit_error(rows, k64)
+        assert (np.abs(out[0, a].cpu().numpy() - ref) <= out_error(ref, spread, delta)).all()
+        assert (np.abs(lse[0, a].cpu().numpy() - ref_lse) <= delta + 2.0 ** -18 + 2.0 ** -23 * np.abs(ref_lse)).all()
+
+
+@pytest.mark.parametrize("bits,axis", [(4, 0), (2, 0), (16, 0), (8, 1)])
+@pytest.mark.parametrize("N", [2, 5, 70])
+def test_weights_of_many_long_heads(orc, bits, axis, N):
+    rng = np.random.default_rng(34)
+    heads, n = 512, 4500
+    cfg, one, keys, _ = make(orc, rng, 1, 1, 4, n, 70, bits, 32, axis)
+    q = half(rng, 1, 4, N, D)
+    ref = check_weights(cfg, one, keys, [n], 70, q, 0.0)
+    c, cache = many(cfg, one, heads)
+    _, _, lse = weigh(cfg, one, q)
+    w = torch.full((heads, 1, n + 70), 3.0, device="cuda")
+    kvqp.accumulate_weights(c, dev(np.repeat(q, heads, 0)), lse.repeat(heads, 1, 1), cache, w, decay=0.0)
+    single = torch.full((1, 1, n + 70), 3.0, device="cuda")
+    kvqp.accumulate_weights(cfg, dev(q), lse, one, single, decay=0.0)
+    assert torch.equal(w, single.expand(heads, 1, n + 70))
+    assert np.isfinite(ref).all()
+
+
+def weigh(cfg, cache, q):
+    """Sums of the rows' softmax over the cache alone (each drafted row hidden from all)."""
+    N = q.shape[2]
+    kn = torch.zeros((1, cfg.n_kv_heads, N, D), dtype=torch.float16, device="cuda")
+    lse = torch.empty((1, cfg.n_q_heads, N), device="cuda")
+    mask = torch.zeros((N, (N + 31) // 32), dtype=torch.int32, device="cuda")
+    return kvqp.tree_attn(cfg, dev(q), kn, kn, mask, cache, lse=lse), mask, lse
+
+
+@pytest.mark.parametrize("bits,axis", [(4, 0), (8, 1), (16, 0)])
+def test_weights_of_heads_with_very_unlike_counts(orc, bits, axis):
+    rng = np.random.default_rng(35)
+    counts = [4001, 1, 0, 33, 2000, 4000]
+    cfg, cache, keys, _ = make(orc, rng, 2, 3, 2, 4001, 35, bits, 32, axis, counts=counts)
+    for N in (3, 20, 40):
+        check_weights(cfg, cache, keys, counts, 35, half(rng, 2, 6, N, D), 0.9)
+
+
+def test_rows_that_saw_nothing_may_hold_anything(orc):
+    """A padded row (its sum is -inf) adds nothing to the weights, whatever its query holds."""
+    rng = np.random.default_rng(36)
+    for N, bits, axis in ((3, 4, 0), (6, 2, 1), (18, 16, 0), (40, 8, 0)):
+        cfg, cache, keys, _ = make(orc, rng, 1, 2, 4, 300, 50, bits, 32, axis)
+        q = half(rng, 1, 8, N, D)
+        lse = torch.full((1, 8, N), 6.0, device="cuda")
+        lse[0, 3, 1] = lse[0, 5] = -torch.inf
+        q0, q1 = q.copy(), q.copy()
+        q0[0, 3, 1] = q0[0, 5] = 0
+        q1[0, 3, 1] = np.nan
+        q1[0, 5] = np.inf
+        a, b = (kvqp.accumulate_weights(cfg, dev(x), lse, cache, torch.zeros((1, 2, 350), device="cuda")) for x in (q0, q1))
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+def test_a_scale_of_almost_nothing(orc):
+    """Every visible token has the same weight then, and the others none."""
+    rng = np.random.default_rng(37)
+    cfg, cache, keys, values = make(orc, rng, 1, 2, 4, 45, 3, 4, 32, 0)
+    c = kvqp.Cfg(**{**cfg.__dict__, "sm_scale": 1.2e-38})
+    q, kn, vn = draft(rng, 1, 2, 4, 6, scale=2.0 ** -12)
+    lse = torch.empty((1, 8, 6), device="cuda")
+    out = kvqp.tree_attn(c, dev(q), dev(kn), dev(vn), None, cache, lse=lse).cpu().numpy().astype(np.float64)
+    for h in range(8):
+        for i in range(6):
+            v = np.concatenate([values[h // 4], vn[0, h // 4, :i + 1].astype(np.float64)])
+            # (the mean: values rounded once, the output once, 60 sums in binary32)
+            assert np.abs(out[0, h, i] - v.mean(0)).max() <= 2.0 ** -11 * (np.abs(v).mean(0) + np.abs(v.mean(0))).max() + 2.0 ** -17 * np.abs(v).max()
+            assert abs(lse[0, h, i].item() - np.log(len(v))) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("n,unit,n_keep,bits,G,axis", [(9000, 1, 5000, 2, 64, 1), (33100, 1, 20001, 2, 128, 1), (40003, 1, 777, 4, 32, 1),
+                                                       (33100, 32, 30010, 4, 32, 0), (70000, 64, 2000, 2, 64, 0), (33500, 1, 33499, 16, 32, 0)])
+def test_evictions_from_long_heads(orc, n, unit, n_keep, bits, G, axis):
+    """More units than a workgroup's keys of one, eight and thirty-two to a thread."""
+    rng = np.random.default_rng(38)
+    cfg, src, _, _ = make(orc, rng, 1, 1, 1, n, 3, bits, G, axis)
+    w = np.exp(rng.standard_normal((1, 1, n + 3))).astype(np.float32)
+    w[0, 0, rng.integers(0, n, n // 10)] = 1.0            # (ties at the cut)
+    short = n % unit
+    kept = short + (n_keep - short) // unit * unit
+    check_evict(orc, cfg, src, w, n_keep, unit, [n], target(cfg, kept, 3, 0), 3)

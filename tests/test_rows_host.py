@@ -175,3 +175,11 @@ def test_host_side_is_clean_under_asan_and_ubsan(tmp_path):
     exe = str(tmp_path / "rows_driver")
     run([clang, "-fsanitize=address", "-fsanitize=undefined"] + objs + ["-o", exe])
     assert "rows_driver: clean" in run([exe], env=ENV)
+
+
+def test_token_counts_that_indexes_cannot_hold_are_refused():
+    """Words of a head's value codes have 32-bit numbers in the kernels: 2^26 tokens of 16 bits are the most."""
+    most = 1 << 26
+    assert tree(cache=struct(n_kept=most + 1)) == UNSUPPORTED and tree(cache=struct(n_cap=most + 32)) == UNSUPPORTED
+    assert weigh(cache=struct(n_kept=most + 1)) == UNSUPPORTED
+    assert evict(src=struct(n_kept=most + 1)) == UNSUPPORTED and evict(dst=struct(1 << 28, n_cap=most + 32)) == UNSUPPORTED
