@@ -77,7 +77,72 @@ __device__ __forceinline__ uint32_t waves_before(const uint32_t* s, int wave, in
     return v + __builtin_amdgcn_update_dpp(0u, v, 0x140 /* row_mirror */, 0xF, 0xF, true);
 }
 
-// One head per workgroup.  Every wave has a stretch of consecutive units, 64 at a time; The keys of up to
+// Sum over the lanes up to this one: within rows of 16 lanes, then the rows' totals.
+__device__ __forceinline__ uint32_t lanes_up_to(uint32_t v) {
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x111 /* row_shr:1 */, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x112 /* row_shr:2 */, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x114 /* row_shr:4 */, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x118 /* row_shr:8 */, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0u, v, 0x142 /* row_bcast:15 */, 0xA, 0xF, false);
+    return v + __builtin_amdgcn_update_dpp(0u, v, 0x143 /* row_bcast:31 */, 0xC, 0xF, false);
+}
+// Lanes below this one whose bit is set, and `more`.
+__device__ __forceinline__ uint32_t lanes_below(unsigned long long bits, uint32_t more) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, more));
+}
+constexpr uint32_t kOddTurn = 16u;       // the odd lanes' histogram has its bins this far apart from the others', in other banks
+
+// The same for up to 256 units a head: a thread counts the units that come before its own, by score and then by position.
+// (Whole evictions of 8 heads, and by the selection below: 33 units of 32 tokens 7.7 us and 10.3, 256 of 32 tokens 13.6 and 15.4, 256 single
+// tokens 9.1 and 8.7.)
+constexpr int kFewUnits = 256;
+__global__ __launch_bounds__(kFewUnits) void pick_of_few(const EvictArgs a) {
+    __shared__ uint4 s_key[kFewUnits / 4];
+    __shared__ int s_unit[kFewUnits];
+    __shared__ uint32_t s_wave[4];
+    const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = source_tokens(a, bh);
+    const Cut cut = cut_of(n, a.n_keep, a.unit);
+    const uint32_t key = tid < cut.units ? unit_key(a.weights + (size_t)bh * a.w_cap, tid, a.unit) : 0u;
+    reinterpret_cast<uint32_t*>(s_key)[tid] = key;
+    __syncthreads();
+    uint32_t before = 0u;
+#pragma unroll 1
+    for (int b = 0; 64 * b < cut.units; ++b) {           // (keys past the last unit are 0, and come after every unit)
+        const uint4* keys = s_key + 16 * b;
+        if (b != wave) {          // (equal keys of lower units come before this one, those of higher ones after it)
+            const uint32_t least = key + (b > wave);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint4 k = keys[j];
+                before += (k.x >= least) + (k.y >= least) + (k.z >= least) + (k.w >= least);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint4 k = keys[j];
+                before += (k.x >= key + (4 * j >= lane)) + (k.y >= key + (4 * j + 1 >= lane)) + (k.z >= key + (4 * j + 2 >= lane)) + (k.w >= key + (4 * j + 3 >= lane));
+            }
+        }
+    }
+    const bool stays = tid < cut.units && before < (uint32_t)cut.keep_units;
+    const unsigned long long all = __builtin_amdgcn_ballot_w64(stays);
+    if (lane == 0) s_wave[wave] = (uint32_t)__builtin_popcountll(all);
+    __syncthreads();
+    uint32_t at = lanes_below(all, 0u);
+    for (int w = 0; w < wave; ++w) at += s_wave[w];
+    if (stays) s_unit[at] = tid;
+    __syncthreads();
+    const int whole = cut.keep_units * a.unit, unit_log2 = __builtin_ctz(a.unit);
+    for (int i = tid; i < cut.kept; i += kFewUnits) {
+        const int t = i < whole ? s_unit[i >> unit_log2] * a.unit + (i & (a.unit - 1)) : cut.units * a.unit + i - whole;
+        a.idx[(size_t)bh * a.bound + i] = t;
+        if (a.list) a.list[(size_t)bh * a.bound + i] = t;
+    }
+    if (a.dst.head_n_kept && tid == 0) a.dst.head_n_kept[bh] = cut.kept;
+}
+
+// One head per workgroup.  Every wave has a stretch of consecutive units, 64 at a time.  The keys of up to
 // KEYS such steps stay in LDS (KEYS == 0: any number, read again in every pass).
 template <int KEYS, int THREADS>
 __global__ __launch_bounds__(THREADS) void pick_heaviest(const EvictArgs a) {
@@ -123,12 +188,24 @@ __global__ __launch_bounds__(THREADS) void pick_heaviest(const EvictArgs a) {
             for (int j = 0; j < steps; ++j) own[64 * j] = u0 + 64 * j + lane < cut.units ? unit_key(w, u0 + 64 * j + lane, a.unit) : 0u;
         }
     }
-    // body(unit, its key, whether there is such a unit) for the wave's units, in order.  (Rolled up: every launch fetches its code anew, and
-    // keys in registers, with the loops unrolled, took 20 us instead of 15 for 16 heads of 12003.)
+    // body(unit, its key, whether there is such a unit) for the wave's units, in order.  (Four steps' keys are read together and the rest is
+    // rolled up: every launch fetches its code anew, and keys in registers, with the loops unrolled, took 20 us instead of 15 for 16 heads of 12003.)
+    const int u1 = min(u0 + 64 * steps, cut.units);
     auto each = [&](auto body) {
-        for (int j = 0; j < steps; ++j) {
-            const int u = u0 + 64 * j + lane;
-            body(u, KEYS > 0 ? own[64 * j] : u < cut.units ? unit_key(w, u, a.unit) : 0u, u < cut.units);
+        constexpr int BATCH = KEYS > 4 ? 4 : 1;
+#pragma unroll 1
+        for (int j0 = 0; j0 < steps; j0 += BATCH) {
+            uint32_t k[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int u = u0 + 64 * (j0 + j) + lane;
+                k[j] = KEYS > 0 ? own[64 * (j0 + j)] : u < u1 ? unit_key(w, u, a.unit) : 0u;
+            }
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int u = u0 + 64 * (j0 + j) + lane;
+                body(u, k[j], u < u1);
+            }
         }
     };
 
@@ -142,24 +219,27 @@ __global__ __launch_bounds__(THREADS) void pick_heaviest(const EvictArgs a) {
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
         uint32_t* hist = s_hist[pass & 1];
+        // (the first pass finds few bins full: even and odd lanes have a histogram each, so that fewer of them wait for one counter)
+        uint32_t* mine = pass == 0 && (lane & 1) ? s_hist[1] : hist;
+        const uint32_t turn = pass == 0 && (lane & 1) ? kOddTurn : 0u;
         each([&](int, uint32_t k, bool valid) {
-            if (valid && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1u);
+            if (valid && (k & mask) == prefix) atomicAdd(&mine[((k >> shift) & ((1u << bits) - 1u)) ^ turn], 1u);
         });
         __syncthreads();
         // bins from the highest down: thread t has PER of them
         uint32_t c[PER], all = 0u;
 #pragma unroll
         for (int b = 0; b < PER; ++b) {
-            c[b] = hist[kBins - 1 - PER * tid - b];
-            hist[kBins - 1 - PER * tid - b] = 0u;           // (for the pass after the next)
+            const int bin = kBins - 1 - PER * tid - b;
+            c[b] = hist[bin];
+            hist[bin] = 0u;           // (for the pass after the next)
+            if (pass == 0) {
+                c[b] += s_hist[1][bin ^ kOddTurn];
+                s_hist[1][bin ^ kOddTurn] = 0u;
+            }
             all += c[b];
         }
-        uint32_t before = all;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(before, d);
-            if (lane >= d) before += o;
-        }
+        uint32_t before = lanes_up_to(all);
         if (lane == 63) s_wave[0][wave] = before;
         __syncthreads();
         before += waves_before(s_wave[0], wave, lane) - all;
@@ -187,14 +267,16 @@ __global__ __launch_bounds__(THREADS) void pick_heaviest(const EvictArgs a) {
     __syncthreads();
     above = waves_before(s_wave[1], wave, lane);
     equal = waves_before(s_wave[2], wave, lane);
-    const unsigned long long below = (1ull << lane) - 1ull;
     each([&](int u, uint32_t k, bool valid) {
         k &= mask;
         const unsigned long long ba = __builtin_amdgcn_ballot_w64(valid && k > prefix), be = __builtin_amdgcn_ballot_w64(valid && k == prefix);
-        const uint32_t e = equal + (uint32_t)__builtin_popcountll(be & below);
-        const uint32_t at = above + (uint32_t)__builtin_popcountll(ba & below) + min(e, want);
-        if (valid && (k > prefix || (k == prefix && e < want)))
-            for (int t = 0; t < a.unit; ++t) put((int)at * a.unit + t, u * a.unit + t);
+        const uint32_t e = lanes_below(be, equal);
+        const uint32_t at = lanes_below(ba, above) + min(e, want);
+        if (valid && (k > prefix || (k == prefix && e < want))) {
+            if (a.unit == 1) put((int)at, u);
+            else
+                for (int t = 0; t < a.unit; ++t) put((int)at * a.unit + t, u * a.unit + t);
+        }
         above += (uint32_t)__builtin_popcountll(ba);
         equal += (uint32_t)__builtin_popcountll(be);
     });
@@ -222,10 +304,11 @@ __device__ __forceinline__ uint32_t as_u32(h2v h) { union { uint32_t u; h2v h; }
 // One key group's parameters, by channel.
 struct GroupParams { float zero, inv; };
 
-template <int BITS, int TB, bool REGROUP>
+// REGROUP: 0, or log2 of the group size where key groups are formed anew (a workgroup has whole ones).
+template <int BITS, int REGROUP>
 __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, int key_axis) {
     constexpr bool QUANT = BITS != 16;
-    constexpr int GROUPS = REGROUP ? TB / 32 < 4 ? TB / 32 : 4 : 1;
+    constexpr int TB = REGROUP == 7 ? 128 : 64, GROUPS = REGROUP ? TB >> REGROUP : 1;
     __shared__ int s_idx[TB];
     __shared__ ValuePlace s_place[TB];
     __shared__ uint32_t s_min[REGROUP ? 4 * GROUPS * 64 : 1], s_max[REGROUP ? 4 * GROUPS * 64 : 1];    // [wave][group][channel pair]
@@ -335,33 +418,39 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
         uint32_t word = 0u;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int t = token_of(w, e);
-            const uint32_t field = BITS == 16 ? (got[w][e] >> s_place[t].shift) & 0xFFFFu : __builtin_amdgcn_ubfe(got[w][e], s_place[t].shift, BITS);
-            word |= (t < ntok ? field : 0u) << (16 * (e / HALF) + BITS * (e % HALF));
+            const uint32_t shift = s_place[token_of(w, e)].shift;
+            const uint32_t field = BITS == 16 ? (got[w][e] >> shift) & 0xFFFFu : __builtin_amdgcn_ubfe(got[w][e], shift, BITS);
+            word |= field << (16 * (e / HALF) + BITS * (e % HALF));
+        }
+        if (ntok < TB) {       // (uniform) the head's last tokens: zeros behind them
+            uint32_t there = 0u;
+#pragma unroll
+            for (int e = 0; e < E; ++e) there |= (token_of(w, e) < ntok ? (1u << BITS) - 1u : 0u) << (16 * (e / HALF) + BITS * (e % HALF));
+            word &= there;
         }
         const int i = w * kMoveThreads + tid;
         if (i / SBW * SB < ntok) vd[i] = word;
     }
 
     if constexpr (QUANT) {
-        if (key_axis == KVQP_KEY_PER_CHANNEL) {
+        if (REGROUP || key_axis == KVQP_KEY_PER_CHANNEL) {
             // keys per channel: the groups' rows of scales and zeros, and (REGROUP) the codes of groups that are formed anew
-            const int group = 1 << a.group_log2;
-            const size_t sg = (size_t)((a.src_cap + group - 1) >> a.group_log2), dg = (size_t)((a.dst_cap + group - 1) >> a.group_log2);
-            const int groups = (ntok + group - 1) >> a.group_log2;
+            const int group_log2 = REGROUP ? REGROUP : a.group_log2, group = 1 << group_log2;
+            const size_t sg = (size_t)((a.src_cap + group - 1) >> group_log2), dg = (size_t)((a.dst_cap + group - 1) >> group_log2);
+            const int groups = (ntok + group - 1) >> group_log2;
             if constexpr (!REGROUP) {
                 for (int i = tid; i < groups * (kHeadDim / 2); i += kMoveThreads) {
                     const int g = i / (kHeadDim / 2), d = i % (kHeadDim / 2);
                     if (t0 & (group - 1)) continue;      // (a group that began in an earlier workgroup's tokens)
-                    const size_t from = ((size_t)bh * sg + (s_idx[g << a.group_log2] >> a.group_log2)) * (kHeadDim / 2) + d;
-                    const size_t to = ((size_t)bh * dg + (t0 >> a.group_log2) + g) * (kHeadDim / 2) + d;
+                    const size_t from = ((size_t)bh * sg + (s_idx[g << group_log2] >> group_log2)) * (kHeadDim / 2) + d;
+                    const size_t to = ((size_t)bh * dg + (t0 >> group_log2) + g) * (kHeadDim / 2) + d;
                     ((uint32_t*)a.dst.k_scale)[to] = ((const uint32_t*)a.src.k_scale)[from];
                     ((uint32_t*)a.dst.k_zero)[to] = ((const uint32_t*)a.src.k_zero)[from];
                 }
             } else {
                 constexpr int R = TB / 16;          // a thread's rows: r, r + 16, ..., channels 8 c8 .. 8 c8 + 7
                 const int c8 = tid & 15, r = tid >> 4, wave = tid >> 6;
-                const int rpg_log2 = a.group_log2 - 4;         // 2, 4 or 8 of a thread's rows make a group
+                constexpr int rpg_log2 = REGROUP - 4;         // 2, 4 or 8 of a thread's rows make a group
                 const uint32_t* kc = (const uint32_t*)a.src.k_codes + (size_t)bh * a.src_cap * (4 * BITS);
                 const uint16_t* ks = (const uint16_t*)a.src.k_scale + (size_t)bh * sg * kHeadDim + 8 * c8;
                 const uint16_t* kz = (const uint16_t*)a.src.k_zero + (size_t)bh * sg * kHeadDim + 8 * c8;
@@ -374,8 +463,8 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
                     if constexpr (BITS == 8) { const uint2 u = *reinterpret_cast<const uint2*>(kc + (size_t)t * 32 + 2 * c8); code[j][0] = u.x; code[j][1] = u.y; }
                     else if constexpr (BITS == 4) code[j][0] = kc[(size_t)t * 16 + c8];
                     else code[j][0] = kc[(size_t)t * 8 + c8 / 2] >> (8 * (c8 & 1));
-                    s4[j] = *reinterpret_cast<const uint4*>(ks + (size_t)(t >> a.group_log2) * kHeadDim);
-                    z4[j] = *reinterpret_cast<const uint4*>(kz + (size_t)(t >> a.group_log2) * kHeadDim);
+                    s4[j] = *reinterpret_cast<const uint4*>(ks + (size_t)(t >> group_log2) * kHeadDim);
+                    z4[j] = *reinterpret_cast<const uint4*>(kz + (size_t)(t >> group_log2) * kHeadDim);
                 }
                 // bit of element e's field in its word
                 auto bit_of = [](int e) { return BITS == 8 ? 8 * (e % 4 / 2) + 16 * (e % 2) : BITS * (e / 2) + 16 * (e % 2); };
@@ -390,8 +479,8 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
                         x[j][e / 2][e % 2] = (_Float16)fminf(fmaxf(v, -65504.0f), 65504.0f);
                     }
                 }
-                // minima and maxima of the groups' channels: a thread's rows, the wave's four row lanes, the four waves.  Rows past
-                // the count repeat the last token, which is of the last group.
+                // minima and maxima of the groups' channels: a thread's rows, the wave's four row lanes, the four waves.  (Rows past
+                // the count repeat the last token, which is of the last group.)
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
                     if (g >= groups) break;       // (uniform)
@@ -400,7 +489,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
                         h2v lo = {(_Float16)65504.0f, (_Float16)65504.0f}, hi = -lo;
 #pragma unroll
                         for (int j = 0; j < R; ++j)
-                            if (min(j >> rpg_log2, groups - 1) == g) { lo = __builtin_elementwise_min(lo, x[j][q]); hi = __builtin_elementwise_max(hi, x[j][q]); }
+                            if (j >> rpg_log2 == g) { lo = __builtin_elementwise_min(lo, x[j][q]); hi = __builtin_elementwise_max(hi, x[j][q]); }
                         lo = __builtin_elementwise_min(lo, as_h2(xor_rows(as_u32(lo), false))); hi = __builtin_elementwise_max(hi, as_h2(xor_rows(as_u32(hi), false)));
                         lo = __builtin_elementwise_min(lo, as_h2(xor_rows(as_u32(lo), true))); hi = __builtin_elementwise_max(hi, as_h2(xor_rows(as_u32(hi), true)));
                         if ((tid & 48) == 0) { s_min[(wave * GROUPS + g) * 64 + 4 * c8 + q] = as_u32(lo); s_max[(wave * GROUPS + g) * 64 + 4 * c8 + q] = as_u32(hi); }
@@ -409,9 +498,9 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
                 __syncthreads();
                 // A group whose tokens were one group before: it begins where one began, has no gap, and is as long as that one.
                 auto same_group = [&](int g, int& first) {
-                    const int members = min(group, ntok - (g << a.group_log2));
-                    first = s_idx[g << a.group_log2];
-                    return (first & (group - 1)) == 0 && s_idx[(g << a.group_log2) + members - 1] - first == members - 1 && members == min(group, n_src - first);
+                    const int members = min(group, ntok - (g << group_log2));
+                    first = s_idx[g << group_log2];
+                    return (first & (group - 1)) == 0 && s_idx[(g << group_log2) + members - 1] - first == members - 1 && members == min(group, n_src - first);
                 };
                 for (int i = tid; i < groups * kHeadDim; i += kMoveThreads) {
                     const int g = i / kHeadDim, d = i % kHeadDim;
@@ -426,7 +515,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
                     s_par[i] = {lo, sf == 0.0f ? 0.0f : __fdiv_rn(1.0f, sf)};
                     int first;
                     const bool same = same_group(g, first);
-                    const size_t from = ((size_t)bh * sg + (first >> a.group_log2)) * kHeadDim + d, to = ((size_t)bh * dg + (t0 >> a.group_log2) + g) * kHeadDim + d;
+                    const size_t from = ((size_t)bh * sg + (first >> group_log2)) * kHeadDim + d, to = ((size_t)bh * dg + (t0 >> group_log2) + g) * kHeadDim + d;
                     ((uint16_t*)a.dst.k_scale)[to] = same ? ((const uint16_t*)a.src.k_scale)[from] : __half_as_ushort(sh);
                     ((uint16_t*)a.dst.k_zero)[to] = same ? ((const uint16_t*)a.src.k_zero)[from] : __half_as_ushort(__float2half_rn(lo));
                 }
@@ -443,13 +532,18 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
 #pragma unroll
                     for (int j = 0; j < R; ++j) {
                         const int t = r + 16 * j;
-                        if ((j >> rpg_log2) != g || t >= rows) continue;      // (the same for the 16 lanes of a row)
+                        if (j >> rpg_log2 != g || t >= rows) continue;      // (the same for the 16 lanes of a row)
                         uint32_t w[2] = {0u, 0u};
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const float c = rintf(__fmul_rn(__fsub_rn((float)x[j][e / 2][e % 2], par[e].zero), par[e].inv));
-                            w[BITS == 8 ? e / 4 : 0] |= (uint32_t)fminf(fmaxf(c, 0.0f), (float)((1 << BITS) - 1)) << bit_of(e);
+                            // (added to 3 2^22, a number is rounded to a whole one, half to even, in the lowest bits:
+                            // five instructions a code instead of seven)
+                            const float c = __fadd_rn(__fmul_rn(__fsub_rn((float)x[j][e / 2][e % 2], par[e].zero), par[e].inv), 12582912.0f);
+                            w[BITS == 8 ? e / 4 : 0] += __float_as_uint(__builtin_amdgcn_fmed3f(c, 12582912.0f, 12582912.0f + (float)((1 << BITS) - 1))) << bit_of(e);
                         }
+                        // (what the number that was added leaves above the codes)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[BITS == 8 ? e / 4 : 0] -= __float_as_uint(12582912.0f) << bit_of(e);
                         if (same) { w[0] = BITS == 2 ? code[j][0] & 0x00FF00FFu : code[j][0]; if constexpr (BITS == 8) w[1] = code[j][1]; }
                         if (t >= ntok) w[0] = w[1] = 0u;
                         if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out + (size_t)t * 32 + 2 * c8) = make_uint2(w[0], w[1]);
@@ -470,14 +564,18 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
 template <int BITS>
 hipError_t move_bits(const EvictArgs& a0, int heads, int key_axis, bool regroup, hipStream_t stream) {
     EvictArgs a = a0;
-    const int tb = regroup && a.group_log2 == 7 ? 128 : 64;
+    const int tb = regroup && a.group_log2 == 7 ? 128 : 64;          // (as move_tokens has it)
     a.token_blocks = (a.bound + tb - 1) / tb;
     const dim3 grid(a.token_blocks + 1, heads), block(kMoveThreads);
     if constexpr (BITS != 16) {
-        if (regroup && tb == 128) { move_tokens<BITS, 128, true><<<grid, block, 0, stream>>>(a, key_axis); return hipGetLastError(); }
-        if (regroup) { move_tokens<BITS, 64, true><<<grid, block, 0, stream>>>(a, key_axis); return hipGetLastError(); }
+        if (regroup) {
+            if (a.group_log2 == 5) move_tokens<BITS, 5><<<grid, block, 0, stream>>>(a, key_axis);
+            else if (a.group_log2 == 6) move_tokens<BITS, 6><<<grid, block, 0, stream>>>(a, key_axis);
+            else move_tokens<BITS, 7><<<grid, block, 0, stream>>>(a, key_axis);
+            return hipGetLastError();
+        }
     }
-    move_tokens<BITS, 64, false><<<grid, block, 0, stream>>>(a, key_axis);
+    move_tokens<BITS, 0><<<grid, block, 0, stream>>>(a, key_axis);
     return hipGetLastError();
 }
 
@@ -496,7 +594,8 @@ hipError_t launch_evict(const kvqp_cfg& cfg, const kvqp_cache& src, const float*
     a.group_log2 = cfg.bits == 16 || cfg.group_size == 128 ? 7 : cfg.group_size == 64 ? 6 : 5;
     const int heads = cfg.batch * cfg.n_kv_heads;
     const int units = src.n_kept / unit;
-    if (units <= 1024) pick_heaviest<4, 256><<<dim3(heads), dim3(256), 0, stream>>>(a);
+    if (units <= kFewUnits) pick_of_few<<<dim3(heads), dim3(kFewUnits), 0, stream>>>(a);
+    else if (units <= 1024) pick_heaviest<4, 256><<<dim3(heads), dim3(256), 0, stream>>>(a);
     else if (units <= 8192) pick_heaviest<8, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
     else if (units <= 32768) pick_heaviest<32, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
     else pick_heaviest<0, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
