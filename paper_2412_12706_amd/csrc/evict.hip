@@ -4,14 +4,19 @@
 //   score[u] = float(sum over the unit's tokens of weight[t]), summed in binary64
 //   kept     = the m highest scores, equal ones going to the lower unit, in ascending order
 //
-// Two launches.  pick_heaviest finds the cut of one head per workgroup: a radix selection on 32-bit order keys (11 + 11 + 10
-// bits, a histogram in LDS each) and one ordered pass that writes the survivors.  move_tokens gathers: nothing is rounded
-// anew -- codes, scales and zeros of values, of keys per token and of whole key groups are copied bit by bit, value codes
-// from and into the tile-transposed words -- except where tokens of different key groups form a new one (keys per channel,
-// units smaller than a group): those keys are read back as binary16 numbers and quantized again, by the cache's quantizer.
-// (A new group whose tokens were one group before is copied too: what lies before the first token that leaves is never touched.)
-// Both are bound by memory: the survivors' bytes are read and written once (a value word holds 4 to 16 tokens, so
-// what lies between survivors comes along).
+// Two launches.  pick_heaviest finds the cut of one head per workgroup: a radix selection on 32-bit order keys (11 + 11 +
+// 10 bits, a histogram in LDS each) and one ordered pass that writes the survivors; up to 256 units are ranked by counting
+// instead, and for small caches the second launch does that, too.  move_tokens gathers: nothing is rounded anew -- codes,
+// scales and zeros of values, of keys per token and of whole key groups are copied bit by bit, value codes from and into
+// the tile-transposed words -- except where tokens of different key groups form a new one (keys per channel, units smaller
+// than a group): those keys are read back as binary16 numbers and quantized again, by the cache's quantizer.  (A new group
+// whose tokens were one group before is copied too: what lies before the first token that leaves is never touched.)
+// Many heads are bound by memory: the survivors' bytes are read and written once (a value word holds 4 to 16 tokens, so
+// what lies between survivors comes along).  256 heads of 8192 tokens to 6144, 4 bits: 110.8 us for 533 MB, 4.8 TB/s of the
+// 5.2 that a large copy reaches, behind 12.4 us of selection.  Few heads are bound by latency, keys that are quantized again
+// by vector instructions (16 heads of 12003 tokens to 8001, 2 bits: 12.4 + 18 us, where 27 MB would take 6).
+#include <type_traits>
+
 #include "kvqp_internal.h"
 
 namespace kvqp {
@@ -96,20 +101,20 @@ constexpr uint32_t kOddTurn = 16u;       // the odd lanes' histogram has its bin
 // (Whole evictions of 8 heads, and by the selection below: 33 units of 32 tokens 7.7 us and 10.3, 256 of 32 tokens 13.6 and 15.4, 256 single
 // tokens 9.1 and 8.7.)
 constexpr int kFewUnits = 256;
-__global__ __launch_bounds__(kFewUnits) void pick_of_few(const EvictArgs a) {
-    __shared__ uint4 s_key[kFewUnits / 4];
-    __shared__ int s_unit[kFewUnits];
-    __shared__ uint32_t s_wave[4];
-    const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = source_tokens(a, bh);
-    const Cut cut = cut_of(n, a.n_keep, a.unit);
+struct FewUnits {
+    uint4 key[kFewUnits / 4];
+    int unit[kFewUnits];            // those that stay, in order
+    uint32_t wave[4];
+};
+__device__ __forceinline__ void rank_few(const EvictArgs& a, int bh, const Cut& cut, FewUnits& s) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t key = tid < cut.units ? unit_key(a.weights + (size_t)bh * a.w_cap, tid, a.unit) : 0u;
-    reinterpret_cast<uint32_t*>(s_key)[tid] = key;
+    reinterpret_cast<uint32_t*>(s.key)[tid] = key;
     __syncthreads();
     uint32_t before = 0u;
 #pragma unroll 1
     for (int b = 0; 64 * b < cut.units; ++b) {           // (keys past the last unit are 0, and come after every unit)
-        const uint4* keys = s_key + 16 * b;
+        const uint4* keys = s.key + 16 * b;
         if (b != wave) {          // (equal keys of lower units come before this one, those of higher ones after it)
             const uint32_t least = key + (b > wave);
 #pragma unroll
@@ -127,19 +132,29 @@ __global__ __launch_bounds__(kFewUnits) void pick_of_few(const EvictArgs a) {
     }
     const bool stays = tid < cut.units && before < (uint32_t)cut.keep_units;
     const unsigned long long all = __builtin_amdgcn_ballot_w64(stays);
-    if (lane == 0) s_wave[wave] = (uint32_t)__builtin_popcountll(all);
+    if (lane == 0) s.wave[wave] = (uint32_t)__builtin_popcountll(all);
     __syncthreads();
     uint32_t at = lanes_below(all, 0u);
-    for (int w = 0; w < wave; ++w) at += s_wave[w];
-    if (stays) s_unit[at] = tid;
+    for (int w = 0; w < wave; ++w) at += s.wave[w];
+    if (stays) s.unit[at] = tid;
     __syncthreads();
-    const int whole = cut.keep_units * a.unit, unit_log2 = __builtin_ctz(a.unit);
-    for (int i = tid; i < cut.kept; i += kFewUnits) {
-        const int t = i < whole ? s_unit[i >> unit_log2] * a.unit + (i & (a.unit - 1)) : cut.units * a.unit + i - whole;
+}
+// The token of place i
+__device__ __forceinline__ int token_at(const EvictArgs& a, const Cut& cut, const FewUnits& s, int i) {
+    const int whole = cut.keep_units * a.unit;
+    return i < whole ? s.unit[i >> __builtin_ctz(a.unit)] * a.unit + (i & (a.unit - 1)) : cut.units * a.unit + i - whole;
+}
+__global__ __launch_bounds__(kFewUnits) void pick_of_few(const EvictArgs a) {
+    __shared__ FewUnits s;
+    const int bh = blockIdx.x;
+    const Cut cut = cut_of(source_tokens(a, bh), a.n_keep, a.unit);
+    rank_few(a, bh, cut, s);
+    for (int i = threadIdx.x; i < cut.kept; i += kFewUnits) {
+        const int t = token_at(a, cut, s, i);
         a.idx[(size_t)bh * a.bound + i] = t;
         if (a.list) a.list[(size_t)bh * a.bound + i] = t;
     }
-    if (a.dst.head_n_kept && tid == 0) a.dst.head_n_kept[bh] = cut.kept;
+    if (a.dst.head_n_kept && threadIdx.x == 0) a.dst.head_n_kept[bh] = cut.kept;
 }
 
 // One head per workgroup.  Every wave has a stretch of consecutive units, 64 at a time.  The keys of up to
@@ -305,7 +320,8 @@ __device__ __forceinline__ uint32_t as_u32(h2v h) { union { uint32_t u; h2v h; }
 struct GroupParams { float zero, inv; };
 
 // REGROUP: 0, or log2 of the group size where key groups are formed anew (a workgroup has whole ones).
-template <int BITS, int REGROUP>
+// RANKS: every workgroup finds its head's survivors itself; idx is not there.
+template <int BITS, int REGROUP, bool RANKS>
 __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, int key_axis) {
     constexpr bool QUANT = BITS != 16;
     constexpr int TB = REGROUP == 7 ? 128 : 64, GROUPS = REGROUP ? TB >> REGROUP : 1;
@@ -313,11 +329,14 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
     __shared__ ValuePlace s_place[TB];
     __shared__ uint32_t s_min[REGROUP ? 4 * GROUPS * 64 : 1], s_max[REGROUP ? 4 * GROUPS * 64 : 1];    // [wave][group][channel pair]
     __shared__ GroupParams s_par[REGROUP ? GROUPS * kHeadDim : 1];
+    __shared__ std::conditional_t<RANKS, FewUnits, char> s_few;
     const int bh = blockIdx.y, tid = threadIdx.x;
     const int n_src = source_tokens(a, bh);
-    const int kept = cut_of(n_src, a.n_keep, a.unit).kept;
+    const Cut cut = cut_of(n_src, a.n_keep, a.unit);
+    const int kept = cut.kept;
     if ((int)blockIdx.x >= a.token_blocks) {
         // the tail, its weights, and zeros for tokens to come
+        if (RANKS && a.dst.head_n_kept && tid == 0) a.dst.head_n_kept[bh] = kept;
         const size_t from = (size_t)bh * a.src.tail_cap * kHeadDim, to = (size_t)bh * a.dst.tail_cap * kHeadDim;
         for (int i = tid; i < a.src.tail_len * 16; i += kMoveThreads) {
             reinterpret_cast<uint4*>((uint16_t*)a.dst.tail_k + to)[i] = reinterpret_cast<const uint4*>((const uint16_t*)a.src.tail_k + from)[i];
@@ -333,8 +352,16 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
     const int t0 = blockIdx.x * TB;
     if (t0 >= kept) return;
     const int ntok = min(TB, kept - t0), rows = rows32(ntok);
+    if constexpr (RANKS) rank_few(a, bh, cut, s_few);
     if (tid < TB) {
-        const int t = a.idx[(size_t)bh * a.bound + t0 + min(tid, ntok - 1)];
+        const int i = t0 + min(tid, ntok - 1);
+        int t;
+        if constexpr (RANKS) {
+            t = token_at(a, cut, s_few, i);
+            if (a.list) a.list[(size_t)bh * a.bound + i] = t;
+        } else {
+            t = a.idx[(size_t)bh * a.bound + i];
+        }
         s_idx[tid] = t;
         s_place[tid] = value_place<BITS>(t);
     }
@@ -561,7 +588,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
     }
 }
 
-template <int BITS>
+template <int BITS, bool RANKS>
 hipError_t move_bits(const EvictArgs& a0, int heads, int key_axis, bool regroup, hipStream_t stream) {
     EvictArgs a = a0;
     const int tb = regroup && a.group_log2 == 7 ? 128 : 64;          // (as move_tokens has it)
@@ -569,14 +596,23 @@ hipError_t move_bits(const EvictArgs& a0, int heads, int key_axis, bool regroup,
     const dim3 grid(a.token_blocks + 1, heads), block(kMoveThreads);
     if constexpr (BITS != 16) {
         if (regroup) {
-            if (a.group_log2 == 5) move_tokens<BITS, 5><<<grid, block, 0, stream>>>(a, key_axis);
-            else if (a.group_log2 == 6) move_tokens<BITS, 6><<<grid, block, 0, stream>>>(a, key_axis);
-            else move_tokens<BITS, 7><<<grid, block, 0, stream>>>(a, key_axis);
+            if (a.group_log2 == 5) move_tokens<BITS, 5, RANKS><<<grid, block, 0, stream>>>(a, key_axis);
+            else if (a.group_log2 == 6) move_tokens<BITS, 6, RANKS><<<grid, block, 0, stream>>>(a, key_axis);
+            else move_tokens<BITS, 7, RANKS><<<grid, block, 0, stream>>>(a, key_axis);
             return hipGetLastError();
         }
     }
-    move_tokens<BITS, 0><<<grid, block, 0, stream>>>(a, key_axis);
+    move_tokens<BITS, 0, RANKS><<<grid, block, 0, stream>>>(a, key_axis);
     return hipGetLastError();
+}
+template <bool RANKS>
+hipError_t move(const EvictArgs& a, const kvqp_cfg& cfg, int heads, bool regroup, hipStream_t stream) {
+    switch (cfg.bits) {
+        case 2: return move_bits<2, RANKS>(a, heads, cfg.key_axis, regroup, stream);
+        case 4: return move_bits<4, RANKS>(a, heads, cfg.key_axis, regroup, stream);
+        case 8: return move_bits<8, RANKS>(a, heads, cfg.key_axis, regroup, stream);
+        default: return move_bits<16, RANKS>(a, heads, cfg.key_axis, regroup, stream);
+    }
 }
 
 }  // namespace
@@ -594,6 +630,10 @@ hipError_t launch_evict(const kvqp_cfg& cfg, const kvqp_cache& src, const float*
     a.group_log2 = cfg.bits == 16 || cfg.group_size == 128 ? 7 : cfg.group_size == 64 ? 6 : 5;
     const int heads = cfg.batch * cfg.n_kv_heads;
     const int units = src.n_kept / unit;
+    const bool regroup = cfg.bits != 16 && cfg.key_axis == KVQP_KEY_PER_CHANNEL && unit % cfg.group_size != 0;
+    // Where moving takes two workgroups per CU at most, each ranks its head's few units for itself and one launch does all (4 bits; 8 heads of
+    // 33 units of 32 tokens, 272 workgroups: 5.9 us, 7.8 in two launches; 32 heads of 32 units, 512: 7.2 and 9.0; 64 heads, 1024: 13.0 and 11.4).
+    if (units <= kFewUnits && (long long)heads * (bound / 64 + 2) <= 512) return move<true>(a, cfg, heads, regroup, stream);
     if (units <= kFewUnits) pick_of_few<<<dim3(heads), dim3(kFewUnits), 0, stream>>>(a);
     else if (units <= 1024) pick_heaviest<4, 256><<<dim3(heads), dim3(256), 0, stream>>>(a);
     else if (units <= 8192) pick_heaviest<8, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
@@ -601,13 +641,7 @@ hipError_t launch_evict(const kvqp_cfg& cfg, const kvqp_cache& src, const float*
     else pick_heaviest<0, 1024><<<dim3(heads), dim3(1024), 0, stream>>>(a);
     const hipError_t rc = hipGetLastError();
     if (rc != hipSuccess) return rc;
-    const bool regroup = cfg.bits != 16 && cfg.key_axis == KVQP_KEY_PER_CHANNEL && unit % cfg.group_size != 0;
-    switch (cfg.bits) {
-        case 2: return move_bits<2>(a, heads, cfg.key_axis, regroup, stream);
-        case 4: return move_bits<4>(a, heads, cfg.key_axis, regroup, stream);
-        case 8: return move_bits<8>(a, heads, cfg.key_axis, regroup, stream);
-        default: return move_bits<16>(a, heads, cfg.key_axis, regroup, stream);
-    }
+    return move<false>(a, cfg, heads, regroup, stream);
 }
 
 }  // namespace kvqp

@@ -159,3 +159,16 @@ def test_evictions_from_long_heads(orc, n, unit, n_keep, bits, G, axis):
     short = n % unit
     kept = short + (n_keep - short) // unit * unit
     check_evict(orc, cfg, src, w, n_keep, unit, [n], target(cfg, kept, 3, 0), 3)
+
+
+@pytest.mark.parametrize("kind", ["zeros", "two values", "nan", "infinite", "different"])
+@pytest.mark.parametrize("n,unit,n_keep", [(1, 1, 1), (63, 1, 20), (130, 1, 65), (256, 1, 255), (257, 1, 100), (300, 64, 65), (8192, 32, 4000), (8250, 32, 8193), (1025, 1, 1024)])
+def test_ties_among_few_units(orc, kind, n, unit, n_keep):
+    rng = np.random.default_rng(39)
+    shape = (1, 2, n + 3)
+    cfg, src, _, _ = make(orc, rng, 1, 2, 1, n, 3, 4, 32, 1)
+    w = {"zeros": lambda: np.zeros(shape), "two values": lambda: rng.integers(0, 2, shape) * 0.25, "nan": lambda: np.where(rng.random(shape) < 0.02, np.nan, rng.integers(0, 3, shape)),
+         "infinite": lambda: np.where(rng.random(shape) < 0.05, np.inf, 1.0), "different": lambda: np.exp(2 * rng.standard_normal(shape))}[kind]().astype(np.float32)
+    short = n % unit
+    kept = n if n <= n_keep else short + (n_keep - short) // unit * unit
+    check_evict(orc, cfg, src, w, n_keep, unit, [n] * 2, target(cfg, kept, 3, 0), 3)
