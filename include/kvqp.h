@@ -427,8 +427,10 @@ int kvqp_append_tail_ragged(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_to
  * kvqp_evict takes the cache back to its budget.
  *
  * Common to the three: cfg fields used are batch, heads, head_dim, bits, group_size, key_axis and
- * sm_scale, and decode_cache_hint, where AUTO here means STREAM for calls on more than 96 MB of codes and KEEP for others.  Caches with outlier filtering are not taken (UNSUPPORTED).  Head-level counts
- * (cache->head_n_kept) are read on the device, where a count above n_kept is cut to n_kept.
+ * sm_scale, and decode_cache_hint, where AUTO here means STREAM for calls on more than 96 MB of
+ * codes and KEEP for others.  Caches with outlier filtering, and of more than 2^26 tokens per head,
+ * are not taken (UNSUPPORTED).  Head-level counts (cache->head_n_kept) are read on the device, where a
+ * count above n_kept is cut to n_kept.
  * q, k_new, v_new, out and the cache's codes, per-channel scales and zeros and tails have to be aligned to
  * 16 bytes, everything else to its own size and the scales and zeros that belong to tokens to 4 (INVALID_ARG).
  */
@@ -464,8 +466,8 @@ int kvqp_tree_workspace_init(void *workspace, size_t workspace_bytes, void *hip_
  * does not attend does not reach it, whatever it holds, infinities and NaN included.
  * n_kept and tail_len may be 0.  Reproducible bit for bit.
  * Numerical range: the product of a query element, scaled so that its row's largest is 64 .. 128,
- * and its channel's key scale must stay below 65504 (a scale of 511), and with per-token keys a
- * code times its scale; weights are exact to 2^-22, values are rounded to binary16 once.
+ * and its channel's key scale must stay below 65504 (a scale of 511), and so must a code times
+ * its scale; weights are exact to 2^-22, values are rounded to binary16 once.
  * Workspace: kvqp_tree_workspace_bytes, 16-byte aligned, prepared once with kvqp_tree_workspace_init.  One may
  * serve calls of any configurations for which it is large enough; calls that share one must not overlap in time
  * (calls issued on one stream never do), calls with different ones are independent.

@@ -20,13 +20,14 @@
 //
 // Exactness.  Logits are exact to about 2^-22 although the operands are binary16:
 //   keys per channel: the codes times q * s split into binary16 hi + lo parts (v_pk_mul, and v_pk_fma for
-//     what the product lost); q . z comes from a product of sixteen groups' zeros at a time.  (Codes are
-//     whole numbers: as subnormals code * 2^-24, which cost one AND, the matrix unit lines products up by their nominal exponents
-//     and loses what lies below, 2e-5 of a weight);
+//     what the product lost), or above 32 rows code * s split so times q; q . z comes from a product of
+//     sixteen groups' zeros at a time.  (Codes are whole numbers: as subnormals code * 2^-24, which cost one
+//     AND, the matrix unit lines products up by their nominal exponents and loses what lies below, 2e-5 of a weight);
 //   keys per token: code * s split the same way times q, and z (its rows are constant over a group of
 //     channels) times the sums of q over 32 channels, again hi + lo.
 // Query rows are scaled by a power of two to a largest element of 64 .. 128, so that the lo parts do
-// not run into binary16's subnormals; products above 65504 would overflow (a scale of 512 and more).
+// not run into binary16's subnormals; products above 65504 would overflow (a scale of 512 and more, of 257
+// and more where 8-bit codes take it).
 // Weights enter the second product as hi + lo too; values as one binary16 number, code * s + z
 // rounded once, which is the accuracy of the value itself at 16 bits.
 #include <algorithm>
@@ -400,17 +401,37 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const Ke
             sc.q = *reinterpret_cast<const uint4*>(&strip.k_scale[16 * kb + 4 * s]);
 #pragma unroll
             for (int H = 0; H < 2; ++H) key_whole<BITS>(fields, k.w[H], s, a[H].h);
+            if constexpr (RT <= 2) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const Frag q = query(rt, s);
-                Frag hi, lo;
+                for (int rt = 0; rt < RT; ++rt) {
+                    const Frag q = query(rt, s);
+                    Frag hi, lo;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    hi.h[r] = q.h[r] * sc.h[r];
-                    lo.h[r] = __builtin_elementwise_fma(q.h[r], sc.h[r], -hi.h[r]);
+                    for (int r = 0; r < 4; ++r) {
+                        hi.h[r] = q.h[r] * sc.h[r];
+                        lo.h[r] = __builtin_elementwise_fma(q.h[r], sc.h[r], -hi.h[r]);
+                    }
+                    acc[rt][0] = mfma(a[0], hi, acc[rt][0]); acc[rt][1] = mfma(a[1], hi, acc[rt][1]);
+                    acc[rt][0] = mfma(a[0], lo, acc[rt][0]); acc[rt][1] = mfma(a[1], lo, acc[rt][1]);
                 }
-                acc[rt][0] = mfma(a[0], hi, acc[rt][0]); acc[rt][1] = mfma(a[1], hi, acc[rt][1]);
-                acc[rt][0] = mfma(a[0], lo, acc[rt][0]); acc[rt][1] = mfma(a[1], lo, acc[rt][1]);
+            } else {
+                // (Four tiles of rows: the codes take the scales, which are two tiles.  32 layers of 8192 tokens, 64 rows: 162.5 -> 158.5 us, their
+                // weights 95.3 -> 88.8.)
+                Frag b[2];
+#pragma unroll
+                for (int H = 0; H < 2; ++H)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const h2v c = a[H].h[r];
+                        a[H].h[r] = c * sc.h[r];
+                        b[H].h[r] = __builtin_elementwise_fma(c, sc.h[r], -a[H].h[r]);
+                    }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const Frag q = query(rt, s);
+                    acc[rt][0] = mfma(a[0], q, acc[rt][0]); acc[rt][1] = mfma(a[1], q, acc[rt][1]);
+                    acc[rt][0] = mfma(b[0], q, acc[rt][0]); acc[rt][1] = mfma(b[1], q, acc[rt][1]);
+                }
             }
         } else if constexpr (kToken) {
             Frag b[2];
