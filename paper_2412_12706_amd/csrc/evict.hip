@@ -14,7 +14,7 @@
 // Many heads are bound by memory: the survivors' bytes are read and written once (a value word holds 4 to 16 tokens, so
 // what lies between survivors comes along).  256 heads of 8192 tokens to 6144, 4 bits: 110.8 us for 533 MB, 4.8 TB/s of the
 // 5.2 that a large copy reaches, behind 12.4 us of selection.  Few heads are bound by latency, keys that are quantized again
-// by vector instructions (16 heads of 12003 tokens to 8001, 2 bits: 12.4 + 18 us, where 27 MB would take 6).
+// by vector instructions (16 heads of 12003 tokens to 8001, 2 bits: 12 + 18.6 us, vector ALUs 90 % busy, where 27 MB would take 5).
 #include <type_traits>
 
 #include "kvqp_internal.h"
@@ -632,7 +632,7 @@ hipError_t launch_evict(const kvqp_cfg& cfg, const kvqp_cache& src, const float*
     const int units = src.n_kept / unit;
     const bool regroup = cfg.bits != 16 && cfg.key_axis == KVQP_KEY_PER_CHANNEL && unit % cfg.group_size != 0;
     // Where moving takes two workgroups per CU at most, each ranks its head's few units for itself and one launch does all (4 bits; 8 heads of
-    // 33 units of 32 tokens, 272 workgroups: 5.9 us, 7.8 in two launches; 32 heads of 32 units, 512: 7.2 and 9.0; 64 heads, 1024: 13.0 and 11.4).
+    // 33 units of 32 tokens, 136 workgroups: 5.9 us, 7.8 in two launches; 32 heads of 32 units, 480: 7.2 and 9.0; 64 heads, 960: 13.0 and 11.4).
     if (units <= kFewUnits && (long long)heads * (bound / 64 + 2) <= 512) return move<true>(a, cfg, heads, regroup, stream);
     if (units <= kFewUnits) pick_of_few<<<dim3(heads), dim3(kFewUnits), 0, stream>>>(a);
     else if (units <= 1024) pick_heaviest<4, 256><<<dim3(heads), dim3(256), 0, stream>>>(a);
