@@ -464,7 +464,7 @@ int kvqp_tree_workspace_init(void *workspace, size_t workspace_bytes, void *hip_
  *          over everything the row attends
  * A row that attends nothing (an empty cache and an empty mask) gets zeros and -inf.  What a row
  * does not attend does not reach it, whatever it holds, infinities and NaN included.
- * n_kept and tail_len may be 0.  Reproducible bit for bit.
+ * n_kept and tail_len may be 0.  Reproducible bit for bit.  out and lse lie apart from all that is read.
  * Numerical range: the product of a query element, scaled so that its row's largest is 64 .. 128,
  * and its channel's key scale must stay below 65504 (a scale of 511), and so must a code times
  * its scale; weights are exact to 2^-22, values are rounded to binary16 once.

@@ -540,12 +540,15 @@ def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=
     if weights_out is not None:
         cap_out = weights_out.shape[-1]
         _want("weights_out", weights_out, torch.float32, (*heads, cap_out), device)
+    kept = min(n_keep, cache.n_kept)
+    if cache.head_n_kept is None and n_keep < cache.n_kept and unit > 1:
+        short = cache.n_kept % unit
+        kept = short + (n_keep - short) // unit * unit
     if idx_out is not None:
-        kept = min(n_keep, cache.n_kept)
-        if cache.head_n_kept is None and n_keep < cache.n_kept and unit > 1:
-            short = cache.n_kept % unit
-            kept = short + (n_keep - short) // unit * unit
         _want("idx_out", idx_out, torch.int32, (*heads, kept), device)
+    rows = dst.n_cap or (kept + 31) // 32 * 32
+    if dst.buffers["k_codes"].nbytes < heads[0] * heads[1] * rows * 16 * cfg.bits or dst.buffers["tail_k"].nbytes < heads[0] * heads[1] * dst.tail_cap * 256:
+        raise ValueError(f"evict: dst has no room for {rows} packed tokens and {dst.tail_cap} tail rows per head")
     made = None
     if workspace is None:
         workspace = made = alloc_evict_workspace(cfg, cache, weights.device)

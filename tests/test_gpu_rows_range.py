@@ -172,3 +172,102 @@ def test_ties_among_few_units(orc, kind, n, unit, n_keep):
     short = n % unit
     kept = n if n <= n_keep else short + (n_keep - short) // unit * unit
     check_evict(orc, cfg, src, w, n_keep, unit, [n] * 2, target(cfg, kept, 3, 0), 3)
+
+
+@pytest.mark.parametrize("bits,axis,N", [(4, 0, 3), (2, 1, 6), (16, 0, 15), (8, 0, 30)])
+def test_a_row_of_anything_stays_alone(orc, bits, axis, N):
+    """A padded row's query may hold NaN or infinities: the other rows' results are the same bits."""
+    rng = np.random.default_rng(40)
+    cfg, cache, keys, values = make(orc, rng, 1, 2, 4, 1200, 20, bits, 32, axis)
+    q, kn, vn = draft(rng, 1, 2, 4, N)
+    out, lse = check_tree(cfg, cache, keys, values, q, kn, vn, chain(N), None)
+    bad = q.copy()
+    bad[0, 2, 1] = np.nan
+    bad[0, 6, 0, 5] = np.inf
+    bad[0, 7, N - 1] = -np.inf
+    lse2 = torch.empty((1, 8, N), device="cuda")
+    out2 = kvqp.tree_attn(cfg, dev(bad), dev(kn), dev(vn), None, cache, lse=lse2).cpu().numpy().astype(np.float64)
+    same = np.ones((8, N), bool)
+    same[2, 1] = same[6, 0] = same[7, N - 1] = False
+    assert np.array_equal(out2[0][same], out[0][same]) and np.array_equal(lse2.cpu().numpy()[0][same], lse[0][same])
+    assert not np.isfinite(out2[0][~same]).any()
+
+
+def test_captured_calls_that_make_their_own_workspaces(orc):
+    rng = np.random.default_rng(41)
+    cfg, cache, keys, values = make(orc, rng, 1, 2, 4, 2600, 32, 4, 32, 1)
+    q, kn, vn = (dev(x) for x in draft(rng, 1, 2, 4, 8))
+    w = dev(np.exp(rng.standard_normal((1, 2, 2640))).astype(np.float32))
+    eager, into = kvqp.tree_attn(cfg, q, kn, vn, None, cache), [target(cfg, 2000, 32, 0) for _ in range(2)]
+    kvqp.evict(cfg, cache, w, 2000, into[0])
+    out = torch.empty_like(q)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        kvqp.tree_attn(cfg, q, kn, vn, None, cache, out=out)
+        kvqp.evict(cfg, cache, w, 2000, into[1])
+        again = kvqp.tree_attn(cfg, q, kn, vn, None, cache)
+    for _ in range(4):
+        out.zero_()
+        for t in into[1].buffers.values():
+            t.zero_()
+        g.replay()
+        assert torch.equal(kvqp.tree_attn(cfg, q, kn, vn, None, cache), eager)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(again, eager)
+        for k, t in into[0].buffers.items():
+            assert torch.equal(t, into[1].buffers[k]), k
+
+
+@pytest.mark.parametrize("bits,G,axis,unit,ragged", [(4, 32, 0, 1, False), (2, 64, 1, 1, True), (8, 128, 0, 128, False), (16, 32, 0, 32, True), (2, 32, 0, 1, True)])
+def test_evictions_from_a_layout_with_room(orc, bits, G, axis, unit, ragged):
+    """src laid out for more tokens than it has (n_cap), dst for others again."""
+    rng = np.random.default_rng(42)
+    counts = [450, 449, 0, 300] if ragged else [450] * 4
+    cfg, src, _, _ = make(orc, rng, 2, 2, 1, 450, 6, bits, G, axis, counts=counts if ragged else None, n_cap=640)
+    w = np.exp(2 * rng.standard_normal((2, 2, 470))).astype(np.float32)
+    check_evict(orc, cfg, src, w, 333, unit, counts, target(cfg, 384, 9, 384, ragged=ragged), 6)
+
+
+def test_caches_of_more_than_four_gigabytes(orc):
+    """Heads whose codes begin past 2^32 bytes."""
+    rng = np.random.default_rng(43)
+    heads, n, N = 600, 30000, 2
+    cfg, one, keys, values = make(orc, rng, 1, 1, 2, n, 5, 16, 32, 0)
+    c, cache = many(cfg, one, heads)
+    assert cache.buffers["k_codes"].numel() > 1 << 32
+    q, kn, vn = draft(rng, 1, 1, 2, N)
+    k64, v64 = (np.concatenate([a[0], b[0, 0].astype(np.float64)]) for a, b in ((keys, kn), (values, vn)))
+    lse = torch.empty((heads, 2, N), device="cuda")
+    out = kvqp.tree_attn(c, *(dev(np.repeat(x, heads, 0)) for x in (q, kn, vn)), None, cache, lse=lse)
+    assert torch.equal(out, out[:1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))
+    seen = np.concatenate([np.ones((N, n + 5), bool), chain(N)[0]], 1)
+    for a in range(2):
+        rows = q[0, a].astype(np.float64)
+        ref, ref_lse, spread = attention(rows, k64, v64, seen)
+        assert (np.abs(out[-1, a].cpu().numpy() - ref) <= out_error(ref, spread, logit_error(rows, k64))).all()
+    lse1 = torch.full((1, 2, N), 10.0, device="cuda")
+    w1 = kvqp.accumulate_weights(cfg, dev(q), lse1, one, torch.zeros((1, 1, n + 5), device="cuda"))
+    w = kvqp.accumulate_weights(c, dev(np.repeat(q, heads, 0)), lse1.repeat(heads, 1, 1), cache, torch.zeros((heads, 1, n + 5), device="cuda"))
+    assert torch.equal(w, w1.expand_as(w))
+    single, dst = target(cfg, 29000, 5, 0), target(c, 29000, 5, 0)
+    kvqp.evict(cfg, one, w1, 29000, single)
+    kvqp.evict(c, cache, w, 29000, dst)
+    for name in ("k_codes", "v_codes", "tail_k", "tail_v"):
+        a = dst.buffers[name].view(heads, -1)
+        b = single.buffers[name].view(1, -1)
+        if name.startswith("tail"):       # (the rest of the room for tail rows is left alone)
+            a, b = a[:, :5 * 256], b[:, :5 * 256]
+        assert torch.equal(a, b.expand_as(a)), name
+
+
+def test_a_cache_without_room_is_refused(orc):
+    rng = np.random.default_rng(44)
+    cfg, src, _, _ = make(orc, rng, 1, 2, 1, 300, 5, 4, 32, 1)
+    w = dev(np.ones((1, 2, 305), np.float32))
+    for n_layout, tail_cap in ((128, 5), (200, 4)):
+        dst = target(cfg, n_layout, tail_cap, 0)
+        dst.tail_cap = 5
+        with pytest.raises(ValueError, match="no room"):
+            kvqp.evict(cfg, src, w, 200, dst)
+    assert kvqp.evict(cfg, src, w, 200, target(cfg, 200, 5, 0)).n_kept == 200
