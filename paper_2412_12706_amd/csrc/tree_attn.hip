@@ -7,8 +7,9 @@
 //   lse[r] = log sum_t exp(l[r, t])      out[r] = sum_t exp(l[r, t] - lse[r]) V[t]
 //   weight[t] = sum_r exp(l[r, t] - lse[r])
 // K and V are code * scale + zero of the packed part, and plain rows of the tail and of the drafted
-// tokens.  The cache is read once per 64 rows; a row costs 512 multiply-adds per token, so up to
-// some 64 rows the call is bound by memory at 4 bits, beyond that by instruction issue.
+// tokens.  The cache is read once per 64 rows; a row costs 512 multiply-adds per token, and every
+// operand twice (see below).  32 layers of 8192 tokens at 4 bits (345 MB): 16 rows take 68.5 us, 5.0
+// TB/s, bound by memory; 32 rows 92 us and 64 rows 158 us, bound by instruction issue and power.
 //
 // Layout on gfx950.  A wave takes blocks of 32 tokens, for all rows of its workgroup (16, 32 or 64).
 // Both products run transposed, S^T[token, row] = K Q^T and O^T[channel, row] = V^T P^T, with
@@ -49,9 +50,9 @@ union Frag {  // one MFMA 16x16x32 f16 input operand of a lane: 8 halves
     uint4 q;
 };
 
-// The most waves of a workgroup, by its rows in tiles of 16: 16, 12 or 8, as many as the registers of a CU leave room for
-// (128, 168 and 256 per lane; codes of 16 bits want 168 for one tile, too).  A launch may use fewer.
-constexpr int most_waves(int bits, int rt) { return rt == 1 ? (bits == 16 ? 12 : 16) : rt == 2 ? 12 : 8; }
+// The most waves of a workgroup, by its rows in tiles of 16: as many as the registers of a CU leave room for (168 and 256 per lane).
+// A launch may use fewer.  (Sixteen for one tile, with 128 registers each: 73.4 us where twelve take 68.5, 32 layers of 8192 tokens, 16 rows.)
+constexpr int most_waves(int rt) { return rt <= 2 ? 12 : 8; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegBig = -1.0e30f;     // reference of a row that has seen nothing
@@ -86,8 +87,6 @@ __device__ __forceinline__ float rows4_add(float v) {
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-// (one instruction, without the two that quiet NaNs first)
-__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
@@ -491,39 +490,47 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
     }
 }
 // Moves references where logits have passed them, turns acc + bias (a block's logits before the rows' factors, -inf where unseen) into weights x
-// and adds them up.
+// and adds them up.  (The highest logit is looked for behind the multiplication: numbers out of the matrix unit would be quieted first, an
+// instruction each.)
 template <int RT>
 __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[RT][2], const float (&factor)[RT], const float (&bias)[RT], float (&x)[RT][8]) {
+    auto logits = [&](int rt) {
+        const float add = __builtin_fmaf(bias[rt], factor[rt], -st.ref[rt]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[rt][j] = __builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], add);
+    };
+    auto highest = [](const float (&v)[8]) {
+        return fmaxf(fmaxf(fmaxf(fmaxf(v[0], v[1]), v[2]), fmaxf(fmaxf(v[3], v[4]), v[5])), fmaxf(v[6], v[7]));
+    };
     bool past = false;
-    float top[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const f4v &p = acc[rt][0], &q = acc[rt][1];
-        top[rt] = max3(max3(max3(p[0], p[1], p[2]), p[3], q[0]), max3(q[1], q[2], q[3]), q[3]) + bias[rt];
-        top[rt] *= factor[rt];
-        past |= top[rt] > st.ref[rt] + kSlack;
+        logits(rt);
+        past |= highest(x[rt]) > kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const float t = rows4_max(top[rt]);          // (all four lanes of a row decide alike)
+            float l[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) l[j] = (acc[rt][j >> 2][j & 3] + bias[rt]) * factor[rt];
+            const float t = rows4_max(highest(l));          // (all four lanes of a row decide alike)
             const float ref = t > st.ref[rt] + kSlack ? t - kBoost : st.ref[rt];
             const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref);
             st.ref[rt] = ref;
             st.sum[rt] *= f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) st.o[rt][c] *= f;
+            logits(rt);
         }
     }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const float add = __builtin_fmaf(bias[rt], factor[rt], -st.ref[rt]);
+    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], add));
+            x[rt][j] = __builtin_amdgcn_exp2f(x[rt][j]);
             st.sum[rt] += x[rt][j];
         }
-    }
 }
 // Weights as operands: pair i holds tokens 4 kb + i and 16 + 4 kb + i; hi + lo parts, cut toward zero.
 struct WeightOperand { Frag hi, lo; };
@@ -593,9 +600,9 @@ struct __align__(16) PlainTile { uint16_t v[32 * kPlainStride]; };
 template <int RT> union WaveScratch { struct { ScaleStrip strip; float bias[kBiasBlocks * 16 * RT]; } packed; PlainTile tile; };
 constexpr int kMostSplits = 64;
 constexpr int join_tiles(int rt) { return rt == 4 ? 2 : 1; }
-template <int BITS, int RT> union __align__(16) TreeShared {
-    struct { QueryTiles<RT> sq; WaveScratch<RT> wave[most_waves(BITS, RT)]; } run;
-    struct { f4v o[most_waves(BITS, RT)][join_tiles(RT) * 8][64]; float ref[most_waves(BITS, RT)][16 * RT], sum[most_waves(BITS, RT)][16 * RT]; } join;
+template <int RT> union __align__(16) TreeShared {
+    struct { QueryTiles<RT> sq; WaveScratch<RT> wave[most_waves(RT)]; } run;
+    struct { f4v o[most_waves(RT)][join_tiles(RT) * 8][64]; float ref[most_waves(RT)][16 * RT], sum[most_waves(RT)][16 * RT]; } join;
     struct { float weight[kMostSplits][16 * RT], sum[kMostSplits][16 * RT], inverse[16 * RT]; } last;       // of a row block's splits
 };
 // One row block's partial results in the workspace, written and read with accesses at device scope (sc1): workgroups of one row block
@@ -639,8 +646,8 @@ __device__ __forceinline__ float inverse_sum(float sum) { return sum > 0.0f ? 1.
 __device__ __forceinline__ float log_sum(float ref, float sum) { return sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2; }
 
 template <int BITS, int AXIS, int RT, bool ONCE>
-__global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4) void tree_attn(const TreeArgs a) {
-    __shared__ TreeShared<BITS, RT> sh;
+__global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_attn(const TreeArgs a) {
+    __shared__ TreeShared<RT> sh;
     __shared__ int s_last;
     QueryTiles<RT>& sq = sh.run.sq;
 
@@ -865,15 +872,15 @@ __global__ __launch_bounds__(64 * most_waves(BITS, RT), most_waves(BITS, RT) / 4
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         // (all of them requested at once; a wave that is not there repeats the first, at weight 0)
-        float r[most_waves(BITS, RT)], s[most_waves(BITS, RT)];
+        float r[most_waves(RT)], s[most_waves(RT)];
 #pragma unroll
-        for (int w = 0; w < most_waves(BITS, RT); ++w) { r[w] = sh.join.ref[w < waves ? w : 0][16 * rt + n]; s[w] = sh.join.sum[w < waves ? w : 0][16 * rt + n]; }
+        for (int w = 0; w < most_waves(RT); ++w) { r[w] = sh.join.ref[w < waves ? w : 0][16 * rt + n]; s[w] = sh.join.sum[w < waves ? w : 0][16 * rt + n]; }
         ref[rt] = r[0];
 #pragma unroll
-        for (int w = 1; w < most_waves(BITS, RT); ++w) ref[rt] = fmaxf(ref[rt], r[w]);
+        for (int w = 1; w < most_waves(RT); ++w) ref[rt] = fmaxf(ref[rt], r[w]);
         sum[rt] = 0.f;
 #pragma unroll
-        for (int w = 0; w < most_waves(BITS, RT); ++w) sum[rt] = __builtin_fmaf(w < waves ? s[w] : 0.f, __builtin_amdgcn_exp2f(r[w] - ref[rt]), sum[rt]);
+        for (int w = 0; w < most_waves(RT); ++w) sum[rt] = __builtin_fmaf(w < waves ? s[w] : 0.f, __builtin_amdgcn_exp2f(r[w] - ref[rt]), sum[rt]);
         const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref[rt]);
 #pragma unroll
         for (int t = 0; t < 8; ++t) st.o[rt][t] *= f;
@@ -1234,7 +1241,7 @@ TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len) {
     // every CU, but sixteen splits are enough until each has 32 blocks (joining them takes longer than what the others save).
     p.most_splits = (int)std::max(1LL, std::min(256 / base, (long long)kMostSplits));
     p.n_splits = units <= 20 ? 1 : std::max(1, std::min({p.most_splits, (units + 4) / 8, std::max(16, units / 32)}));
-    p.n_waves = units <= 4 ? 4 : std::min(base >= 128 && p.n_splits == 1 ? 12 : 8, most_waves(cfg.bits, p.row_tiles));
+    p.n_waves = units <= 4 ? 4 : std::min(base >= 128 && p.n_splits == 1 ? 12 : 8, most_waves(p.row_tiles));
     const size_t one = (size_t)base * (16 * p.row_tiles) * (kHeadDim + 2) * sizeof(float);
     p.ws_bytes = p.n_splits > 1 ? kTreeCounterBytes + one * p.n_splits : 0;
     p.ws_bound = p.most_splits > 1 ? kTreeCounterBytes + one * p.most_splits : 0;
