@@ -51,7 +51,8 @@ union Frag {  // one MFMA 16x16x32 f16 input operand of a lane: 8 halves
 };
 
 // The most waves of a workgroup, by its rows in tiles of 16: as many as the registers of a CU leave room for (168 and 256 per lane).
-// A launch may use fewer.  (Sixteen for one tile, with 128 registers each: 73.4 us where twelve take 68.5, 32 layers of 8192 tokens, 16 rows.)
+// A launch may use fewer.  (Sixteen for one tile, with 128 registers each: 73.4 us where twelve
+// take 68.5, 32 layers of 8192 tokens, 16 rows.)
 constexpr int most_waves(int rt) { return rt <= 2 ? 12 : 8; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -490,47 +491,40 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
     }
 }
 // Moves references where logits have passed them, turns acc + bias (a block's logits before the rows' factors, -inf where unseen) into weights x
-// and adds them up.  (The highest logit is looked for behind the multiplication: numbers out of the matrix unit would be quieted first, an
-// instruction each.)
+// and adds them up.
 template <int RT>
 __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[RT][2], const float (&factor)[RT], const float (&bias)[RT], float (&x)[RT][8]) {
-    auto logits = [&](int rt) {
-        const float add = __builtin_fmaf(bias[rt], factor[rt], -st.ref[rt]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[rt][j] = __builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], add);
-    };
-    auto highest = [](const float (&v)[8]) {
-        return fmaxf(fmaxf(fmaxf(fmaxf(v[0], v[1]), v[2]), fmaxf(fmaxf(v[3], v[4]), v[5])), fmaxf(v[6], v[7]));
-    };
     bool past = false;
+    float top[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        logits(rt);
-        past |= highest(x[rt]) > kSlack;
+        const f4v &p = acc[rt][0], &q = acc[rt][1];
+        // (behind the matrix unit: the compiler's own instructions, which it makes wait for the sums.  Quieting them costs nothing that is seen; the
+        // highest of the products below instead, kept beside the sums, takes registers: 48.2 -> 50.9 us for 256 rows over 16384 tokens.)
+        top[rt] = (fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]))) + bias[rt]) * factor[rt];
+        past |= top[rt] > st.ref[rt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            float l[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) l[j] = (acc[rt][j >> 2][j & 3] + bias[rt]) * factor[rt];
-            const float t = rows4_max(highest(l));          // (all four lanes of a row decide alike)
+            const float t = rows4_max(top[rt]);          // (all four lanes of a row decide alike)
             const float ref = t > st.ref[rt] + kSlack ? t - kBoost : st.ref[rt];
             const float f = __builtin_amdgcn_exp2f(st.ref[rt] - ref);
             st.ref[rt] = ref;
             st.sum[rt] *= f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) st.o[rt][c] *= f;
-            logits(rt);
         }
     }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < RT; ++rt) {
+        const float add = __builtin_fmaf(bias[rt], factor[rt], -st.ref[rt]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x[rt][j] = __builtin_amdgcn_exp2f(x[rt][j]);
+            x[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], add));
             st.sum[rt] += x[rt][j];
         }
+    }
 }
 // Weights as operands: pair i holds tokens 4 kb + i and 16 + 4 kb + i; hi + lo parts, cut toward zero.
 struct WeightOperand { Frag hi, lo; };
