@@ -9,7 +9,7 @@
 // K and V are code * scale + zero of the packed part, and plain rows of the tail and of the drafted
 // tokens.  The cache is read once per 64 rows; a row costs 512 multiply-adds per token, and every
 // operand twice (see below).  32 layers of 8192 tokens at 4 bits (345 MB): 16 rows take 68.5 us, 5.0
-// TB/s, bound by memory; 32 rows 92 us and 64 rows 158 us, bound by instruction issue and power.
+// TB/s, bound by memory; 32 rows 96 us and 64 rows 158 us, bound by instruction issue and power.
 //
 // Layout on gfx950.  A wave takes blocks of 32 tokens, for all rows of its workgroup (16, 32 or 64).
 // Both products run transposed, S^T[token, row] = K Q^T and O^T[channel, row] = V^T P^T, with
@@ -88,6 +88,9 @@ __device__ __forceinline__ float rows4_add(float v) {
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// The higher of two numbers out of the matrix unit, as the middle one of three: fmaxf would quiet both first, an instruction each, and an
+// instruction written in assembly would not wait for the matrix unit.
+__device__ __forceinline__ float higher(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, 3.4028235e38f); }
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
@@ -499,9 +502,7 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const f4v &p = acc[rt][0], &q = acc[rt][1];
-        // (behind the matrix unit: the compiler's own instructions, which it makes wait for the sums.  Quieting them costs nothing that is seen; the
-        // highest of the products below instead, kept beside the sums, takes registers: 48.2 -> 50.9 us for 256 rows over 16384 tokens.)
-        top[rt] = (fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]))) + bias[rt]) * factor[rt];
+        top[rt] = (higher(higher(higher(p[0], p[1]), higher(p[2], p[3])), higher(higher(q[0], q[1]), higher(q[2], q[3]))) + bias[rt]) * factor[rt];
         past |= top[rt] > st.ref[rt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(past) != 0ull) {
