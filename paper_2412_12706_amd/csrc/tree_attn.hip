@@ -29,8 +29,11 @@
 // Query rows are scaled by a power of two to a largest element of 64 .. 128, so that the lo parts do
 // not run into binary16's subnormals; products above 65504 would overflow (a scale of 512 and more, of 257
 // and more where 8-bit codes take it).
-// Weights enter the second product as hi + lo too; values as one binary16 number, code * s + z
-// rounded once, which is the accuracy of the value itself at 16 bits.
+// Weights enter the second product as hi + lo too, and values as half a code times s, hi + lo (half, so that a
+// group that spans all of binary16's range does not overflow; what is computed from plain rows is halved with it, the outputs doubled at the
+// end), while the zeros take a product of their own: its rows are the groups of channels.  (A value rounded to binary16, code * s + z, adds as
+// much error as the output's own rounding: 2.8e-4 where the formula rounded once has 2.1e-4.  The parts cost ten matrix instructions a block and
+// tile of rows: 32 layers of 8192 tokens, 32 rows: 99 -> 110 us; one layer of 16384 tokens, 256 rows: 49 -> 55.)
 #include <algorithm>
 #include <initializer_list>
 
@@ -119,41 +122,42 @@ template <int BITS> struct Fields {
 #pragma unroll
             for (uint32_t& m : mask) asm("" : "+v"(m));
     }
-    template <int SH> __device__ __forceinline__ static h2v whole(uint32_t w, uint32_t m) {
+    template <int SH, bool HALVED> __device__ __forceinline__ static h2v whole(uint32_t w, uint32_t m) {
+        constexpr float kUnit = (HALVED ? 0.5f : 1.0f) / (1 << SH);
         const h2v x = as_h2((w & m) | 0x64006400u);
-        if constexpr (SH == 0) return x - splat(1024.0f);
-        else return __builtin_elementwise_fma(x, splat(1.0f / (1 << SH)), splat(-1024.0f / (1 << SH)));
+        if constexpr (kUnit == 1.0f) return x - splat(1024.0f);
+        else return __builtin_elementwise_fma(x, splat(kUnit), splat(-1024.0f * kUnit));
     }
-    // eight codes of one (4 bits, 2 bits: half of one) or two words
-    __device__ __forceinline__ void eight(uint32_t a, uint32_t b, h2v* c) const {
+    // eight codes (or their halves) of one (4 bits, 2 bits: half of one) or two words
+    template <bool HALVED> __device__ __forceinline__ void eight(uint32_t a, uint32_t b, h2v* c) const {
         if constexpr (BITS == 8) {
-            c[0] = whole<0>(a, mask[0]); c[1] = whole<0>(a >> 8, mask[0]);
-            c[2] = whole<0>(b, mask[0]); c[3] = whole<0>(b >> 8, mask[0]);
+            c[0] = whole<0, HALVED>(a, mask[0]); c[1] = whole<0, HALVED>(a >> 8, mask[0]);
+            c[2] = whole<0, HALVED>(b, mask[0]); c[3] = whole<0, HALVED>(b >> 8, mask[0]);
         } else if constexpr (BITS == 4) {
-            c[0] = whole<0>(a, mask[0]); c[1] = whole<4>(a, mask[1]);
-            c[2] = whole<0>(a >> 8, mask[0]); c[3] = whole<4>(a >> 8, mask[1]);
+            c[0] = whole<0, HALVED>(a, mask[0]); c[1] = whole<4, HALVED>(a, mask[1]);
+            c[2] = whole<0, HALVED>(a >> 8, mask[0]); c[3] = whole<4, HALVED>(a >> 8, mask[1]);
         } else if constexpr (BITS == 2) {
-            c[0] = whole<0>(a, mask[0]); c[1] = whole<2>(a, mask[1]); c[2] = whole<4>(a, mask[2]); c[3] = whole<6>(a, mask[3]);
+            c[0] = whole<0, HALVED>(a, mask[0]); c[1] = whole<2, HALVED>(a, mask[1]); c[2] = whole<4, HALVED>(a, mask[2]); c[3] = whole<6, HALVED>(a, mask[3]);
         }
     }
 };
 // Eight consecutive channels of a key row (step s of a lane's 32 channels): c[r] is the pair 8 s + 2 r, + 1.
 template <int BITS>
 __device__ __forceinline__ void key_whole(const Fields<BITS>& f, const uint32_t (&w)[BITS], int s, h2v* c) {
-    if constexpr (BITS == 8) f.eight(w[2 * s], w[2 * s + 1], c);
-    else if constexpr (BITS == 4) f.eight(w[s], 0u, c);
-    else if constexpr (BITS == 2) f.eight((s & 1) ? w[s >> 1] >> 8 : w[s >> 1], 0u, c);
+    if constexpr (BITS == 8) f.template eight<false>(w[2 * s], w[2 * s + 1], c);
+    else if constexpr (BITS == 4) f.template eight<false>(w[s], 0u, c);
+    else if constexpr (BITS == 2) f.template eight<false>((s & 1) ? w[s >> 1] >> 8 : w[s >> 1], 0u, c);
 }
-// Value codes of a 32-token block, channel tile `tile`: pair i holds tokens 4 kb + i and 16 + 4 kb + i of channel 16 tile + n.
+// Halves of the value codes of a 32-token block, channel tile `tile`: pair i holds tokens 4 kb + i and 16 + 4 kb + i of channel 16 tile + n.
 template <int BITS> struct VGeom {
     static constexpr int kWpt = v_words_per_tile(BITS);
     static constexpr int kWords = 8 * kWpt;            // a lane's words of a superblock
 };
 template <int BITS>
-__device__ __forceinline__ void value_whole(const Fields<BITS>& f, const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v* c) {
-    if constexpr (BITS == 8) f.eight(w[2 * tile], w[2 * tile + 1], c);
-    else if constexpr (BITS == 4) f.eight(w[tile], 0u, c);
-    else if constexpr (BITS == 2) f.eight(w[tile] >> (8 * odd), 0u, c);
+__device__ __forceinline__ void value_halves(const Fields<BITS>& f, const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v* c) {
+    if constexpr (BITS == 8) f.template eight<true>(w[2 * tile], w[2 * tile + 1], c);
+    else if constexpr (BITS == 4) f.template eight<true>(w[tile], 0u, c);
+    else if constexpr (BITS == 2) f.template eight<true>(w[tile] >> (8 * odd), 0u, c);
 }
 
 }  // namespace
@@ -481,7 +485,8 @@ __device__ __forceinline__ void strip_keys(const KeyWords<BITS, AXIS>& k, ScaleS
 
 // ---- state of a wave's rows ----
 template <int RT> struct RowState {
-    f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n
+    f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n (below 16 bits: its half)
+    f4v z[RT];             // below 16 bits: the packed tokens' zeros' share, channels 32 i .. + 31 of row 16 rt + n, the same in the four lanes
     float ref[RT], sum[RT];
 };
 template <int RT>
@@ -491,6 +496,7 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
         st.ref[rt] = kNegBig; st.sum[rt] = 0.f;
 #pragma unroll
         for (int t = 0; t < 8; ++t) st.o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
+        st.z[rt] = f4v{0.f, 0.f, 0.f, 0.f};
     }
 }
 // Moves references where logits have passed them, turns acc + bias (a block's logits before the rows' factors, -inf where unseen) into weights x
@@ -515,6 +521,7 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
             st.sum[rt] *= f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) st.o[rt][c] *= f;
+            st.z[rt] *= f;
         }
     }
 #pragma unroll
@@ -645,6 +652,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     __shared__ TreeShared<RT> sh;
     __shared__ int s_last;
     QueryTiles<RT>& sq = sh.run.sq;
+    constexpr float kPart = BITS != 16 ? 0.5f : 1.0f;      // what of an output RowState::o holds
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -718,7 +726,13 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
                 if constexpr (BITS != 16) strip_values<BITS>(a, vw, strip, lane);
-                Frag s, z;
+                if constexpr (BITS != 16) {      // (lane n has the zeros of the group that channel 32 (n % 4) is in)
+                    Frag z;
+                    z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * ((32 * (n & 3)) >> a.group_log2) + 4 * kb]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) st.z[rt] = mfma(z, p[rt].lo, mfma(z, p[rt].hi, st.z[rt]));
+                }
+                Frag s;
 #pragma unroll
                 for (int tile = 0; tile < 8; ++tile) {
                     Frag v;
@@ -726,21 +740,31 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v.u[i] = vw.w[4 * tile + i];
                     } else {
+                        Frag lo;
                         h2v c[4];
-                        value_whole<BITS>(fields, vw.w, tile, blk & 1, c);
+                        value_halves<BITS>(fields, vw.w, tile, blk & 1, c);
                         if ((tile & 1) == 0) {       // (a group has at least two tiles)
                             const int g = (16 * tile) >> a.group_log2;
                             s.q = *reinterpret_cast<const uint4*>(&strip.v_scale[16 * g + 4 * kb]);
-                            z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * g + 4 * kb]);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v.h[i] = __builtin_elementwise_fma(c[i], s.h[i], z.h[i]);
+                        for (int i = 0; i < 4; ++i) {
+                            v.h[i] = c[i] * s.h[i];
+                            lo.h[i] = __builtin_elementwise_fma(c[i], s.h[i], -v.h[i]);
+                        }
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) st.o[rt][tile] = mfma(lo, p[rt].hi, st.o[rt][tile]);
                     }
                     value_product<RT>(st, v, tile, p);
                     if (tile & 1) end_step<RT>();
                 }
                 load_values<BITS, ONCE>(base, a.group_log2, next, lane, vw);
             }
+            if constexpr (BITS != 16)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int tile = 0; tile < 8; ++tile) st.o[rt][tile] += kPart * st.z[rt][tile >> 1];
         }
     }
 
@@ -804,7 +828,11 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
             softmax_step<RT>(st, acc, factor, none, x);
             WeightOperand p[RT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
+            for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[rt][j] *= kPart;
+                weight_operand(x[rt], minus, p[rt]);
+            }
             if (drafted && __builtin_amdgcn_ballot_w64(odd_value) != 0ull) {
                 // Values that are not finite reach only the rows that see them (a weight of 0 would make them NaN in the matrix product):
                 // they are added here, one token at a time, and taken out of the tile.
@@ -914,7 +942,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
 #pragma unroll
                 for (int rt = 1; rt < JOIN; ++rt) total = (slot >> 3) == rt ? sum[j0 + rt] : total;
                 const int r = row0 + 16 * (j0 + (slot >> 3)) + n;
-                if (r < a.rows) *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * t + 4 * kb) = halves_of(o, inverse_sum(total));
+                if (r < a.rows) *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * t + 4 * kb) = halves_of(o, inverse_sum(total) / kPart);
             }
         }
     }
@@ -967,7 +995,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                     top = higher;
                 }
                 if (r < a.rows) {
-                    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * ((item >> 6) & 7) + 4 * kb) = halves_of(o, inverse_sum(total));
+                    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * ((item >> 6) & 7) + 4 * kb) = halves_of(o, inverse_sum(total) / kPart);
                     if (a.lse && (item & 0x1C0) == 0 && kb == 0) a.lse[(size_t)bh * a.rows + r] = log_sum(top, total);
                 }
             }
@@ -1015,7 +1043,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                                 sh.last.weight[s1 + u][threadIdx.x] = g[u];
                             }
                         }
-                        sh.last.inverse[threadIdx.x] = inverse_sum(total);
+                        sh.last.inverse[threadIdx.x] = inverse_sum(total) / kPart;
                         const int r = row0 + threadIdx.x;
                         if (a.lse && r < a.rows) a.lse[(size_t)bh * a.rows + r] = log_sum(top, total);
                     }
