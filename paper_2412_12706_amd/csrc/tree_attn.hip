@@ -1108,17 +1108,12 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
 #pragma unroll 1
     for (int row0 = 0; row0 < a.rows; row0 += RT * 16) {
         if (row0) __syncthreads();
-        QueryPieces<RT> pieces = request_queries<RT>(a, bh, row0);
-#pragma unroll
-        for (int j = 0; j < RT; ++j) {        // (a row that sees nothing may hold anything)
-            const int r = row0 + (threadIdx.x >> 4) + j * (kWeightThreads >> 4);
-            if (r < a.rows && a.lse[(size_t)bh * a.rows + r] == -INFINITY) pieces.w[j] = make_uint4(0u, 0u, 0u, 0u);
-        }
+        const QueryPieces<RT> pieces = request_queries<RT>(a, bh, row0);
         stage_queries<RT>(pieces, sq);
         if (threadIdx.x < RT * 16) {
             const int r = row0 + threadIdx.x;
             const float l = r < a.rows ? a.lse[(size_t)bh * a.rows + r] : -INFINITY;
-            s_lse[threadIdx.x] = l == -INFINITY ? -INFINITY : -l;        // (a row that sees nothing gives nothing)
+            s_lse[threadIdx.x] = l == -INFINITY ? -INFINITY : -l;
         }
         __syncthreads();
         const float decay = row0 ? 1.0f : a.decay;
@@ -1126,6 +1121,9 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
         float factor[RT], minus_lse[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) { factor[rt] = sq.factor[16 * rt + n] * a.sm_scale; minus_lse[rt] = s_lse[16 * rt + n]; }
+        // A row that saw nothing, and one past the last, gives nothing whatever it and the keys hold: its lane does not take part.  (A row of zeros
+        // times an infinite key is NaN, and no addend makes that 0.)
+        auto gives = [&](int rt) { return minus_lse[rt] != -INFINITY; };
         auto weight = [&](float logit, int rt, float add) { return __builtin_amdgcn_exp2f(__builtin_fmaf(logit, factor[rt], add) * kLog2e); };
         // lane n < 8 of a row of lanes stores token 16 (n / 4) + 4 kb + n % 4
         auto store = [&](const float (&cs)[8], float* w, int t0, int len) {
@@ -1157,13 +1155,12 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
                 strip_keys<BITS, AXIS>(kw, strip, lane);
                 key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
                 load_keys<BITS, AXIS, ONCE>(base, a.group_log2, min(blk + kWeightWaves, end - 1), lane, kw);
-                float cs[8];
+                float cs[8] = {};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    cs[j] = weight(acc[0][j >> 2][j & 3], 0, add[0]);
+                for (int rt = 0; rt < RT; ++rt)
+                    if (gives(rt))
 #pragma unroll
-                    for (int rt = 1; rt < RT; ++rt) cs[j] += weight(acc[rt][j >> 2][j & 3], rt, add[rt]);
-                }
+                        for (int j = 0; j < 8; ++j) cs[j] += weight(acc[rt][j >> 2][j & 3], rt, add[rt]);
                 store(cs, weights, 32 * blk, n_tok);
             }
         }
@@ -1185,7 +1182,8 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
             float cs[8] = {};
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const int last = a.tail_len - a.n_new + (row0 + 16 * rt + n) % a.n_new - t0 - 4 * kb;      // the last row of the tail that the query row sees
+                // the last row of the tail that the query row sees
+                const int last = gives(rt) ? a.tail_len - a.n_new + (row0 + 16 * rt + n) % a.n_new - t0 - 4 * kb : -1;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) cs[j] += 16 * (j >> 2) + (j & 3) <= last ? weight(acc[rt][j >> 2][j & 3], rt, minus_lse[rt]) : 0.0f;
             }
