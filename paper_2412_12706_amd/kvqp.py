@@ -6,6 +6,7 @@ if the library is missing, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import struct as _struct
@@ -266,6 +267,26 @@ def _entry(name):
     return _fn[name]
 
 
+def _memory_of(stream):
+    """What is allocated in this context is the stream's: memory that is free on the current one may still have work pending there."""
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
+def _empty_output(like, stream):
+    """Memory for a call's output; with a stream of its own it is that stream's, and kept until the current one, too, is done with it."""
+    import torch
+    if stream is None:
+        return torch.empty_like(like)
+    with _memory_of(stream):
+        out = torch.empty_like(like)
+    if out.is_cuda:
+        out.record_stream(torch.cuda.current_stream(out.device))
+    return out
+
+
 def alloc_workspace(nbytes: int, device="cuda"):
     import torch
     return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
@@ -407,8 +428,8 @@ def _same_device(name, device, *tensors):
             raise ValueError(f"{name}: a buffer on {t.device} and tensors on GPU {device}")
 
 
-def _call(name, device, stream, temporary, args):
-    """Calls an entry point with that GPU as the current one; a buffer that the call made itself stays the stream's until the work is done."""
+def _call(name, device, stream, args):
+    """Calls an entry point with that GPU as the current one."""
     import torch
     if _lib is None:
         lib()
@@ -419,8 +440,6 @@ def _call(name, device, stream, temporary, args):
         rc = _fn_rows[name](*args, _stream_handle(stream))
     if rc:
         raise KvqpError(rc, name)
-    if temporary is not None and stream is not None:
-        temporary.record_stream(stream)
 
 
 def _sized(entry, cfg: Cfg, n: int) -> int:
@@ -446,9 +465,11 @@ def tree_workspace_init(workspace, stream=None):
 
 
 def alloc_tree_workspace(cfg: Cfg, n_rows: int, device="cuda", stream=None):
-    """A workspace for tree_attn calls of n_rows rows on caches of any token count, prepared for its first use."""
+    """A workspace for tree_attn calls of n_rows rows on caches of any token count, prepared for its first use; with a stream it is for calls
+    on that one."""
     nbytes = tree_workspace_bytes(cfg, n_rows)
-    workspace = alloc_workspace(nbytes, device)
+    with _memory_of(stream):
+        workspace = alloc_workspace(nbytes, device)
     return tree_workspace_init(workspace, stream) if nbytes else workspace
 
 
@@ -502,14 +523,13 @@ def tree_attn(cfg: Cfg, q, k_new, v_new, mask, cache: Cache, out=None, lse=None,
     if lse is not None:
         _want("lse", lse, torch.float32, (b, cfg.n_q_heads, n), device)
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty_output(q, stream)
     else:
         _want("out", out, half, q.shape, device)
-    made = None
     if workspace is None:
-        workspace = made = alloc_tree_workspace(cfg, n, q.device, stream)
+        workspace = alloc_tree_workspace(cfg, n, q.device, stream)
     _same_device("tree_attn", device, workspace, cache.buffers["k_codes"])
-    _call("kvqp_tree_attn", device, stream, made,
+    _call("kvqp_tree_attn", device, stream,
           (cfg._bytes(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _addr(mask), per_batch, n, cache._bytes(), out.data_ptr(), _addr(lse),
            workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     return out
@@ -525,7 +545,7 @@ def accumulate_weights(cfg: Cfg, q, lse, cache: Cache, weights, decay: float = 1
     _want("lse", lse, torch.float32, (b, cfg.n_q_heads, n), device)
     _want("weights", weights, torch.float32, (b, cfg.n_kv_heads, cap), device)
     _same_device("accumulate_weights", device, cache.buffers["k_codes"])
-    _call("kvqp_accumulate_weights", device, stream, None,
+    _call("kvqp_accumulate_weights", device, stream,
           (cfg._bytes(), q.data_ptr(), lse.data_ptr(), n, cache._bytes(), weights.data_ptr(), cap, decay))
     return weights
 
@@ -549,12 +569,12 @@ def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=
     rows = dst.n_cap or (kept + 31) // 32 * 32
     if dst.buffers["k_codes"].nbytes < heads[0] * heads[1] * rows * 16 * cfg.bits or dst.buffers["tail_k"].nbytes < heads[0] * heads[1] * dst.tail_cap * 256:
         raise ValueError(f"evict: dst has no room for {rows} packed tokens and {dst.tail_cap} tail rows per head")
-    made = None
     if workspace is None:
-        workspace = made = alloc_evict_workspace(cfg, cache, weights.device)
+        with _memory_of(stream):
+            workspace = alloc_evict_workspace(cfg, cache, weights.device)
     _same_device("evict", device, workspace, cache.buffers["k_codes"], dst.buffers["k_codes"])
     cs = dst.struct()
-    _call("kvqp_evict", device, stream, made,
+    _call("kvqp_evict", device, stream,
           (cfg._bytes(), cache._bytes(), weights.data_ptr(), cap, n_keep, unit, C.byref(cs), _addr(weights_out), cap_out, _addr(idx_out),
            workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     dst.n_kept, dst.tail_len = cs.n_kept, cs.tail_len
