@@ -301,15 +301,18 @@ def decode_workspace_init(cfg: Cfg, workspace, stream=None):
 
 
 def alloc_decode_workspace(cfg: Cfg, device="cuda", stream=None):
-    """A decode workspace of kvqp_workspace_bytes' size, prepared for its first use."""
-    return decode_workspace_init(cfg, alloc_workspace(workspace_bytes(cfg)[1], device), stream)
+    """A decode workspace of kvqp_workspace_bytes' size, prepared for its first use; with a stream it is for calls on that one."""
+    with _memory_of(stream):
+        workspace = alloc_workspace(workspace_bytes(cfg)[1], device)
+    return decode_workspace_init(cfg, workspace, stream)
 
 
 def compress(cfg: Cfg, q_obs, k, v, cache: Cache, idx_out=None, workspace=None, stream=None, unrefined_out=None):
     """kvqp_compress: q_obs [B,Hq,W,D], k/v [B,Hkv,L,D] half tensors on the device;
     unrefined_out: int32 device tensor [B*Hkv] or None."""
     if workspace is None:
-        workspace = alloc_workspace(workspace_bytes(cfg)[0], k.device)
+        with _memory_of(stream):
+            workspace = alloc_workspace(workspace_bytes(cfg)[0], k.device)
     cs = cache.struct()
     rc = _entry("kvqp_compress")(cfg._bytes(), _addr(q_obs), _addr(k), _addr(v), C.byref(cs), _addr(idx_out),
                                  _addr(unrefined_out), workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
@@ -323,7 +326,8 @@ def compress_ragged(cfg: Cfg, q_obs, k, v, head_budget, cache: Cache, idx_out=No
                     unrefined_out=None):
     """kvqp_compress_ragged: head_budget is a host sequence of batch * Hkv token counts."""
     if workspace is None:
-        workspace = alloc_workspace(workspace_bytes(cfg)[0], k.device)
+        with _memory_of(stream):
+            workspace = alloc_workspace(workspace_bytes(cfg)[0], k.device)
     n = cfg.batch * cfg.n_kv_heads
     if len(head_budget) != n:
         raise ValueError(f"head_budget needs {n} entries")
@@ -394,8 +398,7 @@ def append_tail_ragged(cfg: Cfg, cache: Cache, n_tokens: int, head_count, stream
 def decode_attn(cfg: Cfg, q, cache: Cache, out=None, workspace=None, stream=None):
     """kvqp_decode_attn: q [B,Hq,D] half -> out [B,Hq,D] half."""
     if out is None:
-        import torch
-        out = torch.empty_like(q)
+        out = _empty_output(q, stream)
     if workspace is None:
         workspace = alloc_decode_workspace(cfg, q.device, stream)
     rc = _entry("kvqp_decode_attn")(cfg._bytes(), _addr(q), cache._bytes(), out.data_ptr(), workspace.data_ptr(),

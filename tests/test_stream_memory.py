@@ -84,3 +84,29 @@ def test_memory_just_freed_on_the_current_stream_is_not_taken(orc, monkeypatch):
     places = [out.data_ptr(), taken[0][10], taken[1][10]]
     assert not any(a <= p < b for p in places for a, b in spans)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("name", ["compress", "compress_ragged", "decode_attn", "alloc_decode_workspace"])
+def test_compress_and_decode_on_another_stream_take_that_streams_memory(monkeypatch, name):
+    monkeypatch.setattr(kvqp, "decode_workspace_init", lambda cfg, workspace, stream=None: workspace)
+    monkeypatch.setattr(kvqp, "_entry", lambda entry: lambda *a: 0)
+    kvqp.lib()
+    monkeypatch.setattr(kvqp, "_stream_handle", lambda stream: 0)
+    cfg = kvqp.Cfg(batch=1, n_q_heads=8, n_kv_heads=2, seq_len=288, window=32, budget=256)
+    cache = kvqp.alloc_cache(cfg, device="cpu", ragged=name == "compress_ragged")
+    q, k = torch.zeros((1, 8, 32, D), dtype=torch.float16), torch.zeros((1, 2, 288, D), dtype=torch.float16)
+    # (compress_ragged calls the library itself: without a workspace's address it launches nothing)
+    monkeypatch.setattr(kvqp, "_ptr", lambda t: None)
+    call = {"compress": lambda s: kvqp.compress(cfg, q, k, k, cache, stream=s),
+            "compress_ragged": lambda s: kvqp.compress_ragged(cfg, q, k, k, [256, 100], cache, stream=s),
+            "decode_attn": lambda s: kvqp.decode_attn(cfg, q[:, :, 0], cache, stream=s),
+            "alloc_decode_workspace": lambda s: kvqp.alloc_decode_workspace(cfg, "cpu", s)}[name]
+    recorder = Recorder(monkeypatch)
+    for stream, where in ((None, "current"), (types.SimpleNamespace(cuda_stream=0x9009), 0x9009)):
+        recorder.seen.clear()
+        if name == "compress_ragged":
+            with pytest.raises(kvqp.KvqpError):
+                call(stream)
+        else:
+            call(stream)
+        assert recorder.seen and set(recorder.seen) == {where}
