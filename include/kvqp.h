@@ -438,8 +438,8 @@ int kvqp_append_tail_ragged(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_to
 /* The most query rows per query head of kvqp_tree_attn and kvqp_accumulate_weights. */
 #define KVQP_MOST_ROWS 256
 
-/* Workspace bytes of kvqp_tree_attn for n_rows drafted tokens and a cache of any token count
- * (0: none is needed, and NULL is taken).  Host only. */
+/* Workspace bytes that every call of kvqp_tree_attn with at most n_rows drafted tokens is content with, whatever the
+ * cache's token count (0: none is needed, and NULL is taken).  Host only. */
 int kvqp_tree_workspace_bytes(const kvqp_cfg *cfg, int32_t n_rows, size_t *bytes);
 
 /*

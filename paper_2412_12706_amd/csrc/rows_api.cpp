@@ -2,6 +2,8 @@
 // As everywhere, a call is checked on the host before anything is enqueued.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "kvqp_checks.h"
 
 using namespace kvqp;
@@ -36,7 +38,10 @@ int kvqp_tree_workspace_bytes(const kvqp_cfg* cfg, int32_t n_rows, size_t* bytes
     if (rc) return rc;
     if (!bytes || n_rows < 1) return KVQP_ERR_INVALID_ARG;
     if (n_rows > KVQP_MOST_ROWS) return KVQP_ERR_UNSUPPORTED;
+    // (not the most for the most rows: fewer row blocks get more splits.  What fills its row block needs as much as any with the same blocks.)
+    const int gq = cfg->n_q_heads / cfg->n_kv_heads;
     *bytes = plan_tree(*cfg, n_rows, 0, 0).ws_bound;
+    for (int rows = 16; rows < gq * n_rows; rows += rows < 64 ? rows : 64) *bytes = std::max(*bytes, plan_tree(*cfg, rows / gq, 0, 0).ws_bound);
     return KVQP_OK;
 }
 

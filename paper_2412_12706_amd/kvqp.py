@@ -468,7 +468,7 @@ def tree_workspace_init(workspace, stream=None):
 
 
 def alloc_tree_workspace(cfg: Cfg, n_rows: int, device="cuda", stream=None):
-    """A workspace for tree_attn calls of n_rows rows on caches of any token count, prepared for its first use; with a stream it is for calls
+    """A workspace for tree_attn calls of at most n_rows rows on caches of any token count, prepared for its first use; with a stream it is for calls
     on that one."""
     nbytes = tree_workspace_bytes(cfg, n_rows)
     with _memory_of(stream):
