@@ -431,6 +431,24 @@ def _same_device(name, device, *tensors):
             raise ValueError(f"{name}: a buffer on {t.device} and tensors on GPU {device}")
 
 
+def _check_room(what, cfg: Cfg, cache: Cache, rows: int, device):
+    """A cache that a call fills: its buffers hold so many packed tokens per head, and the tail rows that they state."""
+    import torch
+    heads, bits, group = cfg.batch * cfg.n_kv_heads, cfg.bits, max(cfg.group_size, 1)      # (what a cfg may not hold the library refuses)
+    block = 64 if bits == 2 else 32
+    per_token = 0 if bits == 16 else rows * (cfg.head_dim // group) * 2
+    key = per_token if bits == 16 or cfg.key_axis == KEY_PER_TOKEN else -(-rows // group) * cfg.head_dim * 2
+    tail = cache.tail_cap * cfg.head_dim * 2
+    need = (rows * 16 * bits, -(-rows // block) * block * 16 * bits, key, key, per_token, per_token, tail, tail)
+    for name, n in zip(_NAMES, need):
+        if cache.buffers[name].nbytes < heads * n:
+            raise ValueError(f"{what} has no room for {rows} packed tokens and {cache.tail_cap} tail rows per head: {name} holds "
+                             f"{cache.buffers[name].nbytes} bytes of {heads * n}")
+    counts = cache.head_n_kept
+    if counts is not None:
+        _want(f"{what}.head_n_kept", counts, torch.int32, counts.shape if counts.numel() == heads else (heads,), device)
+
+
 def _call(name, device, stream, args):
     """Calls an entry point with that GPU as the current one."""
     import torch
@@ -569,9 +587,7 @@ def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=
         kept = short + (n_keep - short) // unit * unit
     if idx_out is not None:
         _want("idx_out", idx_out, torch.int32, (*heads, kept), device)
-    rows = dst.n_cap or (kept + 31) // 32 * 32
-    if dst.buffers["k_codes"].nbytes < heads[0] * heads[1] * rows * 16 * cfg.bits or dst.buffers["tail_k"].nbytes < heads[0] * heads[1] * dst.tail_cap * 256:
-        raise ValueError(f"evict: dst has no room for {rows} packed tokens and {dst.tail_cap} tail rows per head")
+    _check_room("evict: dst", cfg, dst, dst.n_cap or (kept + 31) // 32 * 32, device)
     if workspace is None:
         with _memory_of(stream):
             workspace = alloc_evict_workspace(cfg, cache, weights.device)
