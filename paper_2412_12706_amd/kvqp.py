@@ -11,6 +11,7 @@ import ctypes as C
 import os
 import struct as _struct
 from dataclasses import dataclass, field
+from operator import lt as _less
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libkvqp.so")
@@ -433,19 +434,21 @@ def _same_device(name, device, *tensors):
 
 def _check_room(what, cfg: Cfg, cache: Cache, rows: int, device):
     """A cache that a call fills: its buffers hold so many packed tokens per head, and the tail rows that they state."""
-    import torch
-    heads, bits, group = cfg.batch * cfg.n_kv_heads, cfg.bits, max(cfg.group_size, 1)      # (what a cfg may not hold the library refuses)
+    b, heads, bits, group = cache.buffers, cfg.batch * cfg.n_kv_heads, cfg.bits, max(cfg.group_size, 1)      # (what a cfg may not hold the library refuses)
     block = 64 if bits == 2 else 32
-    per_token = 0 if bits == 16 else rows * (cfg.head_dim // group) * 2
-    key = per_token if bits == 16 or cfg.key_axis == KEY_PER_TOKEN else -(-rows // group) * cfg.head_dim * 2
-    tail = cache.tail_cap * cfg.head_dim * 2
-    need = (rows * 16 * bits, -(-rows // block) * block * 16 * bits, key, key, per_token, per_token, tail, tail)
-    for name, n in zip(_NAMES, need):
-        if cache.buffers[name].nbytes < heads * n:
-            raise ValueError(f"{what} has no room for {rows} packed tokens and {cache.tail_cap} tail rows per head: {name} holds "
-                             f"{cache.buffers[name].nbytes} bytes of {heads * n}")
+    codes = heads * 16 * bits
+    per_token = 0 if bits == 16 else heads * rows * (cfg.head_dim // group) * 2
+    key = per_token if bits == 16 or cfg.key_axis == KEY_PER_TOKEN else heads * -(-rows // group) * cfg.head_dim * 2
+    tail = heads * cache.tail_cap * cfg.head_dim * 2
+    need = (codes * rows, codes * block * -(-rows // block), key, key, per_token, per_token, tail, tail)
+    have = (b["k_codes"].nbytes, b["v_codes"].nbytes, b["k_scale"].nbytes, b["k_zero"].nbytes, b["v_scale"].nbytes, b["v_zero"].nbytes,
+            b["tail_k"].nbytes, b["tail_v"].nbytes)        # (written out: this runs on every call)
+    if any(map(_less, have, need)):
+        name, n, m = next(x for x in zip(_NAMES, have, need) if x[1] < x[2])
+        raise ValueError(f"{what} has no room for {rows} packed tokens and {cache.tail_cap} tail rows per head: {name} holds {n} bytes of {m}")
     counts = cache.head_n_kept
     if counts is not None:
+        import torch
         _want(f"{what}.head_n_kept", counts, torch.int32, counts.shape if counts.numel() == heads else (heads,), device)
 
 
