@@ -27,11 +27,9 @@
 //   keys per token: code * s split the same way times q, and z (its rows are constant over a group of
 //     channels) times the sums of q over 32 channels, again hi + lo.
 // Query rows are scaled by a power of two to a largest element of 64 .. 128, so that the lo parts do
-// not run into binary16's subnormals; products above 65504 would overflow (a scale of 512 and more, of 257
-// and more where 8-bit codes take it).
-// Weights enter the second product as hi + lo too, and values as half a code times s, hi + lo (half, so that a
-// group that spans all of binary16's range does not overflow; what is computed from plain rows is halved with it, the outputs doubled at the
-// end), while the zeros take a product of their own: its rows are the groups of channels.  (A value rounded to binary16, code * s + z, adds as
+// not run into binary16's subnormals.  Products that a large scale would take out of binary16's range are formed apart (wide_bits).
+// Weights enter the second product as hi + lo too, and values as code * s, hi + lo, while the zeros take a product of their own: its rows are
+// the groups of channels.  (A value rounded to binary16, code * s + z, adds as
 // much error as the output's own rounding: 2.8e-4 where the formula rounded once has 2.1e-4.  The parts cost ten matrix instructions a block and
 // tile of rows: 32 layers of 8192 tokens, 32 rows: 99 -> 110 us; one layer of 16384 tokens, 256 rows: 49 -> 55.)
 #include <algorithm>
@@ -122,42 +120,41 @@ template <int BITS> struct Fields {
 #pragma unroll
             for (uint32_t& m : mask) asm("" : "+v"(m));
     }
-    template <int SH, bool HALVED> __device__ __forceinline__ static h2v whole(uint32_t w, uint32_t m) {
-        constexpr float kUnit = (HALVED ? 0.5f : 1.0f) / (1 << SH);
+    template <int SH> __device__ __forceinline__ static h2v whole(uint32_t w, uint32_t m) {
         const h2v x = as_h2((w & m) | 0x64006400u);
-        if constexpr (kUnit == 1.0f) return x - splat(1024.0f);
-        else return __builtin_elementwise_fma(x, splat(kUnit), splat(-1024.0f * kUnit));
+        if constexpr (SH == 0) return x - splat(1024.0f);
+        else return __builtin_elementwise_fma(x, splat(1.0f / (1 << SH)), splat(-1024.0f / (1 << SH)));
     }
-    // eight codes (or their halves) of one (4 bits, 2 bits: half of one) or two words
-    template <bool HALVED> __device__ __forceinline__ void eight(uint32_t a, uint32_t b, h2v* c) const {
+    // eight codes of one (4 bits, 2 bits: half of one) or two words
+    __device__ __forceinline__ void eight(uint32_t a, uint32_t b, h2v* c) const {
         if constexpr (BITS == 8) {
-            c[0] = whole<0, HALVED>(a, mask[0]); c[1] = whole<0, HALVED>(a >> 8, mask[0]);
-            c[2] = whole<0, HALVED>(b, mask[0]); c[3] = whole<0, HALVED>(b >> 8, mask[0]);
+            c[0] = whole<0>(a, mask[0]); c[1] = whole<0>(a >> 8, mask[0]);
+            c[2] = whole<0>(b, mask[0]); c[3] = whole<0>(b >> 8, mask[0]);
         } else if constexpr (BITS == 4) {
-            c[0] = whole<0, HALVED>(a, mask[0]); c[1] = whole<4, HALVED>(a, mask[1]);
-            c[2] = whole<0, HALVED>(a >> 8, mask[0]); c[3] = whole<4, HALVED>(a >> 8, mask[1]);
+            c[0] = whole<0>(a, mask[0]); c[1] = whole<4>(a, mask[1]);
+            c[2] = whole<0>(a >> 8, mask[0]); c[3] = whole<4>(a >> 8, mask[1]);
         } else if constexpr (BITS == 2) {
-            c[0] = whole<0, HALVED>(a, mask[0]); c[1] = whole<2, HALVED>(a, mask[1]); c[2] = whole<4, HALVED>(a, mask[2]); c[3] = whole<6, HALVED>(a, mask[3]);
+            c[0] = whole<0>(a, mask[0]); c[1] = whole<2>(a, mask[1]); c[2] = whole<4>(a, mask[2]); c[3] = whole<6>(a, mask[3]);
         }
     }
 };
 // Eight consecutive channels of a key row (step s of a lane's 32 channels): c[r] is the pair 8 s + 2 r, + 1.
 template <int BITS>
 __device__ __forceinline__ void key_whole(const Fields<BITS>& f, const uint32_t (&w)[BITS], int s, h2v* c) {
-    if constexpr (BITS == 8) f.template eight<false>(w[2 * s], w[2 * s + 1], c);
-    else if constexpr (BITS == 4) f.template eight<false>(w[s], 0u, c);
-    else if constexpr (BITS == 2) f.template eight<false>((s & 1) ? w[s >> 1] >> 8 : w[s >> 1], 0u, c);
+    if constexpr (BITS == 8) f.eight(w[2 * s], w[2 * s + 1], c);
+    else if constexpr (BITS == 4) f.eight(w[s], 0u, c);
+    else if constexpr (BITS == 2) f.eight((s & 1) ? w[s >> 1] >> 8 : w[s >> 1], 0u, c);
 }
-// Halves of the value codes of a 32-token block, channel tile `tile`: pair i holds tokens 4 kb + i and 16 + 4 kb + i of channel 16 tile + n.
+// Value codes of a 32-token block, channel tile `tile`: pair i holds tokens 4 kb + i and 16 + 4 kb + i of channel 16 tile + n.
 template <int BITS> struct VGeom {
     static constexpr int kWpt = v_words_per_tile(BITS);
     static constexpr int kWords = 8 * kWpt;            // a lane's words of a superblock
 };
 template <int BITS>
-__device__ __forceinline__ void value_halves(const Fields<BITS>& f, const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v* c) {
-    if constexpr (BITS == 8) f.template eight<true>(w[2 * tile], w[2 * tile + 1], c);
-    else if constexpr (BITS == 4) f.template eight<true>(w[tile], 0u, c);
-    else if constexpr (BITS == 2) f.template eight<true>(w[tile] >> (8 * odd), 0u, c);
+__device__ __forceinline__ void value_whole(const Fields<BITS>& f, const uint32_t (&w)[VGeom<BITS>::kWords], int tile, int odd, h2v* c) {
+    if constexpr (BITS == 8) f.eight(w[2 * tile], w[2 * tile + 1], c);
+    else if constexpr (BITS == 4) f.eight(w[tile], 0u, c);
+    else if constexpr (BITS == 2) f.eight(w[tile] >> (8 * odd), 0u, c);
 }
 
 }  // namespace
@@ -376,19 +373,63 @@ __device__ __forceinline__ void refresh_bias(const HeadBase& h, int group_log2, 
     lds_order();
 }
 
+// Scales that would take a product out of binary16's range: 0x8000 in each half of two scales that is LIMIT (its bits) or more.  (They are not
+// negative: the sum's sign bit says it.)
+template <uint32_t LIMIT> __device__ __forceinline__ uint32_t wide_bits(uint32_t scales) { return (scales + (0x8000u - LIMIT) * 0x10001u) & 0x80008000u; }
+__device__ __forceinline__ bool any(bool mine) { return __builtin_amdgcn_ballot_w64(mine) != 0ull; }
+__device__ __forceinline__ uint32_t scaled(uint32_t two, float by) { return as_u32(as_h2(two) * splat(by)); }
+// Keys: 256 and more (255 codes, and 128 q's, times less stay below 65504).  They are left out of a block's product and get another one, kWide
+// taken from the scale and given to the other operand, so that the small ones beside them lose nothing.  (Almost no block has any; looking for
+// them, here and among the values, takes 2 % of a launch: 32 layers of 8192 tokens, 32 rows: 110 -> 113 us.)
+constexpr uint32_t kWideKey = 0x5C00u;
+constexpr float kWide = 256.0f;
+// Values: where the highest code times the scale would pass 65504; the block's scales and zeros are quartered then, and the weights four times as large.
+template <int BITS> constexpr uint32_t kWideValue = BITS == 2 ? 0x7400u : BITS == 4 ? 0x6C00u : 0x5C00u;       // 16384, 4096, 256
+
+// Makes a block's key scales ready for the product: the wide ones are taken out and returned, times 1 / kWide (the others' places: 0); keys
+// per channel: the rest goes to the strip, whence every lane reads its 32 channels.
+template <int BITS, int AXIS>
+__device__ __forceinline__ uint32_t ready_keys(KeyWords<BITS, AXIS>& k, ScaleStrip& strip, int lane, bool& wide) {
+    wide = false;
+    uint32_t out = 0u;
+    if constexpr (BITS != 16) {
+        constexpr bool kChannel = AXIS == KVQP_KEY_PER_CHANNEL;
+        uint32_t two = kChannel ? k.scale[0] : k.scale[0] | k.scale[1] << 16;
+        const uint32_t bits = wide_bits<kWideKey>(two);
+        wide = any(bits != 0u);
+        if (wide) {
+            const uint32_t mask = (bits >> 15) * 0xFFFFu;
+            out = scaled(two & mask, 1.0f / kWide);
+            two &= ~mask;
+            if constexpr (kChannel) k.scale[0] = two;
+            else { k.scale[0] = two & 0xFFFFu; k.scale[1] = two >> 16; }
+        }
+        if constexpr (kChannel) {
+            lds_order();
+            strip.k_scale[lane] = k.scale[0];
+            lds_order();
+        }
+    }
+    return out;
+}
 // Logits of a block for RT row tiles, before the rows' factors (and, keys per channel, without q . z): acc[rt][H][i] is token 16 H + 4 kb + i of row 16 rt + n.  The four
-// steps of eight channels run outermost, so that only one step's operands are held beside the sums.
-template <int BITS, int AXIS, int RT>
-__device__ __forceinline__ void key_product(const Fields<BITS>& fields, const KeyWords<BITS, AXIS>& k, const uint4* frag, const uint32_t* sums, ScaleStrip& strip, int lane, f4v (&acc)[RT][2]) {
+// steps of eight channels run outermost, so that only one step's operands are held beside the sums.  WIDE: those of scales taken by 1 / kWide, added to acc.
+template <int BITS, int AXIS, int RT, bool WIDE>
+__device__ __forceinline__ void key_products(const Fields<BITS>& fields, const KeyWords<BITS, AXIS>& k, const uint4* frag, const uint32_t* sums, ScaleStrip& strip, int lane, f4v (&acc)[RT][2]) {
     constexpr bool kChannel = BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL, kToken = BITS != 16 && AXIS == KVQP_KEY_PER_TOKEN;
+    constexpr bool kCodes = kChannel && RT <= 2;       // codes by themselves are an operand
     const int kb = lane >> 4;
     auto query = [&](int rt, int s) {
         Frag q;
         q.q = frag[(4 * rt + s) * 64 + lane];
+        if constexpr (WIDE && !kCodes)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) q.h[r] *= splat(kWide);
         return q;
     };
+    if constexpr (!WIDE)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
         end_step<RT>();
@@ -407,8 +448,13 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const Ke
             Frag sc;
             sc.q = *reinterpret_cast<const uint4*>(&strip.k_scale[16 * kb + 4 * s]);
 #pragma unroll
-            for (int H = 0; H < 2; ++H) key_whole<BITS>(fields, k.w[H], s, a[H].h);
-            if constexpr (RT <= 2) {
+            for (int H = 0; H < 2; ++H) {
+                key_whole<BITS>(fields, k.w[H], s, a[H].h);
+                if constexpr (WIDE && kCodes)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) a[H].h[r] *= splat(kWide);
+            }
+            if constexpr (kCodes) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const Frag q = query(rt, s);
@@ -461,7 +507,7 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const Ke
             }
         }
     }
-    if constexpr (kToken) {
+    if constexpr (kToken && !WIDE) {
         Frag z[2];
 #pragma unroll
         for (int H = 0; H < 2; ++H) { z[H].u[0] = k.zero[H] * 0x10001u; z[H].u[1] = z[H].u[2] = z[H].u[3] = 0u; }
@@ -473,20 +519,35 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, const Ke
         }
     }
 }
-// Keys per channel: the group's scales and zeros to the strip, whence every lane reads its 32 channels.
-template <int BITS, int AXIS>
-__device__ __forceinline__ void strip_keys(const KeyWords<BITS, AXIS>& k, ScaleStrip& strip, int lane) {
-    if constexpr (BITS != 16 && AXIS == KVQP_KEY_PER_CHANNEL) {
-        lds_order();
-        strip.k_scale[lane] = k.scale[0];
-        lds_order();
-    }
+
+// The same from a block's keys as they were loaded.
+template <int BITS, int AXIS, int RT>
+__device__ __forceinline__ void key_product(const Fields<BITS>& fields, KeyWords<BITS, AXIS>& k, const uint4* frag, const uint32_t* sums, ScaleStrip& strip, int lane, f4v (&acc)[RT][2]) {
+    bool wide;
+    const uint32_t wide_scales = ready_keys<BITS, AXIS>(k, strip, lane, wide);
+    key_products<BITS, AXIS, RT, false>(fields, k, frag, sums, strip, lane, acc);
+    if constexpr (BITS != 16)
+        if (wide) {
+            // (unseen, or the unpacked codes stay in registers from the first product on, and others spill)
+#pragma unroll
+            for (int H = 0; H < 2; ++H)
+#pragma unroll
+                for (uint32_t& w : k.w[H]) asm volatile("" : "+v"(w));
+            if constexpr (AXIS == KVQP_KEY_PER_CHANNEL) {
+                lds_order();
+                strip.k_scale[lane] = wide_scales;
+                lds_order();
+            } else {
+                k.scale[0] = wide_scales & 0xFFFFu; k.scale[1] = wide_scales >> 16;
+            }
+            key_products<BITS, AXIS, RT, true>(fields, k, frag, sums, strip, lane, acc);
+        }
 }
 
 // ---- state of a wave's rows ----
 template <int RT> struct RowState {
-    f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n (below 16 bits: its half)
-    f4v z[RT];             // below 16 bits: the packed tokens' zeros' share, channels 32 i .. + 31 of row 16 rt + n, the same in the four lanes
+    f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n
+    f4v z;                 // below 16 bits: the packed tokens' zeros' share, channels 32 i .. + 31 of row 16 kb + n (one tile: of row n, in all four lanes)
     float ref[RT], sum[RT];
 };
 template <int RT>
@@ -496,8 +557,8 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
         st.ref[rt] = kNegBig; st.sum[rt] = 0.f;
 #pragma unroll
         for (int t = 0; t < 8; ++t) st.o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
-        st.z[rt] = f4v{0.f, 0.f, 0.f, 0.f};
     }
+    st.z = f4v{0.f, 0.f, 0.f, 0.f};
 }
 // Moves references where logits have passed them, turns acc + bias (a block's logits before the rows' factors, -inf where unseen) into weights x
 // and adds them up.
@@ -521,7 +582,7 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
             st.sum[rt] *= f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) st.o[rt][c] *= f;
-            st.z[rt] *= f;
+            if (RT == 1 || rt == (int)(threadIdx.x >> 4 & 3)) st.z *= f;
         }
     }
 #pragma unroll
@@ -652,7 +713,6 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
     __shared__ TreeShared<RT> sh;
     __shared__ int s_last;
     QueryTiles<RT>& sq = sh.run.sq;
-    constexpr float kPart = BITS != 16 ? 0.5f : 1.0f;      // what of an output RowState::o holds
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -710,7 +770,6 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                     for (int rt = 0; rt < RT; ++rt) bias[rt] = biases[turn * (16 * RT) + 16 * rt + n];
                     turn = (turn + 1) % kBiasBlocks;
                 }
-                strip_keys<BITS, AXIS>(kw, strip, lane);
                 key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
                 load_keys<BITS, AXIS, ONCE>(base, a.group_log2, next, lane, kw);
                 if (32 * blk + 32 > n_tok) {     // (uniform) the head's last block: tokens past its count are unseen
@@ -722,15 +781,32 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                 }
                 float x[RT][8];
                 softmax_step<RT>(st, acc, factor, bias, x);
+                if constexpr (BITS != 16)
+                    if (any(wide_bits<kWideValue<BITS>>(vw.scale) != 0u)) {
+                        vw.scale = scaled(vw.scale, 0.25f); vw.zero = scaled(vw.zero, 0.25f);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[rt][j] *= 4.0f;
+                    }
                 WeightOperand p[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
                 if constexpr (BITS != 16) strip_values<BITS>(a, vw, strip, lane);
-                if constexpr (BITS != 16) {      // (lane n has the zeros of the group that channel 32 (n % 4) is in)
+                if constexpr (BITS != 16) {
+                    // Lane n has the zeros of the group that channel 32 (n % 4) is in, so all four lanes of a row get the same four sums, and lane kb keeps
+                    // those of tile kb: one register of four, not one a tile.
                     Frag z;
                     z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * ((32 * (n & 3)) >> a.group_log2) + 4 * kb]);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) st.z[rt] = mfma(z, p[rt].lo, mfma(z, p[rt].hi, st.z[rt]));
+                    for (int rt = 0; rt < RT; ++rt) {
+                        if constexpr (RT == 1) {
+                            st.z = mfma(z, p[rt].lo, mfma(z, p[rt].hi, st.z));
+                        } else {
+                            const f4v sums = mfma(z, p[rt].lo, mfma(z, p[rt].hi, f4v{0.f, 0.f, 0.f, 0.f}));
+                            if (rt == kb) st.z += sums;
+                        }
+                    }
                 }
                 Frag s;
 #pragma unroll
@@ -742,7 +818,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                     } else {
                         Frag lo;
                         h2v c[4];
-                        value_halves<BITS>(fields, vw.w, tile, blk & 1, c);
+                        value_whole<BITS>(fields, vw.w, tile, blk & 1, c);
                         if ((tile & 1) == 0) {       // (a group has at least two tiles)
                             const int g = (16 * tile) >> a.group_log2;
                             s.q = *reinterpret_cast<const uint4*>(&strip.v_scale[16 * g + 4 * kb]);
@@ -764,7 +840,10 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                    for (int tile = 0; tile < 8; ++tile) st.o[rt][tile] += kPart * st.z[rt][tile >> 1];
+                    for (int i = 0; i < 4; ++i) {
+                        const float z = RT == 1 ? st.z[i] : __shfl(st.z[i], 16 * rt + n);
+                        st.o[rt][2 * i] += z; st.o[rt][2 * i + 1] += z;
+                    }
         }
     }
 
@@ -828,11 +907,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
             softmax_step<RT>(st, acc, factor, none, x);
             WeightOperand p[RT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[rt][j] *= kPart;
-                weight_operand(x[rt], minus, p[rt]);
-            }
+            for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
             if (drafted && __builtin_amdgcn_ballot_w64(odd_value) != 0ull) {
                 // Values that are not finite reach only the rows that see them (a weight of 0 would make them NaN in the matrix product):
                 // they are added here, one token at a time, and taken out of the tile.
@@ -942,7 +1017,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
 #pragma unroll
                 for (int rt = 1; rt < JOIN; ++rt) total = (slot >> 3) == rt ? sum[j0 + rt] : total;
                 const int r = row0 + 16 * (j0 + (slot >> 3)) + n;
-                if (r < a.rows) *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * t + 4 * kb) = halves_of(o, inverse_sum(total) / kPart);
+                if (r < a.rows) *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * t + 4 * kb) = halves_of(o, inverse_sum(total));
             }
         }
     }
@@ -995,7 +1070,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                     top = higher;
                 }
                 if (r < a.rows) {
-                    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * ((item >> 6) & 7) + 4 * kb) = halves_of(o, inverse_sum(total) / kPart);
+                    *reinterpret_cast<uint2*>(a.out + ((size_t)bh * a.rows + r) * kHeadDim + 16 * ((item >> 6) & 7) + 4 * kb) = halves_of(o, inverse_sum(total));
                     if (a.lse && (item & 0x1C0) == 0 && kb == 0) a.lse[(size_t)bh * a.rows + r] = log_sum(top, total);
                 }
             }
@@ -1043,7 +1118,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                                 sh.last.weight[s1 + u][threadIdx.x] = g[u];
                             }
                         }
-                        sh.last.inverse[threadIdx.x] = inverse_sum(total) / kPart;
+                        sh.last.inverse[threadIdx.x] = inverse_sum(total);
                         const int r = row0 + threadIdx.x;
                         if (a.lse && r < a.rows) a.lse[(size_t)bh * a.rows + r] = log_sum(top, total);
                     }
@@ -1152,7 +1227,6 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
                     for (int rt = 0; rt < RT; ++rt) add[rt] = __builtin_fmaf(biases[turn * (16 * RT) + 16 * rt + n], factor[rt], minus_lse[rt]);
                     turn = (turn + 1) % kBiasBlocks;
                 }
-                strip_keys<BITS, AXIS>(kw, strip, lane);
                 key_product<BITS, AXIS, RT>(fields, kw, sq.frag, sq.sums, strip, lane, acc);
                 load_keys<BITS, AXIS, ONCE>(base, a.group_log2, min(blk + kWeightWaves, end - 1), lane, kw);
                 float cs[8] = {};
