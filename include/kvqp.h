@@ -428,7 +428,9 @@ int kvqp_append_tail_ragged(const kvqp_cfg *cfg, kvqp_cache *cache, int32_t n_to
  *
  * Common to the three: cfg fields used are batch, heads, head_dim, bits, group_size, key_axis and
  * sm_scale, and decode_cache_hint, where AUTO here means STREAM for calls on more than 96 MB of
- * codes and KEEP for others.  Caches with outlier filtering, and of more than 2^26 tokens per head,
+ * codes and KEEP for others.  STREAM has an effect where memory may bound a call: in kvqp_tree_attn up to 32 query rows per KV head
+ * (n_q_heads / n_kv_heads * n_rows; at 16 bits any number, and only the values' loads), in kvqp_accumulate_weights up to 16 below 16 bits; calls
+ * of more rows load normally whatever it says.  Caches with outlier filtering, and of more than 2^26 tokens per head,
  * are not taken (UNSUPPORTED).  Head-level counts (cache->head_n_kept) are read on the device, where a
  * count above n_kept is cut to n_kept.
  * q, k_new, v_new, out and the cache's codes, per-channel scales and zeros and tails have to be aligned to
