@@ -468,7 +468,8 @@ int kvqp_tree_workspace_init(void *workspace, size_t workspace_bytes, void *hip_
  * does not attend does not reach it, whatever it holds, infinities and NaN included.
  * n_kept and tail_len may be 0.  Reproducible bit for bit.  out and lse lie apart from all that is read.
  * Numerical range: any finite queries, scales and zeros.  A logit is exact to about 2^-21 of the magnitudes of its
- * products (of a query's element with a code times its scale, and with a zero), weights to 2^-22, values to 2^-21 of what their group spans.
+ * products (of a query's element with a code times its scale, and with a zero); a weight to 2^-21 of itself and 2^-32 of the row's largest, a value
+ * to 2^-21 of what its group spans.
  * Workspace: kvqp_tree_workspace_bytes, 16-byte aligned, prepared once with kvqp_tree_workspace_init.  One may
  * serve calls of any configurations for which it is large enough; calls that share one must not overlap in time
  * (calls issued on one stream never do), calls with different ones are independent.

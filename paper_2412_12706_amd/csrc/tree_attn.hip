@@ -58,8 +58,9 @@ constexpr int most_waves(int rt) { return rt <= 2 ? 12 : 8; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegBig = -1.0e30f;     // reference of a row that has seen nothing
-// A row's reference moves when a logit (log2) passes it by kSlack, and then to kBoost below that logit: weights stay
-// under 2^kSlack, and those of 2^-22 of the largest keep all bits of their hi + lo parts.
+// A row's reference moves when a logit (log2) passes it by kSlack, and then to kBoost below that logit: a wave's largest weight of a row is 2^kBoost
+// to 2^kSlack, and the hi + lo parts (binary16, cut toward zero) are off by 2^-21 of a weight down to 2^-3, 2^-11 of the largest and less.  Smaller
+// ones' lo parts end at binary16's lowest step: 2^-24, 2^-32 of the largest.
 constexpr float kSlack = 12.0f, kBoost = 8.0f;
 
 __device__ __forceinline__ h2v as_h2(uint32_t u) { union { uint32_t u; h2v h; } c; c.u = u; return c.h; }
