@@ -511,6 +511,8 @@ def tree_mask(parents, device="cuda"):
     sequence itself; a sequence of such sequences makes one mask per batch item.  Every token sees itself and its ancestors.
     int32 [n, ceil(n / 32)] or [batch, n, ceil(n / 32)]."""
     import torch
+    if hasattr(parents, "tolist"):      # (an element of a tensor is a tensor, too)
+        parents = parents.tolist()
     several = len(parents) > 0 and hasattr(parents[0], "__len__")
     out = []
     for tree in (parents if several else [parents]):
