@@ -586,6 +586,7 @@ def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=
     if weights_out is not None:
         cap_out = weights_out.shape[-1]
         _want("weights_out", weights_out, torch.float32, (*heads, cap_out), device)
+    n_keep = max(-1, min(n_keep, (1 << 31) - 1))          # (as many as a C integer holds)
     kept = min(n_keep, cache.n_kept)
     if cache.head_n_kept is None and n_keep < cache.n_kept and unit > 1:
         short = cache.n_kept % unit
