@@ -31,7 +31,7 @@
 // Weights enter the second product as hi + lo too, and values as code * s, hi + lo, while the zeros take a product of their own: its rows are
 // the groups of channels.  (A value rounded to binary16, code * s + z, adds as
 // much error as the output's own rounding: 2.8e-4 where the formula rounded once has 2.1e-4.  The parts cost ten matrix instructions a block and
-// tile of rows: 32 layers of 8192 tokens, 32 rows: 99 -> 110 us; one layer of 16384 tokens, 256 rows: 49 -> 55.)
+// tile of rows: 32 layers of 8192 tokens, 32 rows: 101 -> 110 us; one layer of 16384 tokens, 256 rows: 49 -> 56.)
 #include <algorithm>
 #include <initializer_list>
 
@@ -381,10 +381,11 @@ __device__ __forceinline__ bool any(bool mine) { return __builtin_amdgcn_ballot_
 __device__ __forceinline__ uint32_t scaled(uint32_t two, float by) { return as_u32(as_h2(two) * splat(by)); }
 // Keys: 256 and more (255 codes, and 128 q's, times less stay below 65504).  They are left out of a block's product and get another one, kWide
 // taken from the scale and given to the other operand, so that the small ones beside them lose nothing.  (Almost no block has any; looking for
-// them, here and among the values, takes 2 % of a launch: 32 layers of 8192 tokens, 32 rows: 110 -> 113 us.)
+// them, here and among the values, takes six instructions of some five hundred.)
 constexpr uint32_t kWideKey = 0x5C00u;
 constexpr float kWide = 256.0f;
-// Values: where the highest code times the scale would pass 65504; the block's scales and zeros are quartered then, and the weights four times as large.
+// Values: where the highest code times the scale would pass 65504; the block's scales and zeros are quartered then, and with them, for the time
+// being, the outputs so far.
 template <int BITS> constexpr uint32_t kWideValue = BITS == 2 ? 0x7400u : BITS == 4 ? 0x6C00u : 0x5C00u;       // 16384, 4096, 256
 
 // Makes a block's key scales ready for the product: the wide ones are taken out and returned, times 1 / kWide (the others' places: 0); keys
@@ -548,7 +549,10 @@ __device__ __forceinline__ void key_product(const Fields<BITS>& fields, KeyWords
 // ---- state of a wave's rows ----
 template <int RT> struct RowState {
     f4v o[RT][8];          // O^T: channel 16 tile + 4 kb + i of row 16 rt + n
-    f4v z;                 // below 16 bits: the packed tokens' zeros' share, channels 32 i .. + 31 of row 16 kb + n (one tile: of row n, in all four lanes)
+    // Below 16 bits, the packed tokens' zeros' share: channels 32 i .. + 31 of row 16 rt + n, the same in its four lanes.  With four tiles of rows
+    // lane kb has tile kb's alone, or others spill (16384 tokens, 256 rows: 61.4 us with one for each, 56.0 so; two tiles, 32 layers of 8192 tokens:
+    // 110.6 with one for each, 112.5 so).
+    f4v z[RT <= 2 ? RT : 1];
     float ref[RT], sum[RT];
 };
 template <int RT>
@@ -559,7 +563,16 @@ __device__ __forceinline__ void clear(RowState<RT>& st) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) st.o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
     }
-    st.z = f4v{0.f, 0.f, 0.f, 0.f};
+    for (f4v& z : st.z) z = f4v{0.f, 0.f, 0.f, 0.f};
+}
+// (outputs alone)
+template <int RT>
+__device__ __forceinline__ void rescale(RowState<RT>& st, float by) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) st.o[rt][c] *= by;
+    for (f4v& z : st.z) z *= by;
 }
 // Moves references where logits have passed them, turns acc + bias (a block's logits before the rows' factors, -inf where unseen) into weights x
 // and adds them up.
@@ -583,7 +596,8 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
             st.sum[rt] *= f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) st.o[rt][c] *= f;
-            if (RT == 1 || rt == (int)(threadIdx.x >> 4 & 3)) st.z *= f;
+            if constexpr (RT <= 2) st.z[rt] *= f;
+            else if (rt == (int)(threadIdx.x >> 4 & 3)) st.z[0] *= f;
         }
     }
 #pragma unroll
@@ -594,6 +608,7 @@ __device__ __forceinline__ void softmax_step(RowState<RT>& st, const f4v (&acc)[
             x[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[rt][j >> 2][j & 3], factor[rt], add));
             st.sum[rt] += x[rt][j];
         }
+        asm("" : "+v"(st.sum[rt]));       // (or the compiler adds up behind the products, and keeps 8 RT weights in registers until then)
     }
 }
 // Weights as operands: pair i holds tokens 4 kb + i and 16 + 4 kb + i; hi + lo parts, cut toward zero.
@@ -782,31 +797,27 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                 }
                 float x[RT][8];
                 softmax_step<RT>(st, acc, factor, bias, x);
-                if constexpr (BITS != 16)
-                    if (any(wide_bits<kWideValue<BITS>>(vw.scale) != 0u)) {
+                bool wide = false;
+                if constexpr (BITS != 16) {
+                    wide = any(wide_bits<kWideValue<BITS>>(vw.scale) != 0u);
+                    if (wide) {
                         vw.scale = scaled(vw.scale, 0.25f); vw.zero = scaled(vw.zero, 0.25f);
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) x[rt][j] *= 4.0f;
+                        rescale<RT>(st, 0.25f);
                     }
+                }
                 WeightOperand p[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) weight_operand(x[rt], minus, p[rt]);
                 if constexpr (BITS != 16) strip_values<BITS>(a, vw, strip, lane);
                 if constexpr (BITS != 16) {
-                    // Lane n has the zeros of the group that channel 32 (n % 4) is in, so all four lanes of a row get the same four sums, and lane kb keeps
-                    // those of tile kb: one register of four, not one a tile.
+                    // (lane n has the zeros of the group that channel 32 (n % 4) is in)
                     Frag z;
                     z.q = *reinterpret_cast<const uint4*>(&strip.v_zero[16 * ((32 * (n & 3)) >> a.group_log2) + 4 * kb]);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        if constexpr (RT == 1) {
-                            st.z = mfma(z, p[rt].lo, mfma(z, p[rt].hi, st.z));
-                        } else {
-                            const f4v sums = mfma(z, p[rt].lo, mfma(z, p[rt].hi, f4v{0.f, 0.f, 0.f, 0.f}));
-                            if (rt == kb) st.z += sums;
-                        }
+                        const f4v sums = mfma(z, p[rt].lo, mfma(z, p[rt].hi, RT <= 2 ? st.z[RT <= 2 ? rt : 0] : f4v{0.f, 0.f, 0.f, 0.f}));
+                        if constexpr (RT <= 2) st.z[rt] = sums;
+                        else if (rt == kb) st.z[0] += sums;
                     }
                 }
                 Frag s;
@@ -835,6 +846,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                     value_product<RT>(st, v, tile, p);
                     if (tile & 1) end_step<RT>();
                 }
+                if (wide) rescale<RT>(st, 4.0f);
                 load_values<BITS, ONCE>(base, a.group_log2, next, lane, vw);
             }
             if constexpr (BITS != 16)
@@ -842,7 +854,7 @@ __global__ __launch_bounds__(64 * most_waves(RT), most_waves(RT) / 4) void tree_
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float z = RT == 1 ? st.z[i] : __shfl(st.z[i], 16 * rt + n);
+                        const float z = RT <= 2 ? st.z[RT <= 2 ? rt : 0][i] : __shfl(st.z[0][i], 16 * rt + n);
                         st.o[rt][2 * i] += z; st.o[rt][2 * i + 1] += z;
                     }
         }
