@@ -14,7 +14,8 @@
 // Many heads are bound by memory: the survivors' bytes are read and written once (a value word holds 4 to 16 tokens, so
 // what lies between survivors comes along).  256 heads of 8192 tokens to 6144, 4 bits: 110.8 us for 533 MB, 4.8 TB/s of the
 // 5.2 that a large copy reaches, behind 12.4 us of selection.  Few heads are bound by latency, keys that are quantized again
-// by vector instructions (16 heads of 12003 tokens to 8001, 2 bits: 12 + 18.6 us, vector ALUs 90 % busy, where 27 MB would take 5).
+// by vector instructions (16 heads of 12003 tokens to 8001, 2 bits: 12 + 18.6 us, vector ALUs 90 % busy, where 27 MB would take 5; a key code takes
+// 24 of them, nine for its group's minimum and maximum and eight to be quantized again, a value field eight).
 #include <type_traits>
 
 #include "kvqp_internal.h"
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens(const EvictArgs a, i
     __syncthreads();
 
     // Everything is requested before anything is stored: one trip to memory for a workgroup, not one per kind of data
-    // (32 heads of 8192 tokens to 6144, 4 bits: 211 us with a trip for each, 113 this way).
+    // (256 heads of 8192 tokens to 6144, 4 bits: 211 us with a trip for each, 113 this way).
     float weight = 0.0f;
     if (a.weights_out && tid < ntok) weight = a.weights[(size_t)bh * a.w_cap + s_idx[tid]];
     // scales and zeros that belong to tokens: 4, 2 or 1 numbers a token and array; a thread has one token of one or two of four arrays

@@ -8,8 +8,8 @@
 //   weight[t] = sum_r exp(l[r, t] - lse[r])
 // K and V are code * scale + zero of the packed part, and plain rows of the tail and of the drafted
 // tokens.  The cache is read once per 64 rows; a row costs 512 multiply-adds per token, and every
-// operand twice (see below).  32 layers of 8192 tokens at 4 bits (345 MB): 16 rows take 68.5 us, 5.0
-// TB/s, bound by memory; 32 rows 96 us and 64 rows 158 us, bound by instruction issue and power.
+// operand twice (see below).  32 layers of 8192 tokens at 4 bits (345 MB), on cards that differ by a tenth: 16 rows take 79 to 86 us (4.0 to
+// 4.4 TB/s), 32 rows 103 to 118 and 64 rows 192, bound by instruction issue and power.
 //
 // Layout on gfx950.  A wave takes blocks of 32 tokens, for all rows of its workgroup (16, 32 or 64).
 // Both products run transposed, S^T[token, row] = K Q^T and O^T[channel, row] = V^T P^T, with
@@ -1343,10 +1343,11 @@ TreePlan plan_tree(const kvqp_cfg& cfg, int n_rows, int n_kept, int tail_len) {
     p.row_blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
     const long long base = (long long)cfg.batch * cfg.n_kv_heads * p.row_blocks;
     const int units = (n_kept + 31) / 32 + (tail_len + 31) / 32 + (n_rows + 31) / 32;
-    // By 105 shapes of 1 to 48 sequences, 32 to 16384 tokens and 4 to 80 rows, each with 4 to 16 waves and 1 to 32 splits: eight waves
-    // are within 3 % of the best nearly everywhere (four where there are no more blocks, twelve 3 to 8 % faster where every CU has a long
-    // head to itself); a split pays from 20 blocks of 32 tokens on (34 blocks, 16 rows: 9.7 us in four, 11.0 in one), with a block for every wave, on
-    // every CU, but sixteen splits are enough until each has 32 blocks (joining them takes longer than what the others save).
+    // By 105 shapes of 1 to 48 sequences, 32 to 16384 tokens and 4 to 80 rows, each with 4 to 12 waves and 1 to 32 splits, the rule is within 3 %
+    // of the best in 95, 10 % off at most (profiles/tree_plan_sweep.txt): eight waves (four where there are no more blocks, twelve where every CU
+    // has a long head to itself); splits from 20 blocks of 32 tokens on (34 blocks, 4 rows: 9.8 us in four, 12.4 in one), one to eight blocks, or
+    // about a block to a wave, as far as there are CUs, but sixteen splits are enough until each has 32 blocks (joining more takes longer than
+    // they save).
     p.most_splits = (int)std::max(1LL, std::min(256 / base, (long long)kMostSplits));
     p.n_splits = units <= 20 ? 1 : std::max(1, std::min({p.most_splits, (units + 4) / 8, std::max(16, units / 32)}));
     p.n_waves = units <= 4 ? 4 : std::min(base >= 128 && p.n_splits == 1 ? 12 : 8, most_waves(p.row_tiles));
