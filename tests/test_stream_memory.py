@@ -110,3 +110,25 @@ def test_compress_and_decode_on_another_stream_take_that_streams_memory(monkeypa
         else:
             call(stream)
         assert recorder.seen and set(recorder.seen) == {where}
+
+
+@pytest.mark.gpu
+def test_a_captured_call_on_the_capturing_stream_makes_its_own_memory(orc):
+    import numpy as np
+    from tests.rows_util import half, make
+    rng = np.random.default_rng(54)
+    cfg, cache, _, _ = make(orc, rng, 1, 2, 4, 2600, 20, 4, 32, 0)
+    q, kn, vn = (torch.from_numpy(half(rng, *s)).cuda() for s in ((1, 8, 5, D), (1, 2, 5, D), (1, 2, 5, D)))
+    want, step = kvqp.tree_attn(cfg, q, kn, vn, None, cache), kvqp.decode_attn(cfg, q[:, :, 0].contiguous(), cache)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    one = q[:, :, 0].contiguous()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        out = kvqp.tree_attn(cfg, q, kn, vn, None, cache, stream=s)
+        out1 = kvqp.decode_attn(cfg, one, cache, stream=s)
+    for _ in range(4):
+        out.zero_(), out1.zero_()
+        g.replay()
+        again = kvqp.tree_attn(cfg, q, kn, vn, None, cache)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(out1, step) and torch.equal(again, want)
