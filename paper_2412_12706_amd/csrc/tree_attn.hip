@@ -1247,7 +1247,10 @@ __global__ __launch_bounds__(kWeightThreads, 4) void add_weights(const TreeArgs 
                 for (int rt = 0; rt < RT; ++rt)
                     if (gives(rt))
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) cs[j] += weight(acc[rt][j >> 2][j & 3], rt, add[rt]);
+                        for (int j = 0; j < 8; ++j) {
+                            const float w = weight(acc[rt][j >> 2][j & 3], rt, add[rt]);
+                            cs[j] = rt ? cs[j] + w : w;
+                        }
                 store(cs, weights, 32 * blk, n_tok);
             }
         }
