@@ -529,6 +529,173 @@ int kvqp_evict(const kvqp_cfg *cfg, const kvqp_cache *src, const float *weights,
                kvqp_cache *dst, float *weights_out, int32_t w_cap_out, int32_t *idx_out, void *workspace, size_t workspace_bytes,
                void *hip_stream);
 
+/*
+ * ---- Rotary positions, and a paged cache of 8-bit codes ----
+ *
+ * Everything above takes keys and queries that have been rotated to their positions, and prunes
+ * a prompt (Section 3, "KV Pruning", at prefill) whose keys and values somebody holds.  The calls
+ * below are that other side: a program that serves many sequences keeps what is not pruned yet in
+ * pages, 8 bits an element, and takes a prompt out of them when it is to be pruned.  They are used
+ * together: kvqp_rope_frequencies and kvqp_rope_table once; kvqp_paged_append for the rows of
+ * every step or piece of a prompt (it rotates queries and keys on the way); kvqp_paged_attn for their
+ * attention; kvqp_paged_read and kvqp_compress for a prompt that is pruned.  kvqp_rotate is the
+ * rotation alone.
+ *
+ * Their rows are binary16 or bfloat16 (dtype), computed with in binary32 and rounded once.
+ */
+#define KVQP_HALF 0
+#define KVQP_BFLOAT16 1
+
+/*
+ * Rotary positions: the pair of channels (x1, x2) number j of a row at position p becomes
+ *   (x1 c - x2 s, x2 c + x1 s),   c = m cos(p f_j),  s = m sin(p f_j),
+ * f_j the frequencies and m a magnitude (1 unless a scaling for long contexts has another); every
+ * product and sum is rounded to binary32 by itself.  Pair j is channels (2j, 2j + 1) of an interleaved layout,
+ * else (j, j + rot_dim / 2).  Channels from rot_dim on stay as they are.
+ */
+typedef struct kvqp_rope {
+    const float *table;    /* DEVICE float [n_positions, rot_dim / 2, 2]: c and s, aligned to 16 bytes */
+    int32_t n_positions;   /* >= 1 */
+    int32_t rot_dim;       /* a multiple of 16, 16 .. 128 */
+    int32_t interleaved;   /* 0 or 1 */
+} kvqp_rope;
+
+/*
+ * Frequencies f_j = base^(-2 j / rot_dim), j < rot_dim / 2, changed for contexts longer than a model was trained for:
+ *   KVQP_ROPE_PLAIN   as they are
+ *   KVQP_ROPE_LINEAR  f_j / factor: positions are interpolated
+ *   KVQP_ROPE_BASE    base * factor^(rot_dim / (rot_dim - 2)) in place of base: the lowest frequency is divided by
+ *                     factor, the highest stays
+ *   KVQP_ROPE_PARTS   by the turns r_j = context * f_j / (2 pi) that a pair makes within the trained context: f_j where
+ *                     r_j >= high, f_j / factor where r_j <= low, between them g f_j + (1 - g) f_j / factor with
+ *                     g = (r_j - low) / (high - low)
+ * factor, context, low and high are read where a kind has them: finite, factor >= 1, context > 0, 0 <= low < high.  All of it in binary64.
+ *   inv_freq  HOST double [rot_dim / 2]
+ * Host only.
+ */
+#define KVQP_ROPE_PLAIN 0
+#define KVQP_ROPE_LINEAR 1
+#define KVQP_ROPE_BASE 2
+#define KVQP_ROPE_PARTS 3
+int kvqp_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double context, double low, double high,
+                          double *inv_freq);
+
+/* Fills a table of n_positions positions: angles, cosines and sines in binary64, times magnitude, rounded once.
+ *   inv_freq  HOST double [rot_dim / 2], finite; read before the call returns
+ *   table     DEVICE float [n_positions, rot_dim / 2, 2], aligned to 8 bytes */
+int kvqp_rope_table(const double *inv_freq, int32_t rot_dim, int32_t n_positions, double magnitude, float *table, void *hip_stream);
+
+/* Rows of 128 channels somewhere in memory: strides in elements, multiples of 8, data aligned to 16 bytes;
+ * a row's channels are next to each other. */
+typedef struct kvqp_rows {
+    void *data;            /* DEVICE */
+    int64_t batch_stride, head_stride, row_stride;
+} kvqp_rows;
+
+/*
+ * Rotates the rows x [batch, heads, rows, 128] into out (x itself, by its address and strides, or apart from it, strides of 0
+ * in x allowed, in out not where an axis has more than one entry).
+ *   positions  DEVICE int32 [rows], or [batch, rows] with positions_per_batch != 0; NULL: first + row.  A row whose
+ *              position is negative is left as it was in out; one behind the table becomes NaN in its rotated channels.
+ *   inverse    rotates back: the transposed rotation, which is the gradient of the rotation as well
+ * first >= 0, and without positions first + rows <= n_positions.  rows = 0 does nothing.
+ */
+int kvqp_rotate(const kvqp_rope *rope, int32_t dtype, int32_t batch, int32_t heads, int32_t rows, const kvqp_rows *x, const kvqp_rows *out,
+                const int32_t *positions, int32_t positions_per_batch, int32_t first, int32_t inverse, void *hip_stream);
+
+/*
+ * A paged cache of one layer: a pool of pages, each with page_tokens = P consecutive tokens of one sequence for all
+ * KV heads.  All buffers are the caller's device memory, aligned to 16 bytes.
+ *
+ *   k_codes  [n_pages, Hkv, P, 128] bytes,  v_codes  [n_pages, Hkv, 128, P] bytes (channel by channel, as the P.V product reads them)
+ *   k_scale, v_scale  float [n_pages, Hkv]: the scale of a page's block of P tokens of one head, a power of two
+ *   open_k, open_v  dtype [n_open, Hkv, 2 P, 128]: the last rows of a sequence in 16 bits, token t in row t % (2 P)
+ *
+ * Quantizer: a block is quantized when its P tokens are there, from its 16-bit rows: with a = max |x| the scale is 2^e, e the least
+ * integer >= -126 with a <= M 2^e, and the code of x is x 2^-e, rounded to the nearest (ties to even): an e4m3 number (the OCP format, M = 448)
+ * or an integer (M = 127), by form.  So a block's codes do not depend on the calls that brought its tokens.  Powers of two: a code times its scale is exact.
+ *   Rows are stored finite: a NaN in a new row (after the rotation) counts as 0, what lies beyond the type's largest number as that number.
+ *
+ * Sequence b has lengths[b] tokens.  Its whole blocks, tokens 0 .. lengths[b] / P * P - 1, are read from the pages table[b][0],
+ * table[b][1], ..., and the tokens behind them, its open block, from open_k / open_v, place open_slot[b] (b itself where open_slot is NULL).
+ * The two last blocks' rows stay in the open part as well, so a sequence may be cut back (lengths[b] lowered) to no less than P tokens below the
+ * greatest length it has had, as after drafted tokens that were not accepted; pages may be shared by sequences that begin alike (the open part is not shared, and may be copied).
+ * What the device arrays say is checked there: an entry of table or open_slot that names no page or place stands for tokens that are not
+ * stored and not attended; lengths beyond max_pages * P or below 0 and row_start entries outside 0 .. n_rows or descending never lead out of the buffers, but
+ * what is computed then is unspecified.
+ */
+#define KVQP_E4M3 0
+#define KVQP_INT8 1
+typedef struct kvqp_pages {
+    int32_t dtype;         /* KVQP_HALF or KVQP_BFLOAT16 */
+    int32_t form;          /* KVQP_E4M3 or KVQP_INT8 */
+    int32_t page_tokens;   /* P: 16, 32 or 64 */
+    int32_t n_pages;       /* >= 1 */
+    int32_t max_pages;     /* entries of a sequence in table; max_pages * P <= 2^30 */
+    int32_t n_open;        /* places in open_k / open_v; >= batch where open_slot is NULL */
+    void *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+    void *open_k, *open_v;
+    const int32_t *table;      /* DEVICE int32 [batch, max_pages] */
+    const int32_t *lengths;    /* DEVICE int32 [batch] */
+    const int32_t *open_slot;  /* DEVICE int32 [batch] or NULL */
+} kvqp_pages;
+
+/*
+ * Common to the three calls below: cfg fields used are batch (sequences), n_q_heads, n_kv_heads, head_dim and sm_scale (the others have to be
+ * valid).  lengths include the tokens of the call at hand: the rows of sequence b are row_start[b] .. row_start[b + 1] - 1 of the call's row arrays, and
+ * they are the last tokens of the sequence, row i of n at position lengths[b] - n + i; so append and attend see the same lengths.
+ *   row_start  DEVICE int32 [batch + 1], ascending, within 0 .. n_rows; NULL: one row per sequence (n_rows == batch).
+ * Rows of the arrays that belong to no sequence (from row_start[batch] on, as in a padded batch) are neither read nor written.
+ * Everything is enqueued on the stream, nothing depends on the values of lengths on the host: a captured call serves all later steps.
+ */
+
+/*
+ * Appends rows: keys (rotated by rope, if given, to their position, or to positions[row]) and values go to the open block, blocks that
+ * are full now to their pages, and the rotated queries to q_out.
+ *   q   dtype [n_rows, Hq, 128], rows q_stride elements apart, or NULL;  k, v  dtype [n_rows, Hkv, 128], rows k_stride, v_stride apart
+ *       (strides multiples of 8, at least a row; addresses aligned to 16 bytes: slices of one fused projection, for instance)
+ *   q_out  dtype [n_rows, Hq, 128], contiguous; q itself (contiguous then) or apart from all that is read; NULL where q is NULL
+ *   positions  DEVICE int32 [n_rows] or NULL (rope given): as for kvqp_rotate, but a negative position means that the row is not rotated
+ * Pages that are written belong to one sequence alone.  The call may be repeated for the same lengths where no more than P rows are
+ * appended, or rows from a block's beginning on.
+ */
+int kvqp_paged_append(const kvqp_cfg *cfg, const kvqp_pages *pages, const kvqp_rope *rope, const void *q, int64_t q_stride, const void *k,
+                      int64_t k_stride, const void *v, int64_t v_stride, int32_t n_rows, const int32_t *row_start, const int32_t *positions,
+                      void *q_out, void *hip_stream);
+
+/* Workspace bytes that every kvqp_paged_attn call of at most n_rows rows is content with, whatever the lengths.  Host only. */
+int kvqp_paged_workspace_bytes(const kvqp_cfg *cfg, int32_t n_rows, size_t *bytes);
+
+/* Prepares such a workspace, once after its allocation: zeroes the KVQP_PAGED_COUNTERS bytes of arrival counters at its head with a small kernel
+ * enqueued on the stream.  Every launch that completes leaves them zero.
+ * Errors: WORKSPACE when it is NULL or smaller than the counters, INVALID_ARG when it is not aligned to 16 bytes. */
+#define KVQP_PAGED_COUNTERS 16384
+int kvqp_paged_workspace_init(void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention of the rows over their sequences: Softmax(sm_scale q k^T) v over the tokens up to the row's own position, with window > 0 over the last
+ * window of those (the row's own included); sequences whose tokens before a window are gone may have any entry in table there.
+ *   q    dtype [n_rows, Hq, 128], rows q_stride elements apart (multiple of 8, at least a row)
+ *   out  dtype [n_rows, Hq, 128], contiguous;  lse  float [n_rows, Hq] or NULL: natural logarithm of the sum of exp(logit)
+ * A row that attends nothing gets zeros and -inf.  What a row does not attend does not reach it.  Reproducible bit for bit.
+ * out and lse lie apart from all that is read.
+ * Numerical range: any finite rows.  Products are exact, sums binary32; a weight enters the value product as a binary16 number (2^-12 of itself, or 2^-29 of the
+ * row's largest, where that is more), a value below 2^-24 of the largest scale among its sequence's pages loses bits.
+ * Workspace: kvqp_paged_workspace_bytes, 16-byte aligned, prepared once.  It may serve calls of any configurations for which it is large
+ * enough; calls that share one must not overlap in time.
+ */
+int kvqp_paged_attn(const kvqp_cfg *cfg, const kvqp_pages *pages, const void *q, int64_t q_stride, int32_t n_rows, const int32_t *row_start,
+                    int32_t window, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Reads tokens first .. first + count - 1 of every sequence into plain rows, as kvqp_compress takes them (dtype KVQP_HALF):
+ *   k_out, v_out  dtype [batch, Hkv, count, 128]: code times scale, cut to the type's largest number; the open block's rows as they are; zeros from lengths[b] on
+ *                 and for tokens without a page.  Apart from all that is read.
+ * first, count >= 0, first + count <= max_pages * P.
+ */
+int kvqp_paged_read(const kvqp_cfg *cfg, const kvqp_pages *pages, int32_t first, int32_t count, void *k_out, void *v_out, void *hip_stream);
+
 /* Static string for a return code. */
 const char *kvqp_strerror(int code);
 

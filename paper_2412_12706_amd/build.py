@@ -20,8 +20,10 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkvqp.so")
 # (the attention kernels, most of the work, are one object per bit width)
-SOURCES = [f"{src}.hip:{bits}" for src in ("decode_attn", "tree_attn") for bits in (4, 8, 2, 16)] + [
-    "quant_pack.hip", "score_select.hip", "evict.hip", "decode_attn.hip", "tree_attn.hip", "kvqp_api.cpp", "rows_api.cpp"]
+# (... and those over pages one per row type and form of codes)
+SOURCES = [f"{src}.hip:{bits}" for src in ("decode_attn", "tree_attn") for bits in (4, 8, 2, 16)] + [f"paged_attn.hip:{form}" for form in (1, 2, 3, 4)] + [
+    "quant_pack.hip", "score_select.hip", "evict.hip", "pages.hip", "decode_attn.hip", "tree_attn.hip", "paged_attn.hip", "kvqp_api.cpp", "rows_api.cpp",
+    "pages_api.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument", "-mllvm", "-amdgpu-mfma-vgpr-form",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

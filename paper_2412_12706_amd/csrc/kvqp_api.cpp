@@ -9,7 +9,7 @@ using namespace kvqp;
 
 extern "C" {
 
-int kvqp_version(void) { return 600; }
+int kvqp_version(void) { return 700; }
 
 const char* kvqp_strerror(int code) {
     switch (code) {

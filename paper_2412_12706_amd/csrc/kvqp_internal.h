@@ -155,4 +155,18 @@ hipError_t launch_append_tail(const kvqp_cfg& cfg, const kvqp_cache& cache, int 
 hipError_t launch_select(const kvqp_cfg& cfg, const void* q_obs, const void* k, int32_t* idx, int32_t* list, int32_t* unrefined,
                          void* ws, const CompressPlan& plan, const int32_t* head_n, bool score, hipStream_t stream);
 
+// Rotary positions and the paged cache (pages.hip, paged_attn.hip).
+hipError_t launch_rope_table(const double* inv_freq, int rot_dim, int n_positions, double magnitude, float* table, hipStream_t stream);
+hipError_t launch_rotate(const kvqp_rope& rope, int dtype, int batch, int heads, int rows, const kvqp_rows& x, const kvqp_rows& out,
+                         const int32_t* positions, bool positions_per_batch, int first, bool inverse, hipStream_t stream);
+hipError_t launch_paged_append(const kvqp_cfg& cfg, const kvqp_pages& g, const kvqp_rope* rope, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, int n_rows, const int32_t* row_start, const int32_t* positions, void* q_out,
+                               hipStream_t stream);
+hipError_t launch_paged_read(const kvqp_cfg& cfg, const kvqp_pages& g, int first, int count, void* k_out, void* v_out, hipStream_t stream);
+size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows);      // of every call with at most n_rows rows
+size_t paged_workspace_need(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows, bool has_starts);
+hipError_t launch_paged_init(void* ws, hipStream_t stream);         // zeroes the counters
+hipError_t launch_paged_attn(const kvqp_cfg& cfg, const kvqp_pages& g, const void* q, int64_t q_stride, int n_rows, const int32_t* row_start, int window,
+                             void* out, float* lse, void* ws, hipStream_t stream);
+
 }  // namespace kvqp

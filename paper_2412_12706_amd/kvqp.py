@@ -23,8 +23,11 @@ CACHE_AUTO, CACHE_STREAM, CACHE_KEEP = 0, 1, 2     # kvqp_cfg.decode_cache_hint
 EXPORTS = ["kvqp_cache_sizes", "kvqp_cache_sizes_cap", "kvqp_outlier_sizes", "kvqp_workspace_bytes", "kvqp_compress",
            "kvqp_compress_ragged", "kvqp_quantize_selected", "kvqp_quantize_selected_ragged", "kvqp_append_tail", "kvqp_append_tail_ragged", "kvqp_decode_attn", "kvqp_decode_attn_static", "kvqp_decode_workspace_init",
            "kvqp_tree_workspace_bytes", "kvqp_tree_workspace_init", "kvqp_tree_attn", "kvqp_accumulate_weights", "kvqp_evict_workspace_bytes", "kvqp_evict",
+           "kvqp_rope_frequencies", "kvqp_rope_table", "kvqp_rotate", "kvqp_paged_append", "kvqp_paged_workspace_bytes", "kvqp_paged_workspace_init",
+           "kvqp_paged_attn", "kvqp_paged_read",
            "kvqp_strerror", "kvqp_version"]
 MOST_ROWS = 256     # KVQP_MOST_ROWS
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3     # scalings of rope_frequencies
 
 
 class KvqpError(RuntimeError):
@@ -54,6 +57,9 @@ class CacheStruct(C.Structure):
 _pack_cfg = _struct.Struct("12i2f2i").pack
 _pack_cache = _struct.Struct("8P4i5P").pack
 assert _struct.calcsize("12i2f2i") == C.sizeof(CfgStruct) and _struct.calcsize("8P4i5P") == C.sizeof(CacheStruct)
+_pack_rope = _struct.Struct("P3i4x").pack           # kvqp_rope
+_pack_rows = _struct.Struct("P3q").pack             # kvqp_rows
+_pack_pages = _struct.Struct("6i9P").pack           # kvqp_pages
 
 _lib = None
 # Entry points once more, for this module's own calls: a cfg (and a cache that is only read) goes in as its bytes, a pointer as a number.
@@ -108,6 +114,18 @@ def lib():
         for name, args in {"kvqp_tree_attn": (cfg, ptr, ptr, ptr, ptr, i32, i32, C.c_char_p, ptr, ptr, ptr, size, ptr),
                            "kvqp_accumulate_weights": (cfg, ptr, ptr, i32, C.c_char_p, ptr, i32, C.c_float, ptr),
                            "kvqp_evict": (cfg, C.c_char_p, ptr, i32, i32, i32, ptr, ptr, i32, ptr, ptr, size, ptr)}.items():
+            entry = L[name]
+            entry.argtypes = args
+            _fn_rows[name] = entry
+        dbl, i64 = C.c_double, C.c_int64
+        L.kvqp_rope_frequencies.argtypes = [i32, dbl, i32, dbl, dbl, dbl, dbl, C.POINTER(dbl)]
+        L.kvqp_rope_table.argtypes = [C.POINTER(dbl), i32, i32, dbl, ptr, ptr]
+        L.kvqp_paged_workspace_bytes.argtypes = [C.POINTER(CfgStruct), i32, C.POINTER(size)]
+        L.kvqp_paged_workspace_init.argtypes = [ptr, size, ptr]
+        for name, args in {"kvqp_rotate": (cfg, i32, i32, i32, i32, cfg, cfg, ptr, i32, i32, i32, ptr),
+                           "kvqp_paged_append": (cfg, cfg, cfg, ptr, i64, ptr, i64, ptr, i64, i32, ptr, ptr, ptr, ptr),
+                           "kvqp_paged_attn": (cfg, cfg, ptr, i64, i32, ptr, i32, ptr, ptr, ptr, size, ptr),
+                           "kvqp_paged_read": (cfg, cfg, i32, i32, ptr, ptr, ptr)}.items():
             entry = L[name]
             entry.argtypes = args
             _fn_rows[name] = entry
@@ -604,3 +622,260 @@ def evict(cfg: Cfg, cache: Cache, weights, n_keep: int, dst: Cache, weights_out=
            workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     dst.n_kept, dst.tail_len = cs.n_kept, cs.tail_len
     return dst
+
+
+# ---- rotary positions, and the paged cache of 8-bit codes ----
+
+def rope_frequencies(rot_dim: int = 128, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0, context: float = 1.0,
+                     low: float = 1.0, high: float = 32.0):
+    """kvqp_rope_frequencies: the rot_dim / 2 frequencies, a list of floats."""
+    out = (C.c_double * (max(rot_dim, 2) // 2))()
+    rc = lib().kvqp_rope_frequencies(rot_dim, base, scaling, factor, context, low, high, out)
+    if rc:
+        raise KvqpError(rc, "kvqp_rope_frequencies")
+    return list(out)
+
+
+@dataclass
+class Rope:
+    """A table of cosines and sines [n_positions, rot_dim / 2, 2] (float32, on the device) and how it turns a row."""
+    table: object
+    rot_dim: int = 128
+    interleaved: bool = False
+
+    def _bytes(self) -> bytes:
+        t = self.table
+        return _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))
+
+
+def rope_table(n_positions: int, inv_freq, magnitude: float = 1.0, interleaved: bool = False, device="cuda", stream=None) -> Rope:
+    """kvqp_rope_table: a Rope for positions 0 .. n_positions - 1 with these frequencies (rope_frequencies gives some)."""
+    import torch
+    pairs = len(inv_freq)
+    with _memory_of(stream):
+        table = torch.empty((max(n_positions, 1), pairs, 2), dtype=torch.float32, device=device)
+    with torch.cuda.device(table.device):
+        rc = lib().kvqp_rope_table((C.c_double * pairs)(*inv_freq), 2 * pairs, n_positions, magnitude, table.data_ptr(), _stream_ptr(stream))
+    if rc:
+        raise KvqpError(rc, "kvqp_rope_table")
+    return Rope(table, 2 * pairs, interleaved)
+
+
+def _want_rope(rope: Rope, device):
+    import torch
+    t = rope.table
+    _want("rope.table", t, torch.float32, (t.shape[0], rope.rot_dim // 2, 2), device)
+
+
+def _row_type(what, t, device, dtype=None):
+    """0 or 1 (KVQP_HALF, KVQP_BFLOAT16) of a tensor of rows, whose channels lie next to each other."""
+    import torch
+    if (dtype is None and t.dtype not in (torch.float16, torch.bfloat16)) or (dtype is not None and t.dtype is not dtype) or t.get_device() != device or device < 0:
+        raise ValueError(f"{what}: a tensor of {dtype or 'float16 or bfloat16'} on GPU {device} is needed, not {t.dtype} on {t.device}")
+    if t.dim() < 1 or t.shape[-1] != 128 or t.stride(-1) != 1:
+        raise ValueError(f"{what}: rows of 128 adjacent channels are needed, not shape {tuple(t.shape)} with strides {t.stride()}")
+    return int(t.dtype is torch.bfloat16)
+
+
+def rotate(rope: Rope, x, positions=None, first: int = 0, out=None, inverse: bool = False, stream=None):
+    """kvqp_rotate: x [B,H,N,128] float16 or bfloat16, strided as it may be, -> out (contiguous unless given; x itself is allowed).
+    positions int32 [N] or [B,N], or None for first, first + 1, ..."""
+    import torch
+    device = x.get_device()
+    if x.dim() != 4:
+        raise ValueError(f"x: four axes are needed, not shape {tuple(x.shape)}")
+    kind = _row_type("x", x, device)
+    _want_rope(rope, device)
+    b, h, n, _ = x.shape
+    per_batch = 0
+    if positions is not None:
+        per_batch = int(positions.dim() == 2)
+        _want("positions", positions, torch.int32, (b, n) if per_batch else (n,), device)
+    if out is None:
+        with _memory_of(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if stream is not None and out.is_cuda:
+            out.record_stream(torch.cuda.current_stream(out.device))
+    else:
+        _row_type("out", out, device, x.dtype)
+        if out.shape != x.shape:
+            raise ValueError(f"out: shape {tuple(x.shape)} is needed, not {tuple(out.shape)}")
+    if x.numel() == 0:
+        return out
+    _call("kvqp_rotate", device, stream,
+          (rope._bytes(), kind, b, h, n, _pack_rows(x.data_ptr(), *x.stride()[:3]), _pack_rows(out.data_ptr(), *out.stride()[:3]), _addr(positions),
+           per_batch, first, int(inverse)))
+    return out
+
+
+@dataclass
+class Pages:
+    """Device buffers of one layer's paged cache (kvqp_pages): k_codes [n_pages,Hkv,P,128] and v_codes [n_pages,Hkv,128,P], both float8_e4m3fn or both int8;
+    k_scale, v_scale float32 [n_pages,Hkv]; open_k, open_v [n_open,Hkv,2P,128] float16 or bfloat16; table int32 [B,max_pages]; lengths int32 [B]; open_slot
+    int32 [B] or None."""
+    k_codes: object
+    v_codes: object
+    k_scale: object
+    v_scale: object
+    open_k: object
+    open_v: object
+    table: object
+    lengths: object
+    open_slot: object = None
+
+    @property
+    def page_tokens(self) -> int:
+        return self.k_codes.shape[2]
+
+    def _bytes(self, cfg: Cfg, device) -> bytes:
+        """kvqp_pages, with all buffers as it states them."""
+        import torch
+        k = self.k_codes
+        n, heads, p, _ = k.shape
+        half, form = self.open_k.dtype, k.dtype
+        if form not in (torch.float8_e4m3fn, torch.int8) or half not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"pages: codes of float8_e4m3fn or int8 and open rows of float16 or bfloat16 are needed, not {form} and {half}")
+        kv, n_open, most = cfg.n_kv_heads, self.open_k.shape[0], self.table.shape[-1]
+        _want("pages.k_codes", k, form, (n, kv, p, 128), device)
+        _want("pages.v_codes", self.v_codes, form, (n, kv, 128, p), device)
+        _want("pages.k_scale", self.k_scale, torch.float32, (n, kv), device)
+        _want("pages.v_scale", self.v_scale, torch.float32, (n, kv), device)
+        _want("pages.open_k", self.open_k, half, (n_open, kv, 2 * p, 128), device)
+        _want("pages.open_v", self.open_v, half, (n_open, kv, 2 * p, 128), device)
+        _want("pages.table", self.table, torch.int32, (cfg.batch, most), device)
+        _want("pages.lengths", self.lengths, torch.int32, (cfg.batch,), device)
+        if self.open_slot is not None:
+            _want("pages.open_slot", self.open_slot, torch.int32, (cfg.batch,), device)
+        return _pack_pages(half is torch.bfloat16, form is torch.int8, p, n, most, n_open, k.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(),
+                           self.v_scale.data_ptr(), self.open_k.data_ptr(), self.open_v.data_ptr(), self.table.data_ptr(), self.lengths.data_ptr(),
+                           _addr(self.open_slot) or 0)
+
+
+def alloc_pages(cfg: Cfg, n_pages: int, max_pages: int, page_tokens: int = 16, dtype=None, form="e4m3", n_open: int | None = None, device="cuda") -> Pages:
+    """Buffers for n_pages pages and cfg.batch sequences of at most max_pages of them: lengths 0, a table without pages (-1), for the caller to fill.
+    dtype: of the rows (float16 unless given); form: "e4m3" or "int8"; n_open: places for open blocks (one per sequence unless given)."""
+    import torch
+    if form not in ("e4m3", "int8"):
+        raise ValueError(f"form: \"e4m3\" or \"int8\", not {form!r}")
+    heads, n_open = cfg.n_kv_heads, cfg.batch if n_open is None else n_open
+    code = {"dtype": torch.float8_e4m3fn if form == "e4m3" else torch.int8, "device": device}
+    row = {"dtype": dtype or torch.float16, "device": device}
+    scale, count = {"dtype": torch.float32, "device": device}, {"dtype": torch.int32, "device": device}
+    return Pages(torch.empty((n_pages, heads, page_tokens, 128), **code), torch.empty((n_pages, heads, 128, page_tokens), **code),
+                 torch.empty((n_pages, heads), **scale), torch.empty((n_pages, heads), **scale),
+                 torch.empty((n_open, heads, 2 * page_tokens, 128), **row), torch.empty((n_open, heads, 2 * page_tokens, 128), **row),
+                 torch.full((cfg.batch, max_pages), -1, **count), torch.zeros(cfg.batch, **count))
+
+
+def _packed_rows(what, t, heads, n, device, dtype):
+    """The stride of the rows of a tensor [n, heads, 128] whose heads lie next to each other."""
+    _row_type(what, t, device, dtype)
+    if t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or (heads > 1 and t.stride(1) != 128):
+        raise ValueError(f"{what}: shape {(n, heads, 128)} with adjacent heads is needed, not {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if n > 1 else heads * 128
+
+
+def _want_starts(cfg: Cfg, row_start, device):
+    if row_start is not None:
+        import torch
+        _want("row_start", row_start, torch.int32, (cfg.batch + 1,), device)
+
+
+def paged_append(cfg: Cfg, pages: Pages, k, v, row_start=None, q=None, rope: Rope | None = None, positions=None, q_out=None, stream=None):
+    """kvqp_paged_append: k, v [n,Hkv,128] and q [n,Hq,128] or None, slices of a fused projection allowed; pages.lengths include the new rows.
+    row_start int32 [B+1], or None for one row per sequence; positions int32 [n] or None.  Returns the rotated queries (q_out), or None."""
+    import torch
+    device, dtype, n = k.get_device(), pages.open_k.dtype, k.shape[0]
+    layout = pages._bytes(cfg, device)
+    ks, vs = _packed_rows("k", k, cfg.n_kv_heads, n, device, dtype), _packed_rows("v", v, cfg.n_kv_heads, n, device, dtype)
+    _want_starts(cfg, row_start, device)
+    qs = 0
+    if q is not None:
+        qs = _packed_rows("q", q, cfg.n_q_heads, n, device, dtype)
+        if q_out is None:
+            with _memory_of(stream):
+                q_out = torch.empty((n, cfg.n_q_heads, 128), dtype=dtype, device=q.device)
+            if stream is not None and q_out.is_cuda:
+                q_out.record_stream(torch.cuda.current_stream(q_out.device))
+        else:
+            _want("q_out", q_out, dtype, (n, cfg.n_q_heads, 128), device)
+    elif q_out is not None:
+        raise ValueError("q_out: there is no q")
+    if rope is not None:
+        _want_rope(rope, device)
+    if positions is not None:
+        _want("positions", positions, torch.int32, (n,), device)
+    if n == 0 and row_start is not None:
+        return q_out
+    _call("kvqp_paged_append", device, stream,
+          (cfg._bytes(), layout, None if rope is None else rope._bytes(), _addr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, n, _addr(row_start),
+           _addr(positions), _addr(q_out)))
+    return q_out
+
+
+def paged_workspace_bytes(cfg: Cfg, n_rows: int) -> int:
+    return _sized("kvqp_paged_workspace_bytes", cfg, n_rows)
+
+
+def paged_workspace_init(workspace, stream=None):
+    """kvqp_paged_workspace_init: zero the arrival counters at the head of a workspace of paged_attn."""
+    import torch
+    with torch.cuda.device(workspace.device):
+        rc = lib().kvqp_paged_workspace_init(_ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if rc:
+        raise KvqpError(rc, "kvqp_paged_workspace_init")
+    return workspace
+
+
+def alloc_paged_workspace(cfg: Cfg, n_rows: int, device="cuda", stream=None):
+    """A workspace for paged_attn calls of at most n_rows rows, prepared for its first use; with a stream it is for calls on that one."""
+    with _memory_of(stream):
+        workspace = alloc_workspace(paged_workspace_bytes(cfg, n_rows), device)
+    return paged_workspace_init(workspace, stream)
+
+
+def paged_attn(cfg: Cfg, pages: Pages, q, row_start=None, window: int = 0, out=None, lse=None, workspace=None, stream=None):
+    """kvqp_paged_attn: q [n,Hq,128] (rows apart as they may be) -> out [n,Hq,128]; row_start int32 [B+1], or None for one row per sequence;
+    lse float32 [n,Hq] or None."""
+    import torch
+    device, dtype, n = q.get_device(), pages.open_k.dtype, q.shape[0]
+    layout = pages._bytes(cfg, device)
+    qs = _packed_rows("q", q, cfg.n_q_heads, n, device, dtype)
+    _want_starts(cfg, row_start, device)
+    if lse is not None:
+        _want("lse", lse, torch.float32, (n, cfg.n_q_heads), device)
+    if out is None:
+        with _memory_of(stream):
+            out = torch.empty((n, cfg.n_q_heads, 128), dtype=dtype, device=q.device)
+        if stream is not None and out.is_cuda:
+            out.record_stream(torch.cuda.current_stream(out.device))
+    else:
+        _want("out", out, dtype, (n, cfg.n_q_heads, 128), device)
+    if n == 0 and row_start is not None:
+        return out
+    if workspace is None:
+        workspace = alloc_paged_workspace(cfg, n, q.device, stream)
+    _same_device("paged_attn", device, workspace)
+    _call("kvqp_paged_attn", device, stream,
+          (cfg._bytes(), layout, q.data_ptr(), qs, n, _addr(row_start), window, out.data_ptr(), _addr(lse), workspace.data_ptr(),
+           workspace.numel() * workspace.element_size()))
+    return out
+
+
+def paged_read(cfg: Cfg, pages: Pages, count: int, first: int = 0, k_out=None, v_out=None, stream=None):
+    """kvqp_paged_read: tokens first .. first + count - 1 of every sequence as k, v [B,Hkv,count,128]; float16 ones are what compress takes."""
+    import torch
+    device, dtype = pages.k_codes.get_device(), pages.open_k.dtype
+    layout = pages._bytes(cfg, device)
+    shape, outs = (cfg.batch, cfg.n_kv_heads, max(count, 0), 128), []
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is None:
+            with _memory_of(stream):
+                t = torch.empty(shape, dtype=dtype, device=pages.k_codes.device)
+            if stream is not None and t.is_cuda:
+                t.record_stream(torch.cuda.current_stream(t.device))
+        else:
+            _want(name, t, dtype, shape, device)
+        outs.append(t)
+    _call("kvqp_paged_read", device, stream, (cfg._bytes(), layout, first, count, outs[0].data_ptr(), outs[1].data_ptr()))
+    return tuple(outs)

@@ -1,0 +1,160 @@
+"""What the tests of rotary positions and the paged cache share: the definitions in plain torch on the CPU (include/kvqp.h states them), and caches made from them."""
+import math
+
+import torch
+
+from paper_2412_12706_amd import kvqp
+
+D = 128
+HALF, BF16 = torch.float16, torch.bfloat16
+
+
+def rows(g, *shape, dtype=HALF, by=1.0):
+    return (torch.randn(shape, generator=g, dtype=torch.float32) * by).to(dtype)
+
+
+def rotated(x, position, table, rot, interleaved=False, inverse=False):
+    """x: [..., D] float32 (each product and sum rounded to it) or float64; position: int64, x's leading axes; table [n, rot / 2, 2]"""
+    turn = position >= 0
+    cs = table[position.clamp(0, table.shape[0] - 1)].to(x.dtype)
+    cs = torch.where((position >= table.shape[0])[..., None, None], torch.full_like(cs, math.nan), cs)
+    a, b = (x[..., 0:rot:2], x[..., 1:rot:2]) if interleaved else (x[..., :rot // 2], x[..., rot // 2:rot])
+    c, s = cs[..., 0], -cs[..., 1] if inverse else cs[..., 1]
+    u, w = a * c - b * s, b * c + a * s
+    y = x.clone()
+    if interleaved:
+        y[..., 0:rot:2], y[..., 1:rot:2] = u, w
+    else:
+        y[..., :rot // 2], y[..., rot // 2:rot] = u, w
+    return torch.where(turn.unsqueeze(-1), y, x)
+
+
+def finite(x, dtype):
+    most = torch.finfo(dtype).max
+    return torch.where(x.isnan(), torch.zeros_like(x), x).clamp(-most, most).to(dtype)
+
+
+def quantized(x, form):
+    """A block [tokens, D] of 16-bit rows -> codes, e (the scale's exponent), by the definition: the least e >= -126 with max |x| <= M 2^e"""
+    most = 448 if form == "e4m3" else 127
+    a = float(x.double().abs().max())
+    e = -126
+    if a > 0:
+        e = max(-126, math.ceil(math.log2(a / most)) - 2)
+        while a > most * 2.0 ** e:
+            e += 1
+    y = (x.double() * 2.0 ** -e).float()       # exact
+    return (y.to(torch.float8_e4m3fn) if form == "e4m3" else torch.round(y).to(torch.int8)), e
+
+
+class Made:
+    """Sequences as 16-bit rows, and a cache on the CPU that holds them by the definition."""
+
+    def __init__(self, g, lengths, hkv, page=16, dtype=HALF, form="e4m3", spare=3, extra_pages=2, by=(1.0, 1.0)):
+        b = len(lengths)
+        self.lengths, self.hkv, self.page, self.dtype, self.form = list(lengths), hkv, page, dtype, form
+        self.most = max(1, -(-max(lengths) // page)) + extra_pages
+        n_pages = b * self.most + spare
+        order = torch.randperm(n_pages, generator=g)
+        self.table = order[:b * self.most].view(b, self.most).to(torch.int32)
+        fp8 = torch.float8_e4m3fn if form == "e4m3" else torch.int8
+        # what nothing is stored in holds NaN (or, as integers, large numbers)
+        self.k_codes = torch.full((n_pages, hkv, page, D), 0x7F, dtype=torch.uint8).view(fp8)
+        self.v_codes = torch.full((n_pages, hkv, D, page), 0x7F, dtype=torch.uint8).view(fp8)
+        self.k_scale, self.v_scale = (torch.full((n_pages, hkv), math.nan) for _ in range(2))
+        self.open_k, self.open_v = (torch.full((b, hkv, 2 * page, D), math.nan, dtype=dtype) for _ in range(2))
+        loud = torch.ones(D)
+        loud[[5, 40, 77, 121]] = 10.0
+        self.k = [finite(torch.randn((hkv, t, D), generator=g) * loud * by[0], dtype) for t in lengths]
+        self.v = [finite(torch.randn((hkv, t, D), generator=g) * by[1], dtype) for t in lengths]
+        for i, t in enumerate(lengths):
+            self.put(i, 0, t)
+
+    def put(self, i, begin, t, k=None, v=None):
+        """Sequence i's tokens begin .. t - 1 arrive (from self.k, self.v), block by block."""
+        p = self.page
+        last = (t - 1) // p
+        for j in range(max(begin, (last - 1) * p, 0), t):
+            self.open_k[i, :, j % (2 * p)], self.open_v[i, :, j % (2 * p)] = self.k[i][:, j], self.v[i][:, j]
+        for block in range(begin // p, t // p):
+            page = int(self.table[i, block])
+            for h in range(self.hkv):
+                for name, x in (("k", self.k), ("v", self.v)):
+                    codes, e = quantized(x[i][h, block * p:(block + 1) * p], self.form)
+                    getattr(self, name + "_codes")[page, h] = codes if name == "k" else codes.view(torch.uint8).t().contiguous().view(codes.dtype)
+                    getattr(self, name + "_scale")[page, h] = 2.0 ** e
+
+    def numbers(self, i, name, length=None):
+        """What sequence i holds as 64-bit numbers, [hkv, length, D]: whole blocks from their codes, the rest from the open part"""
+        t, p = self.lengths[i] if length is None else length, self.page
+        out = torch.zeros((self.hkv, t, D), dtype=torch.float64)
+        for block in range(t // p):
+            page = int(self.table[i, block])
+            codes = getattr(self, name + "_codes")[page]
+            x = codes.float().double() * getattr(self, name + "_scale")[page].double().view(-1, 1, 1)
+            out[:, block * p:(block + 1) * p] = x if name == "k" else x.transpose(1, 2)
+        for j in range(t // p * p, t):
+            out[:, j] = getattr(self, "open_" + name)[i, :, j % (2 * p)].double()
+        return out
+
+    NAMES = ("k_codes", "v_codes", "k_scale", "v_scale", "open_k", "open_v")
+
+    def pages(self, device="cuda", lengths=None):
+        t = [x.to(device) for x in (*(getattr(self, n) for n in self.NAMES), self.table, torch.tensor(self.lengths if lengths is None else lengths, dtype=torch.int32))]
+        return kvqp.Pages(*t)
+
+    def same(self, pages):
+        """Every buffer bit for bit, NaN of any kind as one"""
+        for name in self.NAMES:
+            want, got = getattr(self, name), getattr(pages, name).cpu()
+            if name.startswith(("k_codes", "v_codes")):
+                assert torch.equal(want.view(torch.uint8), got.view(torch.uint8)), name
+            else:
+                gone = want.isnan()
+                assert torch.equal(gone, got.isnan()), name
+                assert torch.equal(want[~gone], got[~gone]), name
+
+
+def starts_of(counts):
+    out = [0]
+    for n in counts:
+        out.append(out[-1] + n)
+    return out
+
+
+def attention(q, k, v, positions, window, scale):
+    """q [n, hq, D] float64 at `positions`, k, v [hkv, t, D] -> out, lse, and how far a kernel may be off before its output is rounded: weights enter the value
+    product as binary16 numbers (2^-12 of themselves), logits are binary32 sums of 128 products and four more roundings, a bfloat16 query is divided
+    by a power of two and rounded at 2^-25 of its largest, weights below 2^-28 of the largest may be lost, sums of n terms are binary32 ones in some order (the
+    outputs in as many steps as there are 32 tokens, a few waves and splits)."""
+    n, hq, _ = q.shape
+    hkv, t, _ = k.shape
+    gq = hq // hkv
+    out, lse = torch.zeros((n, hq, D), dtype=torch.float64), torch.full((n, hq), -math.inf, dtype=torch.float64)
+    off, off_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    token = torch.arange(t)
+    for i in range(n):
+        pos = positions[i]
+        sees = (token <= pos) & ((token > pos - window) if window else True)
+        if not bool(sees.any()):
+            continue
+        for a in range(hq):
+            kk, vv = k[a // gq][sees], v[a // gq][sees]
+            x = (kk @ q[i, a]) * scale
+            lse[i, a] = torch.logsumexp(x, 0)
+            w = torch.softmax(x, 0)
+            out[i, a] = w @ vv
+            d = 132 * 2.0 ** -24 * float((kk.abs() @ q[i, a].abs()).max()) * scale + 2.0 ** -25 * float(q[i, a].abs().max() * kk.abs().sum(1).max()) * scale
+            steps = (kk.shape[0] / 32 + 80) * 2.0 ** -24
+            off[i, a] = (2.0 ** -12 + 2 * d + 2 * steps) * (w @ vv.abs()) + kk.shape[0] * 2.0 ** -28 * float(w.max()) * vv.abs().amax(0)
+            off_lse[i, a] = d + steps + 2.0 ** -22 * abs(float(lse[i, a]))
+    return out, lse, off, off_lse
+
+
+def near(got, want, off, dtype):
+    """got (of `dtype`) rounds something within `off` of want."""
+    got = got.double().cpu()
+    tiny = 2.0 ** -25 if dtype is HALF else 0.0      # half a step of the smallest numbers
+    allowed = off + torch.finfo(dtype).eps / 2 * (want.abs() + off) + tiny
+    worst = ((got - want).abs() / allowed.clamp(min=1e-300))
+    assert bool((worst <= 1).all()) and bool(torch.isfinite(got).all()), float(worst.max())
