@@ -3,6 +3,7 @@
 // One object per row type and form: KVQP_PAGED_BITS 1 + 2 * bfloat16 + int8 compiles the kernels, none the launches.
 #include <hip/hip_runtime.h>
 
+#include <stdlib.h>
 #include <algorithm>
 
 #include "pages.h"
@@ -20,10 +21,13 @@ struct AttnArgs {
     float logit_scale;      // sm_scale / ln 2
     int window, page_log2;
     int per_piece;          // rows of the call that a workgroup has at most
-    int n_splits;
+    int slots;              // workgroups of a KV head
+    int most_shares;        // how many shares the work of a KV head is cut into, about; 0: sequences are not split
+    int least_groups;       // groups of 64 tokens that a share has at least
+    bool once;              // loads of codes go round the memory-side cache
 };
 
-template <bool BF, bool INT8> hipError_t paged_rows_form(const AttnArgs& a, int row_tiles, dim3 grid, hipStream_t stream);
+template <bool BF, bool INT8> hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream);
 
 #ifdef KVQP_PAGED_BITS
 
@@ -72,390 +76,362 @@ __device__ __forceinline__ f4v product_of_rows(uint4 a, uint4 b, f4v c) {      /
 __device__ __forceinline__ float inverse_sum(float sum) { return sum > 0.f ? 1.f / sum : sum; }      // (a row that sees nothing: zeros; NaN stays)
 __device__ __forceinline__ float log_sum(float ref, float sum) { return sum == 0.f ? -INFINITY : (ref - kLift + __builtin_amdgcn_logf(sum)) * kLn2; }
 
-// Partial results of the splits of one piece and head: outputs in the order of the accumulators, and (reference, sum) of the rows.
+// Partial results of one workgroup of a split piece: outputs in the order of the accumulators, and (reference, sum) of the rows.
 struct Partials {
     __amdgpu_buffer_rsrc_t at;
-    int states, rt;
-    __device__ __forceinline__ Partials(const AttnArgs& a, int group, int rt_) : states(a.n_splits * rt_ * 8192), rt(rt_) {
-        const int bytes = states + a.n_splits * rt_ * 128;
-        at = __builtin_amdgcn_make_buffer_rsrc(a.part + (size_t)group * bytes, 0, bytes, 0x00020000);
+    int states, bytes;
+    // part: the first of `splits` workgroups' results, which follow each other
+    __device__ __forceinline__ Partials(const AttnArgs& a, int64_t part, int splits, int row_tiles) : states(row_tiles * 8192), bytes(row_tiles * 8320) {
+        at = __builtin_amdgcn_make_buffer_rsrc(a.part + part * bytes, 0, splits * bytes, 0x00020000);
     }
     __device__ __forceinline__ void put_output(int split, int item, f4v o) const {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, o), at, (split * rt * 512 + item) * 16, 0, kDeviceScope);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, o), at, split * bytes + item * 16, 0, kDeviceScope);
     }
     __device__ __forceinline__ void put_state(int split, int row, float ref, float sum) const {
         const u2v v = {__float_as_uint(ref), __float_as_uint(sum)};
-        __builtin_amdgcn_raw_buffer_store_b64(v, at, states + (split * rt * 16 + row) * 8, 0, kDeviceScope);
+        __builtin_amdgcn_raw_buffer_store_b64(v, at, split * bytes + states + row * 8, 0, kDeviceScope);
     }
     __device__ __forceinline__ f4v output(int split, int item) const {
-        return __builtin_bit_cast(f4v, __builtin_amdgcn_raw_buffer_load_b128(at, (split * rt * 512 + item) * 16, 0, kDeviceScope));
+        return __builtin_bit_cast(f4v, __builtin_amdgcn_raw_buffer_load_b128(at, split * bytes + item * 16, 0, kDeviceScope));
     }
     __device__ __forceinline__ float2 state(int split, int row) const {
-        const u2v v = __builtin_amdgcn_raw_buffer_load_b64(at, states + (split * rt * 16 + row) * 8, 0, kDeviceScope);
+        const u2v v = __builtin_amdgcn_raw_buffer_load_b64(at, split * bytes + states + row * 8, 0, kDeviceScope);
         return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1]));
     }
 };
 
-// ---- few rows: the tokens are split over waves and workgroups ----
-//
-// A wave takes 64 tokens at a time.  S^T = K Q^T by products of 16 tokens and 16 rows: a lane's column is a row (query head and new token) and its
-// group kb of 16 lanes holds tokens 16 kb .. 16 kb + 15, in an order that makes its logits, turned into weights, the second operand of
-// O^T = V^T P^T without leaving the lane; the first operand is 16 consecutive bytes of a channel, as pages store values.
-constexpr int kSegment = 512;      // pages whose numbers and scales are in LDS at a time
-template <int RT> constexpr int rows_waves() { return RT == 4 ? 4 : 8; }
+// ---- what both kernels do with a piece of a sequence's rows ----
 
-template <int RT, int NW>
-union RowsShared {
-    struct { int page[kSegment]; float k_scale[kSegment], v_scale[kSegment]; } seg;
-    uint16_t open_v[64][kHeadDim + 8];
-    struct { f4v o[NW][8][64]; float ref[NW][16 * RT], sum[NW][16 * RT]; } join;
+// Which sequence, piece of its rows and split of its tokens a workgroup has.  Only the device knows the lengths, so every workgroup looks at all of them:
+// the work of a KV head, groups of 64 tokens times pieces of rows, is cut into shares of about the same size, and a sequence of g groups is split
+// into g / share, rounded, for each of its pieces.  (1.5 shares and more are split, so the split sequences' workgroups are at most 4/3 most_shares.)
+struct Slot {
+    Sequence seq;
+    int piece, split, splits;
+    int part;               // number of the piece's first workgroup among those of split pieces
+};
+struct SlotShared {
+    float work[4];
+    int workgroups[4], parts[4];
+    Slot found;
+};
+__device__ __forceinline__ Slot find_slot(const AttnArgs& a, int slot, SlotShared& sh) {
+    const PageArgs& p = a.p;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, most = p.max_pages << a.page_log2;
+    struct Share { Sequence seq; int pieces, groups; };
+    auto look = [&](int b) {
+        Share s = {{b, b, 0, 0}, 0, 0};
+        if (b >= p.batch) return s;
+        const int r0 = p.row_start ? p.row_start[b] : b, r1 = p.row_start ? p.row_start[b + 1] : b + 1, length = p.lengths[b];
+        s.seq.row0 = min(max(r0, 0), p.n_rows);
+        s.seq.rows = max(min(r1, p.n_rows) - s.seq.row0, 0);
+        s.seq.length = min(max(length, 0), most);
+        s.pieces = (s.seq.rows + a.per_piece - 1) / a.per_piece;
+        const int seen = a.window > 0 ? min(s.seq.length, a.window + min(s.seq.rows, a.per_piece)) : s.seq.length;
+        s.groups = (seen + 63) / 64;
+        return s;
+    };
+    Share mine = look(threadIdx.x);
+    float share = 0.f;
+    if (a.most_shares > 0) {
+        float work = (float)mine.pieces * (float)mine.groups;
+        for (int b = threadIdx.x + 256; b < p.batch; b += 256) {
+            const Share s = look(b);
+            work += (float)s.pieces * (float)s.groups;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
+        if (lane == 0) sh.work[wave] = work;
+    }
+    if (threadIdx.x == 0) sh.found.seq.b = -1;
+    __syncthreads();
+    if (a.most_shares > 0) share = fmaxf(((sh.work[0] + sh.work[1]) + (sh.work[2] + sh.work[3])) / (float)a.most_shares, (float)a.least_groups);
+    int workgroups = 0, parts = 0;      // of the sequences before these 256
+    for (int b0 = 0; b0 < p.batch; b0 += 256) {
+        if (b0) mine = look(b0 + threadIdx.x);
+        const int splits = a.most_shares > 0 ? max((int)((float)mine.groups / share + 0.5f), 1) : 1, n = mine.pieces * splits, m = splits > 1 ? n : 0;
+        int upto = n, parts_upto = m;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(upto, d), y = __shfl_up(parts_upto, d);
+            if (lane >= d) { upto += x; parts_upto += y; }
+        }
+        if (lane == 63) { sh.workgroups[wave] = upto; sh.parts[wave] = parts_upto; }
+        __syncthreads();
+        for (int v = 0; v < 4; ++v) {
+            if (v < wave) { upto += sh.workgroups[v]; parts_upto += sh.parts[v]; }
+        }
+        const int at = slot - (workgroups + upto - n);
+        if (at >= 0 && at < n) sh.found = {mine.seq, at / splits, at % splits, splits, parts + parts_upto - m + at / splits * splits};
+        workgroups += (sh.workgroups[0] + sh.workgroups[1]) + (sh.workgroups[2] + sh.workgroups[3]);
+        parts += (sh.parts[0] + sh.parts[1]) + (sh.parts[2] + sh.parts[3]);
+        __syncthreads();
+        if (sh.found.seq.b >= 0) break;
+    }
+    const Slot s = sh.found;
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    return {{uniform(s.seq.b), uniform(s.seq.row0), uniform(s.seq.rows), uniform(s.seq.length)}, uniform(s.piece), uniform(s.split), uniform(s.splits), uniform(s.part)};
+}
+
+// The tokens that a workgroup's rows see, in groups of 64 from token 0: whole blocks, and open tokens behind them.
+struct Range {
+    Sequence seq;
+    int i0, n;                  // rows of the sequence: i0 .. i0 + n - 1
+    int first, last;            // their positions
+    int begin, closed, open;    // where the open block begins; whole blocks' tokens that are seen end there; open tokens that are seen
+    int lo;                     // first token that any row sees
+    int ga, gb;                 // groups of this workgroup
+    int split, active, part;    // its number among those that have some, and where their results go
+    __device__ __forceinline__ bool find(const AttnArgs& a, int slot, SlotShared& sh) {
+        const Slot s = find_slot(a, slot, sh);
+        seq = s.seq;
+        if (seq.b < 0 || (s.splits > 1 && s.part + s.splits > 2 * a.most_shares)) return false;      // (the second: lengths that change meanwhile)
+        i0 = s.piece * a.per_piece;
+        n = min(a.per_piece, seq.rows - i0);
+        first = seq.position(i0);
+        last = first + n - 1;
+        begin = seq.length >> a.page_log2 << a.page_log2;
+        lo = a.window > 0 ? max(first - a.window + 1, 0) : 0;
+        closed = min(last + 1, begin);
+        open = max(last + 1 - begin, 0);
+        const int g_lo = lo / 64, groups = closed > lo ? (closed + 63) / 64 - g_lo : 0;
+        const int each = max((groups + s.splits - 1) / s.splits, a.least_groups);
+        split = s.split; part = s.part;
+        active = max((groups + each - 1) / each, 1);
+        ga = g_lo + split * each;
+        gb = min(ga + each, g_lo + groups);
+        return split < active;
+    }
+    // (a head's parts are next to each other)
+    __device__ __forceinline__ int64_t part_of_head(const AttnArgs& a, int h) const { return (int64_t)h * (2 * a.most_shares) + part; }
 };
 
-template <bool BF, bool INT8, int RT>
-__global__ __launch_bounds__(64 * rows_waves<RT>()) void paged_rows(const AttnArgs a) {
-    constexpr int NW = rows_waves<RT>();
-    __shared__ RowsShared<RT, NW> sh;
-    __shared__ int s_found, s_last;
-    __shared__ unsigned int s_top;
-    const PageArgs& p = a.p;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kb = lane >> 4;
-    const int piece = blockIdx.x, h = blockIdx.y, split = blockIdx.z, P = 1 << a.page_log2;
-    const int b = __builtin_amdgcn_readfirstlane(owner_of_piece(p, piece, a.per_piece, 1, &s_found));
-    if (b < 0) return;
-    const Sequence seq = sequence_of(p, b, P);
-    const int i0 = (piece - first_piece(p, b, seq.row0, a.per_piece, 1)) * a.per_piece, n = min(a.per_piece, seq.rows - i0);
-    if (n <= 0) return;
-
-    // What the rows see: whole blocks in 64 tokens at a time (groups), and open tokens.
-    const int last = seq.position(i0 + n - 1), first = seq.position(i0);
-    const int begin = seq.length >> a.page_log2 << a.page_log2;
-    const int lo = a.window > 0 ? max(first - a.window + 1, 0) : 0, hi = last + 1;
-    const int closed = min(hi, begin);
-    const int g_lo = lo / 64, groups = closed > lo ? (closed + 63) / 64 - g_lo : 0;
-    const int per_split = max((groups + a.n_splits - 1) / a.n_splits, NW);
-    const int active = max((groups + per_split - 1) / per_split, 1);
-    if (split >= active) return;
-    const int ga = g_lo + split * per_split, gb = min(ga + per_split, g_lo + groups);
-    const int seen_by_all = min(first + 1, closed), hidden_to_some = a.window > 0 ? last - a.window + 1 : 0;
-
-    // The rows: queries as the second operand, 8 channels of 64 (s >> 1) + 16 kb + 8 (s & 1) a step.
-    h8v q[RT][4];
-    float scale[RT];           // of logits in the exponent's base, with the factor that a bfloat16 row was divided by
-    int position[RT];          // of the lane's row; -1 where there is none
-    int64_t q_at[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = 16 * rt + c, i = r / p.gq;
-        const bool there = i < n;
-        position[rt] = there ? seq.position(i0 + i) : -1;
-        q_at[rt] = (int64_t)(seq.row0 + i0 + (there ? i : 0)) * a.q_stride + (h * p.gq + r % p.gq) * kHeadDim + 16 * kb;
-        scale[rt] = a.logit_scale;
-        uint4 w[4];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) w[s] = there ? *reinterpret_cast<const uint4*>(a.q + q_at[rt] + 64 * (s >> 1) + 8 * (s & 1)) : make_uint4(0, 0, 0, 0);
-        if constexpr (BF) {
-            // A row over a power of two is a row of binary16 numbers, but for what is below 2^-24 of its largest: codes meet it without a conversion to bfloat16.
-            float m = 0.f;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const f8v x = numbers<true>(w[s]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x[j]));
-            }
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -120), 120);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) q[rt][s] = __builtin_convertvector(numbers<true>(w[s]) * two_to(-e), h8v);
-            scale[rt] *= two_to(e);
-        } else {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) q[rt][s] = __builtin_bit_cast(h8v, w[s]);
-        }
-    }
-
+// Of one row tile a lane has one row (column c) and eight tokens at a time; O^T of the tile is eight accumulators of 16 channels.
+template <int RT>
+struct Sums {
     f4v o[RT][8];
     float ref[RT], sum[RT];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        ref[rt] = kNegBig; sum[rt] = 0.f;
+        for (int rt = 0; rt < RT; ++rt) {
+            ref[rt] = kNegBig; sum[rt] = 0.f;
 #pragma unroll
-        for (int t = 0; t < 8; ++t) o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < 8; ++t) o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
+        }
     }
-    // Logits of one row tile (four to each of four token tiles) into weights; O and the sum follow the reference.
-    auto weigh = [&](int rt, f4v (&x)[4], f8v (&w)[2]) {
-        float m = x[0][0];
+    __device__ __forceinline__ void times(float f) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) m = fmaxf(m, x[t][i]);
+            for (int t = 0; t < 8; ++t) o[rt][t] *= f;
+    }
+    // Products of queries and keys, times f > 0 the logits, into weights; O and the sum follow the reference, which moves when a row has gone far beyond it.
+    __device__ __forceinline__ f8v weigh(int rt, const f4v (&x)[2], float f) {
+        float m = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3]))) * f;
         if (__any(m > ref[rt] + kLag)) {
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
             m = fmaxf(m, ref[rt]);
-            const float f = __builtin_amdgcn_exp2f(ref[rt] - m);
+            const float by = __builtin_amdgcn_exp2f(ref[rt] - m);
             ref[rt] = m;
-            sum[rt] *= f;
+            sum[rt] *= by;
 #pragma unroll
-            for (int t = 0; t < 8; ++t) o[rt][t] *= f;
+            for (int t = 0; t < 8; ++t) o[rt][t] *= by;
         }
         const float by = kLift - ref[rt];
+        f8v w;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(x[t][i] + by);
-                sum[rt] += e;
-                w[t >> 1][4 * (t & 1) + i] = e;
-            }
-    };
-
-    float v_top = two_to(-126);        // values are accumulated over the largest scale so far: codes times 2^0 and less fit binary16
-    const int seg_groups = kSegment >> (6 - a.page_log2);
-    for (int s0 = ga; s0 < gb; s0 += seg_groups) {
-        const int s1 = min(s0 + seg_groups, gb), first_block = s0 << (6 - a.page_log2), blocks = (s1 - s0) << (6 - a.page_log2);
-        __syncthreads();
-        if (threadIdx.x == 0) s_top = __float_as_uint(v_top);
-        __syncthreads();
-        int holes = 0;
-        float top = 0.f;
-        for (int i = threadIdx.x; i < blocks; i += 64 * NW) {
-            const int block = first_block + i;
-            int page = -1;
-            if ((int64_t)block * P < closed) page = page_of(p, b, block);
-            float ks = 0.f, vs = 0.f;
-            if (page >= 0) { ks = p.k_scale[(int64_t)page * p.n_kv_heads + h]; vs = p.v_scale[(int64_t)page * p.n_kv_heads + h]; }
-            if (page < 0 && (int64_t)block * P < closed && block * P + P > lo) holes = 1;
-            sh.seg.page[i] = page; sh.seg.k_scale[i] = ks; sh.seg.v_scale[i] = vs;
-            top = fmaxf(top, vs);
-        }
-        atomicMax(&s_top, __float_as_uint(top));
-        holes = __syncthreads_or(holes);
-        top = __uint_as_float(s_top);
-        if (top > v_top) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int t = 0; t < 8; ++t) o[rt][t] *= v_top / top;
-            v_top = top;
-        }
-        const float v_over = 1.f / v_top;
-
-        u4v kw[8], vw[8];
-        auto load_keys = [&](int g) {
-            const int token = 16 * (c >> 2) + (c & 3), at = (g - s0) * 64 + token;
-            const int page = max(sh.seg.page[at >> a.page_log2], 0);
-            const uint8_t* k = p.k_codes + (((int64_t)page * p.n_kv_heads + h) * P + (at & (P - 1))) * kHeadDim + 16 * kb;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) kw[2 * t + half] = *reinterpret_cast<const u4v*>(k + 4 * t * kHeadDim + 64 * half);
-        };
-        auto load_values = [&](int g) {
-            const int at = (g - s0) * 64 + 16 * kb;
-            const int page = max(sh.seg.page[at >> a.page_log2], 0);
-            const uint8_t* v = p.v_codes + ((int64_t)page * p.n_kv_heads + h) * (P * kHeadDim) + c * P + (at & (P - 1));
-#pragma unroll
-            for (int t = 0; t < 8; ++t) vw[t] = *reinterpret_cast<const u4v*>(v + 16 * t * P);
-        };
-        int g = s0 + wave;
-        if (g < s1) { load_keys(g); load_values(g); }
-        for (; g < s1; g += NW) {
-            const int mine = ((g - s0) * 64 + 16 * kb) >> a.page_log2;       // the page of the lane's 16 tokens
-            const float ks = sh.seg.k_scale[mine], vs = sh.seg.v_scale[mine] * v_over;
-            const bool there = sh.seg.page[mine] >= 0;
-            const int next = g + NW;
-            f4v x[RT][4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) x[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const u4v w = kw[2 * t + half];
-                    const h8v k0 = halves_of_codes<INT8>(w[0], w[1], 1.f), k1 = halves_of_codes<INT8>(w[2], w[3], 1.f);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[rt][2 * half], x[rt][t], 0, 0, 0);
-                        x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[rt][2 * half + 1], x[rt][t], 0, 0, 0);
-                    }
-                }
-            }
-            if (next < s1) load_keys(next);
-            const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
-            h8v w[RT][2];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float f = ks * scale[rt];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) x[rt][t] *= f;
-                if (edge) {
-                    const int low = a.window > 0 ? position[rt] - a.window : -1;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int token = 64 * g + 16 * kb + 4 * t + i;
-                            if (!(there && token <= position[rt] && token > low)) x[rt][t][i] = -INFINITY;
-                        }
-                }
-                f8v e[2];
-                weigh(rt, x[rt], e);
-                w[rt][0] = __builtin_convertvector(e[0], h8v);
-                w[rt][1] = __builtin_convertvector(e[1], h8v);
-            }
-            if (edge && !there) {      // (nothing was stored there: it may hold NaN)
-#pragma unroll
-                for (int t = 0; t < 8; ++t) vw[t] = u4v{0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const h8v v0 = halves_of_codes<INT8>(vw[t][0], vw[t][1], vs), v1 = halves_of_codes<INT8>(vw[t][2], vw[t][3], vs);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[rt][0], o[rt][t], 0, 0, 0);
-                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[rt][1], o[rt][t], 0, 0, 0);
-                }
-            }
-            if (next < s1) load_values(next);
-        }
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], f, by));
+        sum[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        return w;
     }
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int t = 0; t < 8; ++t) o[rt][t] *= v_top;
-    __syncthreads();
+};
+// (a masked product is minus infinity: the factor must not be 0, also where a block of zeros has the smallest scale)
+__device__ __forceinline__ float logit_factor(float key_scale, float row_scale) { return fmaxf(key_scale * row_scale, 1e-36f); }
 
-    // The open tokens, by one wave of the last split, in the rows' own type; bfloat16 weights are two numbers each, so that they are as exact as the others.
-    const int slot = slot_of(p, b), open = max(hi - begin, 0);
-    if (open > 0 && slot >= 0 && split == active - 1 && wave == (gb - ga) % NW) {
-        const int64_t at = ((int64_t)slot * p.n_kv_heads + h) * (2 * P * kHeadDim);
-        const int from = begin & (2 * P - 1);            // (a block's rows are next to each other)
-        for (int i = lane; i < 64 * 16; i += 64) {
-            const int t = i >> 4;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (t < open) v = *reinterpret_cast<const uint4*>(p.open_v + at + (from + t) * kHeadDim + 8 * (i & 15));
-            *reinterpret_cast<uint4*>(&sh.open_v[t][8 * (i & 15)]) = v;
-        }
-        uint4 kr[4][4];
+// Row r of a workgroup: new token r / gq of its piece, query head r % gq of the KV head's.
+__device__ __forceinline__ const uint16_t* query_at(const AttnArgs& a, const Range& w, int h, int r) {
+    const int i = r / a.p.gq;
+    return a.q + (int64_t)(w.seq.row0 + w.i0 + (i < w.n ? i : 0)) * a.q_stride + (h * a.p.gq + r % a.p.gq) * kHeadDim;
+}
+__device__ __forceinline__ int64_t result_at(const AttnArgs& a, const Range& w, int h, int r) {
+    return (int64_t)(w.seq.row0 + w.i0 + r / a.p.gq) * (a.p.gq * a.p.n_kv_heads) + h * a.p.gq + r % a.p.gq;
+}
+template <bool BF>
+__device__ __forceinline__ void store_out(const AttnArgs& a, const Range& w, int h, int r, int t, int kb, f4v x, float by) {
+    x *= by;
+    uint2 y;
+    if constexpr (BF) {
+        typedef __bf16 b4v __attribute__((ext_vector_type(4)));
+        y = __builtin_bit_cast(uint2, __builtin_convertvector(x, b4v));
+    } else {
+        typedef _Float16 h4v __attribute__((ext_vector_type(4)));
+        y = __builtin_bit_cast(uint2, __builtin_convertvector(x, h4v));
+    }
+    *reinterpret_cast<uint2*>(a.out + result_at(a, w, h, r) * kHeadDim + 16 * t + 4 * kb) = y;
+}
+
+// A row's query as binary16 fragments: 8 channels from 32 s + 8 kb (or, WIDE, 64 (s >> 1) + 16 kb + 8 (s & 1): 16 bytes of a key at a time) for the lane's
+// column.  A bfloat16 row over a power of two is a row of binary16 numbers, but for what is below 2^-24 of its largest: so codes meet it without a
+// conversion to bfloat16, and the logits' factor takes the power back.
+template <bool BF, bool WIDE>
+__device__ __forceinline__ float query_fragments(const uint16_t* q, bool there, int kb, float logit_scale, h8v (&out)[4]) {
+    uint4 w[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int off = 16 * (c >> 2) + 4 * t + (c & 3);
+    for (int s = 0; s < 4; ++s)
+        w[s] = there ? *reinterpret_cast<const uint4*>(q + (WIDE ? 64 * (s >> 1) + 16 * kb + 8 * (s & 1) : 32 * s + 8 * kb)) : make_uint4(0, 0, 0, 0);
+    if constexpr (BF) {
+        float m = 0.f;
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                kr[t][s] = off < open ? *reinterpret_cast<const uint4*>(p.open_k + at + (from + off) * kHeadDim + 64 * (s >> 1) + 16 * kb + 8 * (s & 1)) : make_uint4(0, 0, 0, 0);
+        for (int s = 0; s < 4; ++s) {
+            const f8v x = numbers<true>(w[s]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x[j]));
         }
-        uint4 w[RT][2], w_rest[RT][2];
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -120), 120);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) out[s] = __builtin_convertvector(numbers<true>(w[s]) * two_to(-e), h8v);
+        return logit_scale * two_to(e);
+    } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) out[s] = __builtin_bit_cast(h8v, w[s]);
+        return logit_scale;
+    }
+}
+
+// Open tokens, for one wave's rows r0 ..: in the rows' own type; bfloat16 weights are two numbers each, so that they are as exact as binary16 ones.
+// Values come from LDS ([64][kHeadDim + 8], zeros behind the last).
+typedef uint16_t OpenValues[64][kHeadDim + 8];
+__device__ __forceinline__ void stage_open_values(const AttnArgs& a, const Range& w, int h, int slot, OpenValues& s_v, int thread, int threads) {
+    const int P = 1 << a.page_log2, from = w.begin & (2 * P - 1);            // (a block's rows are next to each other)
+    const uint16_t* v = a.p.open_v + ((int64_t)slot * a.p.n_kv_heads + h) * (2 * P * kHeadDim) + from * kHeadDim;
+    for (int i = thread; i < (w.open + 31) / 32 * 32 * 16; i += threads) {
+        const int t = i >> 4;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (t < w.open) x = *reinterpret_cast<const uint4*>(v + t * kHeadDim + 8 * (i & 15));
+        *reinterpret_cast<uint4*>(&s_v[t][8 * (i & 15)]) = x;
+    }
+}
+template <bool BF, int RT>
+__device__ __forceinline__ void attend_open(const AttnArgs& a, const Range& w, int h, int slot, const OpenValues& s_v, int r0, Sums<RT>& st) {
+    const int lane = threadIdx.x & 63, c = lane & 15, kb = lane >> 4, P = 1 << a.page_log2, from = w.begin & (2 * P - 1);
+    const uint16_t* keys = a.p.open_k + ((int64_t)slot * a.p.n_kv_heads + h) * (2 * P * kHeadDim) + from * kHeadDim;
+    // 32 tokens at a time, in their order: of tile t of them a lane has tokens 16 t + 4 kb .. + 3.
+#pragma unroll 1
+    for (int t0 = 0; t0 < w.open; t0 += 32) {
+        f4v x[RT][2];
+        uint4 k[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int off = t0 + 16 * t + c;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) k[t][s] = off < w.open ? *reinterpret_cast<const uint4*>(keys + off * kHeadDim + 32 * s + 8 * kb) : make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            uint4 qr[4];
+            const int r = r0 + 16 * rt + c, i = r / a.p.gq;
+            const uint16_t* rows = query_at(a, w, h, r);
+            const int position = i < w.n ? w.first + i : -1, low = a.window > 0 ? position - a.window : -1;
+            uint4 q[4];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if constexpr (BF) qr[s] = position[rt] >= 0 ? *reinterpret_cast<const uint4*>(a.q + q_at[rt] + 64 * (s >> 1) + 8 * (s & 1)) : make_uint4(0, 0, 0, 0);
-                else qr[s] = __builtin_bit_cast(uint4, q[rt][s]);
-            }
-            const int low = a.window > 0 ? position[rt] - a.window : -1;
-            f4v x[4];
+            for (int s = 0; s < 4; ++s) q[s] = i < w.n ? *reinterpret_cast<const uint4*>(rows + 32 * s + 8 * kb) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                x[t] = f4v{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < 2; ++t) {
+                x[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s < 4; ++s) x[t] = product_of_rows<BF>(kr[t][s], qr[s], x[t]);
+                for (int s = 0; s < 4; ++s) x[rt][t] = product_of_rows<BF>(k[t][s], q[s], x[rt][t]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int off = 16 * kb + 4 * t + i, token = begin + off;
-                    x[t][i] = off < open && token <= position[rt] && token > low ? x[t][i] * a.logit_scale : -INFINITY;
+                for (int j = 0; j < 4; ++j) {
+                    const int off = t0 + 16 * t + 4 * kb + j, token = w.begin + off;
+                    const bool hidden = (off >= w.open) | (token > position) | (token <= low);
+                    x[rt][t][j] = hidden ? -INFINITY : x[rt][t][j];
                 }
             }
-            f8v e[2];
-            weigh(rt, x, e);
+        }
+        uint4 e[RT], e_rest[RT];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                w[rt][s] = rounded<BF>(e[s]);
-                if constexpr (BF) w_rest[rt][s] = rounded<BF>(e[s] - numbers<BF>(w[rt][s]));
+        for (int rt = 0; rt < RT; ++rt) {
+            const f8v y = st.weigh(rt, x[rt], a.logit_scale);
+            e[rt] = rounded<BF>(y);
+            if constexpr (BF) e_rest[rt] = rounded<BF>(y - numbers<BF>(e[rt]));
+        }
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = t0 + 16 * (j >> 1) + 4 * kb + 2 * (j & 1);
+                v[j] = (uint32_t)s_v[r][16 * t + c] | (uint32_t)s_v[r + 1][16 * t + c] << 16;
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                st.o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), e[rt], st.o[rt][t]);
+                if constexpr (BF) st.o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), e_rest[rt], st.o[rt][t]);
             }
         }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                uint32_t v[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    v[j] = (uint32_t)sh.open_v[16 * kb + 8 * s + 2 * j][16 * t + c] | (uint32_t)sh.open_v[16 * kb + 8 * s + 2 * j + 1][16 * t + c] << 16;
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), w[rt][s], o[rt][t]);
-                    if constexpr (BF) o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), w_rest[rt][s], o[rt][t]);
-                }
-            }
     }
-    __syncthreads();
+}
 
-    // ---- the waves' results together ----
+// Numbers and scales of a stretch of pages, in LDS.
+constexpr int kSegment = 512;
+struct Segment {
+    int page[kSegment];
+    float k_scale[kSegment], v_scale[kSegment];
+};
+// In two steps, so that codes can be requested before the scales have come.  Returns whether a block that is seen has no page.
+template <int THREADS>
+__device__ __forceinline__ bool look_up_pages(const AttnArgs& a, const Range& w, int first_block, int blocks, Segment& seg, int (&mine)[kSegment / THREADS]) {
+    int holes = 0;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        sum[rt] += __shfl_xor(sum[rt], 16);
-        sum[rt] += __shfl_xor(sum[rt], 32);
-        if (kb == 0) { sh.join.ref[wave][16 * rt + c] = ref[rt]; sh.join.sum[wave][16 * rt + c] = sum[rt]; }
+    for (int u = 0; u < kSegment / THREADS; ++u) {
+        const int i = threadIdx.x + THREADS * u, block = first_block + i;
+        mine[u] = -1;
+        if (i < blocks && (block << a.page_log2) < w.closed) {
+            mine[u] = page_of(a.p, w.seq.b, block);
+            if (mine[u] < 0 && (block + 1) << a.page_log2 > w.lo) holes = 1;
+        }
+        seg.page[i] = mine[u];
     }
+    return __syncthreads_or(holes) != 0;
+}
+// top: the largest scale of values so far, of all threads in *s_top
+template <int THREADS>
+__device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float top, Segment& seg, const int (&mine)[kSegment / THREADS], unsigned int* s_top) {
+    float most = top;
+#pragma unroll
+    for (int u = 0; u < kSegment / THREADS; ++u) {
+        float ks = 1.f, vs = 0.f;
+        if (mine[u] >= 0) { ks = a.p.k_scale[(int64_t)mine[u] * a.p.n_kv_heads + h]; vs = a.p.v_scale[(int64_t)mine[u] * a.p.n_kv_heads + h]; }
+        const int i = threadIdx.x + THREADS * u;
+        seg.k_scale[i] = ks; seg.v_scale[i] = vs;
+        most = fmaxf(most, vs);
+    }
+    if (most > top) atomicMax(s_top, __float_as_uint(most));
     __syncthreads();
-    const int group = piece * p.n_kv_heads + h, per_row = p.gq;
-    const Partials parts(a, group, RT);
-    auto out_at = [&](int r) { return ((int64_t)(seq.row0 + i0 + r / per_row) * p.gq * p.n_kv_heads + h * p.gq + r % per_row); };
-    const int rows = n * p.gq;
-    auto store_out = [&](int r, int t, f4v x, float by) {
-        x *= by;
-        uint2 w;
-        if constexpr (BF) {
-            typedef __bf16 b4v __attribute__((ext_vector_type(4)));
-            w = __builtin_bit_cast(uint2, __builtin_convertvector(x, b4v));
-        } else {
-            typedef _Float16 h4v __attribute__((ext_vector_type(4)));
-            w = __builtin_bit_cast(uint2, __builtin_convertvector(x, h4v));
-        }
-        *reinterpret_cast<uint2*>(a.out + out_at(r) * kHeadDim + 16 * t + 4 * kb) = w;
-    };
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        float top = kNegBig, total = 0.f;
-        for (int w = 0; w < NW; ++w) top = fmaxf(top, sh.join.ref[w][16 * rt + c]);
-        for (int w = 0; w < NW; ++w) total = __builtin_fmaf(sh.join.sum[w][16 * rt + c], __builtin_amdgcn_exp2f(sh.join.ref[w][16 * rt + c] - top), total);
-        const float f = __builtin_amdgcn_exp2f(ref[rt] - top);
-        if (rt) __syncthreads();
-#pragma unroll
-        for (int t = 0; t < 8; ++t) sh.join.o[wave][t][lane] = o[rt][t] * f;
-        __syncthreads();
-        const int r = 16 * rt + c;
-        if (wave == 0 && kb == 0) {
-            if (active > 1) parts.put_state(split, r, top, total);
-            else if (a.lse && r < rows) a.lse[out_at(r)] = log_sum(top, total);
-        }
-        for (int t = wave; t < 8; t += NW) {
-            f4v x = {0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < NW; ++w) x += sh.join.o[w][t][lane];
-            if (active > 1) parts.put_output(split, (8 * rt + t) * 64 + lane, x);
-            else if (r < rows) store_out(r, t, x, inverse_sum(total));
-        }
-    }
-    if (active == 1) return;
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(*s_top));
+}
 
-    // ---- the last workgroup to arrive joins the splits, in their order ----
-    // The partials were stored past this die's L2, and the wait returns when the stores have been acknowledged from there; so whoever sees the
-    // counter sees them, with loads that do not look into its own L2.
+// The last workgroup of a piece and head to arrive joins their splits, in their order.
+// The partials were stored past this die's L2, and the wait returns when the stores have been acknowledged from there; so whoever sees the
+// counter sees them, with loads that do not look into its own L2.
+template <bool BF>
+__device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, int h, int row_tiles, const Partials& parts, int* s_last) {
+    const int active = w.active;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
-        unsigned int* count = &a.arrivals[group];
+        unsigned int* count = &a.arrivals[w.part_of_head(a, h)];
         const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = before == (unsigned)(active - 1);
-        if (s_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *s_last = before == (unsigned)(active - 1);
+        if (*s_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
-    if (!s_last) return;
-    for (int item = threadIdx.x; item < RT * 512; item += 64 * NW) {
+    if (!*s_last) return;
+    const int c = threadIdx.x & 15, kb = (threadIdx.x & 63) >> 4, rows = w.n * a.p.gq;
+    for (int item = threadIdx.x; item < row_tiles * 512; item += blockDim.x) {
         const int r = 16 * (item >> 9) + c;
         float top = kNegBig, total = 0.f;
         f4v x = {0.f, 0.f, 0.f, 0.f};
@@ -475,49 +451,425 @@ __global__ __launch_bounds__(64 * rows_waves<RT>()) void paged_rows(const AttnAr
             x *= f; total *= f;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float w = s0 + u < active ? __builtin_amdgcn_exp2f(m[u].x - higher) : 0.f;
-                x += v[u] * w;
-                total = __builtin_fmaf(m[u].y, w, total);
+                const float by = s0 + u < active ? __builtin_amdgcn_exp2f(m[u].x - higher) : 0.f;
+                x += v[u] * by;
+                total = __builtin_fmaf(m[u].y, by, total);
             }
             top = higher;
         }
         if (r < rows) {
-            store_out(r, (item >> 6) & 7, x, inverse_sum(total));
-            if (a.lse && (item & 0x1C0) == 0 && kb == 0) a.lse[out_at(r)] = log_sum(top, total);
+            store_out<BF>(a, w, h, r, (item >> 6) & 7, kb, x, inverse_sum(total));
+            if (a.lse && (item & 0x1C0) == 0 && kb == 0) a.lse[result_at(a, w, h, r)] = log_sum(top, total);
         }
     }
 }
 
+// ---- few rows: the tokens are split over waves and workgroups ----
+//
+// A wave takes 64 tokens at a time.  S^T = K Q^T by products of 16 tokens and 16 rows: a lane's column is a row (query head and new token) and its
+// group kb of 16 lanes holds tokens 16 kb .. 16 kb + 15, in an order that makes its logits, turned into weights, the second operand of
+// O^T = V^T P^T without leaving the lane; the first operand is 16 consecutive bytes of a channel, as pages store values.
+constexpr int kRowsWaves = 4;
+
+template <int RT, int NW>
+union RowsShared {
+    struct { h8v q[RT][4][64]; Segment seg; } run;
+    OpenValues open_v;
+    struct { f4v o[NW][8][64]; float ref[NW][16 * RT], sum[NW][16 * RT]; } join;
+};
+
+template <bool BF, bool INT8, int RT>
+__global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(const AttnArgs a) {
+    constexpr int NW = kRowsWaves, THREADS = 64 * NW;
+    __shared__ RowsShared<RT, NW> sh;
+    __shared__ SlotShared s_slot;
+    __shared__ int s_last;
+    __shared__ unsigned int s_top;
+    const PageArgs& p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kb = lane >> 4;
+    const int h = blockIdx.x % p.n_kv_heads, P = 1 << a.page_log2;
+    Range w;
+    if (!w.find(a, blockIdx.x / p.n_kv_heads, s_slot)) return;
+    const int ga = w.ga, gb = w.gb, active = w.active, split = w.split;
+    const int seen_by_all = min(w.first + 1, w.closed), hidden_to_some = a.window > 0 ? w.last - a.window + 1 : 0;
+
+    float scale[RT];           // of logits in the exponent's base
+    int position[RT];          // of the lane's row; -1 where there is none
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = 16 * rt + c, i = r / p.gq;
+        position[rt] = i < w.n ? w.first + i : -1;
+        h8v q[4];
+        scale[rt] = query_fragments<BF, true>(query_at(a, w, h, r), i < w.n, kb, a.logit_scale, q);
+        if (wave == 0) {       // (in LDS: a wave reads a fragment once for all tokens of a group)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) sh.run.q[rt][s][lane] = q[s];
+        }
+    }
+    Sums<RT> st;
+    st.clear();
+
+    float v_top = two_to(-126);        // values are accumulated over the largest scale so far: codes times 2^0 and less fit binary16
+    Segment& seg = sh.run.seg;
+    const int seg_groups = kSegment >> (6 - a.page_log2);
+    for (int s0 = ga; s0 < gb; s0 += seg_groups) {
+        const int s1 = min(s0 + seg_groups, gb);
+        int mine[kSegment / THREADS];
+        __syncthreads();
+        if (threadIdx.x == 0) s_top = __float_as_uint(v_top);
+        const bool holes = look_up_pages<THREADS>(a, w, s0 << (6 - a.page_log2), (s1 - s0) << (6 - a.page_log2), seg, mine);
+
+        u4v kw[8], vw[8];
+        auto load_keys = [&](int g) {
+            const int token = 16 * (c >> 2) + (c & 3), at = (g - s0) * 64 + token;
+            const int page = max(seg.page[at >> a.page_log2], 0);
+            const uint8_t* k = p.k_codes + (((int64_t)page * p.n_kv_heads + h) * P + (at & (P - 1))) * kHeadDim + 16 * kb;
+            if (a.once) {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) kw[t] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(k + 4 * (t >> 1) * kHeadDim + 64 * (t & 1)));
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) kw[t] = *reinterpret_cast<const u4v*>(k + 4 * (t >> 1) * kHeadDim + 64 * (t & 1));
+            }
+        };
+        auto load_values = [&](int g) {
+            const int at = (g - s0) * 64 + 16 * kb;
+            const int page = max(seg.page[at >> a.page_log2], 0);
+            const uint8_t* v = p.v_codes + ((int64_t)page * p.n_kv_heads + h) * (P * kHeadDim) + c * P + (at & (P - 1));
+            if (a.once) {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) vw[t] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(v + 16 * t * P));
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) vw[t] = *reinterpret_cast<const u4v*>(v + 16 * t * P);
+            }
+        };
+        int g = s0 + wave;
+        if (g < s1) { load_keys(g); load_values(g); }
+        const float top = look_up_scales<THREADS>(a, h, v_top, seg, mine, &s_top);
+        if (top > v_top) {
+            st.times(v_top / top);
+            v_top = top;
+        }
+        const float v_over = 1.f / v_top;
+        for (; g < s1; g += NW) {
+            const int at = ((g - s0) * 64 + 16 * kb) >> a.page_log2;       // the page of the lane's 16 tokens
+            const float ks = seg.k_scale[at], vs = seg.v_scale[at] * v_over;
+            const bool there = seg.page[at] >= 0;
+            const int next = g + NW;
+            const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
+            if (edge && !there) {      // (nothing was stored there: it may hold NaN)
+#pragma unroll
+                for (int t = 0; t < 8; ++t) vw[t] = u4v{0, 0, 0, 0};
+            }
+            // Half of the tokens at a time, tokens 16 kb + 8 half .. + 7 of a lane: fewer registers.
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f4v x[RT][2];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    h8v q[RT];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) q[rt] = sh.run.q[rt][s][lane];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const u4v y = kw[2 * (2 * half + t) + (s >> 1)];
+                        const h8v k = halves_of_codes<INT8>(y[2 * (s & 1)], y[2 * (s & 1) + 1], 1.f);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt], x[rt][t], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);      // (what is converted ahead of its product costs registers)
+                }
+                if (half == 1 && next < s1) load_keys(next);
+                h8v e[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    if (edge) {
+                        const int low = a.window > 0 ? position[rt] - a.window : -1;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int token = 64 * g + 16 * kb + 8 * half + j;
+                            const bool hidden = !there | (token > position[rt]) | (token <= low);
+                            x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
+                        }
+                    }
+                    e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], logit_factor(ks, scale[rt])), h8v);
+                }
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    const h8v v = halves_of_codes<INT8>(vw[t][2 * half], vw[t][2 * half + 1], vs);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, e[rt], st.o[rt][t], 0, 0, 0);
+                    if (t & 1) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (next < s1) load_values(next);
+        }
+    }
+    st.times(v_top);
+    __syncthreads();
+    const int slot = w.open > 0 && split == active - 1 ? slot_of(p, w.seq.b) : -1;
+    if (slot >= 0 && wave == (gb - ga) % NW) {       // (a wave that has the fewest groups)
+        stage_open_values(a, w, h, slot, sh.open_v, lane, 64);
+        __builtin_amdgcn_wave_barrier();
+        attend_open<BF, RT>(a, w, h, slot, sh.open_v, 0, st);
+    }
+    __syncthreads();
+
+    // ---- the waves' results together ----
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        st.sum[rt] += __shfl_xor(st.sum[rt], 16);
+        st.sum[rt] += __shfl_xor(st.sum[rt], 32);
+        if (kb == 0) { sh.join.ref[wave][16 * rt + c] = st.ref[rt]; sh.join.sum[wave][16 * rt + c] = st.sum[rt]; }
+    }
+    __syncthreads();
+    const int rows = w.n * p.gq;
+    const Partials parts(a, w.part_of_head(a, h), active, RT);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float top = kNegBig, total = 0.f;
+        for (int v = 0; v < NW; ++v) top = fmaxf(top, sh.join.ref[v][16 * rt + c]);
+        for (int v = 0; v < NW; ++v) total = __builtin_fmaf(sh.join.sum[v][16 * rt + c], __builtin_amdgcn_exp2f(sh.join.ref[v][16 * rt + c] - top), total);
+        const float f = __builtin_amdgcn_exp2f(st.ref[rt] - top);
+        if (rt) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 8; ++t) sh.join.o[wave][t][lane] = st.o[rt][t] * f;
+        __syncthreads();
+        const int r = 16 * rt + c;
+        if (wave == 0 && kb == 0) {
+            if (active > 1) parts.put_state(split, r, top, total);
+            else if (a.lse && r < rows) a.lse[result_at(a, w, h, r)] = log_sum(top, total);
+        }
+        for (int t = wave; t < 8; t += NW) {
+            f4v x = {0.f, 0.f, 0.f, 0.f};
+            for (int v = 0; v < NW; ++v) x += sh.join.o[v][t][lane];
+            if (active > 1) parts.put_output(split, (8 * rt + t) * 64 + lane, x);
+            else if (r < rows) store_out<BF>(a, w, h, r, t, kb, x, inverse_sum(total));
+        }
+    }
+    if (active > 1) join_splits<BF>(a, w, h, RT, parts, &s_last);
+}
+
+// ---- many rows: the rows are split over waves, which share the tokens ----
+//
+// Each of four waves has 16 RT rows to itself and goes over all tokens of its workgroup, 64 at a time.  Codes become binary16 numbers once, on their way
+// into LDS, where the tile after the next is being built while two are in use; products and layouts are those of the kernel above.
+constexpr int kTileWaves = 4;
+struct TilesShared {
+    union {
+        struct { h8v k[2][64 * 16], v[2][64 * 16]; } tile;
+        OpenValues open_v;
+    };
+    Segment seg;
+};
+// Where 8 channels (chunk) of a key, and 8 tokens (chunk) of a channel, lie in a tile: 16 lanes of consecutive rows read 16 different places of 256 bytes.
+__device__ __forceinline__ int key_place(int row, int chunk) { return row * 16 + (chunk ^ (row & 15)); }
+__device__ __forceinline__ int value_place(int channel, int chunk) { return (channel >> 1) * 16 + (((channel & 1) * 8 + chunk) ^ ((channel >> 1) & 15)); }
+
+template <bool BF, bool INT8, int RT>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs a) {
+    constexpr int NW = kTileWaves, THREADS = 64 * NW, AHEAD = RT == 1 ? 2 : 1;      // tiles of codes on their way
+    __shared__ TilesShared sh;
+    __shared__ SlotShared s_slot;
+    __shared__ int s_last;
+    __shared__ unsigned int s_top;
+    const PageArgs& p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kb = lane >> 4, P = 1 << a.page_log2;
+    // Heads take turns (with eight of them each die has one head's pages in its L2); later pieces, which see more, begin first.
+    const int h = blockIdx.x % p.n_kv_heads;
+    Range w;
+    if (!w.find(a, a.slots - 1 - blockIdx.x / p.n_kv_heads, s_slot)) return;
+    const int ga = w.ga, gb = w.gb, active = w.active, split = w.split;
+
+    const int r0 = 16 * RT * wave, rows = w.n * p.gq;
+    // (of this wave's rows; a wave without any sees nothing)
+    const int my_first = w.first + r0 / p.gq, my_last = r0 < rows ? w.first + (min(r0 + 16 * RT, rows) - 1) / p.gq : -1;
+    const int seen_by_all = min(my_first + 1, w.closed), hidden_to_some = a.window > 0 ? my_last - a.window + 1 : 0, my_lo = a.window > 0 ? my_first - a.window + 1 : 0;
+    h8v q[RT][4];
+    float scale[RT];
+    int position[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + 16 * rt + c, i = r / p.gq;
+        position[rt] = i < w.n ? w.first + i : -1;
+        scale[rt] = query_fragments<BF, false>(query_at(a, w, h, r), i < w.n, kb, a.logit_scale, q[rt]);
+    }
+    Sums<RT> st;
+    st.clear();
+
+    float v_top = two_to(-126);
+    Segment& seg = sh.seg;
+    const int seg_groups = kSegment >> (6 - a.page_log2);
+    for (int s0 = ga; s0 < gb; s0 += seg_groups) {
+        const int s1 = min(s0 + seg_groups, gb);
+        int mine[kSegment / THREADS];
+        __syncthreads();
+        if (threadIdx.x == 0) s_top = __float_as_uint(v_top);
+        const bool holes = look_up_pages<THREADS>(a, w, s0 << (6 - a.page_log2), (s1 - s0) << (6 - a.page_log2), seg, mine);
+
+        // A thread's share of a tile: 16 bytes of two keys, and 16 tokens of two channels.
+        u4v kw[AHEAD][2], vw[AHEAD][2];
+        auto key_token = [&](int u) { return (threadIdx.x + THREADS * u) >> 3; };
+        auto value_bytes = [&](int u) { return (threadIdx.x + THREADS * u) * 16; };      // into the tile's pages, [channel][P] each
+        auto request = [&](int slot, int g) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int at = (g - s0) * 64 + key_token(u);
+                const int page = max(seg.page[at >> a.page_log2], 0);
+                kw[slot][u] = *reinterpret_cast<const u4v*>(p.k_codes + (((int64_t)page * p.n_kv_heads + h) * P + (at & (P - 1))) * kHeadDim + 16 * (threadIdx.x & 7));
+                const int part = value_bytes(u) >> (a.page_log2 + 7), v_page = max(seg.page[(((g - s0) * 64) >> a.page_log2) + part], 0);
+                vw[slot][u] = *reinterpret_cast<const u4v*>(p.v_codes + ((int64_t)v_page * p.n_kv_heads + h) * (P * kHeadDim) + (value_bytes(u) & (P * kHeadDim - 1)));
+            }
+        };
+        float v_over;
+        auto build = [&](int slot, int g) {
+            h8v* k = sh.tile.k[(g - s0) & 1];
+            h8v* v = sh.tile.v[(g - s0) & 1];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                // (the order of a tile's rows: the kernel above)
+                const int token = key_token(u), row = 16 * ((token >> 2) & 3) + 4 * (token >> 4) + (token & 3), m = threadIdx.x & 7;
+                k[key_place(row, 2 * m)] = halves_of_codes<INT8>(kw[slot][u][0], kw[slot][u][1], 1.f);
+                k[key_place(row, 2 * m + 1)] = halves_of_codes<INT8>(kw[slot][u][2], kw[slot][u][3], 1.f);
+                const int part = value_bytes(u) >> (a.page_log2 + 7), in = value_bytes(u) & (P * kHeadDim - 1), page_at = (((g - s0) * 64) >> a.page_log2) + part;
+                const float vs = seg.v_scale[page_at] * v_over;
+                u4v y = vw[slot][u];
+                if (seg.page[page_at] < 0) y = u4v{0, 0, 0, 0};      // (nothing was stored there: it may hold NaN)
+                const int channel = in >> a.page_log2, chunk = ((part << a.page_log2) + (in & (P - 1))) >> 3;
+                v[value_place(channel, chunk)] = halves_of_codes<INT8>(y[0], y[1], vs);
+                v[value_place(channel, chunk + 1)] = halves_of_codes<INT8>(y[2], y[3], vs);
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (s0 + u < s1) request(u, s0 + u);
+        const float top = look_up_scales<THREADS>(a, h, v_top, seg, mine, &s_top);
+        if (top > v_top) {
+            st.times(v_top / top);
+            v_top = top;
+        }
+        v_over = 1.f / v_top;
+        build(0, s0);
+        if (s0 + AHEAD < s1) request(0, s0 + AHEAD);
+        __syncthreads();
+        for (int g0 = s0; g0 < s1; g0 += AHEAD) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int g = g0 + u;
+                if (g >= s1) break;
+                if (64 * g <= my_last && 64 * g + 63 >= my_lo) {
+                    const h8v* k_tile = sh.tile.k[(g - s0) & 1];
+                    const h8v* v_tile = sh.tile.v[(g - s0) & 1];
+                    const int at = ((g - s0) * 64 + 16 * kb) >> a.page_log2;
+                    const float ks = seg.k_scale[at];
+                    const bool there = seg.page[at] >= 0;
+                    const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        f4v x[RT][2];
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 0; s < 4; ++s)
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) {
+                                const h8v k = k_tile[key_place(16 * (2 * half + t) + c, 4 * s + kb)];
+#pragma unroll
+                                for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][s], x[rt][t], 0, 0, 0);
+                            }
+                        h8v e[RT];
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            if (edge) {
+                                const int low = a.window > 0 ? position[rt] - a.window : -1;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const int token = 64 * g + 16 * kb + 8 * half + j;
+                                    const bool hidden = !there | (token > position[rt]) | (token <= low);
+                                    x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
+                                }
+                            }
+                            e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], logit_factor(ks, scale[rt])), h8v);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 8; ++t) {
+                            const h8v v = v_tile[value_place(16 * t + c, 2 * kb + half)];
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, e[rt], st.o[rt][t], 0, 0, 0);
+                        }
+                    }
+                }
+                if (g + 1 < s1) build((u + 1) % AHEAD, g + 1);
+                if (g + 1 + AHEAD < s1) request((u + 1) % AHEAD, g + 1 + AHEAD);
+                __syncthreads();
+            }
+        }
+    }
+    st.times(v_top);
+    const int slot = w.open > 0 && split == active - 1 ? slot_of(p, w.seq.b) : -1;
+    if (slot >= 0) {
+        __syncthreads();
+        stage_open_values(a, w, h, slot, sh.open_v, threadIdx.x, THREADS);
+        __syncthreads();
+        if (my_last >= w.begin) attend_open<BF, RT>(a, w, h, slot, sh.open_v, r0, st);
+    }
+    const Partials parts(a, w.part_of_head(a, h), active, RT * NW);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float total = st.sum[rt];
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        const int r = r0 + 16 * rt + c;
+        if (kb == 0) {
+            if (active > 1) parts.put_state(split, r, st.ref[rt], total);
+            else if (a.lse && r < rows) a.lse[result_at(a, w, h, r)] = log_sum(st.ref[rt], total);
+        }
+        const float by = inverse_sum(total);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            if (active > 1) parts.put_output(split, (8 * (RT * wave + rt) + t) * 64 + lane, st.o[rt][t]);
+            else if (r < rows) store_out<BF>(a, w, h, r, t, kb, st.o[rt][t], by);
+        }
+    }
+    if (active > 1) join_splits<BF>(a, w, h, RT * NW, parts, &s_last);
+}
+
 template <bool BF, bool INT8>
-hipError_t paged_rows_form(const AttnArgs& a, int row_tiles, dim3 grid, hipStream_t stream) {
-    if (row_tiles == 1) paged_rows<BF, INT8, 1><<<grid, dim3(64 * rows_waves<1>()), 0, stream>>>(a);
-    else if (row_tiles == 2) paged_rows<BF, INT8, 2><<<grid, dim3(64 * rows_waves<2>()), 0, stream>>>(a);
-    else paged_rows<BF, INT8, 4><<<grid, dim3(64 * rows_waves<4>()), 0, stream>>>(a);
+hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream) {
+    const dim3 grid((unsigned)a.slots * a.p.n_kv_heads), threads(256);
+    if (row_tiles == 1) paged_rows<BF, INT8, 1><<<grid, threads, 0, stream>>>(a);
+    else if (row_tiles == 2) paged_rows<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
+    else if (row_tiles == 4) paged_tiles<BF, INT8, 1><<<grid, threads, 0, stream>>>(a);
+    else paged_tiles<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
 }
-template hipError_t paged_rows_form<(KVQP_PAGED_BITS - 1) / 2 != 0, (KVQP_PAGED_BITS - 1) % 2 != 0>(const AttnArgs&, int, dim3, hipStream_t);
+template hipError_t paged_form<(KVQP_PAGED_BITS - 1) / 2 != 0, (KVQP_PAGED_BITS - 1) % 2 != 0>(const AttnArgs&, int, hipStream_t);
 
 #else
 
 // ---- launches ----
-constexpr int kMostParts = 2048;                    // partial results of 16 rows each that a workspace has room for
+constexpr int kMostParts = 8192;                    // partial results of 16 rows each that a workspace has room for
 constexpr size_t kPartBytes = 8192 + 128;
 struct PagedPlan {
-    int row_tiles, per_piece, pieces, n_splits;
+    int row_tiles, per_piece, slots, most_shares, least_groups;
     size_t ws_bytes;
 };
 static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, int64_t most_tokens) {
-    const int gq = cfg.n_q_heads / cfg.n_kv_heads, columns = (n_rows + cfg.batch - 1) / cfg.batch >= 64 ? 64 : (n_rows + cfg.batch - 1) / cfg.batch * gq;
+    // (rows of a call over its sequences, as if they were equal)
+    const int gq = cfg.n_q_heads / cfg.n_kv_heads, each = (n_rows + cfg.batch - 1) / cfg.batch, columns = each >= 128 ? 128 : each * gq;
     PagedPlan r;
-    r.row_tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
+    r.row_tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : columns <= 64 ? 4 : 8;
     r.per_piece = 16 * r.row_tiles / gq;
-    r.pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;
-    const int64_t units = (int64_t)std::max(cfg.batch, n_rows / r.per_piece) * cfg.n_kv_heads, groups = (int64_t)r.pieces * cfg.n_kv_heads;
-    int64_t splits = (1024 + units - 1) / units;
-    splits = std::min({splits, (int64_t)64, kMostParts / (r.row_tiles * groups), most_tokens / 512 + 1});
-    if (groups > KVQP_PAGED_COUNTERS / 4 || splits < 1) splits = 1;
-    r.n_splits = (int)splits;
-    r.ws_bytes = splits > 1 ? KVQP_PAGED_COUNTERS + groups * splits * r.row_tiles * kPartBytes : 0;
+    const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;
+    static const int kT[4] = {getenv("KT1") ? atoi(getenv("KT1")) : 768, getenv("KT2") ? atoi(getenv("KT2")) : 1024, getenv("KT4") ? atoi(getenv("KT4")) : 1024, getenv("KT8") ? atoi(getenv("KT8")) : 512};
+    r.most_shares = std::min(kT[r.row_tiles == 1 ? 0 : r.row_tiles == 2 ? 1 : r.row_tiles == 4 ? 2 : 3], std::min(kMostParts / r.row_tiles, KVQP_PAGED_COUNTERS / 4) / 2) / cfg.n_kv_heads;
+    r.least_groups = 4;
+    if (most_tokens <= 64 * r.least_groups) r.most_shares = 0;
+    r.slots = pieces + (r.most_shares * 4 + 2) / 3;
+    r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;
     return r;
 }
 size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows) {
@@ -530,16 +882,22 @@ size_t paged_workspace_need(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows
 
 PageArgs page_args(const kvqp_cfg& cfg, const kvqp_pages& g, const int32_t* row_start, int n_rows);
 
+// Whether a step's codes are more than what may stay in the memory-side cache, as far as the host knows: the pages that the sequences can have.
+static bool rows_once(const kvqp_cfg& cfg, const kvqp_pages& g) {
+    if (getenv("ONCE")) return atoi(getenv("ONCE"));
+    if (cfg.decode_cache_hint != KVQP_CACHE_AUTO) return cfg.decode_cache_hint == KVQP_CACHE_STREAM;
+    return std::min((double)g.n_pages, (double)cfg.batch * g.max_pages) * g.page_tokens * cfg.n_kv_heads * 2 * kHeadDim > 96.0 * (1 << 20);
+}
+
 hipError_t launch_paged_attn(const kvqp_cfg& cfg, const kvqp_pages& g, const void* q, int64_t q_stride, int n_rows, const int32_t* row_start, int window,
                              void* out, float* lse, void* ws, hipStream_t stream) {
     const PagedPlan plan = plan_paged(cfg, n_rows, row_start != nullptr, (int64_t)g.max_pages * g.page_tokens);
     const AttnArgs a = {page_args(cfg, g, row_start, n_rows), (const uint16_t*)q, q_stride, (uint16_t*)out, lse, (unsigned int*)ws,
                         (char*)ws + KVQP_PAGED_COUNTERS, cfg.sm_scale * 1.4426950408889634f, window, g.page_tokens == 16 ? 4 : g.page_tokens == 32 ? 5 : 6,
-                        plan.per_piece, plan.n_splits};
-    const dim3 grid(plan.pieces, cfg.n_kv_heads, plan.n_splits);
+                        plan.per_piece, plan.slots, plan.most_shares, plan.least_groups, rows_once(cfg, g)};
     if (g.dtype == KVQP_BFLOAT16)
-        return g.form == KVQP_INT8 ? paged_rows_form<true, true>(a, plan.row_tiles, grid, stream) : paged_rows_form<true, false>(a, plan.row_tiles, grid, stream);
-    return g.form == KVQP_INT8 ? paged_rows_form<false, true>(a, plan.row_tiles, grid, stream) : paged_rows_form<false, false>(a, plan.row_tiles, grid, stream);
+        return g.form == KVQP_INT8 ? paged_form<true, true>(a, plan.row_tiles, stream) : paged_form<true, false>(a, plan.row_tiles, stream);
+    return g.form == KVQP_INT8 ? paged_form<false, true>(a, plan.row_tiles, stream) : paged_form<false, false>(a, plan.row_tiles, stream);
 }
 
 __global__ __launch_bounds__(256) void clear_paged_counters(uint32_t* at) {

@@ -15,21 +15,11 @@ struct PageArgs {
     int batch, n_kv_heads, gq, n_pages, max_pages, n_open, n_rows;
 };
 
-// Sequence b as the device arrays state it, cut to what the buffers have.
+// A sequence as the device arrays state it, cut to what the buffers have.
 struct Sequence {
-    int row0, rows, length;     // its rows of the call, and its tokens with them
+    int b, row0, rows, length;     // its number, its rows of the call, and its tokens with them
     __device__ int position(int i) const { return length - rows + i; }      // of row i; negative: no token of the sequence
 };
-
-__device__ inline Sequence sequence_of(const PageArgs& a, int b, int P) {
-    Sequence s;
-    int r0 = b, r1 = b + 1;
-    if (a.row_start) { r0 = a.row_start[b]; r1 = a.row_start[b + 1]; }
-    s.row0 = min(max(r0, 0), a.n_rows);
-    s.rows = min(max(r1, s.row0), a.n_rows) - s.row0;
-    s.length = min(max(a.lengths[b], 0), a.max_pages * P);
-    return s;
-}
 
 __device__ inline int page_of(const PageArgs& a, int b, int block) {      // block < max_pages; -1: no page
     const int page = a.table[(size_t)b * a.max_pages + block];
@@ -42,16 +32,21 @@ __device__ inline int slot_of(const PageArgs& a, int b) {
 
 // Work is numbered by sequence without a sum over those before: sequence b's pieces (at most rows / T + per of them) begin at
 // row_start[b] / T + per * b, which grows by at least as much from one to the next; with one row per sequence piece b is sequence b's.  All threads of a
-// workgroup look for the one that holds `piece`, one sequence each; returns -1 (for all) where there is none.  `found`: a word of LDS.
-__device__ inline int first_piece(const PageArgs& a, int b, int row0, int T, int per) { return a.row_start ? row0 / T + per * b : b; }
-__device__ inline int owner_of_piece(const PageArgs& a, int piece, int T, int per, int* found) {
-    if (!a.row_start) return piece;
-    if (threadIdx.x == 0) *found = -1;
+// workgroup look for the one that holds `piece`, one sequence each, with its length at the same time; b = -1 (for all) where there is none.  `found`: LDS.
+__device__ inline int first_piece(const PageArgs& a, const Sequence& s, int T, int per) { return a.row_start ? s.row0 / T + per * s.b : s.b; }
+__device__ inline Sequence owner_of_piece(const PageArgs& a, int piece, int T, int per, int P, Sequence* found) {
+    const int most = a.max_pages * P;
+    if (!a.row_start) return {piece, piece, 1, min(max(a.lengths[piece], 0), most)};
+    if (threadIdx.x == 0) found->b = -1;
     __syncthreads();
+    Sequence mine = {-2, 0, 0, 0};
     for (int b = threadIdx.x; b < a.batch; b += blockDim.x) {
-        const int r0 = min(max(a.row_start[b], 0), a.n_rows), r1 = min(max(a.row_start[b + 1], 0), a.n_rows);
-        if (r1 > r0 && piece >= r0 / T + per * b && piece < r1 / T + per * (b + 1)) atomicMax(found, b);      // (descending starts may give two)
+        const int r0 = min(max(a.row_start[b], 0), a.n_rows), r1 = min(max(a.row_start[b + 1], 0), a.n_rows), length = a.lengths[b];
+        if (r1 > r0 && piece >= r0 / T + per * b && piece < r1 / T + per * (b + 1)) mine = {b, r0, r1 - r0, min(max(length, 0), most)};
     }
+    if (mine.b >= 0) atomicMax(&found->b, mine.b);      // (descending starts may give two)
+    __syncthreads();
+    if (found->b == mine.b) { found->row0 = mine.row0; found->rows = mine.rows; found->length = mine.length; }
     __syncthreads();
     return *found;
 }

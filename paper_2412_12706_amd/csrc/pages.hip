@@ -170,15 +170,15 @@ __device__ inline float largest(f8v x) {
 template <bool BF, bool INT8, int P>
 __global__ __launch_bounds__(256) void append(AppendArgs a) {
     constexpr int TOKENS = P < 32 ? P : 32, PASSES = P / TOKENS, GROUPS = 32 / TOKENS;
-    __shared__ int found;
+    __shared__ Sequence found;
     __shared__ float s_max[2][4];
     __shared__ __align__(16) uint8_t s_codes[128][P + 4];
     const PageArgs& p = a.p;
-    const int b = owner_of_piece(p, blockIdx.x, P, 2, &found);
+    const Sequence seq = owner_of_piece(p, blockIdx.x, P, 2, P, &found);
+    const int b = seq.b;
     if (b < 0) return;
-    const Sequence seq = sequence_of(p, b, P);
     const int begin = max(seq.position(0), 0), first = begin / P;
-    const int block = first + (int)blockIdx.x - first_piece(p, b, seq.row0, P, 2);
+    const int block = first + (int)blockIdx.x - first_piece(p, seq, P, 2);
     if (block < first || (int64_t)block * P >= seq.length) return;
     const int h = blockIdx.y, u = threadIdx.x & 7, token = (threadIdx.x >> 3) % TOKENS, group = (threadIdx.x >> 3) / TOKENS;
     const int2 at = pieces_of(a.t, u);

@@ -470,12 +470,20 @@ def _check_room(what, cfg: Cfg, cache: Cache, rows: int, device):
         _want(f"{what}.head_n_kept", counts, torch.int32, counts.shape if counts.numel() == heads else (heads,), device)
 
 
+def _current_device() -> int:
+    import torch
+    try:                # (torch.cuda.current_device() takes 0.5 us more)
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
+
+
 def _call(name, device, stream, args):
     """Calls an entry point with that GPU as the current one."""
     import torch
     if _lib is None:
         lib()
-    if torch.cuda.current_device() != device:
+    if _current_device() != device:
         with torch.cuda.device(device):
             rc = _fn_rows[name](*args, _stream_handle(stream))
     else:
@@ -636,16 +644,29 @@ def rope_frequencies(rot_dim: int = 128, base: float = 10000.0, scaling: int = R
     return list(out)
 
 
+class _Described:
+    """An object whose fields describe device memory: they are checked and packed for the library once, and again after one of them is assigned."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, "_packed", None)
+        object.__setattr__(self, name, value)
+
+
 @dataclass
-class Rope:
-    """A table of cosines and sines [n_positions, rot_dim / 2, 2] (float32, on the device) and how it turns a row."""
+class Rope(_Described):
+    """A table of cosines and sines [n_positions, rot_dim / 2, 2] (float32, on the device) and how it turns a row.  The table may be replaced by
+    assignment; it is not resized in place."""
     table: object
     rot_dim: int = 128
     interleaved: bool = False
 
-    def _bytes(self) -> bytes:
-        t = self.table
-        return _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))
+    def _bytes(self, device) -> bytes:
+        if self._packed is None or self._packed[0] != device:
+            import torch
+            t = self.table
+            _want("rope.table", t, torch.float32, (t.shape[0], self.rot_dim // 2, 2), device)
+            object.__setattr__(self, "_packed", (device, _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))))
+        return self._packed[1]
 
 
 def rope_table(n_positions: int, inv_freq, magnitude: float = 1.0, interleaved: bool = False, device="cuda", stream=None) -> Rope:
@@ -661,20 +682,16 @@ def rope_table(n_positions: int, inv_freq, magnitude: float = 1.0, interleaved: 
     return Rope(table, 2 * pairs, interleaved)
 
 
-def _want_rope(rope: Rope, device):
-    import torch
-    t = rope.table
-    _want("rope.table", t, torch.float32, (t.shape[0], rope.rot_dim // 2, 2), device)
-
-
 def _row_type(what, t, device, dtype=None):
-    """0 or 1 (KVQP_HALF, KVQP_BFLOAT16) of a tensor of rows, whose channels lie next to each other."""
+    """0 or 1 (KVQP_HALF, KVQP_BFLOAT16) of a tensor [B, H, N, 128] of rows, whose channels lie next to each other; and its other strides."""
     import torch
-    if (dtype is None and t.dtype not in (torch.float16, torch.bfloat16)) or (dtype is not None and t.dtype is not dtype) or t.get_device() != device or device < 0:
-        raise ValueError(f"{what}: a tensor of {dtype or 'float16 or bfloat16'} on GPU {device} is needed, not {t.dtype} on {t.device}")
-    if t.dim() < 1 or t.shape[-1] != 128 or t.stride(-1) != 1:
-        raise ValueError(f"{what}: rows of 128 adjacent channels are needed, not shape {tuple(t.shape)} with strides {t.stride()}")
-    return int(t.dtype is torch.bfloat16)
+    kind = t.dtype
+    if t.get_device() == device >= 0 and (kind is dtype if dtype is not None else kind is torch.float16 or kind is torch.bfloat16) and t.dim() == 4 and t.shape[3] == 128:
+        a, b, c, one = t.stride()
+        if one == 1:
+            return int(kind is torch.bfloat16), (a, b, c)
+    raise ValueError(f"{what}: a tensor [B, H, N, 128] of {dtype or 'float16 or bfloat16'} on GPU {device} is needed, with adjacent channels, not {t.dtype} "
+                     f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
 def rotate(rope: Rope, x, positions=None, first: int = 0, out=None, inverse: bool = False, stream=None):
@@ -682,10 +699,8 @@ def rotate(rope: Rope, x, positions=None, first: int = 0, out=None, inverse: boo
     positions int32 [N] or [B,N], or None for first, first + 1, ..."""
     import torch
     device = x.get_device()
-    if x.dim() != 4:
-        raise ValueError(f"x: four axes are needed, not shape {tuple(x.shape)}")
-    kind = _row_type("x", x, device)
-    _want_rope(rope, device)
+    kind, x_strides = _row_type("x", x, device)
+    turn = rope._bytes(device)
     b, h, n, _ = x.shape
     per_batch = 0
     if positions is not None:
@@ -696,23 +711,22 @@ def rotate(rope: Rope, x, positions=None, first: int = 0, out=None, inverse: boo
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if stream is not None and out.is_cuda:
             out.record_stream(torch.cuda.current_stream(out.device))
-    else:
-        _row_type("out", out, device, x.dtype)
-        if out.shape != x.shape:
-            raise ValueError(f"out: shape {tuple(x.shape)} is needed, not {tuple(out.shape)}")
+    _, out_strides = _row_type("out", out, device, x.dtype)
+    if out.shape != x.shape:
+        raise ValueError(f"out: shape {tuple(x.shape)} is needed, not {tuple(out.shape)}")
     if x.numel() == 0:
         return out
     _call("kvqp_rotate", device, stream,
-          (rope._bytes(), kind, b, h, n, _pack_rows(x.data_ptr(), *x.stride()[:3]), _pack_rows(out.data_ptr(), *out.stride()[:3]), _addr(positions),
+          (turn, kind, b, h, n, _pack_rows(x.data_ptr(), *x_strides), _pack_rows(out.data_ptr(), *out_strides), _addr(positions),
            per_batch, first, int(inverse)))
     return out
 
 
 @dataclass
-class Pages:
+class Pages(_Described):
     """Device buffers of one layer's paged cache (kvqp_pages): k_codes [n_pages,Hkv,P,128] and v_codes [n_pages,Hkv,128,P], both float8_e4m3fn or both int8;
     k_scale, v_scale float32 [n_pages,Hkv]; open_k, open_v [n_open,Hkv,2P,128] float16 or bfloat16; table int32 [B,max_pages]; lengths int32 [B]; open_slot
-    int32 [B] or None."""
+    int32 [B] or None.  Their contents change as they may, and any may be replaced by assignment; they are not resized in place."""
     k_codes: object
     v_codes: object
     k_scale: object
@@ -729,9 +743,15 @@ class Pages:
 
     def _bytes(self, cfg: Cfg, device) -> bytes:
         """kvqp_pages, with all buffers as it states them."""
+        fits = (device, cfg.n_kv_heads, cfg.batch)
+        if self._packed is None or self._packed[0] != fits:
+            object.__setattr__(self, "_packed", (fits, self._checked(cfg, device)))
+        return self._packed[1]
+
+    def _checked(self, cfg: Cfg, device) -> bytes:
         import torch
         k = self.k_codes
-        n, heads, p, _ = k.shape
+        n, _, p, _ = k.shape
         half, form = self.open_k.dtype, k.dtype
         if form not in (torch.float8_e4m3fn, torch.int8) or half not in (torch.float16, torch.bfloat16):
             raise ValueError(f"pages: codes of float8_e4m3fn or int8 and open rows of float16 or bfloat16 are needed, not {form} and {half}")
@@ -769,10 +789,12 @@ def alloc_pages(cfg: Cfg, n_pages: int, max_pages: int, page_tokens: int = 16, d
 
 def _packed_rows(what, t, heads, n, device, dtype):
     """The stride of the rows of a tensor [n, heads, 128] whose heads lie next to each other."""
-    _row_type(what, t, device, dtype)
-    if t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or (heads > 1 and t.stride(1) != 128):
-        raise ValueError(f"{what}: shape {(n, heads, 128)} with adjacent heads is needed, not {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if n > 1 else heads * 128
+    if t.dtype is dtype and t.get_device() == device >= 0 and t.shape == (n, heads, 128):
+        stride = t.stride()
+        if stride[2] == 1 and (stride[1] == 128 or heads == 1):
+            return stride[0] if n > 1 else heads * 128
+    raise ValueError(f"{what}: a {dtype} tensor of shape {(n, heads, 128)} on GPU {device} is needed, with adjacent heads and channels, not {t.dtype} "
+                     f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
 def _want_starts(cfg: Cfg, row_start, device):
@@ -801,14 +823,13 @@ def paged_append(cfg: Cfg, pages: Pages, k, v, row_start=None, q=None, rope: Rop
             _want("q_out", q_out, dtype, (n, cfg.n_q_heads, 128), device)
     elif q_out is not None:
         raise ValueError("q_out: there is no q")
-    if rope is not None:
-        _want_rope(rope, device)
+    turn = None if rope is None else rope._bytes(device)
     if positions is not None:
         _want("positions", positions, torch.int32, (n,), device)
     if n == 0 and row_start is not None:
         return q_out
     _call("kvqp_paged_append", device, stream,
-          (cfg._bytes(), layout, None if rope is None else rope._bytes(), _addr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, n, _addr(row_start),
+          (cfg._bytes(), layout, turn, _addr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, n, _addr(row_start),
            _addr(positions), _addr(q_out)))
     return q_out
 
