@@ -3,7 +3,6 @@
 // One object per row type and form: KVQP_PAGED_BITS 1 + 2 * bfloat16 + int8 compiles the kernels, none the launches.
 #include <hip/hip_runtime.h>
 
-#include <stdlib.h>
 #include <algorithm>
 
 #include "pages.h"
@@ -22,10 +21,12 @@ struct AttnArgs {
     int window, page_log2;
     int per_piece;          // rows of the call that a workgroup has at most
     int slots;              // workgroups of a KV head
-    int most_shares;        // how many shares the work of a KV head is cut into, about; 0: sequences are not split
-    int least_groups;       // groups of 64 tokens that a share has at least
+    int most_shares;        // how many shares the work of a KV head is cut into at most; 0: sequences are not split
     bool once;              // loads of codes go round the memory-side cache
 };
+
+// Groups of 64 tokens that a workgroup has at least, and the most sequences among which work is shared out.
+constexpr int kLeastGroups = 4, kMostSplitBatch = 512;
 
 template <bool BF, bool INT8> hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream);
 
@@ -79,9 +80,11 @@ __device__ __forceinline__ float log_sum(float ref, float sum) { return sum == 0
 // Partial results of one workgroup of a split piece: outputs in the order of the accumulators, and (reference, sum) of the rows.
 struct Partials {
     __amdgpu_buffer_rsrc_t at;
-    int states, bytes;
+    int bytes, states, joined;      // of a workgroup's results, where the rows' states begin, and those of several workgroups' joined results
+    mutable int states_read;
     // part: the first of `splits` workgroups' results, which follow each other
-    __device__ __forceinline__ Partials(const AttnArgs& a, int64_t part, int splits, int row_tiles) : states(row_tiles * 8192), bytes(row_tiles * 8320) {
+    __device__ __forceinline__ Partials(const AttnArgs& a, int64_t part, int splits, int row_tiles)
+        : bytes(row_tiles * 8448), states(row_tiles * 8192), joined(row_tiles * 8320), states_read(row_tiles * 8192) {
         at = __builtin_amdgcn_make_buffer_rsrc(a.part + part * bytes, 0, splits * bytes, 0x00020000);
     }
     __device__ __forceinline__ void put_output(int split, int item, f4v o) const {
@@ -91,86 +94,116 @@ struct Partials {
         const u2v v = {__float_as_uint(ref), __float_as_uint(sum)};
         __builtin_amdgcn_raw_buffer_store_b64(v, at, split * bytes + states + row * 8, 0, kDeviceScope);
     }
+    __device__ __forceinline__ void put_joined(int split, int row, float ref, float sum) const {
+        const u2v v = {__float_as_uint(ref), __float_as_uint(sum)};
+        __builtin_amdgcn_raw_buffer_store_b64(v, at, split * bytes + joined + row * 8, 0, kDeviceScope);
+    }
+    __device__ __forceinline__ void use_joined(bool yes) const { states_read = yes ? joined : states; }
     __device__ __forceinline__ f4v output(int split, int item) const {
         return __builtin_bit_cast(f4v, __builtin_amdgcn_raw_buffer_load_b128(at, split * bytes + item * 16, 0, kDeviceScope));
     }
     __device__ __forceinline__ float2 state(int split, int row) const {
-        const u2v v = __builtin_amdgcn_raw_buffer_load_b64(at, split * bytes + states + row * 8, 0, kDeviceScope);
+        const u2v v = __builtin_amdgcn_raw_buffer_load_b64(at, split * bytes + states_read + row * 8, 0, kDeviceScope);
         return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1]));
     }
 };
 
 // ---- what both kernels do with a piece of a sequence's rows ----
 
-// Which sequence, piece of its rows and split of its tokens a workgroup has.  Only the device knows the lengths, so every workgroup looks at all of them:
-// the work of a KV head, groups of 64 tokens times pieces of rows, is cut into shares of about the same size, and a sequence of g groups is split
-// into g / share, rounded, for each of its pieces.  (1.5 shares and more are split, so the split sequences' workgroups are at most 4/3 most_shares.)
+// Which sequence, piece of its rows and split of its tokens a workgroup has.  Only the device knows the lengths, so every wave looks at all of them:
+// the work of a KV head, groups of 64 tokens times pieces of rows, is cut into shares of one size, and each piece of a sequence of g groups is split
+// into ceil(g / share).  (Only more than a share is split, so the split pieces' workgroups are less than twice as many as the shares.)
 struct Slot {
     Sequence seq;
     int piece, split, splits;
     int part;               // number of the piece's first workgroup among those of split pieces
 };
-struct SlotShared {
-    float work[4];
-    int workgroups[4], parts[4];
-    Slot found;
-};
-__device__ __forceinline__ Slot find_slot(const AttnArgs& a, int slot, SlotShared& sh) {
+__device__ __forceinline__ Slot find_slot(const AttnArgs& a, int slot, Sequence* s_found) {
     const PageArgs& p = a.p;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, most = p.max_pages << a.page_log2;
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    if (a.most_shares == 0) {
+        const Sequence s = owner_of_piece(p, slot, a.per_piece, 1, 1 << a.page_log2, s_found);
+        const Sequence u = {uniform(s.b), uniform(s.row0), uniform(s.rows), uniform(s.length)};
+        const int piece = u.b < 0 ? 0 : slot - first_piece(p, u, a.per_piece, 1);
+        return {{piece * a.per_piece < u.rows ? u.b : -1, u.row0, u.rows, u.length}, piece, 0, 1, 0};
+    }
+    const int lane = threadIdx.x & 63, most = p.max_pages << a.page_log2;
     struct Share { Sequence seq; int pieces, groups; };
+    // (loads without a branch, so that all are on their way at once; what is behind the last sequence counts for nothing)
     auto look = [&](int b) {
-        Share s = {{b, b, 0, 0}, 0, 0};
-        if (b >= p.batch) return s;
-        const int r0 = p.row_start ? p.row_start[b] : b, r1 = p.row_start ? p.row_start[b + 1] : b + 1, length = p.lengths[b];
+        const int at = min(b, p.batch - 1);
+        int r0 = at, r1 = at + 1;
+        if (p.row_start) { r0 = p.row_start[at]; r1 = p.row_start[at + 1]; }
+        Share s;
+        s.seq.b = b;
         s.seq.row0 = min(max(r0, 0), p.n_rows);
-        s.seq.rows = max(min(r1, p.n_rows) - s.seq.row0, 0);
-        s.seq.length = min(max(length, 0), most);
+        s.seq.rows = b < p.batch ? max(min(r1, p.n_rows) - s.seq.row0, 0) : 0;
+        s.seq.length = min(max(p.lengths[at], 0), most);
         s.pieces = (s.seq.rows + a.per_piece - 1) / a.per_piece;
         const int seen = a.window > 0 ? min(s.seq.length, a.window + min(s.seq.rows, a.per_piece)) : s.seq.length;
         s.groups = (seen + 63) / 64;
         return s;
     };
-    Share mine = look(threadIdx.x);
-    float share = 0.f;
-    if (a.most_shares > 0) {
-        float work = (float)mine.pieces * (float)mine.groups;
-        for (int b = threadIdx.x + 256; b < p.batch; b += 256) {
-            const Share s = look(b);
-            work += (float)s.pieces * (float)s.groups;
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
-        if (lane == 0) sh.work[wave] = work;
+    if (p.batch == 1) {
+        const Share one = look(0);
+        const int splits = max((int)ceilf((float)one.groups / fmaxf((float)one.pieces * (float)one.groups / (float)a.most_shares, (float)kLeastGroups)), 1);
+        const int piece = slot / splits;
+        return {{piece < one.pieces ? 0 : -1, uniform(one.seq.row0), uniform(one.seq.rows), uniform(one.seq.length)}, uniform(piece), uniform(slot % splits), uniform(splits),
+                uniform(piece * splits)};
     }
-    if (threadIdx.x == 0) sh.found.seq.b = -1;
-    __syncthreads();
-    if (a.most_shares > 0) share = fmaxf(((sh.work[0] + sh.work[1]) + (sh.work[2] + sh.work[3])) / (float)a.most_shares, (float)a.least_groups);
-    int workgroups = 0, parts = 0;      // of the sequences before these 256
+    // (lane l has sequences 4 l .. 4 l + 3 of 256)
+    Share mine[4];
+    float work = 0.f;
+    for (int b0 = p.batch > 256 ? 256 : 0; b0 >= 0; b0 -= 256) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            mine[j] = look(b0 + 4 * lane + j);
+            work += (float)mine[j].pieces * (float)mine[j].groups;
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
+    const float share = fmaxf(work / (float)a.most_shares, (float)kLeastGroups);
+    int workgroups = 0, parts = 0;      // of the 256 sequences before
+    Slot s = {{-1, 0, 0, 0}, 0, 0, 1, 0};
     for (int b0 = 0; b0 < p.batch; b0 += 256) {
-        if (b0) mine = look(b0 + threadIdx.x);
-        const int splits = a.most_shares > 0 ? max((int)((float)mine.groups / share + 0.5f), 1) : 1, n = mine.pieces * splits, m = splits > 1 ? n : 0;
-        int upto = n, parts_upto = m;
+        int n[4], m[4], splits[4], upto = 0, parts_upto = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (b0) mine[j] = look(b0 + 4 * lane + j);
+            splits[j] = max((int)ceilf((float)mine[j].groups / share), 1);
+            n[j] = mine[j].pieces * splits[j];
+            m[j] = splits[j] > 1 ? n[j] : 0;
+            upto += n[j]; parts_upto += m[j];
+        }
+        const int own = upto, own_parts = parts_upto;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const int x = __shfl_up(upto, d), y = __shfl_up(parts_upto, d);
             if (lane >= d) { upto += x; parts_upto += y; }
         }
-        if (lane == 63) { sh.workgroups[wave] = upto; sh.parts[wave] = parts_upto; }
-        __syncthreads();
-        for (int v = 0; v < 4; ++v) {
-            if (v < wave) { upto += sh.workgroups[v]; parts_upto += sh.parts[v]; }
+        int at = slot - (workgroups + upto - own), part = parts + parts_upto - own_parts;
+        bool hit = false;
+        Slot t = s;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (!hit && at >= 0 && at < n[j]) {
+                hit = true;
+                t = {mine[j].seq, at / splits[j], at % splits[j], splits[j], part + at / splits[j] * splits[j]};
+            }
+            at -= n[j];
+            part += m[j];
         }
-        const int at = slot - (workgroups + upto - n);
-        if (at >= 0 && at < n) sh.found = {mine.seq, at / splits, at % splits, splits, parts + parts_upto - m + at / splits * splits};
-        workgroups += (sh.workgroups[0] + sh.workgroups[1]) + (sh.workgroups[2] + sh.workgroups[3]);
-        parts += (sh.parts[0] + sh.parts[1]) + (sh.parts[2] + sh.parts[3]);
-        __syncthreads();
-        if (sh.found.seq.b >= 0) break;
+        const uint64_t who = __ballot(hit);
+        if (who) {
+            const int from = __ffsll((unsigned long long)who) - 1;
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, from); };
+            return {{of(t.seq.b), of(t.seq.row0), of(t.seq.rows), of(t.seq.length)}, of(t.piece), of(t.split), of(t.splits), of(t.part)};
+        }
+        workgroups += __builtin_amdgcn_readlane(upto, 63);
+        parts += __builtin_amdgcn_readlane(parts_upto, 63);
     }
-    const Slot s = sh.found;
-    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-    return {{uniform(s.seq.b), uniform(s.seq.row0), uniform(s.seq.rows), uniform(s.seq.length)}, uniform(s.piece), uniform(s.split), uniform(s.splits), uniform(s.part)};
+    return s;
 }
 
 // The tokens that a workgroup's rows see, in groups of 64 from token 0: whole blocks, and open tokens behind them.
@@ -182,8 +215,8 @@ struct Range {
     int lo;                     // first token that any row sees
     int ga, gb;                 // groups of this workgroup
     int split, active, part;    // its number among those that have some, and where their results go
-    __device__ __forceinline__ bool find(const AttnArgs& a, int slot, SlotShared& sh) {
-        const Slot s = find_slot(a, slot, sh);
+    __device__ __forceinline__ bool find(const AttnArgs& a, int slot, Sequence* s_found) {
+        const Slot s = find_slot(a, slot, s_found);
         seq = s.seq;
         if (seq.b < 0 || (s.splits > 1 && s.part + s.splits > 2 * a.most_shares)) return false;      // (the second: lengths that change meanwhile)
         i0 = s.piece * a.per_piece;
@@ -195,7 +228,7 @@ struct Range {
         closed = min(last + 1, begin);
         open = max(last + 1 - begin, 0);
         const int g_lo = lo / 64, groups = closed > lo ? (closed + 63) / 64 - g_lo : 0;
-        const int each = max((groups + s.splits - 1) / s.splits, a.least_groups);
+        const int each = max((groups + s.splits - 1) / s.splits, kLeastGroups);
         split = s.split; part = s.part;
         active = max((groups + each - 1) / each, 1);
         ga = g_lo + split * each;
@@ -279,7 +312,11 @@ __device__ __forceinline__ float query_fragments(const uint16_t* q, bool there, 
     uint4 w[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-        w[s] = there ? *reinterpret_cast<const uint4*>(q + (WIDE ? 64 * (s >> 1) + 16 * kb + 8 * (s & 1) : 32 * s + 8 * kb)) : make_uint4(0, 0, 0, 0);
+        w[s] = *reinterpret_cast<const uint4*>(q + (WIDE ? 64 * (s >> 1) + 16 * kb + 8 * (s & 1) : 32 * s + 8 * kb));
+    if (!there) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) w[s] = make_uint4(0, 0, 0, 0);
+    }
     if constexpr (BF) {
         float m = 0.f;
 #pragma unroll
@@ -325,9 +362,9 @@ __device__ __forceinline__ void attend_open(const AttnArgs& a, const Range& w, i
         uint4 k[2][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int off = t0 + 16 * t + c;
+            const int off = min(t0 + 16 * t + c, w.open - 1);      // (what is behind the last is masked)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) k[t][s] = off < w.open ? *reinterpret_cast<const uint4*>(keys + off * kHeadDim + 32 * s + 8 * kb) : make_uint4(0, 0, 0, 0);
+            for (int s = 0; s < 4; ++s) k[t][s] = *reinterpret_cast<const uint4*>(keys + off * kHeadDim + 32 * s + 8 * kb);
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -336,7 +373,7 @@ __device__ __forceinline__ void attend_open(const AttnArgs& a, const Range& w, i
             const int position = i < w.n ? w.first + i : -1, low = a.window > 0 ? position - a.window : -1;
             uint4 q[4];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) q[s] = i < w.n ? *reinterpret_cast<const uint4*>(rows + 32 * s + 8 * kb) : make_uint4(0, 0, 0, 0);
+            for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const uint4*>(rows + 32 * s + 8 * kb);      // (a row that is not there sees nothing)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 x[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
@@ -380,30 +417,37 @@ struct Segment {
     int page[kSegment];
     float k_scale[kSegment], v_scale[kSegment];
 };
-// In two steps, so that codes can be requested before the scales have come.  Returns whether a block that is seen has no page.
+// In steps, so that other loads can be on their way at the same time.
 template <int THREADS>
-__device__ __forceinline__ bool look_up_pages(const AttnArgs& a, const Range& w, int first_block, int blocks, Segment& seg, int (&mine)[kSegment / THREADS]) {
-    int holes = 0;
+struct PageNumbers {
+    int mine[kSegment / THREADS];
+    int holes;                // a block that is seen has no page
+    __device__ __forceinline__ void request(const AttnArgs& a, const Range& w, int first_block, int blocks) {
+        holes = 0;
 #pragma unroll
-    for (int u = 0; u < kSegment / THREADS; ++u) {
-        const int i = threadIdx.x + THREADS * u, block = first_block + i;
-        mine[u] = -1;
-        if (i < blocks && (block << a.page_log2) < w.closed) {
-            mine[u] = page_of(a.p, w.seq.b, block);
-            if (mine[u] < 0 && (block + 1) << a.page_log2 > w.lo) holes = 1;
+        for (int u = 0; u < kSegment / THREADS; ++u) {
+            const int i = threadIdx.x + THREADS * u, block = first_block + i;
+            const int page = a.p.table[(int64_t)w.seq.b * a.p.max_pages + min(block, a.p.max_pages - 1)];
+            const bool read = i < blocks && (int64_t)block << a.page_log2 < w.closed, there = read && (unsigned)page < (unsigned)a.p.n_pages;
+            mine[u] = there ? page : -1;
+            holes |= read && !there && (block + 1) << a.page_log2 > w.lo;
         }
-        seg.page[i] = mine[u];
     }
-    return __syncthreads_or(holes) != 0;
-}
+    __device__ __forceinline__ bool put(Segment& seg) const {
+#pragma unroll
+        for (int u = 0; u < kSegment / THREADS; ++u) seg.page[threadIdx.x + THREADS * u] = mine[u];
+        return __syncthreads_or(holes) != 0;
+    }
+};
 // top: the largest scale of values so far, of all threads in *s_top
 template <int THREADS>
-__device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float top, Segment& seg, const int (&mine)[kSegment / THREADS], unsigned int* s_top) {
+__device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float top, Segment& seg, const PageNumbers<THREADS>& pages, unsigned int* s_top) {
     float most = top;
 #pragma unroll
     for (int u = 0; u < kSegment / THREADS; ++u) {
-        float ks = 1.f, vs = 0.f;
-        if (mine[u] >= 0) { ks = a.p.k_scale[(int64_t)mine[u] * a.p.n_kv_heads + h]; vs = a.p.v_scale[(int64_t)mine[u] * a.p.n_kv_heads + h]; }
+        const int64_t at = (int64_t)max(pages.mine[u], 0) * a.p.n_kv_heads + h;
+        float ks = a.p.k_scale[at], vs = a.p.v_scale[at];
+        if (pages.mine[u] < 0) { ks = 1.f; vs = 0.f; }
         const int i = threadIdx.x + THREADS * u;
         seg.k_scale[i] = ks; seg.v_scale[i] = vs;
         most = fmaxf(most, vs);
@@ -413,55 +457,95 @@ __device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float 
     return __uint_as_float(__builtin_amdgcn_readfirstlane(*s_top));
 }
 
-// The last workgroup of a piece and head to arrive joins their splits, in their order.
-// The partials were stored past this die's L2, and the wait returns when the stores have been acknowledged from there; so whoever sees the
+// Results of a piece's splits are joined by the last workgroup to arrive, in the order of the splits; where there are more than 16, by 16 at a time, the
+// last of each 16 first, and then the last of those their results (one workgroup that reads 96 splits takes 9 us for 16 rows).
+// Partials are stored past this die's L2, and the wait returns when the stores have been acknowledged from there; so whoever sees the
 // counter sees them, with loads that do not look into its own L2.
-template <bool BF>
-__device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, int h, int row_tiles, const Partials& parts, int* s_last) {
-    const int active = w.active;
+__device__ __forceinline__ bool arrived_last(unsigned int* count, int of, int* s_last) {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
-        unsigned int* count = &a.arrivals[w.part_of_head(a, h)];
         const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        *s_last = before == (unsigned)(active - 1);
+        *s_last = before == (unsigned)(of - 1);
         if (*s_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
-    if (!*s_last) return;
+    return *s_last != 0;
+}
+constexpr int kJoin = 16;
+template <bool BF>
+__device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, int h, int row_tiles, const Partials& parts, int* s_last) {
+    unsigned int* const counts = a.arrivals + w.part_of_head(a, h);
     const int c = threadIdx.x & 15, kb = (threadIdx.x & 63) >> 4, rows = w.n * a.p.gq;
-    for (int item = threadIdx.x; item < row_tiles * 512; item += blockDim.x) {
-        const int r = 16 * (item >> 9) + c;
-        float top = kNegBig, total = 0.f;
-        f4v x = {0.f, 0.f, 0.f, 0.f};
-        for (int s0 = 0; s0 < active; s0 += 4) {
-            f4v v[4];
-            float2 m[4];
+    // results from, from + step, ... below upto: of an item (four channels of a row), `most` of them requested at once.  (What is requested beyond the last costs
+    // time too: 16 where four splits would do makes a call of 1024 tokens 3 us longer.)
+    auto join_by = [&](auto most, int from, int step, int upto, auto take) {
+        constexpr int MOST = decltype(most)::value;
+        for (int item = threadIdx.x; item < row_tiles * 512; item += 256) {
+            const int r = 16 * (item >> 9) + c;
+            float top = kNegBig, total = 0.f;
+            f4v x = {0.f, 0.f, 0.f, 0.f};
+            for (int s0 = from; s0 < upto; s0 += MOST * step) {
+                f4v v[MOST];
+                float2 m[MOST];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int s = min(s0 + u, active - 1);
-                v[u] = parts.output(s, item);
-                m[u] = parts.state(s, r);
+                for (int u = 0; u < MOST; ++u) {
+                    const int s = s0 + u * step < upto ? s0 + u * step : s0;
+                    v[u] = parts.output(s, item);
+                    m[u] = parts.state(s, r);
+                }
+                float higher = top;
+#pragma unroll
+                for (int u = 0; u < MOST; ++u) higher = fmaxf(higher, m[u].x);
+                const float f = __builtin_amdgcn_exp2f(top - higher);
+                x *= f; total *= f;
+#pragma unroll
+                for (int u = 0; u < MOST; ++u) {
+                    const float by = s0 + u * step < upto ? __builtin_amdgcn_exp2f(m[u].x - higher) : 0.f;
+                    x += v[u] * by;
+                    total = __builtin_fmaf(m[u].y, by, total);
+                }
+                top = higher;
             }
-            float higher = top;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) higher = fmaxf(higher, m[u].x);
-            const float f = __builtin_amdgcn_exp2f(top - higher);
-            x *= f; total *= f;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float by = s0 + u < active ? __builtin_amdgcn_exp2f(m[u].x - higher) : 0.f;
-                x += v[u] * by;
-                total = __builtin_fmaf(m[u].y, by, total);
-            }
-            top = higher;
+            take(item, r, x, top, total);
         }
+    };
+    auto join = [&](int from, int step, int upto, auto take) {
+        const int n = (upto - from + step - 1) / step;
+        if (n <= 2) join_by(std::integral_constant<int, 2>{}, from, step, upto, take);
+        else if (n <= 4) join_by(std::integral_constant<int, 4>{}, from, step, upto, take);
+        else if (n <= 8) join_by(std::integral_constant<int, 8>{}, from, step, upto, take);
+        else join_by(std::integral_constant<int, kJoin>{}, from, step, upto, take);
+    };
+    int step = 1;
+    if (w.active > kJoin) {
+        const int from = w.split / kJoin * kJoin, upto = min(from + kJoin, w.active);
+        if (!arrived_last(counts + from, upto - from, s_last)) return;
+        // (an item's result takes its place in the first of the 16, which its own thread has read; a row's state, which others read too, a place of its own)
+        if (upto - from > 1) {
+            join(from, 1, upto, [&](int item, int r, f4v x, float top, float total) {
+                parts.put_output(from, item, x);
+                if ((item & 0x1C0) == 0 && kb == 0) parts.put_joined(from, r, top, total);
+            });
+        } else {
+            for (int r = threadIdx.x; r < 16 * row_tiles; r += 256) {
+                const float2 m = parts.state(from, r);
+                parts.put_joined(from, r, m.x, m.y);
+            }
+        }
+        step = kJoin;
+        if (!arrived_last(counts + 1, (w.active + kJoin - 1) / kJoin, s_last)) return;
+    } else if (!arrived_last(counts, w.active, s_last)) {
+        return;
+    }
+    parts.use_joined(step > 1);
+    join(0, step, w.active, [&](int item, int r, f4v x, float top, float total) {
         if (r < rows) {
             store_out<BF>(a, w, h, r, (item >> 6) & 7, kb, x, inverse_sum(total));
             if (a.lse && (item & 0x1C0) == 0 && kb == 0) a.lse[result_at(a, w, h, r)] = log_sum(top, total);
         }
-    }
+    });
 }
 
 // ---- few rows: the tokens are split over waves and workgroups ----
@@ -482,17 +566,20 @@ template <bool BF, bool INT8, int RT>
 __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(const AttnArgs a) {
     constexpr int NW = kRowsWaves, THREADS = 64 * NW;
     __shared__ RowsShared<RT, NW> sh;
-    __shared__ SlotShared s_slot;
+    __shared__ Sequence s_slot;
     __shared__ int s_last;
     __shared__ unsigned int s_top;
     const PageArgs& p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kb = lane >> 4;
     const int h = blockIdx.x % p.n_kv_heads, P = 1 << a.page_log2;
     Range w;
-    if (!w.find(a, blockIdx.x / p.n_kv_heads, s_slot)) return;
+    if (!w.find(a, blockIdx.x / p.n_kv_heads, &s_slot)) return;
     const int ga = w.ga, gb = w.gb, active = w.active, split = w.split;
     const int seen_by_all = min(w.first + 1, w.closed), hidden_to_some = a.window > 0 ? w.last - a.window + 1 : 0;
 
+    const int seg_groups = kSegment >> (6 - a.page_log2);
+    PageNumbers<THREADS> pages;
+    pages.request(a, w, ga << (6 - a.page_log2), min(gb - ga, seg_groups) << (6 - a.page_log2));
     float scale[RT];           // of logits in the exponent's base
     int position[RT];          // of the lane's row; -1 where there is none
 #pragma unroll
@@ -511,13 +598,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
 
     float v_top = two_to(-126);        // values are accumulated over the largest scale so far: codes times 2^0 and less fit binary16
     Segment& seg = sh.run.seg;
-    const int seg_groups = kSegment >> (6 - a.page_log2);
     for (int s0 = ga; s0 < gb; s0 += seg_groups) {
         const int s1 = min(s0 + seg_groups, gb);
-        int mine[kSegment / THREADS];
         __syncthreads();
         if (threadIdx.x == 0) s_top = __float_as_uint(v_top);
-        const bool holes = look_up_pages<THREADS>(a, w, s0 << (6 - a.page_log2), (s1 - s0) << (6 - a.page_log2), seg, mine);
+        if (s0 > ga) pages.request(a, w, s0 << (6 - a.page_log2), (s1 - s0) << (6 - a.page_log2));
+        const bool holes = pages.put(seg);
 
         u4v kw[8], vw[8];
         auto load_keys = [&](int g) {
@@ -546,17 +632,18 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
         };
         int g = s0 + wave;
         if (g < s1) { load_keys(g); load_values(g); }
-        const float top = look_up_scales<THREADS>(a, h, v_top, seg, mine, &s_top);
+        const float top = look_up_scales<THREADS>(a, h, v_top, seg, pages, &s_top);
         if (top > v_top) {
             st.times(v_top / top);
             v_top = top;
         }
         const float v_over = 1.f / v_top;
-        for (; g < s1; g += NW) {
+        // (more: whether the wave has another group.  The last step is a copy of its own: behind a branch the compiler would not know how many loads are
+        // on their way, and wait for the values that were requested last before it takes the keys)
+        auto step = [&](auto more) {
             const int at = ((g - s0) * 64 + 16 * kb) >> a.page_log2;       // the page of the lane's 16 tokens
             const float ks = seg.k_scale[at], vs = seg.v_scale[at] * v_over;
             const bool there = seg.page[at] >= 0;
-            const int next = g + NW;
             const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
             if (edge && !there) {      // (nothing was stored there: it may hold NaN)
 #pragma unroll
@@ -582,7 +669,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
                     }
                     __builtin_amdgcn_sched_barrier(0);      // (what is converted ahead of its product costs registers)
                 }
-                if (half == 1 && next < s1) load_keys(next);
+                if (half == 1 && decltype(more)::value) load_keys(g + NW);
                 h8v e[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
@@ -605,8 +692,10 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
                     if (t & 1) __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (next < s1) load_values(next);
-        }
+            if (decltype(more)::value) load_values(g + NW);
+        };
+        for (; g + NW < s1; g += NW) step(std::true_type{});
+        if (g < s1) step(std::false_type{});
     }
     st.times(v_top);
     __syncthreads();
@@ -671,9 +760,9 @@ __device__ __forceinline__ int value_place(int channel, int chunk) { return (cha
 
 template <bool BF, bool INT8, int RT>
 __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs a) {
-    constexpr int NW = kTileWaves, THREADS = 64 * NW, AHEAD = RT == 1 ? 2 : 1;      // tiles of codes on their way
+    constexpr int NW = kTileWaves, THREADS = 64 * NW, AHEAD = 1;      // tiles of codes on their way
     __shared__ TilesShared sh;
-    __shared__ SlotShared s_slot;
+    __shared__ Sequence s_slot;
     __shared__ int s_last;
     __shared__ unsigned int s_top;
     const PageArgs& p = a.p;
@@ -681,13 +770,16 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
     // Heads take turns (with eight of them each die has one head's pages in its L2); later pieces, which see more, begin first.
     const int h = blockIdx.x % p.n_kv_heads;
     Range w;
-    if (!w.find(a, a.slots - 1 - blockIdx.x / p.n_kv_heads, s_slot)) return;
+    if (!w.find(a, a.slots - 1 - blockIdx.x / p.n_kv_heads, &s_slot)) return;
     const int ga = w.ga, gb = w.gb, active = w.active, split = w.split;
 
     const int r0 = 16 * RT * wave, rows = w.n * p.gq;
     // (of this wave's rows; a wave without any sees nothing)
     const int my_first = w.first + r0 / p.gq, my_last = r0 < rows ? w.first + (min(r0 + 16 * RT, rows) - 1) / p.gq : -1;
     const int seen_by_all = min(my_first + 1, w.closed), hidden_to_some = a.window > 0 ? my_last - a.window + 1 : 0, my_lo = a.window > 0 ? my_first - a.window + 1 : 0;
+    const int seg_groups = kSegment >> (6 - a.page_log2);
+    PageNumbers<THREADS> pages;
+    pages.request(a, w, ga << (6 - a.page_log2), min(gb - ga, seg_groups) << (6 - a.page_log2));
     h8v q[RT][4];
     float scale[RT];
     int position[RT];
@@ -702,13 +794,12 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
 
     float v_top = two_to(-126);
     Segment& seg = sh.seg;
-    const int seg_groups = kSegment >> (6 - a.page_log2);
     for (int s0 = ga; s0 < gb; s0 += seg_groups) {
         const int s1 = min(s0 + seg_groups, gb);
-        int mine[kSegment / THREADS];
         __syncthreads();
         if (threadIdx.x == 0) s_top = __float_as_uint(v_top);
-        const bool holes = look_up_pages<THREADS>(a, w, s0 << (6 - a.page_log2), (s1 - s0) << (6 - a.page_log2), seg, mine);
+        if (s0 > ga) pages.request(a, w, s0 << (6 - a.page_log2), (s1 - s0) << (6 - a.page_log2));
+        const bool holes = pages.put(seg);
 
         // A thread's share of a tile: 16 bytes of two keys, and 16 tokens of two channels.
         u4v kw[AHEAD][2], vw[AHEAD][2];
@@ -743,17 +834,17 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
                 v[value_place(channel, chunk + 1)] = halves_of_codes<INT8>(y[2], y[3], vs);
             }
         };
+        // (requests behind the last tile repeat it: without a branch the compiler knows how many loads are on their way)
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (s0 + u < s1) request(u, s0 + u);
-        const float top = look_up_scales<THREADS>(a, h, v_top, seg, mine, &s_top);
+        for (int u = 0; u < AHEAD; ++u) request(u, min(s0 + u, s1 - 1));
+        const float top = look_up_scales<THREADS>(a, h, v_top, seg, pages, &s_top);
         if (top > v_top) {
             st.times(v_top / top);
             v_top = top;
         }
         v_over = 1.f / v_top;
         build(0, s0);
-        if (s0 + AHEAD < s1) request(0, s0 + AHEAD);
+        request(0, min(s0 + AHEAD, s1 - 1));
         __syncthreads();
         for (int g0 = s0; g0 < s1; g0 += AHEAD) {
 #pragma unroll
@@ -803,7 +894,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
                     }
                 }
                 if (g + 1 < s1) build((u + 1) % AHEAD, g + 1);
-                if (g + 1 + AHEAD < s1) request((u + 1) % AHEAD, g + 1 + AHEAD);
+                request((u + 1) % AHEAD, min(g + 1 + AHEAD, s1 - 1));
                 __syncthreads();
             }
         }
@@ -842,7 +933,6 @@ hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream) {
     const dim3 grid((unsigned)a.slots * a.p.n_kv_heads), threads(256);
     if (row_tiles == 1) paged_rows<BF, INT8, 1><<<grid, threads, 0, stream>>>(a);
     else if (row_tiles == 2) paged_rows<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
-    else if (row_tiles == 4) paged_tiles<BF, INT8, 1><<<grid, threads, 0, stream>>>(a);
     else paged_tiles<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -852,23 +942,21 @@ template hipError_t paged_form<(KVQP_PAGED_BITS - 1) / 2 != 0, (KVQP_PAGED_BITS 
 
 // ---- launches ----
 constexpr int kMostParts = 8192;                    // partial results of 16 rows each that a workspace has room for
-constexpr size_t kPartBytes = 8192 + 128;
+constexpr size_t kPartBytes = 8192 + 2 * 128;
 struct PagedPlan {
-    int row_tiles, per_piece, slots, most_shares, least_groups;
+    int row_tiles, per_piece, slots, most_shares;
     size_t ws_bytes;
 };
 static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, int64_t most_tokens) {
     // (rows of a call over its sequences, as if they were equal)
     const int gq = cfg.n_q_heads / cfg.n_kv_heads, each = (n_rows + cfg.batch - 1) / cfg.batch, columns = each >= 128 ? 128 : each * gq;
     PagedPlan r;
-    r.row_tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : columns <= 64 ? 4 : 8;
+    r.row_tiles = columns > 64 ? 8 : columns > 16 ? 2 : 1;
     r.per_piece = 16 * r.row_tiles / gq;
     const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;
-    static const int kT[4] = {getenv("KT1") ? atoi(getenv("KT1")) : 768, getenv("KT2") ? atoi(getenv("KT2")) : 1024, getenv("KT4") ? atoi(getenv("KT4")) : 1024, getenv("KT8") ? atoi(getenv("KT8")) : 512};
-    r.most_shares = std::min(kT[r.row_tiles == 1 ? 0 : r.row_tiles == 2 ? 1 : r.row_tiles == 4 ? 2 : 3], std::min(kMostParts / r.row_tiles, KVQP_PAGED_COUNTERS / 4) / 2) / cfg.n_kv_heads;
-    r.least_groups = 4;
-    if (most_tokens <= 64 * r.least_groups) r.most_shares = 0;
-    r.slots = pieces + (r.most_shares * 4 + 2) / 3;
+    r.most_shares = (r.row_tiles == 1 ? 384 : 512) / cfg.n_kv_heads;
+    if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = 0;
+    r.slots = pieces + r.most_shares;
     r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;
     return r;
 }
@@ -884,7 +972,6 @@ PageArgs page_args(const kvqp_cfg& cfg, const kvqp_pages& g, const int32_t* row_
 
 // Whether a step's codes are more than what may stay in the memory-side cache, as far as the host knows: the pages that the sequences can have.
 static bool rows_once(const kvqp_cfg& cfg, const kvqp_pages& g) {
-    if (getenv("ONCE")) return atoi(getenv("ONCE"));
     if (cfg.decode_cache_hint != KVQP_CACHE_AUTO) return cfg.decode_cache_hint == KVQP_CACHE_STREAM;
     return std::min((double)g.n_pages, (double)cfg.batch * g.max_pages) * g.page_tokens * cfg.n_kv_heads * 2 * kHeadDim > 96.0 * (1 << 20);
 }
@@ -894,7 +981,7 @@ hipError_t launch_paged_attn(const kvqp_cfg& cfg, const kvqp_pages& g, const voi
     const PagedPlan plan = plan_paged(cfg, n_rows, row_start != nullptr, (int64_t)g.max_pages * g.page_tokens);
     const AttnArgs a = {page_args(cfg, g, row_start, n_rows), (const uint16_t*)q, q_stride, (uint16_t*)out, lse, (unsigned int*)ws,
                         (char*)ws + KVQP_PAGED_COUNTERS, cfg.sm_scale * 1.4426950408889634f, window, g.page_tokens == 16 ? 4 : g.page_tokens == 32 ? 5 : 6,
-                        plan.per_piece, plan.slots, plan.most_shares, plan.least_groups, rows_once(cfg, g)};
+                        plan.per_piece, plan.slots, plan.most_shares, rows_once(cfg, g)};
     if (g.dtype == KVQP_BFLOAT16)
         return g.form == KVQP_INT8 ? paged_form<true, true>(a, plan.row_tiles, stream) : paged_form<true, false>(a, plan.row_tiles, stream);
     return g.form == KVQP_INT8 ? paged_form<false, true>(a, plan.row_tiles, stream) : paged_form<false, false>(a, plan.row_tiles, stream);
