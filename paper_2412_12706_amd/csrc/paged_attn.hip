@@ -26,7 +26,8 @@ struct AttnArgs {
 };
 
 // Groups of 64 tokens that a workgroup has at least, and the most sequences among which work is shared out.
-constexpr int kLeastGroups = 4, kMostSplitBatch = 512;
+constexpr int kLeastGroups = 4;
+[[maybe_unused]] constexpr int kMostSplitBatch = 512;
 
 template <bool BF, bool INT8> hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream);
 
@@ -474,49 +475,64 @@ __device__ __forceinline__ bool arrived_last(unsigned int* count, int of, int* s
     return *s_last != 0;
 }
 constexpr int kJoin = 16;
-template <bool BF>
-__device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, int h, int row_tiles, const Partials& parts, int* s_last) {
+template <bool BF, int RT>
+__device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, int h, const Partials& parts, int* s_last) {
+    constexpr int row_tiles = RT;
     unsigned int* const counts = a.arrivals + w.part_of_head(a, h);
     const int c = threadIdx.x & 15, kb = (threadIdx.x & 63) >> 4, rows = w.n * a.p.gq;
-    // results from, from + step, ... below upto: of an item (four channels of a row), `most` of them requested at once.  (What is requested beyond the last costs
-    // time too: 16 where four splits would do makes a call of 1024 tokens 3 us longer.)
-    auto join_by = [&](auto most, int from, int step, int upto, auto take) {
-        constexpr int MOST = decltype(most)::value;
-        for (int item = threadIdx.x; item < row_tiles * 512; item += 256) {
-            const int r = 16 * (item >> 9) + c;
-            float top = kNegBig, total = 0.f;
-            f4v x = {0.f, 0.f, 0.f, 0.f};
+    // results from, from + step, ... below upto: MOST of an item (four channels of a row) are requested at once, for ITEMS items of a thread, two of a
+    // row tile and then the next.  (What is requested beyond the last costs time too: 16 where four splits would do makes a call of 1024 tokens 3 us longer.)
+    auto join_by = [&](auto most, auto items, int from, int step, int upto, auto take) {
+        constexpr int MOST = decltype(most)::value, ITEMS = decltype(items)::value, TILES = (ITEMS + 1) / 2;
+        for (int item0 = threadIdx.x; item0 < row_tiles * 512; item0 += 256 * ITEMS) {
+            const int r0 = 16 * (item0 >> 9) + c;
+            float top[TILES], total[TILES];
+            f4v x[ITEMS];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) { top[t] = kNegBig; total[t] = 0.f; }
+#pragma unroll
+            for (int e = 0; e < ITEMS; ++e) x[e] = f4v{0.f, 0.f, 0.f, 0.f};
             for (int s0 = from; s0 < upto; s0 += MOST * step) {
-                f4v v[MOST];
-                float2 m[MOST];
+                f4v v[ITEMS][MOST];
+                float2 m[TILES][MOST];
 #pragma unroll
                 for (int u = 0; u < MOST; ++u) {
                     const int s = s0 + u * step < upto ? s0 + u * step : s0;
-                    v[u] = parts.output(s, item);
-                    m[u] = parts.state(s, r);
-                }
-                float higher = top;
 #pragma unroll
-                for (int u = 0; u < MOST; ++u) higher = fmaxf(higher, m[u].x);
-                const float f = __builtin_amdgcn_exp2f(top - higher);
-                x *= f; total *= f;
+                    for (int t = 0; t < TILES; ++t) m[t][u] = parts.state(s, r0 + 16 * t);
 #pragma unroll
-                for (int u = 0; u < MOST; ++u) {
-                    const float by = s0 + u * step < upto ? __builtin_amdgcn_exp2f(m[u].x - higher) : 0.f;
-                    x += v[u] * by;
-                    total = __builtin_fmaf(m[u].y, by, total);
+                    for (int e = 0; e < ITEMS; ++e) v[e][u] = parts.output(s, item0 + 256 * e);
                 }
-                top = higher;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    float higher = top[t];
+#pragma unroll
+                    for (int u = 0; u < MOST; ++u) higher = fmaxf(higher, m[t][u].x);
+                    const float f = __builtin_amdgcn_exp2f(top[t] - higher);
+                    total[t] *= f;
+#pragma unroll
+                    for (int e = 2 * t; e < ITEMS && e < 2 * t + 2; ++e) x[e] *= f;
+#pragma unroll
+                    for (int u = 0; u < MOST; ++u) {
+                        const float by = s0 + u * step < upto ? __builtin_amdgcn_exp2f(m[t][u].x - higher) : 0.f;
+                        total[t] = __builtin_fmaf(m[t][u].y, by, total[t]);
+#pragma unroll
+                        for (int e = 2 * t; e < ITEMS && e < 2 * t + 2; ++e) x[e] += v[e][u] * by;
+                    }
+                    top[t] = higher;
+                }
             }
-            take(item, r, x, top, total);
+#pragma unroll
+            for (int e = 0; e < ITEMS; ++e) take(item0 + 256 * e, r0 + 16 * (e / 2), x[e], top[e / 2], total[e / 2]);
         }
     };
     auto join = [&](int from, int step, int upto, auto take) {
         const int n = (upto - from + step - 1) / step;
-        if (n <= 2) join_by(std::integral_constant<int, 2>{}, from, step, upto, take);
-        else if (n <= 4) join_by(std::integral_constant<int, 4>{}, from, step, upto, take);
-        else if (n <= 8) join_by(std::integral_constant<int, 8>{}, from, step, upto, take);
-        else join_by(std::integral_constant<int, kJoin>{}, from, step, upto, take);
+        constexpr std::integral_constant<int, RT >= 2 ? 4 : 2> items;
+        if (n <= 2) join_by(std::integral_constant<int, 2>{}, items, from, step, upto, take);
+        else if (n <= 4) join_by(std::integral_constant<int, 4>{}, items, from, step, upto, take);
+        else if (n <= 8) join_by(std::integral_constant<int, 8>{}, items, from, step, upto, take);
+        else join_by(std::integral_constant<int, kJoin>{}, std::integral_constant<int, 1>{}, from, step, upto, take);
     };
     int step = 1;
     if (w.active > kJoin) {
@@ -739,7 +755,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
             else if (r < rows) store_out<BF>(a, w, h, r, t, kb, x, inverse_sum(total));
         }
     }
-    if (active > 1) join_splits<BF>(a, w, h, RT, parts, &s_last);
+    if (active > 1) join_splits<BF, RT>(a, w, h, parts, &s_last);
 }
 
 // ---- many rows: the rows are split over waves, which share the tokens ----
@@ -925,7 +941,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
             else if (r < rows) store_out<BF>(a, w, h, r, t, kb, st.o[rt][t], by);
         }
     }
-    if (active > 1) join_splits<BF>(a, w, h, RT * NW, parts, &s_last);
+    if (active > 1) join_splits<BF, RT * NW>(a, w, h, parts, &s_last);
 }
 
 template <bool BF, bool INT8>
@@ -954,7 +970,7 @@ static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, in
     r.row_tiles = columns > 64 ? 8 : columns > 16 ? 2 : 1;
     r.per_piece = 16 * r.row_tiles / gq;
     const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;
-    r.most_shares = (r.row_tiles == 1 ? 384 : 512) / cfg.n_kv_heads;
+    r.most_shares = (r.row_tiles == 2 ? 512 : 384) / cfg.n_kv_heads;
     if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = 0;
     r.slots = pieces + r.most_shares;
     r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;

@@ -480,10 +480,10 @@ def _current_device() -> int:
 
 def _call(name, device, stream, args):
     """Calls an entry point with that GPU as the current one."""
-    import torch
     if _lib is None:
         lib()
     if _current_device() != device:
+        import torch
         with torch.cuda.device(device):
             rc = _fn_rows[name](*args, _stream_handle(stream))
     else:
