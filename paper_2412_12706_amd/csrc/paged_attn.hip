@@ -241,14 +241,17 @@ struct Range {
 };
 
 // Of one row tile a lane has one row (column c) and eight tokens at a time; O^T of the tile is eight accumulators of 16 channels.
+// A weight is 2^(logit + lift), lift = kLift - reference.  (The sums are of the weights before they are rounded for the value product: a product with ones
+// would save the additions, and leave the sum 2^-12 off.)
 template <int RT>
 struct Sums {
     f4v o[RT][8];
-    float ref[RT], sum[RT];
+    float sums[RT], lift[RT];      // (a lane's sum: of its own tokens)
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            ref[rt] = kNegBig; sum[rt] = 0.f;
+            lift[rt] = -kNegBig;
+            sums[rt] = 0.f;
 #pragma unroll
             for (int t = 0; t < 8; ++t) o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
         }
@@ -261,23 +264,28 @@ struct Sums {
     }
     // Products of queries and keys, times f > 0 the logits, into weights; O and the sum follow the reference, which moves when a row has gone far beyond it.
     __device__ __forceinline__ f8v weigh(int rt, const f4v (&x)[2], float f) {
-        float m = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3]))) * f;
-        if (__any(m > ref[rt] + kLag)) {
+        const float most = fmaxf(fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), x[0][2]), fmaxf(x[0][3], x[1][0])), fmaxf(fmaxf(x[1][1], x[1][2]), x[1][3]));
+        if (__any(__builtin_fmaf(most, f, lift[rt]) > kLift + kLag)) {
+            float m = most * f;
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
-            m = fmaxf(m, ref[rt]);
-            const float by = __builtin_amdgcn_exp2f(ref[rt] - m);
-            ref[rt] = m;
-            sum[rt] *= by;
+            const float lower = fminf(lift[rt], kLift - m), by = __builtin_amdgcn_exp2f(lower - lift[rt]);
+            lift[rt] = lower;
+            sums[rt] *= by;
 #pragma unroll
             for (int t = 0; t < 8; ++t) o[rt][t] *= by;
         }
-        const float by = kLift - ref[rt];
         f8v w;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], f, by));
-        sum[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], f, lift[rt]));
+        sums[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
         return w;
+    }
+    __device__ __forceinline__ float reference(int rt) const { return kLift - lift[rt]; }
+    __device__ __forceinline__ float sum(int rt) const {
+        float x = sums[rt];
+        x += __shfl_xor(x, 16);
+        return x + __shfl_xor(x, 32);
     }
 };
 // (a masked product is minus infinity: the factor must not be 0, also where a block of zeros has the smallest scale)
@@ -719,16 +727,15 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
     if (slot >= 0 && wave == (gb - ga) % NW) {       // (a wave that has the fewest groups)
         stage_open_values(a, w, h, slot, sh.open_v, lane, 64);
         __builtin_amdgcn_wave_barrier();
-        attend_open<BF, RT>(a, w, h, slot, sh.open_v, 0, st);
+        attend_open<BF>(a, w, h, slot, sh.open_v, 0, st);
     }
     __syncthreads();
 
     // ---- the waves' results together ----
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        st.sum[rt] += __shfl_xor(st.sum[rt], 16);
-        st.sum[rt] += __shfl_xor(st.sum[rt], 32);
-        if (kb == 0) { sh.join.ref[wave][16 * rt + c] = st.ref[rt]; sh.join.sum[wave][16 * rt + c] = st.sum[rt]; }
+        const float sum = st.sum(rt);
+        if (kb == 0) { sh.join.ref[wave][16 * rt + c] = st.reference(rt); sh.join.sum[wave][16 * rt + c] = sum; }
     }
     __syncthreads();
     const int rows = w.n * p.gq;
@@ -738,7 +745,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
         float top = kNegBig, total = 0.f;
         for (int v = 0; v < NW; ++v) top = fmaxf(top, sh.join.ref[v][16 * rt + c]);
         for (int v = 0; v < NW; ++v) total = __builtin_fmaf(sh.join.sum[v][16 * rt + c], __builtin_amdgcn_exp2f(sh.join.ref[v][16 * rt + c] - top), total);
-        const float f = __builtin_amdgcn_exp2f(st.ref[rt] - top);
+        const float f = __builtin_amdgcn_exp2f(st.reference(rt) - top);
         if (rt) __syncthreads();
 #pragma unroll
         for (int t = 0; t < 8; ++t) sh.join.o[wave][t][lane] = st.o[rt][t] * f;
@@ -819,32 +826,34 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
 
         // A thread's share of a tile: 16 bytes of two keys, and 16 tokens of two channels.
         u4v kw[AHEAD][2], vw[AHEAD][2];
+        // (a wave's 64 pieces are of one page whatever the page size, so a page's place is worked out by scalar instructions)
         auto key_token = [&](int u) { return (threadIdx.x + THREADS * u) >> 3; };
         auto value_bytes = [&](int u) { return (threadIdx.x + THREADS * u) * 16; };      // into the tile's pages, [channel][P] each
+        auto page_place = [&](int g, int u) { return ((g - s0) * 64 + 8 * wave + 32 * u) >> a.page_log2; };      // in the segment, of keys and values alike
         auto request = [&](int slot, int g) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int at = (g - s0) * 64 + key_token(u);
-                const int page = max(seg.page[at >> a.page_log2], 0);
-                kw[slot][u] = *reinterpret_cast<const u4v*>(p.k_codes + (((int64_t)page * p.n_kv_heads + h) * P + (at & (P - 1))) * kHeadDim + 16 * (threadIdx.x & 7));
-                const int part = value_bytes(u) >> (a.page_log2 + 7), v_page = max(seg.page[(((g - s0) * 64) >> a.page_log2) + part], 0);
-                vw[slot][u] = *reinterpret_cast<const u4v*>(p.v_codes + ((int64_t)v_page * p.n_kv_heads + h) * (P * kHeadDim) + (value_bytes(u) & (P * kHeadDim - 1)));
+                const int64_t block = ((int64_t)max(__builtin_amdgcn_readfirstlane(seg.page[page_place(g, u)]), 0) * p.n_kv_heads + h) * (P * kHeadDim);
+                const uint8_t *k = p.k_codes + block, *v = p.v_codes + block;
+                kw[slot][u] = *reinterpret_cast<const u4v*>(k + (uint32_t)((key_token(u) & (P - 1)) * kHeadDim + 16 * (threadIdx.x & 7)));
+                vw[slot][u] = *reinterpret_cast<const u4v*>(v + (uint32_t)(value_bytes(u) & (P * kHeadDim - 1)));
             }
         };
         float v_over;
         auto build = [&](int slot, int g) {
             h8v* k = sh.tile.k[(g - s0) & 1];
             h8v* v = sh.tile.v[(g - s0) & 1];
+            const bool gaps = holes || 64 * (g + 1) > w.closed;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 // (the order of a tile's rows: the kernel above)
                 const int token = key_token(u), row = 16 * ((token >> 2) & 3) + 4 * (token >> 4) + (token & 3), m = threadIdx.x & 7;
                 k[key_place(row, 2 * m)] = halves_of_codes<INT8>(kw[slot][u][0], kw[slot][u][1], 1.f);
                 k[key_place(row, 2 * m + 1)] = halves_of_codes<INT8>(kw[slot][u][2], kw[slot][u][3], 1.f);
-                const int part = value_bytes(u) >> (a.page_log2 + 7), in = value_bytes(u) & (P * kHeadDim - 1), page_at = (((g - s0) * 64) >> a.page_log2) + part;
+                const int part = value_bytes(u) >> (a.page_log2 + 7), in = value_bytes(u) & (P * kHeadDim - 1), page_at = page_place(g, u);
                 const float vs = seg.v_scale[page_at] * v_over;
                 u4v y = vw[slot][u];
-                if (seg.page[page_at] < 0) y = u4v{0, 0, 0, 0};      // (nothing was stored there: it may hold NaN)
+                if (gaps && seg.page[page_at] < 0) y = u4v{0, 0, 0, 0};      // (nothing was stored there: it may hold NaN)
                 const int channel = in >> a.page_log2, chunk = ((part << a.page_log2) + (in & (P - 1))) >> 3;
                 v[value_place(channel, chunk)] = halves_of_codes<INT8>(y[0], y[1], vs);
                 v[value_place(channel, chunk + 1)] = halves_of_codes<INT8>(y[2], y[3], vs);
@@ -873,6 +882,9 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
                     const int at = ((g - s0) * 64 + 16 * kb) >> a.page_log2;
                     const float ks = seg.k_scale[at];
                     const bool there = seg.page[at] >= 0;
+                    float factor[RT];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) factor[rt] = logit_factor(ks, scale[rt]);
                     const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -899,7 +911,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
                                     x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
                                 }
                             }
-                            e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], logit_factor(ks, scale[rt])), h8v);
+                            e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], factor[rt]), h8v);
                         }
 #pragma unroll
                         for (int t = 0; t < 8; ++t) {
@@ -921,18 +933,16 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
         __syncthreads();
         stage_open_values(a, w, h, slot, sh.open_v, threadIdx.x, THREADS);
         __syncthreads();
-        if (my_last >= w.begin) attend_open<BF, RT>(a, w, h, slot, sh.open_v, r0, st);
+        if (my_last >= w.begin) attend_open<BF>(a, w, h, slot, sh.open_v, r0, st);
     }
     const Partials parts(a, w.part_of_head(a, h), active, RT * NW);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        float total = st.sum[rt];
-        total += __shfl_xor(total, 16);
-        total += __shfl_xor(total, 32);
+        const float total = st.sum(rt);
         const int r = r0 + 16 * rt + c;
         if (kb == 0) {
-            if (active > 1) parts.put_state(split, r, st.ref[rt], total);
-            else if (a.lse && r < rows) a.lse[result_at(a, w, h, r)] = log_sum(st.ref[rt], total);
+            if (active > 1) parts.put_state(split, r, st.reference(rt), total);
+            else if (a.lse && r < rows) a.lse[result_at(a, w, h, r)] = log_sum(st.reference(rt), total);
         }
         const float by = inverse_sum(total);
 #pragma unroll
