@@ -777,9 +777,13 @@ struct TilesShared {
     };
     Segment seg;
 };
-// Where 8 channels (chunk) of a key, and 8 tokens (chunk) of a channel, lie in a tile: 16 lanes of consecutive rows read 16 different places of 256 bytes.
-__device__ __forceinline__ int key_place(int row, int chunk) { return row * 16 + (chunk ^ (row & 15)); }
-__device__ __forceinline__ int value_place(int channel, int chunk) { return (channel >> 1) * 16 + (((channel & 1) * 8 + chunk) ^ ((channel >> 1) & 15)); }
+// Where 8 channels (chunk) of a key, and 8 tokens (chunk) of a channel, lie in a tile: any eight lanes that read (consecutive rows) or write (the two chunks
+// of a thread's 16 bytes one after the other, whatever the page size) at the same time meet all eight places of 128 bytes.
+__device__ __forceinline__ int key_place(int row, int chunk) { return row * 16 + ((chunk >> 1 | (chunk & 1) << 3) ^ (row & 7)); }
+__device__ __forceinline__ int value_place(int channel, int chunk) {
+    const int line = channel >> 1;
+    return line * 16 + ((chunk >> 1 | (channel & 1) << 2 | (chunk & 1) << 3) ^ ((line & 1) << 1 | (line >> 1 & 1)));
+}
 
 template <bool BF, bool INT8, int RT>
 __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs a) {
