@@ -6,55 +6,65 @@
 namespace kvqp {
 
 // ---- rotation ----
-// Eight threads share a row: thread u has two pieces of eight channels, and with them eight whole pairs, in either layout.
+// Eight threads share a row: thread u has two pieces of eight channels, and with them eight whole pairs, in either layout; the eight threads' first
+// pieces are next to each other, and their second ones (two neighbours a thread: 40 % longer where accesses are not gathered on the way).
 struct Turn {
     const float* table;
     int n_positions, rot_dim;
     bool interleaved, inverse;
 };
-// Numbers (by eights) of thread u's two pieces of a row.
-__device__ inline int2 pieces_of(const Turn& t, int u) {
+// Numbers (by eights) of thread u's two pieces of a row, and whether they turn.
+struct Pieces {
+    int lo, hi;
+    bool lo_turns, hi_turns;
+};
+__device__ inline Pieces pieces_of(const Turn& t, int u) {
+    if (!t.table) return {u, u + 8, false, false};
     const int turning = t.rot_dim >> 4;
-    if (t.interleaved) return make_int2(2 * u, 2 * u + 1);
-    return u < turning ? make_int2(u, u + turning) : make_int2(2 * u, 2 * u + 1);      // (rot_dim / 8 + 2 (u - turning))
+    if (t.interleaved) return {u, u + 8, u < 2 * turning, u + 8 < 2 * turning};
+    if (u < turning) return {u, u + turning, true, true};
+    return {2 * turning + u - turning, 8 + u, false, false};      // (what does not turn, in two halves)
 }
 struct Angles {
     f8v c, s;
 };
-// Of pairs 8 u .. 8 u + 7 at a position; NaN behind the table.
-__device__ inline Angles angles_at(const Turn& t, int position, int u) {
-    Angles g;
+// Of pairs 8 u .. 8 u + 7, or interleaved 4 u .. 4 u + 3 and 32 places on, at a position; NaN behind the table.
+__device__ inline Angles angles_at(const Turn& t, const Pieces& at, int position, int u) {
+    Angles g = {};
     if (position >= t.n_positions) {
         g.c = g.s = f8v(__builtin_nanf(""));
         return g;
     }
-    const float4* at = reinterpret_cast<const float4*>(t.table + (size_t)position * t.rot_dim + 16 * u);
+    const float4* lo = reinterpret_cast<const float4*>(t.table + (size_t)position * t.rot_dim + (t.interleaved ? 8 : 16) * u);
+    const float4* hi = lo + (t.interleaved ? 16 : 2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float4 w = at[j];
+        float4 w = {0.f, 0.f, 0.f, 0.f};
+        if (j < 2 ? at.lo_turns : at.hi_turns) w = j < 2 ? lo[j] : hi[j - 2];
         g.c[2 * j] = w.x; g.s[2 * j] = w.y; g.c[2 * j + 1] = w.z; g.s[2 * j + 1] = w.w;
     }
     if (t.inverse) g.s = -g.s;
     return g;
 }
 // (products and sums rounded one by one, as the definition has it: the build allows no contraction)
-__device__ inline void turn(f8v& x, f8v& y, const Angles& g, bool interleaved) {
+__device__ inline void turn(f8v& x, f8v& y, const Pieces& at, const Angles& g, bool interleaved) {
     if (!interleaved) {
         const f8v a = x * g.c - y * g.s, b = y * g.c + x * g.s;
-        x = a; y = b;
+        if (at.lo_turns) { x = a; y = b; }
         return;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float a = x[2 * j] * g.c[j] - x[2 * j + 1] * g.s[j], b = x[2 * j + 1] * g.c[j] + x[2 * j] * g.s[j];
         const float c = y[2 * j] * g.c[4 + j] - y[2 * j + 1] * g.s[4 + j], d = y[2 * j + 1] * g.c[4 + j] + y[2 * j] * g.s[4 + j];
-        x[2 * j] = a; x[2 * j + 1] = b; y[2 * j] = c; y[2 * j + 1] = d;
+        if (at.lo_turns) { x[2 * j] = a; x[2 * j + 1] = b; }
+        if (at.hi_turns) { y[2 * j] = c; y[2 * j + 1] = d; }
     }
 }
 template <bool BF>
-__device__ inline void turn_words(uint4& x, uint4& y, const Angles& g, bool interleaved) {
+__device__ inline void turn_words(uint4& x, uint4& y, const Pieces& at, const Angles& g, bool interleaved) {
     f8v a = numbers<BF>(x), b = numbers<BF>(y);
-    turn(a, b, g, interleaved);
+    turn(a, b, at, g, interleaved);
     x = rounded<BF>(a); y = rounded<BF>(b);
 }
 
@@ -76,7 +86,8 @@ hipError_t launch_rope_table(const double* inv_freq, int rot_dim, int n_position
     return hipGetLastError();
 }
 
-// Bound by memory.  32 rows of consecutive positions a workgroup, `per` heads of each one after the other with the same angles in registers.
+// Bound by memory.  32 rows of consecutive positions a workgroup, `per` heads of each with the same angles in registers.
+constexpr int kAtOnce = 4;
 struct RotateArgs {
     Turn t;
     const uint16_t* x; int64_t xb, xh, xr;
@@ -90,18 +101,28 @@ __global__ __launch_bounds__(256) void rotate(RotateArgs a) {
     if (row >= a.rows) return;
     const int position = a.positions ? a.positions[batch * a.positions_stride + row] : a.first + row;
     if (position < 0) return;
-    const bool turns = u < (a.t.rot_dim >> 4);
-    const int2 at = pieces_of(a.t, u);
+    const Pieces at = pieces_of(a.t, u);
     Angles g = {};
-    if (turns) g = angles_at(a.t, position, u);
+    if (at.lo_turns) g = angles_at(a.t, at, position, u);
     const int h0 = blockIdx.y * a.per, h1 = min(h0 + a.per, a.heads);
     const uint16_t* x = a.x + batch * a.xb + row * a.xr;
     uint16_t* out = a.out + batch * a.ob + row * a.orow;
-    for (int h = h0; h < h1; ++h) {
-        uint4 lo = *reinterpret_cast<const uint4*>(x + h * a.xh + 8 * at.x), hi = *reinterpret_cast<const uint4*>(x + h * a.xh + 8 * at.y);
-        if (turns) turn_words<BF>(lo, hi, g, a.t.interleaved);
-        *reinterpret_cast<uint4*>(out + h * a.oh + 8 * at.x) = lo;
-        *reinterpret_cast<uint4*>(out + h * a.oh + 8 * at.y) = hi;
+    // (four heads' rows are requested before the first is stored)
+    for (int h = h0; h < h1; h += kAtOnce) {
+        uint4 lo[kAtOnce], hi[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const uint16_t* from = x + min(h + i, h1 - 1) * a.xh;
+            lo[i] = *reinterpret_cast<const uint4*>(from + 8 * at.lo);
+            hi[i] = *reinterpret_cast<const uint4*>(from + 8 * at.hi);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (h + i >= h1) break;
+            if (at.lo_turns) turn_words<BF>(lo[i], hi[i], at, g, a.t.interleaved);
+            *reinterpret_cast<uint4*>(out + (h + i) * a.oh + 8 * at.lo) = lo[i];
+            *reinterpret_cast<uint4*>(out + (h + i) * a.oh + 8 * at.hi) = hi[i];
+        }
     }
 }
 hipError_t launch_rotate(const kvqp_rope& rope, int dtype, int batch, int heads, int rows, const kvqp_rows& x, const kvqp_rows& out,
@@ -158,6 +179,8 @@ __device__ inline f8v finite(f8v x) {
     for (int j = 0; j < 8; ++j) x[j] = x[j] != x[j] ? 0.f : fminf(fmaxf(x[j], -most), most);
     return x;
 }
+template <bool BF>
+__device__ inline uint4 finite_words(uint4 w) { return rounded<BF>(finite<BF>(numbers<BF>(w))); }
 __device__ inline float largest(f8v x) {
     float m = fabsf(x[0]);
 #pragma unroll
@@ -169,7 +192,7 @@ __device__ inline float largest(f8v x) {
 // the tokens that the open part held before.
 template <bool BF, bool INT8, int P>
 __global__ __launch_bounds__(256) void append(AppendArgs a) {
-    constexpr int TOKENS = P < 32 ? P : 32, PASSES = P / TOKENS, GROUPS = 32 / TOKENS;
+    constexpr int TOKENS = P < 32 ? P : 32, PASSES = P / TOKENS, GROUPS = 32 / TOKENS, AT_ONCE = kAtOnce / GROUPS;
     __shared__ Sequence found;
     __shared__ float s_max[2][4];
     __shared__ __align__(16) uint8_t s_codes[128][P + 4];
@@ -181,37 +204,30 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
     const int block = first + (int)blockIdx.x - first_piece(p, seq, P, 2);
     if (block < first || (int64_t)block * P >= seq.length) return;
     const int h = blockIdx.y, u = threadIdx.x & 7, token = (threadIdx.x >> 3) % TOKENS, group = (threadIdx.x >> 3) / TOKENS;
-    const int2 at = pieces_of(a.t, u);
-    const bool turns = a.t.table && u < (a.t.rot_dim >> 4);
+    const Pieces at = pieces_of(a.t, u);
     const int slot = slot_of(p, b), last = (seq.length - 1) / P;
     uint16_t* const open_k = p.open_k + ((int64_t)max(slot, 0) * p.n_kv_heads + h) * (2 * P * kHeadDim);
     uint16_t* const open_v = p.open_v + ((int64_t)max(slot, 0) * p.n_kv_heads + h) * (2 * P * kHeadDim);
     auto row_of = [&](int t) { return seq.row0 + t - seq.position(0); };
     auto angles = [&](int t, bool& turning) {
         Angles g = {};
-        turning = turns;
-        if (turns) {
+        turning = at.lo_turns;
+        if (turning) {
             const int position = a.positions ? a.positions[row_of(t)] : t;
             turning = position >= 0;
-            if (turning) g = angles_at(a.t, position, u);
+            if (turning) g = angles_at(a.t, at, position, u);
         }
         return g;
     };
-    auto key = [&](int t, const Angles& g, bool turning, uint4& lo, uint4& hi) {      // as it is stored
-        const uint16_t* x = a.k + row_of(t) * a.k_stride + h * kHeadDim;
-        f8v y = numbers<BF>(*reinterpret_cast<const uint4*>(x + 8 * at.x)), z = numbers<BF>(*reinterpret_cast<const uint4*>(x + 8 * at.y));
-        if (turning) turn(y, z, g, a.t.interleaved);
+    auto key = [&](const Angles& g, bool turning, uint4& lo, uint4& hi) {      // a row as it came into one as it is stored
+        f8v y = numbers<BF>(lo), z = numbers<BF>(hi);
+        if (turning) turn(y, z, at, g, a.t.interleaved);
         lo = rounded<BF>(finite<BF>(y)); hi = rounded<BF>(finite<BF>(z));
-    };
-    auto value = [&](int t, uint4& lo, uint4& hi) {
-        const uint16_t* x = a.v + row_of(t) * a.v_stride + h * kHeadDim + 16 * u;
-        lo = rounded<BF>(finite<BF>(numbers<BF>(*reinterpret_cast<const uint4*>(x))));
-        hi = rounded<BF>(finite<BF>(numbers<BF>(*reinterpret_cast<const uint4*>(x + 8))));
     };
     auto open_row = [&](uint16_t* open, int t) { return open + (t % (2 * P)) * kHeadDim; };
     auto keep_key = [&](int t, uint4 lo, uint4 hi) {
-        *reinterpret_cast<uint4*>(open_row(open_k, t) + 8 * at.x) = lo;
-        *reinterpret_cast<uint4*>(open_row(open_k, t) + 8 * at.y) = hi;
+        *reinterpret_cast<uint4*>(open_row(open_k, t) + 8 * at.lo) = lo;
+        *reinterpret_cast<uint4*>(open_row(open_k, t) + 8 * at.hi) = hi;
     };
     auto keep_value = [&](int t, uint4 lo, uint4 hi) {
         *reinterpret_cast<uint4*>(open_row(open_v, t) + 16 * u) = lo;
@@ -232,29 +248,42 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
         if (t >= begin && t < seq.length) {
             bool turning;
             const Angles g = angles(t, turning);
+            // (the key's and the value's row, and four query heads' at a time, are requested before anything is stored)
+            const uint16_t *k = a.k + row_of(t) * a.k_stride + h * kHeadDim, *v = a.v + row_of(t) * a.v_stride + h * kHeadDim + 16 * u;
+            if (group == 0) { klo[i] = *reinterpret_cast<const uint4*>(k + 8 * at.lo); khi[i] = *reinterpret_cast<const uint4*>(k + 8 * at.hi); }
+            if (group == GROUPS - 1) { vlo[i] = *reinterpret_cast<const uint4*>(v); vhi[i] = *reinterpret_cast<const uint4*>(v + 8); }
             if (a.q) {
-                for (int r = group; r < p.gq; r += GROUPS) {
-                    const int head = h * p.gq + r;
-                    const uint16_t* x = a.q + row_of(t) * a.q_stride + head * kHeadDim;
-                    uint4 lo = *reinterpret_cast<const uint4*>(x + 8 * at.x), hi = *reinterpret_cast<const uint4*>(x + 8 * at.y);
-                    if (turning) turn_words<BF>(lo, hi, g, a.t.interleaved);
-                    uint16_t* out = a.q_out + ((int64_t)row_of(t) * p.gq * p.n_kv_heads + head) * kHeadDim;
-                    *reinterpret_cast<uint4*>(out + 8 * at.x) = lo;
-                    *reinterpret_cast<uint4*>(out + 8 * at.y) = hi;
+                const uint16_t* x = a.q + row_of(t) * a.q_stride + h * p.gq * kHeadDim;
+                uint16_t* out = a.q_out + ((int64_t)row_of(t) * p.gq * p.n_kv_heads + h * p.gq) * kHeadDim;
+                for (int r = group; r < p.gq; r += GROUPS * AT_ONCE) {
+                    uint4 lo[AT_ONCE], hi[AT_ONCE];
+#pragma unroll
+                    for (int j = 0; j < AT_ONCE; ++j) {
+                        const uint16_t* from = x + min(r + j * GROUPS, p.gq - 1) * kHeadDim;
+                        lo[j] = *reinterpret_cast<const uint4*>(from + 8 * at.lo);
+                        hi[j] = *reinterpret_cast<const uint4*>(from + 8 * at.hi);
+                    }
+#pragma unroll
+                    for (int j = 0; j < AT_ONCE; ++j) {
+                        if (r + j * GROUPS >= p.gq) break;
+                        if (turning) turn_words<BF>(lo[j], hi[j], at, g, a.t.interleaved);
+                        *reinterpret_cast<uint4*>(out + (r + j * GROUPS) * kHeadDim + 8 * at.lo) = lo[j];
+                        *reinterpret_cast<uint4*>(out + (r + j * GROUPS) * kHeadDim + 8 * at.hi) = hi[j];
+                    }
                 }
             }
             if (group == 0) {
-                key(t, g, turning, klo[i], khi[i]);
+                key(g, turning, klo[i], khi[i]);
                 if (keeps) keep_key(t, klo[i], khi[i]);
             }
             if (group == GROUPS - 1) {
-                value(t, vlo[i], vhi[i]);
+                vlo[i] = finite_words<BF>(vlo[i]); vhi[i] = finite_words<BF>(vhi[i]);
                 if (keeps) keep_value(t, vlo[i], vhi[i]);
             }
         } else if (full && t < begin && slot >= 0) {
             if (group == 0) {
-                klo[i] = *reinterpret_cast<const uint4*>(open_row(open_k, t) + 8 * at.x);
-                khi[i] = *reinterpret_cast<const uint4*>(open_row(open_k, t) + 8 * at.y);
+                klo[i] = *reinterpret_cast<const uint4*>(open_row(open_k, t) + 8 * at.lo);
+                khi[i] = *reinterpret_cast<const uint4*>(open_row(open_k, t) + 8 * at.hi);
             }
             if (group == GROUPS - 1) {
                 vlo[i] = *reinterpret_cast<const uint4*>(open_row(open_v, t) + 16 * u);
@@ -283,8 +312,8 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
             const int t = i * TOKENS + token;
             if (group == 0 && page >= 0) {
                 uint8_t* to = p.k_codes + (block_at * P + t) * kHeadDim;
-                *reinterpret_cast<uint2*>(to + 8 * at.x) = codes_of<INT8>(numbers<BF>(klo[i]) * fk);
-                *reinterpret_cast<uint2*>(to + 8 * at.y) = codes_of<INT8>(numbers<BF>(khi[i]) * fk);
+                *reinterpret_cast<uint2*>(to + 8 * at.lo) = codes_of<INT8>(numbers<BF>(klo[i]) * fk);
+                *reinterpret_cast<uint2*>(to + 8 * at.hi) = codes_of<INT8>(numbers<BF>(khi[i]) * fk);
             }
             if (group == GROUPS - 1) {
                 const uint2 lo = codes_of<INT8>(numbers<BF>(vlo[i]) * fv), hi = codes_of<INT8>(numbers<BF>(vhi[i]) * fv);
@@ -309,9 +338,13 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
     for (int t = late * P + token; t < min((late + 1) * P, seq.length); t += TOKENS) {
         bool turning;
         const Angles g = angles(t, turning);
-        uint4 lo, hi;
-        if (group == 0) { key(t, g, turning, lo, hi); keep_key(t, lo, hi); }
-        if (group == GROUPS - 1) { value(t, lo, hi); keep_value(t, lo, hi); }
+        const uint16_t *k = a.k + row_of(t) * a.k_stride + h * kHeadDim, *v = a.v + row_of(t) * a.v_stride + h * kHeadDim + 16 * u;
+        if (group == 0) {
+            uint4 lo = *reinterpret_cast<const uint4*>(k + 8 * at.lo), hi = *reinterpret_cast<const uint4*>(k + 8 * at.hi);
+            key(g, turning, lo, hi);
+            keep_key(t, lo, hi);
+        }
+        if (group == GROUPS - 1) keep_value(t, finite_words<BF>(*reinterpret_cast<const uint4*>(v)), finite_words<BF>(*reinterpret_cast<const uint4*>(v + 8)));
     }
 }
 
