@@ -230,8 +230,8 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
         *reinterpret_cast<uint4*>(open_row(open_k, t) + 8 * at.hi) = hi;
     };
     auto keep_value = [&](int t, uint4 lo, uint4 hi) {
-        *reinterpret_cast<uint4*>(open_row(open_v, t) + 16 * u) = lo;
-        *reinterpret_cast<uint4*>(open_row(open_v, t) + 16 * u + 8) = hi;
+        *reinterpret_cast<uint4*>(open_row(open_v, t) + 8 * u) = lo;
+        *reinterpret_cast<uint4*>(open_row(open_v, t) + 8 * u + 64) = hi;
     };
 
     const bool full = (block + 1) * P <= seq.length;
@@ -249,9 +249,9 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
             bool turning;
             const Angles g = angles(t, turning);
             // (the key's and the value's row, and four query heads' at a time, are requested before anything is stored)
-            const uint16_t *k = a.k + row_of(t) * a.k_stride + h * kHeadDim, *v = a.v + row_of(t) * a.v_stride + h * kHeadDim + 16 * u;
+            const uint16_t *k = a.k + row_of(t) * a.k_stride + h * kHeadDim, *v = a.v + row_of(t) * a.v_stride + h * kHeadDim + 8 * u;
             if (group == 0) { klo[i] = *reinterpret_cast<const uint4*>(k + 8 * at.lo); khi[i] = *reinterpret_cast<const uint4*>(k + 8 * at.hi); }
-            if (group == GROUPS - 1) { vlo[i] = *reinterpret_cast<const uint4*>(v); vhi[i] = *reinterpret_cast<const uint4*>(v + 8); }
+            if (group == GROUPS - 1) { vlo[i] = *reinterpret_cast<const uint4*>(v); vhi[i] = *reinterpret_cast<const uint4*>(v + 64); }
             if (a.q) {
                 const uint16_t* x = a.q + row_of(t) * a.q_stride + h * p.gq * kHeadDim;
                 uint16_t* out = a.q_out + ((int64_t)row_of(t) * p.gq * p.n_kv_heads + h * p.gq) * kHeadDim;
@@ -286,8 +286,8 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
                 khi[i] = *reinterpret_cast<const uint4*>(open_row(open_k, t) + 8 * at.hi);
             }
             if (group == GROUPS - 1) {
-                vlo[i] = *reinterpret_cast<const uint4*>(open_row(open_v, t) + 16 * u);
-                vhi[i] = *reinterpret_cast<const uint4*>(open_row(open_v, t) + 16 * u + 8);
+                vlo[i] = *reinterpret_cast<const uint4*>(open_row(open_v, t) + 8 * u);
+                vhi[i] = *reinterpret_cast<const uint4*>(open_row(open_v, t) + 8 * u + 64);
             }
         }
     }
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
                 const uint2 lo = codes_of<INT8>(numbers<BF>(vlo[i]) * fv), hi = codes_of<INT8>(numbers<BF>(vhi[i]) * fv);
                 const uint32_t w[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s_codes[16 * u + j][t] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+                for (int j = 0; j < 16; ++j) s_codes[8 * u + j + (j < 8 ? 0 : 56)][t] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
             }
         }
         __syncthreads();
@@ -338,13 +338,13 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
     for (int t = late * P + token; t < min((late + 1) * P, seq.length); t += TOKENS) {
         bool turning;
         const Angles g = angles(t, turning);
-        const uint16_t *k = a.k + row_of(t) * a.k_stride + h * kHeadDim, *v = a.v + row_of(t) * a.v_stride + h * kHeadDim + 16 * u;
+        const uint16_t *k = a.k + row_of(t) * a.k_stride + h * kHeadDim, *v = a.v + row_of(t) * a.v_stride + h * kHeadDim + 8 * u;
         if (group == 0) {
             uint4 lo = *reinterpret_cast<const uint4*>(k + 8 * at.lo), hi = *reinterpret_cast<const uint4*>(k + 8 * at.hi);
             key(g, turning, lo, hi);
             keep_key(t, lo, hi);
         }
-        if (group == GROUPS - 1) keep_value(t, finite_words<BF>(*reinterpret_cast<const uint4*>(v)), finite_words<BF>(*reinterpret_cast<const uint4*>(v + 8)));
+        if (group == GROUPS - 1) keep_value(t, finite_words<BF>(*reinterpret_cast<const uint4*>(v)), finite_words<BF>(*reinterpret_cast<const uint4*>(v + 64)));
     }
 }
 

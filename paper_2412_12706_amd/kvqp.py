@@ -470,24 +470,30 @@ def _check_room(what, cfg: Cfg, cache: Cache, rows: int, device):
         _want(f"{what}.head_n_kept", counts, torch.int32, counts.shape if counts.numel() == heads else (heads,), device)
 
 
-def _current_device() -> int:
+_raw = None         # torch's current device, and its current stream's handle on one, as plain functions (the public ones take 3 us more)
+
+
+def _raw_functions():
+    global _raw
     import torch
-    try:                # (torch.cuda.current_device() takes 0.5 us more)
-        return torch._C._cuda_getDevice()
-    except AttributeError:
-        return torch.cuda.current_device()
+    try:
+        _raw = (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    except AttributeError:      # (undocumented names: a torch without them takes the public way)
+        _raw = (torch.cuda.current_device, lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw
 
 
 def _call(name, device, stream, args):
     """Calls an entry point with that GPU as the current one."""
     if _lib is None:
         lib()
-    if _current_device() != device:
+    current, handle = _raw or _raw_functions()
+    if current() != device:
         import torch
         with torch.cuda.device(device):
             rc = _fn_rows[name](*args, _stream_handle(stream))
     else:
-        rc = _fn_rows[name](*args, _stream_handle(stream))
+        rc = _fn_rows[name](*args, handle(device) if stream is None else stream.cuda_stream)
     if rc:
         raise KvqpError(rc, name)
 
@@ -694,31 +700,41 @@ def _row_type(what, t, device, dtype=None):
                      f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
+def _empty_rows(shape, dtype, device, stream):
+    """Memory for a call's output, as _empty_output."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _memory_of(stream):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    if out.is_cuda:
+        out.record_stream(torch.cuda.current_stream(out.device))
+    return out
+
+
 def rotate(rope: Rope, x, positions=None, first: int = 0, out=None, inverse: bool = False, stream=None):
     """kvqp_rotate: x [B,H,N,128] float16 or bfloat16, strided as it may be, -> out (contiguous unless given; x itself is allowed).
     positions int32 [N] or [B,N], or None for first, first + 1, ..."""
-    import torch
     device = x.get_device()
     kind, x_strides = _row_type("x", x, device)
     turn = rope._bytes(device)
-    b, h, n, _ = x.shape
-    per_batch = 0
+    shape = x.shape
+    b, h, n, _ = shape
+    at = per_batch = 0
     if positions is not None:
+        import torch
         per_batch = int(positions.dim() == 2)
         _want("positions", positions, torch.int32, (b, n) if per_batch else (n,), device)
+        at = positions.data_ptr()
     if out is None:
-        with _memory_of(stream):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if stream is not None and out.is_cuda:
-            out.record_stream(torch.cuda.current_stream(out.device))
+        out = _empty_rows(shape, x.dtype, x.device, stream)
     _, out_strides = _row_type("out", out, device, x.dtype)
-    if out.shape != x.shape:
-        raise ValueError(f"out: shape {tuple(x.shape)} is needed, not {tuple(out.shape)}")
-    if x.numel() == 0:
+    if out.shape != shape:
+        raise ValueError(f"out: shape {tuple(shape)} is needed, not {tuple(out.shape)}")
+    if b == 0 or h == 0 or n == 0:
         return out
     _call("kvqp_rotate", device, stream,
-          (turn, kind, b, h, n, _pack_rows(x.data_ptr(), *x_strides), _pack_rows(out.data_ptr(), *out_strides), _addr(positions),
-           per_batch, first, int(inverse)))
+          (turn, kind, b, h, n, _pack_rows(x.data_ptr(), *x_strides), _pack_rows(out.data_ptr(), *out_strides), at, per_batch, first, 1 if inverse else 0))
     return out
 
 
@@ -815,10 +831,7 @@ def paged_append(cfg: Cfg, pages: Pages, k, v, row_start=None, q=None, rope: Rop
     if q is not None:
         qs = _packed_rows("q", q, cfg.n_q_heads, n, device, dtype)
         if q_out is None:
-            with _memory_of(stream):
-                q_out = torch.empty((n, cfg.n_q_heads, 128), dtype=dtype, device=q.device)
-            if stream is not None and q_out.is_cuda:
-                q_out.record_stream(torch.cuda.current_stream(q_out.device))
+            q_out = _empty_rows((n, cfg.n_q_heads, 128), dtype, q.device, stream)
         else:
             _want("q_out", q_out, dtype, (n, cfg.n_q_heads, 128), device)
     elif q_out is not None:
@@ -866,10 +879,7 @@ def paged_attn(cfg: Cfg, pages: Pages, q, row_start=None, window: int = 0, out=N
     if lse is not None:
         _want("lse", lse, torch.float32, (n, cfg.n_q_heads), device)
     if out is None:
-        with _memory_of(stream):
-            out = torch.empty((n, cfg.n_q_heads, 128), dtype=dtype, device=q.device)
-        if stream is not None and out.is_cuda:
-            out.record_stream(torch.cuda.current_stream(out.device))
+        out = _empty_rows((n, cfg.n_q_heads, 128), dtype, q.device, stream)
     else:
         _want("out", out, dtype, (n, cfg.n_q_heads, 128), device)
     if n == 0 and row_start is not None:
@@ -891,10 +901,7 @@ def paged_read(cfg: Cfg, pages: Pages, count: int, first: int = 0, k_out=None, v
     shape, outs = (cfg.batch, cfg.n_kv_heads, max(count, 0), 128), []
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         if t is None:
-            with _memory_of(stream):
-                t = torch.empty(shape, dtype=dtype, device=pages.k_codes.device)
-            if stream is not None and t.is_cuda:
-                t.record_stream(torch.cuda.current_stream(t.device))
+            t = _empty_rows(shape, dtype, pages.k_codes.device, stream)
         else:
             _want(name, t, dtype, shape, device)
         outs.append(t)
