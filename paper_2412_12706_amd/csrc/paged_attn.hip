@@ -45,6 +45,8 @@ constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLift = 4.f, kLag = 10.f;
 constexpr int kDeviceScope = 16;      // sc1 in a buffer access' cache policy
 
+constexpr f4v kZero = {0.f, 0.f, 0.f, 0.f};
+
 // ---- codes as binary16 numbers, times a power of two (times 1 for the keys) ----
 // Eight codes of two words.
 template <bool INT8>
@@ -263,10 +265,14 @@ struct Sums {
             for (int t = 0; t < 8; ++t) o[rt][t] *= f;
     }
     // Products of queries and keys, times f > 0 the logits, into weights; O and the sum follow the reference, which moves when a row has gone far beyond it.
+    // (The highest is sought among the exponents: a sum that comes out of a product would cost a further instruction each.)
     __device__ __forceinline__ f8v weigh(int rt, const f4v (&x)[2], float f) {
-        const float most = fmaxf(fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), x[0][2]), fmaxf(x[0][3], x[1][0])), fmaxf(fmaxf(x[1][1], x[1][2]), x[1][3]));
-        if (__any(__builtin_fmaf(most, f, lift[rt]) > kLift + kLag)) {
-            float m = most * f;
+        f8v w;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_fmaf(x[j >> 2][j & 3], f, lift[rt]);
+        const float most = fmaxf(fmaxf(fmaxf(fmaxf(w[0], w[1]), w[2]), fmaxf(w[3], w[4])), fmaxf(fmaxf(w[5], w[6]), w[7]));
+        if (__any(most > kLift + kLag)) {
+            float m = fmaxf(fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), x[0][2]), fmaxf(x[0][3], x[1][0])), fmaxf(fmaxf(x[1][1], x[1][2]), x[1][3])) * f;
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
             const float lower = fminf(lift[rt], kLift - m), by = __builtin_amdgcn_exp2f(lower - lift[rt]);
@@ -274,10 +280,11 @@ struct Sums {
             sums[rt] *= by;
 #pragma unroll
             for (int t = 0; t < 8; ++t) o[rt][t] *= by;
-        }
-        f8v w;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], f, lift[rt]));
+            for (int j = 0; j < 8; ++j) w[j] = __builtin_fmaf(x[j >> 2][j & 3], f, lower);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(w[j]);
         sums[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
         return w;
     }
@@ -678,8 +685,6 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
             for (int half = 0; half < 2; ++half) {
                 f4v x[RT][2];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     h8v q[RT];
 #pragma unroll
@@ -689,7 +694,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
                         const u4v y = kw[2 * (2 * half + t) + (s >> 1)];
                         const h8v k = halves_of_codes<INT8>(y[2 * (s & 1)], y[2 * (s & 1) + 1], 1.f);
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt], x[rt][t], 0, 0, 0);
+                        for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt], s ? x[rt][t] : kZero, 0, 0, 0);
                     }
                     __builtin_amdgcn_sched_barrier(0);      // (what is converted ahead of its product costs registers)
                 }
@@ -894,14 +899,12 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
                     for (int half = 0; half < 2; ++half) {
                         f4v x[RT][2];
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = f4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
                         for (int s = 0; s < 4; ++s)
 #pragma unroll
                             for (int t = 0; t < 2; ++t) {
                                 const h8v k = k_tile[key_place(16 * (2 * half + t) + c, 4 * s + kb)];
 #pragma unroll
-                                for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][s], x[rt][t], 0, 0, 0);
+                                for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][s], s ? x[rt][t] : kZero, 0, 0, 0);
                             }
                         h8v e[RT];
 #pragma unroll
