@@ -124,7 +124,7 @@ def starts_of(counts):
 
 def attention(q, k, v, positions, window, scale):
     """q [n, hq, D] float64 at `positions`, k, v [hkv, t, D] -> out, lse, and how far a kernel may be off before its output is rounded: weights enter the value
-    product as binary16 numbers (2^-12 of themselves), logits are binary32 sums of 128 products and four more roundings, a bfloat16 query is divided
+    product as binary16 numbers (off by 2^-11 of themselves: the steps above 1 are 2^-10, so 1 + 2^-11 is half a step from both its neighbours), logits are binary32 sums of 128 products and four more roundings, a bfloat16 query is divided
     by a power of two and rounded at 2^-25 of its largest, weights below 2^-28 of the largest may be lost, sums of n terms are binary32 ones in some order (the
     outputs in as many steps as there are 32 tokens, a few waves and splits)."""
     n, hq, _ = q.shape
@@ -146,7 +146,7 @@ def attention(q, k, v, positions, window, scale):
             out[i, a] = w @ vv
             d = 132 * 2.0 ** -24 * float((kk.abs() @ q[i, a].abs()).max()) * scale + 2.0 ** -25 * float(q[i, a].abs().max() * kk.abs().sum(1).max()) * scale
             steps = (kk.shape[0] / 32 + 80) * 2.0 ** -24
-            off[i, a] = (2.0 ** -12 + 2 * d + 2 * steps) * (w @ vv.abs()) + kk.shape[0] * 2.0 ** -28 * float(w.max()) * vv.abs().amax(0)
+            off[i, a] = (2.0 ** -11 + 2 * d + 2 * steps) * (w @ vv.abs()) + kk.shape[0] * 2.0 ** -28 * float(w.max()) * vv.abs().amax(0)
             off_lse[i, a] = d + steps + 2.0 ** -22 * abs(float(lse[i, a]))
     return out, lse, off, off_lse
 
