@@ -164,6 +164,7 @@ hipError_t launch_paged_append(const kvqp_cfg& cfg, const kvqp_pages& g, const k
                                hipStream_t stream);
 hipError_t launch_paged_read(const kvqp_cfg& cfg, const kvqp_pages& g, int first, int count, void* k_out, void* v_out, hipStream_t stream);
 size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows);      // of every call with at most n_rows rows
+int64_t paged_attn_workgroups(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows, bool has_starts);
 size_t paged_workspace_need(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows, bool has_starts);
 hipError_t launch_paged_init(void* ws, hipStream_t stream);         // zeroes the counters
 hipError_t launch_paged_attn(const kvqp_cfg& cfg, const kvqp_pages& g, const void* q, int64_t q_stride, int n_rows, const int32_t* row_start, int window,

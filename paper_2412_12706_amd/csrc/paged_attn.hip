@@ -444,9 +444,11 @@ struct PageNumbers {
         for (int u = 0; u < kSegment / THREADS; ++u) {
             const int i = threadIdx.x + THREADS * u, block = first_block + i;
             const int page = a.p.table[(int64_t)w.seq.b * a.p.max_pages + min(block, a.p.max_pages - 1)];
-            const bool read = i < blocks && (int64_t)block << a.page_log2 < w.closed, there = read && (unsigned)page < (unsigned)a.p.n_pages;
+            // (what is before every row's window may be anything, the scales of a page that another sequence has by now as well: not there)
+            const bool read = i < blocks && (int64_t)block << a.page_log2 < w.closed && (int64_t)(block + 1) << a.page_log2 > w.lo;
+            const bool there = read && (unsigned)page < (unsigned)a.p.n_pages;
             mine[u] = there ? page : -1;
-            holes |= read && !there && (block + 1) << a.page_log2 > w.lo;
+            holes |= read && !there;
         }
     }
     __device__ __forceinline__ bool put(Segment& seg) const {
@@ -772,9 +774,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
 
 // ---- many rows: the rows are split over waves, which share the tokens ----
 //
-// Each of four waves has 16 RT rows to itself and goes over all tokens of its workgroup, 64 at a time.  Codes become binary16 numbers once, on their way
-// into LDS, where the tile after the next is being built while two are in use; products and layouts are those of the kernel above.
-constexpr int kTileWaves = 4;
+// Each of four waves has 32 rows to itself and goes over all tokens of its workgroup, 64 at a time.  Codes become binary16 numbers once, on their way
+// into LDS, where the next tile is built beside the one in use, and the codes of the one after it are on their way; products and layouts are those of the kernel above.
+constexpr int kTileWaves = 4, kTileRows = 2;
 struct TilesShared {
     union {
         struct { h8v k[2][64 * 16], v[2][64 * 16]; } tile;
@@ -790,9 +792,9 @@ __device__ __forceinline__ int value_place(int channel, int chunk) {
     return line * 16 + ((chunk >> 1 | (channel & 1) << 2 | (chunk & 1) << 3) ^ ((line & 1) << 1 | (line >> 1 & 1)));
 }
 
-template <bool BF, bool INT8, int RT>
+template <bool BF, bool INT8>
 __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs a) {
-    constexpr int NW = kTileWaves, THREADS = 64 * NW, AHEAD = 1;      // tiles of codes on their way
+    constexpr int NW = kTileWaves, RT = kTileRows, THREADS = 64 * NW;
     __shared__ TilesShared sh;
     __shared__ Sequence s_slot;
     __shared__ int s_last;
@@ -834,34 +836,34 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
         const bool holes = pages.put(seg);
 
         // A thread's share of a tile: 16 bytes of two keys, and 16 tokens of two channels.
-        u4v kw[AHEAD][2], vw[AHEAD][2];
+        u4v kw[2], vw[2];
         // (a wave's 64 pieces are of one page whatever the page size, so a page's place is worked out by scalar instructions)
         auto key_token = [&](int u) { return (threadIdx.x + THREADS * u) >> 3; };
         auto value_bytes = [&](int u) { return (threadIdx.x + THREADS * u) * 16; };      // into the tile's pages, [channel][P] each
         auto page_place = [&](int g, int u) { return ((g - s0) * 64 + 8 * wave + 32 * u) >> a.page_log2; };      // in the segment, of keys and values alike
-        auto request = [&](int slot, int g) {
+        auto request = [&](int g) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int64_t block = ((int64_t)max(__builtin_amdgcn_readfirstlane(seg.page[page_place(g, u)]), 0) * p.n_kv_heads + h) * (P * kHeadDim);
                 const uint8_t *k = p.k_codes + block, *v = p.v_codes + block;
-                kw[slot][u] = *reinterpret_cast<const u4v*>(k + (uint32_t)((key_token(u) & (P - 1)) * kHeadDim + 16 * (threadIdx.x & 7)));
-                vw[slot][u] = *reinterpret_cast<const u4v*>(v + (uint32_t)(value_bytes(u) & (P * kHeadDim - 1)));
+                kw[u] = *reinterpret_cast<const u4v*>(k + (uint32_t)((key_token(u) & (P - 1)) * kHeadDim + 16 * (threadIdx.x & 7)));
+                vw[u] = *reinterpret_cast<const u4v*>(v + (uint32_t)(value_bytes(u) & (P * kHeadDim - 1)));
             }
         };
         float v_over;
-        auto build = [&](int slot, int g) {
+        auto build = [&](int g) {
             h8v* k = sh.tile.k[(g - s0) & 1];
             h8v* v = sh.tile.v[(g - s0) & 1];
-            const bool gaps = holes || 64 * (g + 1) > w.closed;
+            const bool gaps = holes || 64 * (g + 1) > w.closed || 64 * g < w.lo;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 // (the order of a tile's rows: the kernel above)
                 const int token = key_token(u), row = 16 * ((token >> 2) & 3) + 4 * (token >> 4) + (token & 3), m = threadIdx.x & 7;
-                k[key_place(row, 2 * m)] = halves_of_codes<INT8>(kw[slot][u][0], kw[slot][u][1], 1.f);
-                k[key_place(row, 2 * m + 1)] = halves_of_codes<INT8>(kw[slot][u][2], kw[slot][u][3], 1.f);
+                k[key_place(row, 2 * m)] = halves_of_codes<INT8>(kw[u][0], kw[u][1], 1.f);
+                k[key_place(row, 2 * m + 1)] = halves_of_codes<INT8>(kw[u][2], kw[u][3], 1.f);
                 const int part = value_bytes(u) >> (a.page_log2 + 7), in = value_bytes(u) & (P * kHeadDim - 1), page_at = page_place(g, u);
                 const float vs = seg.v_scale[page_at] * v_over;
-                u4v y = vw[slot][u];
+                u4v y = vw[u];
                 if (gaps && seg.page[page_at] < 0) y = u4v{0, 0, 0, 0};      // (nothing was stored there: it may hold NaN)
                 const int channel = in >> a.page_log2, chunk = ((part << a.page_log2) + (in & (P - 1))) >> 3;
                 v[value_place(channel, chunk)] = halves_of_codes<INT8>(y[0], y[1], vs);
@@ -869,69 +871,63 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
             }
         };
         // (requests behind the last tile repeat it: without a branch the compiler knows how many loads are on their way)
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) request(u, min(s0 + u, s1 - 1));
+        request(s0);
         const float top = look_up_scales<THREADS>(a, h, v_top, seg, pages, &s_top);
         if (top > v_top) {
             st.times(v_top / top);
             v_top = top;
         }
         v_over = 1.f / v_top;
-        build(0, s0);
-        request(0, min(s0 + AHEAD, s1 - 1));
+        build(s0);
+        request(min(s0 + 1, s1 - 1));
         __syncthreads();
-        for (int g0 = s0; g0 < s1; g0 += AHEAD) {
+        for (int g = s0; g < s1; ++g) {
+            if (64 * g <= my_last && 64 * g + 63 >= my_lo) {
+                const h8v* k_tile = sh.tile.k[(g - s0) & 1];
+                const h8v* v_tile = sh.tile.v[(g - s0) & 1];
+                const int at = ((g - s0) * 64 + 16 * kb) >> a.page_log2;
+                const float ks = seg.k_scale[at];
+                const bool there = seg.page[at] >= 0;
+                float factor[RT];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int g = g0 + u;
-                if (g >= s1) break;
-                if (64 * g <= my_last && 64 * g + 63 >= my_lo) {
-                    const h8v* k_tile = sh.tile.k[(g - s0) & 1];
-                    const h8v* v_tile = sh.tile.v[(g - s0) & 1];
-                    const int at = ((g - s0) * 64 + 16 * kb) >> a.page_log2;
-                    const float ks = seg.k_scale[at];
-                    const bool there = seg.page[at] >= 0;
-                    float factor[RT];
+                for (int rt = 0; rt < RT; ++rt) factor[rt] = logit_factor(ks, scale[rt]);
+                const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) factor[rt] = logit_factor(ks, scale[rt]);
-                    const bool edge = holes || 64 * g < hidden_to_some || 64 * g + 64 > seen_by_all;
+                for (int half = 0; half < 2; ++half) {
+                    f4v x[RT][2];
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        f4v x[RT][2];
+                    for (int s = 0; s < 4; ++s)
 #pragma unroll
-                        for (int s = 0; s < 4; ++s)
+                        for (int t = 0; t < 2; ++t) {
+                            const h8v k = k_tile[key_place(16 * (2 * half + t) + c, 4 * s + kb)];
 #pragma unroll
-                            for (int t = 0; t < 2; ++t) {
-                                const h8v k = k_tile[key_place(16 * (2 * half + t) + c, 4 * s + kb)];
-#pragma unroll
-                                for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][s], s ? x[rt][t] : kZero, 0, 0, 0);
-                            }
-                        h8v e[RT];
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) {
-                            if (edge) {
-                                const int low = a.window > 0 ? position[rt] - a.window : -1;
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    const int token = 64 * g + 16 * kb + 8 * half + j;
-                                    const bool hidden = !there | (token > position[rt]) | (token <= low);
-                                    x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
-                                }
-                            }
-                            e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], factor[rt]), h8v);
+                            for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][s], s ? x[rt][t] : kZero, 0, 0, 0);
                         }
+                    h8v e[RT];
 #pragma unroll
-                        for (int t = 0; t < 8; ++t) {
-                            const h8v v = v_tile[value_place(16 * t + c, 2 * kb + half)];
+                    for (int rt = 0; rt < RT; ++rt) {
+                        if (edge) {
+                            const int low = a.window > 0 ? position[rt] - a.window : -1;
 #pragma unroll
-                            for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, e[rt], st.o[rt][t], 0, 0, 0);
+                            for (int j = 0; j < 8; ++j) {
+                                const int token = 64 * g + 16 * kb + 8 * half + j;
+                                const bool hidden = !there | (token > position[rt]) | (token <= low);
+                                x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
+                            }
                         }
+                        e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], factor[rt]), h8v);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) {
+                        const h8v v = v_tile[value_place(16 * t + c, 2 * kb + half)];
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, e[rt], st.o[rt][t], 0, 0, 0);
                     }
                 }
-                if (g + 1 < s1) build((u + 1) % AHEAD, g + 1);
-                request((u + 1) % AHEAD, min(g + 1 + AHEAD, s1 - 1));
-                __syncthreads();
             }
+            if (g + 1 < s1) build(g + 1);
+            request(min(g + 2, s1 - 1));
+            __syncthreads();
         }
     }
     st.times(v_top);
@@ -966,7 +962,7 @@ hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream) {
     const dim3 grid((unsigned)a.slots * a.p.n_kv_heads), threads(256);
     if (row_tiles == 1) paged_rows<BF, INT8, 1><<<grid, threads, 0, stream>>>(a);
     else if (row_tiles == 2) paged_rows<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
-    else paged_tiles<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
+    else paged_tiles<BF, INT8><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
 }
 template hipError_t paged_form<(KVQP_PAGED_BITS - 1) / 2 != 0, (KVQP_PAGED_BITS - 1) % 2 != 0>(const AttnArgs&, int, hipStream_t);
@@ -974,8 +970,7 @@ template hipError_t paged_form<(KVQP_PAGED_BITS - 1) / 2 != 0, (KVQP_PAGED_BITS 
 #else
 
 // ---- launches ----
-constexpr int kMostParts = 8192;                    // partial results of 16 rows each that a workspace has room for
-constexpr size_t kPartBytes = 8192 + 2 * 128;
+constexpr size_t kPartBytes = 8192 + 2 * 128;       // a workgroup's results of 16 rows
 struct PagedPlan {
     int row_tiles, per_piece, slots, most_shares;
     size_t ws_bytes;
@@ -986,16 +981,17 @@ static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, in
     PagedPlan r;
     r.row_tiles = columns > 64 ? 8 : columns > 16 ? 2 : 1;
     r.per_piece = 16 * r.row_tiles / gq;
-    const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;
+    const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;      // (at most: each sequence's last may be short)
     r.most_shares = (r.row_tiles == 2 ? 512 : 384) / cfg.n_kv_heads;
     if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = 0;
     r.slots = pieces + r.most_shares;
     r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;
     return r;
 }
-size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows) {
-    (void)cfg; (void)n_rows;
-    return KVQP_PAGED_COUNTERS + kMostParts * kPartBytes;
+// (a plan's bytes do not fall with the rows)
+size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows) { return std::max(plan_paged(cfg, n_rows, true, INT64_MAX).ws_bytes, (size_t)KVQP_PAGED_COUNTERS); }
+int64_t paged_attn_workgroups(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows, bool has_starts) {
+    return (int64_t)plan_paged(cfg, n_rows, has_starts, (int64_t)g.max_pages * g.page_tokens).slots * cfg.n_kv_heads;
 }
 size_t paged_workspace_need(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows, bool has_starts) {
     return plan_paged(cfg, n_rows, has_starts, (int64_t)g.max_pages * g.page_tokens).ws_bytes;
@@ -1013,7 +1009,7 @@ hipError_t launch_paged_attn(const kvqp_cfg& cfg, const kvqp_pages& g, const voi
                              void* out, float* lse, void* ws, hipStream_t stream) {
     const PagedPlan plan = plan_paged(cfg, n_rows, row_start != nullptr, (int64_t)g.max_pages * g.page_tokens);
     const AttnArgs a = {page_args(cfg, g, row_start, n_rows), (const uint16_t*)q, q_stride, (uint16_t*)out, lse, (unsigned int*)ws,
-                        (char*)ws + KVQP_PAGED_COUNTERS, cfg.sm_scale * 1.4426950408889634f, window, g.page_tokens == 16 ? 4 : g.page_tokens == 32 ? 5 : 6,
+                        (char*)ws + KVQP_PAGED_COUNTERS, cfg.sm_scale * 1.4426950408889634f, (int64_t)window < (int64_t)g.max_pages * g.page_tokens ? window : 0, g.page_tokens == 16 ? 4 : g.page_tokens == 32 ? 5 : 6,
                         plan.per_piece, plan.slots, plan.most_shares, rows_once(cfg, g)};
     if (g.dtype == KVQP_BFLOAT16)
         return g.form == KVQP_INT8 ? paged_form<true, true>(a, plan.row_tiles, stream) : paged_form<true, false>(a, plan.row_tiles, stream);

@@ -14,6 +14,8 @@ bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 
 bool good_type(int dtype) { return dtype == KVQP_HALF || dtype == KVQP_BFLOAT16; }
 // (numbers of rows and tokens are 32 bits in the kernels, with room for a sum)
 constexpr int kMost = 1 << 30;
+// What a launch has at most along an axis, of workgroups of 256 threads.
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 24) - 1;
 
 int check_rope(const kvqp_rope* r) {
     if (!r || !r->table || !aligned(r->table, 16) || r->n_positions < 1) return KVQP_ERR_INVALID_ARG;
@@ -96,7 +98,7 @@ int kvqp_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double 
 
 int kvqp_rope_table(const double* inv_freq, int32_t rot_dim, int32_t n_positions, double magnitude, float* table, void* hip_stream) {
     if (!inv_freq || !table || !aligned(table, 8) || rot_dim < 16 || rot_dim > kHeadDim || rot_dim % 16 || n_positions < 1) return KVQP_ERR_INVALID_ARG;
-    if (n_positions > kMost) return KVQP_ERR_UNSUPPORTED;
+    if (n_positions > kMost || (int64_t)n_positions * (rot_dim / 2) > kMostWorkgroups * 256) return KVQP_ERR_UNSUPPORTED;
     if (!isfinite(magnitude)) return KVQP_ERR_INVALID_ARG;
     for (int j = 0; j < rot_dim / 2; ++j)
         if (!isfinite(inv_freq[j])) return KVQP_ERR_INVALID_ARG;
@@ -142,6 +144,7 @@ int kvqp_rotate(const kvqp_rope* rope, int32_t dtype, int32_t batch, int32_t hea
     if (meet(written, {rope->table, (int64_t)rope->n_positions * rope->rot_dim * 4}) ||
         meet(written, {positions, (positions_per_batch ? (int64_t)batch : 1) * rows * 4}))
         return KVQP_ERR_INVALID_ARG;
+    if (rows > kMostWorkgroups * 32) return KVQP_ERR_UNSUPPORTED;
     const kvqp_rows from = {x->data, xs[0], xs[1], xs[2]}, to = {out->data, os[0], os[1], os[2]};
     if (launch_rotate(*rope, dtype, batch, heads, rows, from, to, positions, positions_per_batch != 0, first, inverse != 0, (hipStream_t)hip_stream) != hipSuccess)
         return KVQP_ERR_HIP;
@@ -160,6 +163,7 @@ int kvqp_paged_append(const kvqp_cfg* cfg, const kvqp_pages* pages, const kvqp_r
     const int hq = cfg->n_q_heads, hkv = cfg->n_kv_heads;
     if ((q && !good_stride(q_stride, hq)) || !good_stride(k_stride, hkv) || !good_stride(v_stride, hkv)) return KVQP_ERR_INVALID_ARG;
     if (n_rows == 0) return KVQP_OK;
+    if ((int64_t)n_rows / pages->page_tokens + 2 * (int64_t)cfg->batch > kMostWorkgroups) return KVQP_ERR_UNSUPPORTED;
     Span pool[kPageSpans];
     page_spans(*cfg, *pages, pool);
     const bool in_place = q == q_out && q_stride == (int64_t)hq * kHeadDim;
@@ -199,6 +203,7 @@ int kvqp_paged_attn(const kvqp_cfg* cfg, const kvqp_pages* pages, const void* q,
     if (!q || !out || window < 0) return KVQP_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !good_stride(q_stride, cfg->n_q_heads)) return KVQP_ERR_INVALID_ARG;
     if (n_rows == 0) return KVQP_OK;
+    if (paged_attn_workgroups(*cfg, *pages, n_rows, row_start != nullptr) > kMostWorkgroups) return KVQP_ERR_UNSUPPORTED;
     const size_t need = paged_workspace_need(*cfg, *pages, n_rows, row_start != nullptr);
     if (need > 0 && (!workspace || workspace_bytes < need)) return KVQP_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return KVQP_ERR_INVALID_ARG;
@@ -218,6 +223,7 @@ int kvqp_paged_read(const kvqp_cfg* cfg, const kvqp_pages* pages, int32_t first,
     if (rc) return rc;
     if (first < 0 || count < 0 || (int64_t)first + count > (int64_t)pages->max_pages * pages->page_tokens) return KVQP_ERR_INVALID_ARG;
     if (count == 0) return KVQP_OK;
+    if (count / 64 + 2 > kMostWorkgroups) return KVQP_ERR_UNSUPPORTED;
     if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return KVQP_ERR_INVALID_ARG;
     Span in[kPageSpans];
     page_spans(*cfg, *pages, in);

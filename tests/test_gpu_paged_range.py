@@ -200,3 +200,30 @@ def test_a_sequence_of_open_tokens_alone_and_empty_calls():
     lse = torch.zeros((3, 8), device="cuda")
     out = kvqp.paged_attn(cfg, pool.pages, q[:3], lse=lse)
     assert bool((out[1] == 0).all()) and bool((lse[1] == -math.inf).all()) and bool(torch.isfinite(lse[[0, 2]]).all())
+
+
+@pytest.mark.parametrize("dtype,form", FORMS)
+@pytest.mark.parametrize("page", [16, 32])
+def test_pages_before_a_window_may_be_anybodys(dtype, form, page):
+    """What the table names before every row's window holds NaN codes and scales of every kind: it reaches nobody.  Few rows, and a piece of a prompt."""
+    for count, window in ((1, 100), (5, 70), (200, 130), (300, 40)):
+        g = generator(page + count)
+        pool = Pool(g, [1000], 2, page, dtype, form, most=80)
+        q = torch.randn((count, 8, D), generator=g, device="cuda").to(dtype)
+        cfg, p = config(1, 8, 2), pool.pages
+        want = pool.check(cfg, q, [count], window)
+        gone = p.table[0, :(1000 - count - window + 1) // page].long()
+        p.k_codes.view(torch.uint8)[gone], p.v_codes.view(torch.uint8)[gone] = 0x7F, 0x7F
+        for i, x in enumerate((math.nan, math.inf, 2.0 ** 100)):
+            p.k_scale[gone[i::3]], p.v_scale[gone[i::3]] = x, x
+        got = kvqp.paged_attn(cfg, p, q, ints([0, count]), window=window)
+        assert torch.equal(got, want)
+
+
+def test_a_window_beyond_every_token_is_none():
+    g = generator(12)
+    pool = Pool(g, [700, 90], 2, 16, HALF, "e4m3", most=50)
+    cfg, q = config(2, 8, 2), torch.randn((400, 8, D), generator=g, device="cuda").to(HALF)
+    want = pool.check(cfg, q, [330, 70])
+    for window in (800, 1 << 30, (1 << 31) - 1):
+        assert torch.equal(kvqp.paged_attn(cfg, pool.pages, q, ints([0, 330, 400]), window=window), want)

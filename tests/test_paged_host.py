@@ -160,6 +160,16 @@ def test_read_refuses(lib, kw, code):
     assert call(lib, "kvqp_paged_read", READ, kw) == code
 
 
+def test_more_than_a_launch_can_have(lib):
+    """2^24 workgroups of 256 threads are more threads than a launch counts."""
+    far = {"k": 1 << 50, "v": 1 << 52, "q": 1 << 54, "q_out": 1 << 56}
+    assert call(lib, "kvqp_paged_append", APPEND, {**far, "n": 1 << 28}) == UNSUPPORTED
+    assert call(lib, "kvqp_paged_attn", ATTN, {"q": 1 << 54, "out": 1 << 56, "lse": 0, "n": 1 << 29}) == UNSUPPORTED
+    assert call(lib, "kvqp_paged_read", READ, {"pages": pages(max_pages=1 << 26), "k": 1 << 54, "v": 1 << 56, "count": 1 << 30}) == UNSUPPORTED
+    assert rotate(lib, rope=rope(n=1 << 30), batch=1, heads=1, rows=1 << 29, x=(1 << 50, 128, 128, 128), out=(1 << 52, 128, 128, 128)) == UNSUPPORTED
+    assert kvqp.lib().kvqp_rope_table((C.c_double * 64)(*[1.0] * 64), 128, 1 << 26, 1.0, A, 0) == UNSUPPORTED
+
+
 def test_calls_of_nothing(lib):
     assert call(lib, "kvqp_paged_append", APPEND, {"n": 0}) == 0 and call(lib, "kvqp_paged_attn", ATTN, {"n": 0}) == 0 and call(lib, "kvqp_paged_read", READ, {"count": 0}) == 0
 
