@@ -1,5 +1,10 @@
 // Attention over the paged cache of 8-bit codes (kvqp_paged_attn).
 //
+//   out = sum_t w_t v_t / sum_t w_t,   w_t = 2^(kLift + l_t - r),   l_t = (sm_scale / ln 2) q k_t,   lse = ln 2 (r - kLift + log2 sum_t w_t),
+// in one pass over the tokens: r is a reference near the largest l_t so far, and O and the sum are brought to a new one when it moves.  Two kernels: paged_rows
+// for up to 64 rows of a KV head (query heads times new tokens), bound by reading the codes, and paged_tiles for more, bound by issue and the matrix cores.
+// Numbers below were measured on an MI355X.
+//
 // One object per row type and form: KVQP_PAGED_BITS 1 + 2 * bfloat16 + int8 compiles the kernels, none the launches.
 #include <hip/hip_runtime.h>
 
@@ -22,11 +27,11 @@ struct AttnArgs {
     int per_piece;          // rows of the call that a workgroup has at most
     int slots;              // workgroups of a KV head
     int most_shares;        // how many shares the work of a KV head is cut into at most; 0: sequences are not split
-    bool once;              // loads of codes go round the memory-side cache
+    bool once;              // loads of codes go past the memory-side cache (one tile of rows)
 };
 
 // Groups of 64 tokens that a workgroup has at least, and the most sequences among which work is shared out.
-constexpr int kLeastGroups = 4;
+constexpr int kLeastGroups = 4;      // (one a wave)
 [[maybe_unused]] constexpr int kMostSplitBatch = 512;
 
 template <bool BF, bool INT8> hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream);
@@ -475,8 +480,9 @@ __device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float 
     return __uint_as_float(__builtin_amdgcn_readfirstlane(*s_top));
 }
 
-// Results of a piece's splits are joined by the last workgroup to arrive, in the order of the splits; where there are more than 16, by 16 at a time, the
-// last of each 16 first, and then the last of those their results (one workgroup that reads 96 splits takes 9 us for 16 rows).
+// Results of a piece's splits are joined by the last workgroup to arrive, in the order of the splits (no atomics on results: the same bits every time); where
+// there are more than 16, by 16 at a time, the last of each 16 first, and then the last of those their results (96 splits of 16 rows read by one workgroup
+// alone took 9 us).
 // Partials are stored past this die's L2, and the wait returns when the stores have been acknowledged from there; so whoever sees the
 // counter sees them, with loads that do not look into its own L2.
 __device__ __forceinline__ bool arrived_last(unsigned int* count, int of, int* s_last) {
@@ -586,6 +592,13 @@ __device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, i
 // A wave takes 64 tokens at a time.  S^T = K Q^T by products of 16 tokens and 16 rows: a lane's column is a row (query head and new token) and its
 // group kb of 16 lanes holds tokens 16 kb .. 16 kb + 15, in an order that makes its logits, turned into weights, the second operand of
 // O^T = V^T P^T without leaving the lane; the first operand is 16 consecutive bytes of a channel, as pages store values.
+//
+// Codes go from memory to registers, each wave's own: nobody else in the workgroup needs them, so LDS would add a round trip.  A wave requests the next 64
+// tokens' keys while it works on values, and their values after that.  32 sequences of 8192 tokens, 8 KV heads of 4 query heads (538 MB): 97 us,
+// 5.5 TB/s, more than a large copy reaches.  One sequence of 1024 tokens: 9.5 us, the chain of launch, lengths, table, codes and join.
+// 17 .. 32 rows take two tiles of 16 (two waves a SIMD by registers), more than 32 several workgroups of 32 each, so that keys and values are read
+// from memory once and from the caches again (40 rows of a KV head for each of 48 sequences of up to 16001 tokens, bfloat16 and int8: 212 us for 791 MB, twice through matrix and vector
+// instructions; tiles of 3 and 4 would need 512 registers a lane, and are not used; the kernel of many rows takes 208 .. 303).
 constexpr int kRowsWaves = 4;
 
 template <int RT, int NW>
@@ -595,7 +608,7 @@ union RowsShared {
     struct { f4v o[NW][8][64]; float ref[NW][16 * RT], sum[NW][16 * RT]; } join;
 };
 
-template <bool BF, bool INT8, int RT>
+template <bool BF, bool INT8, int RT, bool ONCE>
 __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(const AttnArgs a) {
     constexpr int NW = kRowsWaves, THREADS = 64 * NW;
     __shared__ RowsShared<RT, NW> sh;
@@ -643,7 +656,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
             const int token = 16 * (c >> 2) + (c & 3), at = (g - s0) * 64 + token;
             const int page = max(seg.page[at >> a.page_log2], 0);
             const uint8_t* k = p.k_codes + (((int64_t)page * p.n_kv_heads + h) * P + (at & (P - 1))) * kHeadDim + 16 * kb;
-            if (a.once) {
+            if constexpr (ONCE) {
 #pragma unroll
                 for (int t = 0; t < 8; ++t) kw[t] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(k + 4 * (t >> 1) * kHeadDim + 64 * (t & 1)));
             } else {
@@ -655,7 +668,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
             const int at = (g - s0) * 64 + 16 * kb;
             const int page = max(seg.page[at >> a.page_log2], 0);
             const uint8_t* v = p.v_codes + ((int64_t)page * p.n_kv_heads + h) * (P * kHeadDim) + c * P + (at & (P - 1));
-            if (a.once) {
+            if constexpr (ONCE) {
 #pragma unroll
                 for (int t = 0; t < 8; ++t) vw[t] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(v + 16 * t * P));
             } else {
@@ -776,6 +789,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
 //
 // Each of four waves has 32 rows to itself and goes over all tokens of its workgroup, 64 at a time.  Codes become binary16 numbers once, on their way
 // into LDS, where the next tile is built beside the one in use, and the codes of the one after it are on their way; products and layouts are those of the kernel above.
+//
+// A prompt of 8192 tokens, 32 heads: 580 us, 0.95 PFLOP/s (a large matrix product reaches 1.19).  At 2.4 GHz a wave takes 2600 cycles for 64 tokens of its 32 rows:
+// 1024 of matrix instructions, 512 of exponentials, 900 of other vector instructions, and the two waves of a SIMD overlap these little.  No difference
+// made, or longer: operands read from LDS a phase ahead (580), the second half's key product before the first half's exponentials in one block (713: it
+// spills), three waves a SIMD with one tile in LDS (1183: it spills), wave priorities for either phase (606, 620).  32 rows a wave, because each
+// fragment read from LDS then meets two row tiles: LDS is busy for 42 % of the time.
 constexpr int kTileWaves = 4, kTileRows = 2;
 struct TilesShared {
     union {
@@ -960,8 +979,9 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
 template <bool BF, bool INT8>
 hipError_t paged_form(const AttnArgs& a, int row_tiles, hipStream_t stream) {
     const dim3 grid((unsigned)a.slots * a.p.n_kv_heads), threads(256);
-    if (row_tiles == 1) paged_rows<BF, INT8, 1><<<grid, threads, 0, stream>>>(a);
-    else if (row_tiles == 2) paged_rows<BF, INT8, 2><<<grid, threads, 0, stream>>>(a);
+    if (row_tiles == 1 && a.once) paged_rows<BF, INT8, 1, true><<<grid, threads, 0, stream>>>(a);
+    else if (row_tiles == 1) paged_rows<BF, INT8, 1, false><<<grid, threads, 0, stream>>>(a);
+    else if (row_tiles == 2) paged_rows<BF, INT8, 2, false><<<grid, threads, 0, stream>>>(a);
     else paged_tiles<BF, INT8><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -976,13 +996,17 @@ struct PagedPlan {
     size_t ws_bytes;
 };
 static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, int64_t most_tokens) {
-    // (rows of a call over its sequences, as if they were equal)
+    // (rows of a call over its sequences, as if they were equal.  Columns: a KV head's rows of a sequence.  One tile of 16 rows where they fit, for a third wave a
+    // SIMD; 64 columns as two workgroups of 32 take 212 us where the kernel of many rows, half of its rows empty, takes 208 to 303)
     const int gq = cfg.n_q_heads / cfg.n_kv_heads, each = (n_rows + cfg.batch - 1) / cfg.batch, columns = each >= 128 ? 128 : each * gq;
     PagedPlan r;
     r.row_tiles = columns > 64 ? 8 : columns > 16 ? 2 : 1;
     r.per_piece = 16 * r.row_tiles / gq;
     const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;      // (at most: each sequence's last may be short)
-    r.most_shares = (r.row_tiles == 2 ? 512 : 384) / cfg.n_kv_heads;
+    // (shares in all, where three, two and two workgroups fit a CU: more of them even out lengths and make more to join.  256, 384, 512 of one tile: 48 sequences of 1 .. 8192
+    // tokens 94, 107, 88 us, 8 of 4096 20.9, 21.0, 20.1, one of 1024 9.6, 9.7, 9.9.  384, 512, 768 of two: 64 rows of 48 sequences 232, 213, 200, of 4 sequences
+    // 34, 30, 47.  256, 384, 512 of tiles: a piece in a window 73, 63, 80, 512 rows over 16000 tokens 227, 201, 158, 4 x 256 rows 115, 88, 106.)
+    r.most_shares = (r.row_tiles == 8 ? 384 : 512) / cfg.n_kv_heads;
     if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = 0;
     r.slots = pieces + r.most_shares;
     r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;
@@ -999,7 +1023,9 @@ size_t paged_workspace_need(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows
 
 PageArgs page_args(const kvqp_cfg& cfg, const kvqp_pages& g, const int32_t* row_start, int n_rows);
 
-// Whether a step's codes are more than what may stay in the memory-side cache, as far as the host knows: the pages that the sequences can have.
+// Whether a step's codes are more than what may stay in the memory-side cache, as far as the host knows: the pages that the sequences can have.  Loads past it
+// save what allocating there costs where nothing is read again before it is gone (past it and not, three caches of one size in turn: 32 x 8192 tokens of 8 heads, 512 MB,
+// 97 and 103 us; 256 MB 55 and 57; 128 MB 33 and 34; 94 MB 27 and 26; 64 MB 21 and 20).  Where 17 .. 64 rows are, pieces read each other's codes from there, and none go past it.
 static bool rows_once(const kvqp_cfg& cfg, const kvqp_pages& g) {
     if (cfg.decode_cache_hint != KVQP_CACHE_AUTO) return cfg.decode_cache_hint == KVQP_CACHE_STREAM;
     return std::min((double)g.n_pages, (double)cfg.batch * g.max_pages) * g.page_tokens * cfg.n_kv_heads * 2 * kHeadDim > 96.0 * (1 << 20);
