@@ -642,8 +642,8 @@ typedef struct kvqp_pages {
 } kvqp_pages;
 
 /*
- * Common to the three calls below: cfg fields used are batch (sequences), n_q_heads, n_kv_heads, head_dim and sm_scale (the others have to be
- * valid).  lengths include the tokens of the call at hand: the rows of sequence b are row_start[b] .. row_start[b + 1] - 1 of the call's row arrays, and
+ * Common to the three calls below: cfg fields used are batch (sequences), n_q_heads, n_kv_heads, head_dim, sm_scale and for kvqp_paged_attn decode_cache_hint
+ * (the others have to be valid).  lengths include the tokens of the call at hand: the rows of sequence b are row_start[b] .. row_start[b + 1] - 1 of the call's row arrays, and
  * they are the last tokens of the sequence, row i of n at position lengths[b] - n + i; so append and attend see the same lengths.
  *   row_start  DEVICE int32 [batch + 1], ascending, within 0 .. n_rows; NULL: one row per sequence (n_rows == batch).
  * Rows of the arrays that belong to no sequence (from row_start[batch] on, as in a padded batch) are neither read nor written.
@@ -664,7 +664,7 @@ int kvqp_paged_append(const kvqp_cfg *cfg, const kvqp_pages *pages, const kvqp_r
                       int64_t k_stride, const void *v, int64_t v_stride, int32_t n_rows, const int32_t *row_start, const int32_t *positions,
                       void *q_out, void *hip_stream);
 
-/* Workspace bytes that every kvqp_paged_attn call of at most n_rows rows is content with, whatever the lengths.  Host only. */
+/* Workspace bytes that every kvqp_paged_attn call of this cfg and at most n_rows rows is content with, whatever the lengths: 9 MB for a step, at most 52 MB.  Host only. */
 int kvqp_paged_workspace_bytes(const kvqp_cfg *cfg, int32_t n_rows, size_t *bytes);
 
 /* Prepares such a workspace, once after its allocation: zeroes the KVQP_PAGED_COUNTERS bytes of arrival counters at its head with a small kernel
@@ -680,8 +680,11 @@ int kvqp_paged_workspace_init(void *workspace, size_t workspace_bytes, void *hip
  *   out  dtype [n_rows, Hq, 128], contiguous;  lse  float [n_rows, Hq] or NULL: natural logarithm of the sum of exp(logit)
  * A row that attends nothing gets zeros and -inf.  What a row does not attend does not reach it.  Reproducible bit for bit.
  * out and lse lie apart from all that is read.
- * Numerical range: any finite rows.  Products are exact, sums binary32; a weight enters the value product as a binary16 number (2^-12 of itself, or 2^-29 of the
- * row's largest, where that is more), a value below 2^-24 of the largest scale among its sequence's pages loses bits.
+ * Numerical range: rows whose products with keys, times sm_scale, binary32 holds, and values below 2^80.  Products are exact, sums binary32; a weight enters the value
+ * product as a binary16 number (2^-11 of itself, or 2^-29 of the row's largest, where that is more), a value below 2^-24 of the largest scale among its sequence's
+ * pages loses bits, and so does an element of a bfloat16 query below 2^-14 of its row's largest.
+ * decode_cache_hint: KVQP_CACHE_AUTO is KVQP_CACHE_STREAM where the pages that the sequences can have (min(n_pages, batch max_pages)) are more than 96 MB, else
+ * KVQP_CACHE_KEEP; it counts where a KV head has no more than 16 rows of a sequence (query heads times new tokens), as in a step.
  * Workspace: kvqp_paged_workspace_bytes, 16-byte aligned, prepared once.  It may serve calls of any configurations for which it is large
  * enough; calls that share one must not overlap in time.
  */

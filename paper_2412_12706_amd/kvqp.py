@@ -651,7 +651,8 @@ def rope_frequencies(rot_dim: int = 128, base: float = 10000.0, scaling: int = R
 
 
 class _Described:
-    """An object whose fields describe device memory: they are checked and packed for the library once, and again after one of them is assigned."""
+    """An object whose fields describe device memory: they are checked and packed for the library once, and again after one of them is assigned
+    or has other memory than it had."""
 
     def __setattr__(self, name, value):
         object.__setattr__(self, "_packed", None)
@@ -660,18 +661,19 @@ class _Described:
 
 @dataclass
 class Rope(_Described):
-    """A table of cosines and sines [n_positions, rot_dim / 2, 2] (float32, on the device) and how it turns a row.  The table may be replaced by
-    assignment; it is not resized in place."""
+    """A table of cosines and sines [n_positions, rot_dim / 2, 2] (float32, on the device) and how it turns a row.  The table may be replaced; its
+    shape does not change in place."""
     table: object
     rot_dim: int = 128
     interleaved: bool = False
 
     def _bytes(self, device) -> bytes:
-        if self._packed is None or self._packed[0] != device:
+        t = self.table
+        fits = (device, t.data_ptr())
+        if self._packed is None or self._packed[0] != fits:
             import torch
-            t = self.table
             _want("rope.table", t, torch.float32, (t.shape[0], self.rot_dim // 2, 2), device)
-            object.__setattr__(self, "_packed", (device, _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))))
+            object.__setattr__(self, "_packed", (fits, _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))))
         return self._packed[1]
 
 
@@ -742,7 +744,7 @@ def rotate(rope: Rope, x, positions=None, first: int = 0, out=None, inverse: boo
 class Pages(_Described):
     """Device buffers of one layer's paged cache (kvqp_pages): k_codes [n_pages,Hkv,P,128] and v_codes [n_pages,Hkv,128,P], both float8_e4m3fn or both int8;
     k_scale, v_scale float32 [n_pages,Hkv]; open_k, open_v [n_open,Hkv,2P,128] float16 or bfloat16; table int32 [B,max_pages]; lengths int32 [B]; open_slot
-    int32 [B] or None.  Their contents change as they may, and any may be replaced by assignment; they are not resized in place."""
+    int32 [B] or None.  Their contents change as they may, and any may be replaced; shapes do not change in place."""
     k_codes: object
     v_codes: object
     k_scale: object
@@ -759,7 +761,9 @@ class Pages(_Described):
 
     def _bytes(self, cfg: Cfg, device) -> bytes:
         """kvqp_pages, with all buffers as it states them."""
-        fits = (device, cfg.n_kv_heads, cfg.batch)
+        slot = self.open_slot
+        fits = (device, cfg.n_kv_heads, cfg.batch, self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.open_k.data_ptr(),
+                self.open_v.data_ptr(), self.table.data_ptr(), self.lengths.data_ptr(), None if slot is None else slot.data_ptr())
         if self._packed is None or self._packed[0] != fits:
             object.__setattr__(self, "_packed", (fits, self._checked(cfg, device)))
         return self._packed[1]

@@ -259,3 +259,21 @@ def test_the_binding_checks_types_and_shapes(monkeypatch):
     for kw in (dict(x=x.float()), dict(x=x[0]), dict(x=x[..., ::2]), dict(positions=torch.zeros(3, dtype=torch.int32)), dict(positions=torch.zeros((2, 4))), dict(out=x.bfloat16()), dict(out=x[:1])):
         with pytest.raises(ValueError):
             kvqp.rotate(rope, **{"x": x, **kw})
+
+
+def test_memory_that_changes_under_a_field_is_seen(monkeypatch):
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    seen = []
+    monkeypatch.setattr(kvqp, "_call", lambda name, device, stream, args: seen.append(args))
+    c, q = kvqp.Cfg(batch=2, n_q_heads=8, n_kv_heads=2), torch.zeros((2, 8, 128), dtype=torch.float16)
+    kv, p, rope = q[:, :2].contiguous(), kvqp.alloc_pages(c, 8, 4, device="cpu"), kvqp.Rope(torch.zeros((8, 64, 2)))
+    run = lambda: (kvqp.paged_append(c, p, kv, kv, q=q, rope=rope), seen[-1][1:3])[1]
+    first = run()
+    assert run() == first
+    for name in ("k_codes", "v_codes", "k_scale", "v_scale", "open_k", "open_v", "table", "lengths"):
+        t = getattr(p, name)
+        was = run()
+        t.data = t.data.clone()
+        assert run()[0] == kvqp.Pages(p.k_codes, p.v_codes, p.k_scale, p.v_scale, p.open_k, p.open_v, p.table, p.lengths)._bytes(c, 0) != was[0]
+    rope.table.data = rope.table.data.clone()
+    assert run()[1] == kvqp.Rope(rope.table)._bytes(0) != first[1]
