@@ -88,7 +88,7 @@ hipError_t launch_rope_table(const double* inv_freq, int rot_dim, int n_position
 
 // Bound by memory: 4 D bytes a row, and the table once for all heads.  32 rows of consecutive positions a workgroup, `per` heads of each with the same angles in
 // registers.  2 x 16381 rows of 32 heads, interleaved, half of the head (541 MB): 110 us, 4.9 TB/s (a large copy 5.2); non-temporal loads and stores took 174.
-// 32 rows of 32 heads: 6.7 us as a call, 3.3 in a graph.
+// 32 rows of 32 heads: 6.8 us as a call, 3.3 in a graph.
 constexpr int kAtOnce = 4;
 struct RotateArgs {
     Turn t;
@@ -193,7 +193,7 @@ __device__ inline float largest(f8v x) {
 
 // A workgroup has the new tokens of one block of one sequence, for one KV head and its query heads; where the block is full now it quantizes it, with
 // the tokens that the open part held before.  So one launch does all, a block's scale needs no exchange between workgroups, and a step's rows, a few KB a
-// sequence, take the time of a launch and its chain (which sequence, positions, angles, rows): 96 sequences 7.9 us as a call, 7.4 in a graph.  Prompts are bound
+// sequence, take the time of a launch and its chain (which sequence, positions, angles, rows): 96 sequences 8.5 us as a call, 7.4 in a graph.  Prompts are bound
 // by memory: 4 of up to 8191 tokens, 32 query and 8 KV heads (535 MB) 118 us, 4.5 TB/s.  Codes of values are turned channel by channel in LDS.
 template <bool BF, bool INT8, int P>
 __global__ __launch_bounds__(256) void append(AppendArgs a) {
@@ -381,7 +381,7 @@ __device__ inline uint4 rows_of_codes(uint2 w, float scale) {
 }
 
 // A workgroup has 64 tokens, counted from the sequence's beginning, of one head; values are turned back in LDS.  Bound by memory: 2 x 32768 tokens of 8 heads
-// (403 MB) 83 us, 4.8 TB/s; 999 tokens 5.9 us as a call, 4.8 in a graph.
+// (403 MB) 83 us, 4.8 TB/s; 999 tokens 6.3 us as a call, 4.8 in a graph.
 template <bool BF, bool INT8, int P>
 __global__ __launch_bounds__(256) void read(ReadArgs a) {
     constexpr int PAGES = 64 / P;

@@ -1,5 +1,6 @@
 """Attention over pages over the range of calls: batches that are not split, long tables, windows and pieces of prompts in splits, padded batches, shared pages,
 strided queries, graphs with workspaces of their own.  The oracle is plain torch in 64 bits on the GPU, batched over heads and rows."""
+import dataclasses
 import math
 import random
 
@@ -227,3 +228,18 @@ def test_a_window_beyond_every_token_is_none():
     want = pool.check(cfg, q, [330, 70])
     for window in (800, 1 << 30, (1 << 31) - 1):
         assert torch.equal(kvqp.paged_attn(cfg, pool.pages, q, ints([0, 330, 400]), window=window), want)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS)
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_loads_past_the_memory_side_cache_give_the_same(dtype, form, page):
+    """decode_cache_hint is about time alone: a step, drafted rows, holes in the table, a window."""
+    g = generator(page)
+    pool = Pool(g, [1500, 1, 77, 640], 2, page, dtype, form)
+    pool.pages.table[0, 3], pool.pages.table[3, 1] = -1, 1 << 20
+    for counts, window in (([1] * 4, 0), ([2, 1, 0, 2], 0), ([1] * 4, 200), ([7, 1, 5, 8], 90)):
+        q = torch.randn((sum(counts), 16, D), generator=g, device="cuda").to(dtype)
+        got = [kvqp.paged_attn(dataclasses.replace(config(4, 16, 2), decode_cache_hint=hint), pool.pages, q, ints(starts_of(counts)), window=window) for hint in (0, 1, 2)]
+        assert torch.equal(got[0], got[1]) and torch.equal(got[1], got[2]) and bool(torch.isfinite(got[0]).all())
+    pool = Pool(g, [1500, 1, 77, 640], 2, page, dtype, form)
+    pool.check(dataclasses.replace(config(4, 8, 2), decode_cache_hint=1), torch.randn((4, 8, D), generator=g, device="cuda").to(dtype), [1] * 4)
