@@ -27,6 +27,7 @@ struct AttnArgs {
     int per_piece;          // rows of the call that a workgroup has at most
     int slots;              // workgroups of a KV head
     int most_shares;        // how many shares the work of a KV head is cut into at most; 0: sequences are not split
+    int at_once;            // workgroups of a KV head that a single sequence is cut into at most
     bool once;              // loads of codes go past the memory-side cache (one tile of rows)
 };
 
@@ -154,7 +155,8 @@ __device__ __forceinline__ Slot find_slot(const AttnArgs& a, int slot, Sequence*
     };
     if (p.batch == 1) {
         const Share one = look(0);
-        const int splits = max((int)ceilf((float)one.groups / fmaxf((float)one.pieces * (float)one.groups / (float)a.most_shares, (float)kLeastGroups)), 1);
+        // (equal pieces: as many splits as are on the chip together.  512 rows of 32 heads over 16000 tokens: 158 us, with 384 shares 200)
+        const int splits = max(min(a.at_once / max(one.pieces, 1), (one.groups + kLeastGroups - 1) / kLeastGroups), 1);
         const int piece = slot / splits;
         return {{piece < one.pieces ? 0 : -1, uniform(one.seq.row0), uniform(one.seq.rows), uniform(one.seq.length)}, uniform(piece), uniform(slot % splits), uniform(splits),
                 uniform(piece * splits)};
@@ -992,7 +994,7 @@ template hipError_t paged_form<(KVQP_PAGED_BITS - 1) / 2 != 0, (KVQP_PAGED_BITS 
 // ---- launches ----
 constexpr size_t kPartBytes = 8192 + 2 * 128;       // a workgroup's results of 16 rows
 struct PagedPlan {
-    int row_tiles, per_piece, slots, most_shares;
+    int row_tiles, per_piece, slots, most_shares, at_once;
     size_t ws_bytes;
 };
 static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, int64_t most_tokens) {
@@ -1005,10 +1007,11 @@ static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, in
     const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;      // (at most: each sequence's last may be short)
     // (shares in all, where three, two and two workgroups fit a CU: more of them even out lengths and make more to join.  256, 384, 512 of one tile: 48 sequences of 1 .. 8192
     // tokens 94, 107, 88 us, 8 of 4096 20.9, 21.0, 20.1, one of 1024 9.6, 9.7, 9.9.  384, 512, 768 of two: 64 rows of 48 sequences 232, 213, 200, of 4 sequences
-    // 34, 30, 47.  256, 384, 512 of tiles: a piece in a window 73, 63, 80, 512 rows over 16000 tokens 227, 201, 158, 4 x 256 rows 115, 88, 106.)
+    // 34, 30, 47.  256, 384, 512 of tiles: a piece in a window 73, 63, 80, 4 x 256 rows 115, 88, 106.)
     r.most_shares = (r.row_tiles == 8 ? 384 : 512) / cfg.n_kv_heads;
-    if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = 0;
-    r.slots = pieces + r.most_shares;
+    r.at_once = 512 / cfg.n_kv_heads;
+    if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = r.at_once = 0;
+    r.slots = pieces + std::max(r.most_shares, r.at_once);
     r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;
     return r;
 }
@@ -1036,7 +1039,7 @@ hipError_t launch_paged_attn(const kvqp_cfg& cfg, const kvqp_pages& g, const voi
     const PagedPlan plan = plan_paged(cfg, n_rows, row_start != nullptr, (int64_t)g.max_pages * g.page_tokens);
     const AttnArgs a = {page_args(cfg, g, row_start, n_rows), (const uint16_t*)q, q_stride, (uint16_t*)out, lse, (unsigned int*)ws,
                         (char*)ws + KVQP_PAGED_COUNTERS, cfg.sm_scale * 1.4426950408889634f, (int64_t)window < (int64_t)g.max_pages * g.page_tokens ? window : 0, g.page_tokens == 16 ? 4 : g.page_tokens == 32 ? 5 : 6,
-                        plan.per_piece, plan.slots, plan.most_shares, rows_once(cfg, g)};
+                        plan.per_piece, plan.slots, plan.most_shares, plan.at_once, rows_once(cfg, g)};
     if (g.dtype == KVQP_BFLOAT16)
         return g.form == KVQP_INT8 ? paged_form<true, true>(a, plan.row_tiles, stream) : paged_form<true, false>(a, plan.row_tiles, stream);
     return g.form == KVQP_INT8 ? paged_form<false, true>(a, plan.row_tiles, stream) : paged_form<false, false>(a, plan.row_tiles, stream);
