@@ -302,6 +302,29 @@ struct Sums {
         return x + __shfl_xor(x, 32);
     }
 };
+// Eight weights as the second operand of the value product.  For binary16 rows they are two numbers each (TWO), w and what its rounding left: one alone, off by up to 2^-12 of itself,
+// adds nearly as much error as the output's own rounding does (1.1 to 1.5 times the error of the formula rounded once; with two 1.000).  The products with the rest cost a prompt of
+// 8192 tokens 135 us of 725; where reading the codes is the bound, nothing (32 x 8192 tokens 97.4 and 97.8).  Of bfloat16 outputs, whose rounding is eight times as
+// large, one number makes the error 1.0075 times as large at most, and suffices.
+template <bool TWO>
+struct Weights {
+    h8v w, rest;
+    __device__ __forceinline__ void put(f8v y) {
+        w = __builtin_convertvector(y, h8v);
+        if constexpr (TWO) {
+            float minus = -1.f;
+            asm("" : "+s"(minus));      // (a multiply-add takes binary16 as it is; a subtraction, which a known factor would make of it, converts first)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = __builtin_fmaf((float)w[j], minus, y[j]);
+            rest = __builtin_convertvector(y, h8v);
+        }
+    }
+    __device__ __forceinline__ f4v product(h8v v, f4v o) const {
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w, o, 0, 0, 0);
+        if constexpr (TWO) o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest, o, 0, 0, 0);
+        return o;
+    }
+};
 // (a masked product is minus infinity: the factor must not be 0, also where a block of zeros has the smallest scale)
 __device__ __forceinline__ float logit_factor(float key_scale, float row_scale) { return fmaxf(key_scale * row_scale, 1e-36f); }
 
@@ -361,7 +384,7 @@ __device__ __forceinline__ float query_fragments(const uint16_t* q, bool there, 
     }
 }
 
-// Open tokens, for one wave's rows r0 ..: in the rows' own type; bfloat16 weights are two numbers each, so that they are as exact as binary16 ones.
+// Open tokens, for one wave's rows r0 ..: in the rows' own type, weights as two numbers of it each.
 // Values come from LDS ([64][kHeadDim + 8], zeros behind the last).
 typedef uint16_t OpenValues[64][kHeadDim + 8];
 __device__ __forceinline__ void stage_open_values(const AttnArgs& a, const Range& w, int h, int slot, OpenValues& s_v, int thread, int threads) {
@@ -415,7 +438,7 @@ __device__ __forceinline__ void attend_open(const AttnArgs& a, const Range& w, i
         for (int rt = 0; rt < RT; ++rt) {
             const f8v y = st.weigh(rt, x[rt], a.logit_scale);
             e[rt] = rounded<BF>(y);
-            if constexpr (BF) e_rest[rt] = rounded<BF>(y - numbers<BF>(e[rt]));
+            e_rest[rt] = rounded<BF>(y - numbers<BF>(e[rt]));
         }
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
@@ -428,7 +451,7 @@ __device__ __forceinline__ void attend_open(const AttnArgs& a, const Range& w, i
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 st.o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), e[rt], st.o[rt][t]);
-                if constexpr (BF) st.o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), e_rest[rt], st.o[rt][t]);
+                st.o[rt][t] = product_of_rows<BF>(make_uint4(v[0], v[1], v[2], v[3]), e_rest[rt], st.o[rt][t]);
             }
         }
     }
@@ -716,7 +739,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
                     __builtin_amdgcn_sched_barrier(0);      // (what is converted ahead of its product costs registers)
                 }
                 if (half == 1 && decltype(more)::value) load_keys(g + NW);
-                h8v e[RT];
+                Weights<!BF> e[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     if (edge) {
@@ -728,13 +751,13 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
                             x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
                         }
                     }
-                    e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], logit_factor(ks, scale[rt])), h8v);
+                    e[rt].put(st.weigh(rt, x[rt], logit_factor(ks, scale[rt])));
                 }
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
                     const h8v v = halves_of_codes<INT8>(vw[t][2 * half], vw[t][2 * half + 1], vs);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, e[rt], st.o[rt][t], 0, 0, 0);
+                    for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = e[rt].product(v, st.o[rt][t]);
                     if (t & 1) __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -792,7 +815,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
 // Each of four waves has 32 rows to itself and goes over all tokens of its workgroup, 64 at a time.  Codes become binary16 numbers once, on their way
 // into LDS, where the next tile is built beside the one in use, and the codes of the one after it are on their way; products and layouts are those of the kernel above.
 //
-// A prompt of 8192 tokens, 32 heads: 580 us, 0.95 PFLOP/s (a large matrix product reaches 1.19).  At 2.4 GHz a wave takes 2600 cycles for 64 tokens of its 32 rows:
+// A prompt of 8192 tokens, 32 heads: 590 us (bfloat16), 0.93 PFLOP/s (a large matrix product reaches 1.19); binary16, whose weights are two numbers, 725 us.  At 2.4 GHz a wave takes 2600 cycles for 64 tokens of its 32 rows:
 // 1024 of matrix instructions, 512 of exponentials, 900 of other vector instructions, and the two waves of a SIMD overlap these little.  No difference
 // made, or longer: operands read from LDS a phase ahead (580), the second half's key product before the first half's exponentials in one block (713: it
 // spills), three waves a SIMD with one tile in LDS (1183: it spills), wave priorities for either phase (606, 620).  32 rows a wave, because each
@@ -924,7 +947,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
 #pragma unroll
                             for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][s], s ? x[rt][t] : kZero, 0, 0, 0);
                         }
-                    h8v e[RT];
+                    Weights<!BF> e[RT];
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
                         if (edge) {
@@ -936,13 +959,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
                                 x[rt][j >> 2][j & 3] = hidden ? -INFINITY : x[rt][j >> 2][j & 3];
                             }
                         }
-                        e[rt] = __builtin_convertvector(st.weigh(rt, x[rt], factor[rt]), h8v);
+                        e[rt].put(st.weigh(rt, x[rt], factor[rt]));
                     }
 #pragma unroll
                     for (int t = 0; t < 8; ++t) {
                         const h8v v = v_tile[value_place(16 * t + c, 2 * kb + half)];
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, e[rt], st.o[rt][t], 0, 0, 0);
+                        for (int rt = 0; rt < RT; ++rt) st.o[rt][t] = e[rt].product(v, st.o[rt][t]);
                     }
                 }
             }
