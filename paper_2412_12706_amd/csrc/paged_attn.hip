@@ -44,7 +44,7 @@ typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 
-constexpr float kNegBig = -1.0e30f;
+constexpr float kLowest = -3.402823466e38f;      // reference of a row that has seen nothing: binary32 has no logit below it
 constexpr float kLn2 = 0.69314718055994531f;
 // Weights are 2^(kLift + logit - reference) with a reference that may lag behind the row's largest logit by up to kLag: between the two a weight
 // stays below 2^15 and what binary16 holds reaches 2^-29 of the row's largest weight at least (normal numbers to 2^-18).
@@ -259,7 +259,7 @@ struct Sums {
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            lift[rt] = -kNegBig;
+            lift[rt] = -kLowest;
             sums[rt] = 0.f;
 #pragma unroll
             for (int t = 0; t < 8; ++t) o[rt][t] = f4v{0.f, 0.f, 0.f, 0.f};
@@ -282,13 +282,22 @@ struct Sums {
             float m = fmaxf(fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), x[0][2]), fmaxf(x[0][3], x[1][0])), fmaxf(fmaxf(x[1][1], x[1][2]), x[1][3])) * f;
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
-            const float lower = fminf(lift[rt], kLift - m), by = __builtin_amdgcn_exp2f(lower - lift[rt]);
+            // Far from 0 a reference is rounded by whole powers of two, up to 1.5 * 2^-23 m with m's own rounding and this one: from 2^22 on it is that much too low, so that
+            // the row's largest weight is none too small, and what is too large for binary16 then is cut to what the lag allows.  (Logits so near each other are one.)
+            float lower = kLift - m;
+            const float more = __builtin_fmaf(fabsf(m), 0x1p-22f, -1.f);
+            if (more > 0.f && more < INFINITY) lower += more;
+            lower = fminf(lift[rt], lower);
+            const float by = __builtin_amdgcn_exp2f(lower - lift[rt]);
             lift[rt] = lower;
             sums[rt] *= by;
 #pragma unroll
             for (int t = 0; t < 8; ++t) o[rt][t] *= by;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = __builtin_fmaf(x[j >> 2][j & 3], f, lower);
+            for (int j = 0; j < 8; ++j) {
+                w[j] = __builtin_fmaf(x[j >> 2][j & 3], f, lower);
+                w[j] = w[j] > kLift + kLag ? kLift + kLag : w[j];      // (NaN stays)
+            }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(w[j]);
@@ -537,7 +546,7 @@ __device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, i
             float top[TILES], total[TILES];
             f4v x[ITEMS];
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) { top[t] = kNegBig; total[t] = 0.f; }
+            for (int t = 0; t < TILES; ++t) { top[t] = kLowest; total[t] = 0.f; }
 #pragma unroll
             for (int e = 0; e < ITEMS; ++e) x[e] = f4v{0.f, 0.f, 0.f, 0.f};
             for (int s0 = from; s0 < upto; s0 += MOST * step) {
@@ -787,7 +796,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
     const Partials parts(a, w.part_of_head(a, h), active, RT);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        float top = kNegBig, total = 0.f;
+        float top = kLowest, total = 0.f;
         for (int v = 0; v < NW; ++v) top = fmaxf(top, sh.join.ref[v][16 * rt + c]);
         for (int v = 0; v < NW; ++v) total = __builtin_fmaf(sh.join.sum[v][16 * rt + c], __builtin_amdgcn_exp2f(sh.join.ref[v][16 * rt + c] - top), total);
         const float f = __builtin_amdgcn_exp2f(st.reference(rt) - top);
