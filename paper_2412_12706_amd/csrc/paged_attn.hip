@@ -138,11 +138,13 @@ __device__ __forceinline__ Slot find_slot(const AttnArgs& a, int slot, Sequence*
     }
     const int lane = threadIdx.x & 63, most = p.max_pages << a.page_log2;
     struct Share { Sequence seq; int pieces, groups; };
+    bool falling = false;      // starts that descend
     // (loads without a branch, so that all are on their way at once; what is behind the last sequence counts for nothing)
     auto look = [&](int b) {
         const int at = min(b, p.batch - 1);
         int r0 = at, r1 = at + 1;
         if (p.row_start) { r0 = p.row_start[at]; r1 = p.row_start[at + 1]; }
+        falling |= r1 < r0;
         Share s;
         s.seq.b = b;
         s.seq.row0 = min(max(r0, 0), p.n_rows);
@@ -171,6 +173,8 @@ __device__ __forceinline__ Slot find_slot(const AttnArgs& a, int slot, Sequence*
             work += (float)mine[j].pieces * (float)mine[j].groups;
         }
     }
+    // (sequences that have the same rows may be more work than the launch has workgroups for, and a split piece would wait for its last ones: none begins)
+    if (__any(falling)) return {{-1, 0, 0, 0}, 0, 0, 1, 0};
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
     const float share = fmaxf(work / (float)a.most_shares, (float)kLeastGroups);

@@ -243,3 +243,25 @@ def test_loads_past_the_memory_side_cache_give_the_same(dtype, form, page):
         assert torch.equal(got[0], got[1]) and torch.equal(got[1], got[2]) and bool(torch.isfinite(got[0]).all())
     pool = Pool(g, [1500, 1, 77, 640], 2, page, dtype, form)
     pool.check(dataclasses.replace(config(4, 8, 2), decode_cache_hint=1), torch.randn((4, 8, D), generator=g, device="cuda").to(dtype), [1] * 4)
+
+
+@pytest.mark.parametrize("hkv,gq,lengths,n,starts", [
+    (1, 4, [22820, 48308, 37470], 48, [[0, 48, 0, 48], [48, 0, 48, 0], [-5, 48, 20, 100]]),                    # one tile of 16 rows and two
+    (8, 4, [3000 + 517 * i for i in range(20)], 64, [[0, 64] * 10 + [0], [64, 0] * 10 + [64], [5 * i % 64 for i in range(21)]]),
+    (2, 8, [9000, 4000, 12000, 7000], 700, [[0, 700, 0, 700, 0], [0, 350, 300, 700, 650], [700, 0, 700, 699, 700]]),      # tiles of many rows
+    (1, 1, [300 + 37 * i for i in range(300)], 300, [[i % 2 * 300 for i in range(301)], list(range(300, -1, -1))])])      # (looked at in two turns)
+def test_starts_that_descend_leave_the_workspace_as_it_was(hkv, gq, lengths, n, starts):
+    """No result is stated for them, but the arrival counters are zero afterwards, and calls that share the workspace are right."""
+    g, b = generator(hkv + n), len(lengths)
+    pool = Pool(g, lengths, hkv, 16, HALF, "e4m3")
+    cfg = config(b, hkv * gq, hkv)
+    q = torch.randn((n, hkv * gq, D), generator=g, device="cuda").to(HALF)
+    ws = kvqp.alloc_paged_workspace(cfg, n)
+    counts = [n // b + (i < n % b) for i in range(b)]
+    want = kvqp.paged_attn(cfg, pool.pages, q, ints(starts_of(counts)), workspace=ws)
+    for bad in starts:
+        guard = torch.full((3, n, hkv * gq, D), 9.0, dtype=HALF, device="cuda")
+        kvqp.paged_attn(cfg, pool.pages, q, ints(bad), out=guard[1], workspace=ws)
+        assert bool((guard[[0, 2]] == 9).all()) and bool((ws[:16384] == 0).all())
+        assert torch.equal(kvqp.paged_attn(cfg, pool.pages, q, ints(starts_of(counts)), workspace=ws), want)
+    pool.check(cfg, q, counts, workspace=ws)
