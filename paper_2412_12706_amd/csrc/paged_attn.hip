@@ -1033,6 +1033,13 @@ struct PagedPlan {
     int row_tiles, per_piece, slots, most_shares, at_once;
     size_t ws_bytes;
 };
+// Shares in all, where three, two and two workgroups fit a CU: more of them even out lengths and make more to join.  256, 384, 512 of one tile: 48 sequences of 1 .. 8192
+// tokens 94, 107, 88 us, 8 of 4096 20.9, 21.0, 20.1, one of 1024 9.6, 9.7, 9.9.  384, 512, 768 of two: 64 rows of 48 sequences 232, 213, 200, of 4 sequences
+// 34, 30, 47.  256, 384, 512 of tiles: a piece in a window 73, 63, 80, 4 x 256 rows 115, 88, 106.  (With more than 384 heads many rows are not split.)
+static int shares_of(const kvqp_cfg& cfg, int row_tiles) { return (row_tiles == 8 ? 384 : 512) / cfg.n_kv_heads; }
+static size_t workspace_of(const kvqp_cfg& cfg, int row_tiles, int shares) {
+    return shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * shares * row_tiles * kPartBytes : 0;
+}
 static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, int64_t most_tokens) {
     // (rows of a call over its sequences, as if they were equal.  Columns: a KV head's rows of a sequence.  One tile of 16 rows where they fit, for a third wave a
     // SIMD; 64 columns as two workgroups of 32 take 212 us where the kernel of many rows, half of its rows empty, takes 208 to 303)
@@ -1041,18 +1048,22 @@ static PagedPlan plan_paged(const kvqp_cfg& cfg, int n_rows, bool has_starts, in
     r.row_tiles = columns > 64 ? 8 : columns > 16 ? 2 : 1;
     r.per_piece = 16 * r.row_tiles / gq;
     const int pieces = has_starts ? n_rows / r.per_piece + cfg.batch : cfg.batch;      // (at most: each sequence's last may be short)
-    // (shares in all, where three, two and two workgroups fit a CU: more of them even out lengths and make more to join.  256, 384, 512 of one tile: 48 sequences of 1 .. 8192
-    // tokens 94, 107, 88 us, 8 of 4096 20.9, 21.0, 20.1, one of 1024 9.6, 9.7, 9.9.  384, 512, 768 of two: 64 rows of 48 sequences 232, 213, 200, of 4 sequences
-    // 34, 30, 47.  256, 384, 512 of tiles: a piece in a window 73, 63, 80, 4 x 256 rows 115, 88, 106.)
-    r.most_shares = (r.row_tiles == 8 ? 384 : 512) / cfg.n_kv_heads;
-    r.at_once = 512 / cfg.n_kv_heads;
-    if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = r.at_once = 0;
+    r.most_shares = shares_of(cfg, r.row_tiles);
+    if (most_tokens <= 64 * kLeastGroups || cfg.batch > kMostSplitBatch) r.most_shares = 0;
+    r.at_once = r.most_shares ? 512 / cfg.n_kv_heads : 0;
     r.slots = pieces + std::max(r.most_shares, r.at_once);
-    r.ws_bytes = r.most_shares ? KVQP_PAGED_COUNTERS + (size_t)cfg.n_kv_heads * 2 * r.most_shares * r.row_tiles * kPartBytes : 0;
+    r.ws_bytes = workspace_of(cfg, r.row_tiles, r.most_shares);
     return r;
 }
-// (a plan's bytes do not fall with the rows)
-size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows) { return std::max(plan_paged(cfg, n_rows, true, INT64_MAX).ws_bytes, (size_t)KVQP_PAGED_COUNTERS); }
+// (of this plan and those of fewer rows, which may have fewer tiles and, with more than 384 heads, need more)
+size_t paged_workspace_bound(const kvqp_cfg& cfg, int n_rows) {
+    const PagedPlan most = plan_paged(cfg, n_rows, true, INT64_MAX);
+    size_t bytes = KVQP_PAGED_COUNTERS;
+    if (cfg.batch <= kMostSplitBatch)
+        for (int tiles : {1, 2, 8})
+            if (tiles <= most.row_tiles) bytes = std::max(bytes, workspace_of(cfg, tiles, shares_of(cfg, tiles)));
+    return bytes;
+}
 int64_t paged_attn_workgroups(const kvqp_cfg& cfg, const kvqp_pages& g, int n_rows, bool has_starts) {
     return (int64_t)plan_paged(cfg, n_rows, has_starts, (int64_t)g.max_pages * g.page_tokens).slots * cfg.n_kv_heads;
 }

@@ -265,3 +265,15 @@ def test_starts_that_descend_leave_the_workspace_as_it_was(hkv, gq, lengths, n, 
         assert bool((guard[[0, 2]] == 9).all()) and bool((ws[:16384] == 0).all())
         assert torch.equal(kvqp.paged_attn(cfg, pool.pages, q, ints(starts_of(counts)), workspace=ws), want)
     pool.check(cfg, q, counts, workspace=ws)
+
+
+@pytest.mark.parametrize("hkv,gq", [(400, 1), (385, 2), (513, 1)])
+def test_more_heads_than_shares(hkv, gq):
+    """Few rows are split by one share a head, or not at all, many rows not at all; one workspace, made for the most rows, serves all."""
+    g = generator(hkv)
+    pool = Pool(g, [1300], hkv, 16, HALF, "e4m3")
+    cfg = config(1, hkv * gq, hkv)
+    ws = kvqp.alloc_paged_workspace(cfg, 140)
+    for n in (140, 1, 20):
+        pool.check(cfg, torch.randn((n, hkv * gq, D), generator=g, device="cuda").to(HALF), [n], workspace=ws)
+    assert bool((ws[:16384] == 0).all())

@@ -200,6 +200,22 @@ def test_every_call_is_content_with_the_stated_workspace(lib, hq, hkv):
                 assert call(lib, "kvqp_paged_attn", args, {}) == INVALID
 
 
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (32, 8), (8, 1), (256, 32), (384, 384), (385, 385), (400, 400), (1024, 512), (513, 513), (4096, 512), (2048, 2048)])
+def test_a_workspace_for_many_rows_serves_fewer(lib, hq, hkv):
+    """A stated size does not fall with the rows, and calls of fewer rows are content with it (their queries lie over their results: refused behind the workspace's check)."""
+    for batch in (1, 2, 31, 100):
+        c = kvqp.Cfg(batch=batch, n_q_heads=hq, n_kv_heads=hkv)
+        if batch * hkv > 65535:
+            continue
+        ns = [n for n in (1, 2, 8, 9, 64, 128, 140, 400, 4000, 40000) if n == 1 or n >= batch]
+        sizes = [kvqp.paged_workspace_bytes(c, n) for n in ns]
+        assert sizes == sorted(sizes)
+        for n, nbytes in zip(ns, sizes):
+            for fewer in [m for m in (1, batch, 3 * batch, 16 * batch, n // 2, n) if 1 <= m <= n]:
+                args = {**ATTN, "cfg": c._bytes(), "pages": pages(n_open=batch, max_pages=5000), "q": 1 << 50, "out": 1 << 50, "qs": hq * 128, "n": fewer, "ws_bytes": nbytes}
+                assert call(lib, "kvqp_paged_attn", args, {}) == INVALID, (batch, n, fewer)
+
+
 def test_the_binding_refuses_what_is_not_on_a_gpu():
     c = kvqp.Cfg(batch=2, n_q_heads=8, n_kv_heads=2)
     p = kvqp.alloc_pages(c, 8, 4, device="cpu")
