@@ -681,8 +681,7 @@ def rope_table(n_positions: int, inv_freq, magnitude: float = 1.0, interleaved: 
     """kvqp_rope_table: a Rope for positions 0 .. n_positions - 1 with these frequencies (rope_frequencies gives some)."""
     import torch
     pairs = len(inv_freq)
-    with _memory_of(stream):
-        table = torch.empty((max(n_positions, 1), pairs, 2), dtype=torch.float32, device=device)
+    table = _empty_rows((max(n_positions, 1), pairs, 2), torch.float32, device, stream)
     with torch.cuda.device(table.device):
         rc = lib().kvqp_rope_table((C.c_double * pairs)(*inv_freq), 2 * pairs, n_positions, magnitude, table.data_ptr(), _stream_ptr(stream))
     if rc:

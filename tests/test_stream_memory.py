@@ -132,3 +132,43 @@ def test_a_captured_call_on_the_capturing_stream_makes_its_own_memory(orc):
         again = kvqp.tree_attn(cfg, q, kn, vn, None, cache)
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(out1, step) and torch.equal(again, want)
+
+
+def test_a_table_made_on_another_stream_is_kept_until_the_current_one_is_done(monkeypatch):
+    """rope_table(stream=s) takes memory of s, and tells the allocator that the current stream, which goes on to read it, uses it as well."""
+    noted, real = [], torch.empty
+
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+
+        def record_stream(self, stream):
+            noted.append(stream)
+    recorder = Recorder(monkeypatch)
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: (recorder.seen.append(recorder.current[-1]), real(*a, **kw).as_subclass(OnGpu))[1])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: recorder.current[-1])
+    monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
+    monkeypatch.setattr(kvqp, "_stream_ptr", lambda stream: 0)
+    monkeypatch.setattr(kvqp, "lib", lambda: types.SimpleNamespace(kvqp_rope_table=lambda *a: 0))
+    kvqp.rope_table(9, [1.0] * 8, device="cpu")
+    assert recorder.seen == ["current"] and noted == []
+    recorder.seen.clear()
+    kvqp.rope_table(9, [1.0] * 8, device="cpu", stream=types.SimpleNamespace(cuda_stream=0x9009))
+    assert recorder.seen == [0x9009] and noted == ["current"]
+
+
+@pytest.mark.gpu
+def test_a_table_that_is_dropped_while_it_is_read_is_not_handed_out():
+    s, n = torch.cuda.Stream(), 70001
+    torch.cuda.synchronize()
+    rope = kvqp.rope_table(n, kvqp.rope_frequencies(), stream=s)
+    place = rope.table.data_ptr()
+    torch.cuda.current_stream().wait_stream(s)
+    want = kvqp.rope_table(n, kvqp.rope_frequencies()).table
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)                          # (the current stream has work before it reads the table)
+    got = rope.table.clone()
+    del rope
+    with torch.cuda.stream(s):
+        other = torch.full((n, 64, 2), 7.0, device="cuda")
+    torch.cuda.synchronize()
+    assert other.data_ptr() != place and torch.equal(got, want)
