@@ -538,6 +538,7 @@ __device__ __forceinline__ bool arrived_last(unsigned int* count, int of, int* s
 constexpr int kJoin = 16;
 template <bool BF, int RT>
 __device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, int h, const Partials& parts, int* s_last) {
+    static_assert(RT == 1 || RT % 2 == 0, "a thread takes items of two row tiles at a time: an odd number of tiles would end behind the outputs, in the rows' states");
     constexpr int row_tiles = RT;
     unsigned int* const counts = a.arrivals + w.part_of_head(a, h);
     const int c = threadIdx.x & 15, kb = (threadIdx.x & 63) >> 4, rows = w.n * a.p.gq;

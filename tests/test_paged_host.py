@@ -293,3 +293,22 @@ def test_memory_that_changes_under_a_field_is_seen(monkeypatch):
         assert run()[0] == kvqp.Pages(p.k_codes, p.v_codes, p.k_scale, p.v_scale, p.open_k, p.open_v, p.table, p.lengths)._bytes(c, 0) != was[0]
     rope.table.data = rope.table.data.clone()
     assert run()[1] == kvqp.Rope(rope.table)._bytes(0) != first[1]
+
+
+@pytest.mark.parametrize("tiles,compiles", [(2, True), (3, False), (4, True)])
+def test_the_join_is_compiled_for_tiles_that_it_covers(tmp_path, tiles, compiles):
+    """A pass of it takes two row tiles, so three would end behind the outputs: only even numbers compile (host side alone: nothing is built)."""
+    import os
+    import shutil
+    import subprocess
+    from paper_2412_12706_amd import build
+    if shutil.which("hipcc") is None:
+        pytest.skip("no hipcc")
+    with open(os.path.join(build.CSRC, "paged_attn.hip")) as f:
+        text = f.read()
+    launch = "paged_rows<BF, INT8, 2, false><<<"
+    assert launch in text
+    (tmp_path / "x.hip").write_text(text.replace(launch, f"paged_rows<BF, INT8, {tiles}, false><<<"))
+    r = subprocess.run(["hipcc", "-x", "hip", "--offload-arch=gfx950", "--offload-host-only", "-std=c++17", "-I" + os.path.join(build.ROOT, "include"), "-I" + build.CSRC,
+                        "-DKVQP_PAGED_BITS=1", "-fsyntax-only", str(tmp_path / "x.hip")], capture_output=True, text=True, timeout=200)
+    assert (r.returncode == 0) == compiles and ("static assertion" in r.stderr) != compiles, r.stderr[-2000:]
