@@ -277,3 +277,20 @@ def test_more_heads_than_shares(hkv, gq):
     for n in (140, 1, 20):
         pool.check(cfg, torch.randn((n, hkv * gq, D), generator=g, device="cuda").to(HALF), [n], workspace=ws)
     assert bool((ws[:16384] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,form", [(HALF, "int8"), (BF16, "e4m3")])
+@pytest.mark.parametrize("hkv,gq,page,lengths,counts,window", [
+    (1, 1, 16, [20011], [70], 0), (1, 4, 32, [20011], [130], 0),           # 79 splits of a piece: four sixteens and a fifteen
+    (1, 1, 16, [4300], [128], 0), (1, 1, 16, [4300], [5], 0), (1, 8, 64, [8400], [3], 0),      # 17 and 33: one is left over
+    (1, 1, 64, [70003], [129], 0), (1, 2, 16, [70003], [3], 0),            # 274
+    (1, 2, 16, [30000, 11000], [90, 40], 0), (2, 4, 32, [900, 41000, 5], [40, 70, 3], 0), (1, 4, 64, [50000, 300], [200, 9], 30000)])
+def test_joins_of_more_than_sixteen_splits(dtype, form, hkv, gq, page, lengths, counts, window):
+    """By sixteens first, and then theirs, for one, two and eight tiles of rows; again with the workspace as that left it."""
+    g = generator(sum(lengths) + gq)
+    pool = Pool(g, lengths, hkv, page, dtype, form)
+    cfg = config(len(lengths), hkv * gq, hkv)
+    ws = kvqp.alloc_paged_workspace(cfg, sum(counts))
+    q = torch.randn((sum(counts), hkv * gq, D), generator=g, device="cuda").to(dtype)
+    first = pool.check(cfg, q, counts, window, workspace=ws)
+    assert bool((ws[:16384] == 0).all()) and torch.equal(kvqp.paged_attn(cfg, pool.pages, q, ints(starts_of(counts)), window=window, workspace=ws), first)
