@@ -154,3 +154,24 @@ def test_a_captured_rotation_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype,rot,interleaved,inverse", [(HALF, 128, False, False), (BF16, 64, True, True), (BF16, 96, False, True), (HALF, 32, True, False)])
+@pytest.mark.parametrize("b,h,n", [(1, 5, 32763), (2, 5, 32739), (4, 11, 32768), (3, 9, 40001), (1, 3, 131072)])
+def test_several_heads_a_workgroup(dtype, rot, interleaved, inverse, b, h, n):
+    """More than 4096 workgroups of 32 rows and a head: two, four and eight heads take the same angles, the last ones fewer.  Bit for bit, of strided rows, in place and not."""
+    g = torch.Generator(device="cuda").manual_seed(b + h + n)
+    rope = kvqp.rope_table(1500, kvqp.rope_frequencies(rot), interleaved=interleaved)
+    fused = torch.randn((b, n, h + 2, D), generator=g, device="cuda").to(dtype)
+    x, position = fused[:, :, 1:h + 1].transpose(1, 2), torch.randint(0, 1500, (b, n), generator=g, device="cuda")
+    cs = rope.table[position].unsqueeze(1)                 # [b, 1, n, rot / 2, 2]
+    c, s = cs[..., 0], -cs[..., 1] if inverse else cs[..., 1]
+    want = x.float()
+    first, second = (want[..., 0:rot:2], want[..., 1:rot:2]) if interleaved else (want[..., :rot // 2], want[..., rot // 2:rot])
+    u, w = first * c - second * s, second * c + first * s
+    first.copy_(u), second.copy_(w)
+    want, at = want.to(dtype), position.to(torch.int32)
+    assert torch.equal(kvqp.rotate(rope, x, at, inverse=inverse), want)
+    keep = fused.clone()
+    kvqp.rotate(rope, x, at, out=x, inverse=inverse)
+    assert torch.equal(x, want) and torch.equal(fused[:, :, 0], keep[:, :, 0]) and torch.equal(fused[:, :, h + 1], keep[:, :, h + 1])
