@@ -652,11 +652,17 @@ def rope_frequencies(rot_dim: int = 128, base: float = 10000.0, scaling: int = R
 
 class _Described:
     """An object whose fields describe device memory: they are checked and packed for the library once, and again after one of them is assigned
-    or has other memory than it had."""
+    or has other memory than it had.  (Calls of other threads may go on meanwhile: what they packed carries the state that they began with.)"""
+    _packed = None      # (state, where the memory is, bytes)
 
     def __setattr__(self, name, value):
-        object.__setattr__(self, "_packed", None)
         object.__setattr__(self, name, value)
+        object.__setattr__(self, "_state", object())
+
+    def _pack(self, fits, *of):
+        packed = (self._state, fits, self._checked(*of))
+        object.__setattr__(self, "_packed", packed)
+        return packed
 
 
 @dataclass
@@ -668,13 +674,16 @@ class Rope(_Described):
     interleaved: bool = False
 
     def _bytes(self, device) -> bytes:
+        fits, packed = (device, self.table.data_ptr()), self._packed
+        if packed is None or packed[0] is not self._state or packed[1] != fits:
+            packed = self._pack(fits, device)
+        return packed[2]
+
+    def _checked(self, device) -> bytes:
+        import torch
         t = self.table
-        fits = (device, t.data_ptr())
-        if self._packed is None or self._packed[0] != fits:
-            import torch
-            _want("rope.table", t, torch.float32, (t.shape[0], self.rot_dim // 2, 2), device)
-            object.__setattr__(self, "_packed", (fits, _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))))
-        return self._packed[1]
+        _want("rope.table", t, torch.float32, (t.shape[0], self.rot_dim // 2, 2), device)
+        return _pack_rope(t.data_ptr(), t.shape[0], self.rot_dim, bool(self.interleaved))
 
 
 def rope_table(n_positions: int, inv_freq, magnitude: float = 1.0, interleaved: bool = False, device="cuda", stream=None) -> Rope:
@@ -763,9 +772,10 @@ class Pages(_Described):
         slot = self.open_slot
         fits = (device, cfg.n_kv_heads, cfg.batch, self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.open_k.data_ptr(),
                 self.open_v.data_ptr(), self.table.data_ptr(), self.lengths.data_ptr(), None if slot is None else slot.data_ptr())
-        if self._packed is None or self._packed[0] != fits:
-            object.__setattr__(self, "_packed", (fits, self._checked(cfg, device)))
-        return self._packed[1]
+        packed = self._packed
+        if packed is None or packed[0] is not self._state or packed[1] != fits:
+            packed = self._pack(fits, cfg, device)
+        return packed[2]
 
     def _checked(self, cfg: Cfg, device) -> bytes:
         import torch

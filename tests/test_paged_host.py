@@ -312,3 +312,33 @@ def test_the_join_is_compiled_for_tiles_that_it_covers(tmp_path, tiles, compiles
     r = subprocess.run(["hipcc", "-x", "hip", "--offload-arch=gfx950", "--offload-host-only", "-std=c++17", "-I" + os.path.join(build.ROOT, "include"), "-I" + build.CSRC,
                         "-DKVQP_PAGED_BITS=1", "-fsyntax-only", str(tmp_path / "x.hip")], capture_output=True, text=True, timeout=200)
     assert (r.returncode == 0) == compiles and ("static assertion" in r.stderr) != compiles, r.stderr[-2000:]
+
+
+def test_fields_assigned_by_another_thread(monkeypatch):
+    """Calls go on while another thread replaces fields: each finds a description, and the next one after an assignment the new one."""
+    import sys
+    import threading
+    import time
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    c, p, rope = kvqp.Cfg(batch=2, n_q_heads=8, n_kv_heads=2), kvqp.alloc_pages(kvqp.Cfg(batch=2, n_q_heads=8, n_kv_heads=2), 8, 4, device="cpu"), kvqp.Rope(torch.zeros((8, 64, 2)))
+    others, done, interval = [p.lengths.clone() for _ in range(2)], threading.Event(), sys.getswitchinterval()
+
+    def assign():
+        i = 0
+        while not done.is_set():
+            i += 1
+            p.lengths, rope.interleaved = others[i % 2], bool(i % 2)
+    worker = threading.Thread(target=assign)
+    sys.setswitchinterval(1e-6)
+    try:
+        worker.start()
+        until = time.time() + 1.5
+        while time.time() < until:
+            assert len(p._bytes(c, 0)) == len(rope._bytes(0)) + 72
+    finally:
+        done.set()
+        worker.join()
+        sys.setswitchinterval(interval)
+    for i in range(4):
+        p.lengths, rope.interleaved = others[i % 2], bool(i % 2)
+        assert p._bytes(c, 0) == p._checked(c, 0) and rope._bytes(0) == kvqp.Rope(rope.table, interleaved=bool(i % 2))._bytes(0)
