@@ -680,7 +680,8 @@ int kvqp_paged_workspace_init(void *workspace, size_t workspace_bytes, void *hip
  *   out  dtype [n_rows, Hq, 128], contiguous;  lse  float [n_rows, Hq] or NULL: natural logarithm of the sum of exp(logit)
  * A row that attends nothing gets zeros and -inf.  What a row does not attend does not reach it.  Reproducible bit for bit.
  * out and lse lie apart from all that is read.
- * Numerical range: rows whose products with keys, times sm_scale, binary32 holds, and values below 2^80.  Products are exact, sums binary32; a weight enters the value
+ * Numerical range: sm_scale below 2^100 (else UNSUPPORTED); sm_scale times a row's largest element below 2^126, also times the largest key of a page (of whatever channel, as
+ * powers of two of both are taken out of the products); values below 2^80.  Products are exact, sums binary32; a weight enters the value
  * product as two binary16 numbers where rows are binary16 (2^-22 of itself), as one where they are bfloat16 (2^-12; two of bfloat16 at open tokens), or with 2^-29 of the
  * row's largest, where that is more; a value below 2^-24 of the largest scale among its sequence's pages loses bits, and so does an element of a bfloat16 query below 2^-14 of
  * its row's largest.

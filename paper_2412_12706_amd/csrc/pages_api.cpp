@@ -201,6 +201,7 @@ int kvqp_paged_attn(const kvqp_cfg* cfg, const kvqp_pages* pages, const void* q,
     if (rc) return rc;
     if ((rc = check_rows(cfg, n_rows, row_start))) return rc;
     if (!q || !out || window < 0) return KVQP_ERR_INVALID_ARG;
+    if (cfg->sm_scale >= 0x1p100f) return KVQP_ERR_UNSUPPORTED;      // (times the scales of queries and keys it is a factor in binary32)
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !good_stride(q_stride, cfg->n_q_heads)) return KVQP_ERR_INVALID_ARG;
     if (n_rows == 0) return KVQP_OK;
     if (paged_attn_workgroups(*cfg, *pages, n_rows, row_start != nullptr) > kMostWorkgroups) return KVQP_ERR_UNSUPPORTED;

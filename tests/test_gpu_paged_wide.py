@@ -41,7 +41,7 @@ SHAPES = [(16, 300, 1), (32, 2900, 5), (64, 700, 9), (16, 2900, 40)]
 def test_rows_whose_logits_are_all_alike(dtype, form, page, length, count, log2):
     """Every weight is the same, so an output is the mean, whatever the logit; heads of one call have it positive, negative and small."""
     g = torch.Generator().manual_seed(log2)
-    a = 10 if dtype is HALF else 50 if log2 > 50 else 5
+    a = (14 if log2 > 50 else 10) if dtype is HALF else 50 if log2 > 50 else 5
     made = made_with(g, length, page, dtype, form, lambda t: torch.full(t.shape, 2.0 ** a))
     q = torch.zeros((count, 4, D), dtype=dtype)
     q[:, 0, 3], q[:, 1, 3], q[:, 2, 3], q[:, 3, 3] = 2.0 ** a, -(2.0 ** a), 2.0 ** -12, -1.5 * 2.0 ** (a - 1)
@@ -65,7 +65,7 @@ def test_rows_whose_logits_are_all_alike(dtype, form, page, length, count, log2)
 def test_a_token_above_all_others(dtype, form, page, length, count, log2):
     """One token's logit is a third of the others', far below zero, or three times as large, above it: its value is the output."""
     g = torch.Generator().manual_seed(log2 + 1)
-    a = 10 if dtype is HALF else 50 if log2 > 50 else 5
+    a = (14 if log2 > 50 else 10) if dtype is HALF else 50 if log2 > 50 else 5
     for winner in (0, 77, length // 2, length - count - (length - count) % page - 1, length - count):
         for sign in (-1, 1):
             made = made_with(g, length, page, dtype, form, lambda t: torch.where((t == winner) == (sign > 0), 3.0, 1.0) * 2.0 ** a)

@@ -160,6 +160,11 @@ def test_read_refuses(lib, kw, code):
     assert call(lib, "kvqp_paged_read", READ, kw) == code
 
 
+def test_attention_refuses_a_factor_that_binary32_does_not_hold(lib):
+    for scale, code in ((2.0 ** 100, UNSUPPORTED), (3e38, UNSUPPORTED), (2.0 ** 99, 0), (0.0, INVALID)):
+        assert call(lib, "kvqp_paged_attn", {**ATTN, "n": 0} if code == 0 else ATTN, {"cfg": cfg(sm_scale=scale)}) == code
+
+
 def test_more_than_a_launch_can_have(lib):
     """2^24 workgroups of 256 threads are more threads than a launch counts."""
     far = {"k": 1 << 50, "v": 1 << 52, "q": 1 << 54, "q_out": 1 << 56}
