@@ -364,8 +364,8 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Range& w, int
 }
 
 // A row's query as binary16 fragments: 8 channels from 32 s + 8 kb (or, WIDE, 64 (s >> 1) + 16 kb + 8 (s & 1): 16 bytes of a key at a time) for the lane's
-// column.  A bfloat16 row over a power of two is a row of binary16 numbers, but for what is below 2^-24 of its largest: so codes meet it without a
-// conversion to bfloat16, and the logits' factor takes the power back.
+// column.  A bfloat16 row times a power of two, such that its largest element is 2^15 to 2^16, is a row of binary16 numbers, but for what is below 2^-29 of that: so codes
+// meet it without a conversion to bfloat16, and the logits' factor takes the power back.
 template <bool BF, bool WIDE>
 __device__ __forceinline__ float query_fragments(const uint16_t* q, bool there, int kb, float logit_scale, h8v (&out)[4]) {
     uint4 w[4];
@@ -386,7 +386,7 @@ __device__ __forceinline__ float query_fragments(const uint16_t* q, bool there, 
         }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -120), 120);
+        const int e = min(max((int)(__float_as_uint(m) >> 23) - 142, -120), 113);
 #pragma unroll
         for (int s = 0; s < 4; ++s) out[s] = __builtin_convertvector(numbers<true>(w[s]) * two_to(-e), h8v);
         return logit_scale * two_to(e);

@@ -92,3 +92,31 @@ def test_queries_that_are_no_numbers_give_none(count):
         seen = v[:400 - count + 1 + i]
         want = seen.mean(0).expand(2, D)
         near(got[i, [1, 3]], want, (2.0 ** -11 + 2 * steps(400)) * seen.abs().mean(0).expand(2, D), BF16)
+
+
+@pytest.mark.parametrize("form", ["e4m3", "int8"])
+@pytest.mark.parametrize("page,length,count", SHAPES)
+@pytest.mark.parametrize("small", [-16, -20, -27])
+def test_small_elements_of_a_query_that_meet_large_keys(form, page, length, count, small):
+    """A bfloat16 query's largest element meets keys of 0, and one that is 2^16 .. 2^27 times smaller makes the logits."""
+    g = torch.Generator().manual_seed(-small)
+    made = Made(g, [length], 1, page, BF16, form)
+    made.k[0].zero_()
+    made.k[0][0, :, 9] = (torch.randint(-8, 9, (length,), generator=g) * 2.0 ** (-small - 3)).to(BF16)      # (whole numbers of up to 4 bits: codes hold them)
+    made.put(0, 0, length)
+    k, v = made.numbers(0, "k")[0], made.numbers(0, "v")[0]
+    assert torch.equal(k, made.k[0][0].double())
+    q = torch.zeros((count, 2, D), dtype=BF16)
+    q[:, :, 40] = 1.75
+    q[:, 0, 9], q[:, 1, 9] = 6.0 * (1 + 2.0 ** -7) * 2.0 ** small, -3.0 * (1 + 2.0 ** -6) * 2.0 ** small
+    assert torch.equal(q[0, 1, 9].double(), torch.tensor(-3.0 * (1 + 2.0 ** -6) * 2.0 ** small, dtype=torch.float64))
+    got, lse = call(config(1, 2, 1, 1.0), made, q, [count])
+    for i in range(count):
+        seen = slice(0, length - count + 1 + i)
+        x = q[i].double() @ k[seen].t()
+        w = torch.softmax(x, 1)
+        # (logits of up to 6.1 are one product, and a multiplication by a factor that is rounded: 4 roundings)
+        d = 4 * 2.0 ** -24 * 6.1
+        off = (2.0 ** -11 + 2 * d + 2 * steps(length)) * (w @ v[seen].abs()) + length * 2.0 ** -28 * w.amax(1, keepdim=True) * v[seen].abs().amax(0)
+        near(got[i], w @ v[seen], off, BF16)
+        assert bool(((lse[i] - torch.logsumexp(x, 1)).abs() <= d + steps(length) + 2.0 ** -22 * 20).all())
