@@ -683,7 +683,7 @@ int kvqp_paged_workspace_init(void *workspace, size_t workspace_bytes, void *hip
  * Numerical range: sm_scale below 2^100 (else UNSUPPORTED); sm_scale times a row's largest element below 2^126, also times the largest key of a page (of whatever channel, as
  * powers of two of both are taken out of the products); values below 2^80.  Products are exact, sums binary32; a weight enters the value
  * product as two binary16 numbers where rows are binary16 (2^-22 of itself), as one where they are bfloat16 (2^-12; two of bfloat16 at open tokens), or with 2^-29 of the
- * row's largest, where that is more; a value below 2^-24 of the largest scale among its sequence's pages loses bits, and so does an element of a bfloat16 query below 2^-29 of
+ * row's largest, where that is more; a value below 2^-29 of the largest scale among its sequence's pages loses bits, and so does an element of a bfloat16 query below 2^-29 of
  * its row's largest.
  * decode_cache_hint: KVQP_CACHE_AUTO is KVQP_CACHE_STREAM where the pages that the sequences can have (min(n_pages, batch max_pages)) are more than 96 MB, else
  * KVQP_CACHE_KEEP; it counts where a KV head has no more than 16 rows of a sequence (query heads times new tokens), as in a step.

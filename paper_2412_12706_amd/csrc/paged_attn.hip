@@ -500,8 +500,11 @@ struct PageNumbers {
         return __syncthreads_or(holes) != 0;
     }
 };
-// top: the largest scale of values so far, of all threads in *s_top
-template <int THREADS>
+// A value's code of the largest scale is multiplied by as much as binary16 has room for, so that codes of smaller scales are normal numbers for longer (e4m3:
+// 448 2^7; integers: what they are converted by is 1152 2^5).
+template <bool INT8> constexpr float kValueLift = INT8 ? 32.f : 128.f;
+// top: the largest scale of values so far, over kValueLift, of all threads in *s_top
+template <int THREADS, bool INT8>
 __device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float top, Segment& seg, const PageNumbers<THREADS>& pages, unsigned int* s_top) {
     float most = top;
 #pragma unroll
@@ -511,7 +514,7 @@ __device__ __forceinline__ float look_up_scales(const AttnArgs& a, int h, float 
         if (pages.mine[u] < 0) { ks = 1.f; vs = 0.f; }
         const int i = threadIdx.x + THREADS * u;
         seg.k_scale[i] = ks; seg.v_scale[i] = vs;
-        most = fmaxf(most, vs);
+        most = fmaxf(most, vs * (1.f / kValueLift<INT8>));
     }
     if (most > top) atomicMax(s_top, __float_as_uint(most));
     __syncthreads();
@@ -681,7 +684,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
     Sums<RT> st;
     st.clear();
 
-    float v_top = two_to(-126);        // values are accumulated over the largest scale so far: codes times 2^0 and less fit binary16
+    float v_top = two_to(-126);        // values are accumulated over the largest scale so far, divided by kValueLift
     Segment& seg = sh.run.seg;
     for (int s0 = ga; s0 < gb; s0 += seg_groups) {
         const int s1 = min(s0 + seg_groups, gb);
@@ -717,7 +720,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
         };
         int g = s0 + wave;
         if (g < s1) { load_keys(g); load_values(g); }
-        const float top = look_up_scales<THREADS>(a, h, v_top, seg, pages, &s_top);
+        const float top = look_up_scales<THREADS, INT8>(a, h, v_top, seg, pages, &s_top);
         if (top > v_top) {
             st.times(v_top / top);
             v_top = top;
@@ -930,7 +933,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles(const AttnArgs
         };
         // (requests behind the last tile repeat it: without a branch the compiler knows how many loads are on their way)
         request(s0);
-        const float top = look_up_scales<THREADS>(a, h, v_top, seg, pages, &s_top);
+        const float top = look_up_scales<THREADS, INT8>(a, h, v_top, seg, pages, &s_top);
         if (top > v_top) {
             st.times(v_top / top);
             v_top = top;

@@ -120,3 +120,31 @@ def test_small_elements_of_a_query_that_meet_large_keys(form, page, length, coun
         off = (2.0 ** -11 + 2 * d + 2 * steps(length)) * (w @ v[seen].abs()) + length * 2.0 ** -28 * w.amax(1, keepdim=True) * v[seen].abs().amax(0)
         near(got[i], w @ v[seen], off, BF16)
         assert bool(((lse[i] - torch.logsumexp(x, 1)).abs() <= d + steps(length) + 2.0 ** -22 * 20).all())
+
+
+@pytest.mark.parametrize("dtype,form", FORMS)
+@pytest.mark.parametrize("page,length,count", SHAPES)
+def test_small_values_beside_a_page_of_large_ones(dtype, form, page, length, count):
+    """Rows that do not attend the page of the largest values see the others as they are, whose scales are 2^22 (binary16) and 2^26 times smaller."""
+    g = torch.Generator().manual_seed(length)
+    made = Made(g, [length], 1, page, dtype, form)
+    apart = 22 if dtype is HALF else 26
+    high, low = (2.0 ** 13, 2.0 ** (13 - apart)) if dtype is HALF else (2.0 ** 40, 2.0 ** (40 - apart))
+    v = torch.randn((1, length, D), generator=g).clamp(-4, 4) * low
+    v[:, page:2 * page] *= high / low
+    made.v[0] = v.to(dtype)
+    made.k[0].zero_()
+    made.k[0][0, page:2 * page, 3] = -128.0
+    made.put(0, 0, length)
+    q = torch.zeros((count, 1, D), dtype=dtype)
+    q[:, 0, 3] = 2.0
+    got, _ = call(config(1, 1, 1, 1.0), made, q, [count])
+    v = made.numbers(0, "v")[0]
+    for i in range(count):
+        n = length - count + 1 + i
+        seen = torch.cat([v[:page], v[2 * page:n]])
+        # the large ones' weights are e^-256; a value of this type is as near as 2^-24 of the number that a code of 1 stands for in the largest scale times what lies
+        # between that and a half's largest: 2^7 for e4m3, 2^5 for integers
+        scale = high * 8 / (448 if form == "e4m3" else 127)
+        off = (2.0 ** -11 + 2 * steps(n)) * seen.abs().mean(0) + 2.0 ** -25 * scale / (128 if form == "e4m3" else 32)
+        near(got[i, 0], seen.mean(0), off, dtype)
