@@ -636,10 +636,10 @@ __device__ __forceinline__ void join_splits(const AttnArgs& a, const Range& w, i
 // O^T = V^T P^T without leaving the lane; the first operand is 16 consecutive bytes of a channel, as pages store values.
 //
 // Codes go from memory to registers, each wave's own: nobody else in the workgroup needs them, so LDS would add a round trip.  A wave requests the next 64
-// tokens' keys while it works on values, and their values after that.  32 sequences of 8192 tokens, 8 KV heads of 4 query heads (538 MB): 97 us,
-// 5.5 TB/s, more than a large copy reaches.  One sequence of 1024 tokens: 9.5 us, the chain of launch, lengths, table, codes and join.
+// tokens' keys while it works on values, and their values after that.  32 sequences of 8192 tokens, 8 KV heads of 4 query heads (538 MB): 98 us,
+// 5.5 TB/s, more than a large copy reaches.  One sequence of 1024 tokens: 9.6 us, the chain of launch, lengths, table, codes and join.
 // 17 .. 32 rows take two tiles of 16 (two waves a SIMD by registers), more than 32 several workgroups of 32 each, so that keys and values are read
-// from memory once and from the caches again (40 rows of a KV head for each of 48 sequences of up to 16001 tokens, bfloat16 and int8: 212 us for 791 MB, twice through matrix and vector
+// from memory 1.1 times and else from the caches (40 rows of a KV head for each of 48 sequences of up to 16001 tokens, bfloat16 and int8: 212 us for 791 MB, twice through matrix and vector
 // instructions; tiles of 3 and 4 would need 512 registers a lane, and are not used; the kernel of many rows takes 208 .. 303).
 constexpr int kRowsWaves = 4;
 
@@ -832,11 +832,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, RT == 1 ? 3 : 2) void paged_rows(c
 // Each of four waves has 32 rows to itself and goes over all tokens of its workgroup, 64 at a time.  Codes become binary16 numbers once, on their way
 // into LDS, where the next tile is built beside the one in use, and the codes of the one after it are on their way; products and layouts are those of the kernel above.
 //
-// A prompt of 8192 tokens, 32 heads: 590 us (bfloat16), 0.93 PFLOP/s (a large matrix product reaches 1.19); binary16, whose weights are two numbers, 725 us.  At 2.4 GHz a wave takes 2600 cycles for 64 tokens of its 32 rows:
-// 1024 of matrix instructions, 512 of exponentials, 900 of other vector instructions, and the two waves of a SIMD overlap these little.  No difference
-// made, or longer: operands read from LDS a phase ahead (580), the second half's key product before the first half's exponentials in one block (713: it
-// spills), three waves a SIMD with one tile in LDS (1183: it spills), wave priorities for either phase (606, 620).  32 rows a wave, because each
-// fragment read from LDS then meets two row tiles: LDS is busy for 42 % of the time.
+// A prompt of 8192 tokens, 32 heads: 590 us (bfloat16), 0.93 PFLOP/s (a large matrix product reaches 1.19); binary16, whose weights are two numbers, 707 to 750 on four
+// cards.  A wave takes 2600 to 3000 cycles for 64 tokens of its 32 rows (binary16: 3200 and more): 1024 (1536) of matrix instructions, 512 of exponentials, 900 (1030) of other vector
+// instructions, and the two waves of a SIMD overlap these little.  With weights of one number, which took 580 to 590, no difference made, or longer: operands read from LDS a phase
+// ahead (580), the second half's key product before the first half's exponentials in one block (713: it spills), three waves a SIMD with one tile in LDS (1183: it
+// spills), wave priorities for either phase (606, 620).  32 rows a wave, because each fragment read from LDS then meets two row tiles: LDS is busy for 34 to 42 % of the time.
 constexpr int kTileWaves = 4, kTileRows = 2;
 struct TilesShared {
     union {
