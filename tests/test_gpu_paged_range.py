@@ -294,3 +294,26 @@ def test_joins_of_more_than_sixteen_splits(dtype, form, hkv, gq, page, lengths, 
     q = torch.randn((sum(counts), hkv * gq, D), generator=g, device="cuda").to(dtype)
     first = pool.check(cfg, q, counts, window, workspace=ws)
     assert bool((ws[:16384] == 0).all()) and torch.equal(kvqp.paged_attn(cfg, pool.pages, q, ints(starts_of(counts)), window=window, workspace=ws), first)
+
+
+@pytest.mark.parametrize("count", [1, 40])
+def test_a_captured_call_makes_its_own_workspace(count):
+    """Without a workspace a captured call has one of the graph's memory, prepared by every replay; on the current stream, and on the capturing one by name."""
+    g = generator(10 + count)
+    pool = Pool(g, [9000, 300], 2, 16, BF16, "e4m3")
+    cfg, starts = config(2, 8, 2), ints([0, count, 2 * count])
+    q = torch.zeros((2 * count, 8, D), dtype=BF16, device="cuda")
+    kvqp.paged_attn(cfg, pool.pages, q, starts)
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        first = kvqp.paged_attn(cfg, pool.pages, q, starts)
+        second = kvqp.paged_attn(cfg, pool.pages, q, starts, stream=s)
+    for _ in range(4):
+        q.copy_(torch.randn(q.shape, generator=g, device="cuda"))
+        want = kvqp.paged_attn(cfg, pool.pages, q, starts)
+        first.zero_(), second.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, want) and torch.equal(second, want)
